@@ -57,6 +57,7 @@ extern "C" {
 #define STAGE_E_UNSUPPORTED    -7   /* configuration outside what the kernels implement */
 #define STAGE_E_DEVICE         -8   /* a single-launch forward gave up waiting on another workgroup: its outputs are invalid */
 
+#define STAGE_DTYPE_F32  0   /* rows of the last stage's operators only */
 #define STAGE_DTYPE_F16  1
 #define STAGE_DTYPE_BF16 2
 
@@ -343,6 +344,125 @@ int stage_head_attach(Stage* stage, const uint16_t* final_norm, const QuantMatri
  * Errors: INVALID (NULL, no head), CAPACITY (M), HIP. */
 int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out, float* p_out, float* logit_out,
                     float* logits_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The last stage's answer: MXFP4 matrices, sampled tokens and drafted trees.
+ *
+ * MXFP4: blocks of 32 values along a row (the last block of a ragged row is
+ * shorter), each with one E8M0 scale byte, a power of two 2^(byte - 127) (255:
+ * every value of the block is NaN), and E2M1 codes (sign, 2 exponent bits, 1
+ * mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6):
+ *   codes  : uint8 [m][ceil(k/2)]; the low nibble holds the even k;
+ *   scales : uint8 [m][ceil(k/32)].
+ * Tensors are device memory unless said otherwise; row strides `ld` count
+ * elements and may exceed the row length; no alignment beyond the element's is
+ * needed.  stage_mx4_quantize, stage_mx4_dequantize, stage_sample and
+ * stage_tree_accept use no memory of the stage: calls on different streams are
+ * independent and may be captured into a graph.  The other calls use the
+ * stage's workspace, are ordered with the stage's calls like a forward and
+ * refuse a capturing stream (STAGE_E_UNSUPPORTED).  The calling thread's current
+ * device is left as it was.
+ * ------------------------------------------------------------------------ */
+
+/* Largest vocabulary the sampling calls take. */
+#define STAGE_MAX_VOCAB (1 << 20)
+
+/* codes, scales = the rows x [m][k] (F32, F16 or BF16) in MXFP4: a block's scale
+ * is 2^(floor(log2 max|x|) - 2), at least 2^-127; its codes are the nearest
+ * values, ties to the even code, at most 6 times the scale.  A block of zeros has
+ * byte 0, one with a NaN or an infinity byte 255 and zero codes.
+ * Errors: INVALID (NULL, dtype, m or k < 1), SHAPE (ld < k), CAPACITY (m or k
+ * above 2^24, m * k above 2^36), HIP. */
+int stage_mx4_quantize(Stage* stage, const void* x, int dtype, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales,
+                       void* stream);
+
+/* out [m][k] = the values that codes and scales stand for, rounded to `dtype`
+ * (exact in F32, and in BF16 down to its subnormals).  Errors as above. */
+int stage_mx4_dequantize(Stage* stage, const uint8_t* codes, const uint8_t* scales, int m, int k, void* out, int dtype,
+                         int64_t ld, void* stream);
+
+/* A weight matrix W [n][k] in MXFP4, packed once for the products.  Copies codes
+ * and scales (host pointers if on_device == 0); synchronizes the stream.  Bound
+ * to the stage, and freed before it.
+ * Errors: as stage_mx4_quantize, OOM, UNSUPPORTED (capturing stream). */
+typedef struct Mx4Matrix Mx4Matrix;
+int stage_mx4_create(Stage* stage, const uint8_t* codes, const uint8_t* scales, int n, int k, int on_device, void* stream,
+                     Mx4Matrix** out);
+int stage_mx4_free(Mx4Matrix* matrix);
+
+/* out [m][n] = x [m][k] W^T, sums in fp32, rounded once to out_dtype.
+ *   act_bits 16: x (F16 or BF16) enters as it is: as 2 (BF16) or 3 (F16) E4M3
+ *                terms that add up to it, exactly for elements down to 2^-14 of
+ *                their block's largest and to 2^-22 of that one below;
+ *   act_bits  4: x (any dtype) is rounded to MXFP4 first (stage_mx4_quantize).
+ * A row of x with a NaN or an infinity gives NaN, as does a NaN scale of W in
+ * its column.  1 <= m <= STAGE_MAX_PREFILL.  out must not overlap x.  Allocates a
+ * workspace on first use (kept, grown when a larger product comes).
+ * Errors: INVALID (NULL, dtype, act_bits), SHAPE (strides), CAPACITY (m),
+ * UNSUPPORTED (F32 rows with act_bits 16, capturing stream), OOM, HIP. */
+int stage_mx4_product(Mx4Matrix* matrix, const void* x, int x_dtype, int64_t ldx, int m, int act_bits, void* out, int out_dtype,
+                      int64_t ldo, void* stream);
+
+/* stage_head_attach with the LM head [vocab][hidden] in MXFP4 (any group size of
+ * the stage's own weights).  stage_head_top1 and stage_head_sample then use it:
+ * RMSNorm rows rounded to fp16, times the head with act_bits 16.  Synchronizes
+ * the stream.  One head per stage.
+ * Errors: INVALID (NULL), SHAPE (vocab < 1), CAPACITY (vocab), UNSUPPORTED
+ * (already attached, capturing stream), OOM, HIP. */
+int stage_head_attach_mx4(Stage* stage, const uint16_t* final_norm, const uint8_t* codes, const uint8_t* scales, int vocab,
+                          int weights_on_device, void* stream);
+
+/* How a row's token is drawn.  Tokens are ranked highest logit first, lowest
+ * index first among equal ones, with weights exp((logit - max) / temperature).
+ *   temperature : in [1e-3, 1e3]; 0 takes the first of the ranking (p = 1)
+ *   top_k       : keeps the first top_k of the ranking; 0 keeps all
+ *   top_p       : of those, the shortest run whose weight is at least top_p of
+ *                 theirs; 1 keeps all
+ *   min_p       : of those, the ones whose weight is at least min_p of the
+ *                 largest; 0 keeps all
+ * The first of the ranking is always kept.  NaN and -inf logits are not ranked;
+ * +inf ranks as the largest finite number. */
+typedef struct StageSampling {
+    float   temperature;
+    int32_t top_k;
+    float   top_p;
+    float   min_p;
+} StageSampling;
+
+/* For each of the M rows of logits [M][vocab] (F32, F16 or BF16): token_out = the
+ * first kept token, in the ranking's order, at which the running weight passes
+ * u times the kept weight; p_out = its weight over the kept weight.  params: host
+ * [M]; u: device fp32 [M] in [0, 1) (values outside are taken as the nearest
+ * inside).  A row without a ranked token gives token -1 and p 0.
+ * 1 <= M <= STAGE_MAX_ROWS.  The result does not depend on the other rows.
+ * Errors: INVALID (NULL, dtype, params), SHAPE (vocab, ld), CAPACITY (M, vocab),
+ * HIP. */
+int stage_sample(Stage* stage, const void* logits, int dtype, int64_t ld, int M, int vocab, const StageSampling* params,
+                 const float* u, int32_t* token_out, float* p_out, void* stream);
+
+/* stage_head_top1's logits of hidden [M][H], then stage_sample of them.
+ * logits_out (optional, device fp32 [M][vocab]) receives the rows; without it
+ * they stay in a workspace allocated on first use.
+ * Errors: INVALID (NULL, no head, params), CAPACITY (M, vocab), UNSUPPORTED
+ * (capturing stream), OOM, HIP. */
+int stage_head_sample(Stage* stage, const void* hidden, int M, const StageSampling* params, const float* u, int32_t* token_out,
+                      float* p_out, float* logits_out, void* stream);
+
+/* What a verify of drafted trees accepts.  Per slot a tree of n nodes (1 <= n <=
+ * STAGE_MAX_ROWS): parents int32 [n_slots][n], node i's parent in [0, i) (any
+ * other value leaves the node out; node 0 is the root whatever stands there);
+ * tokens [n_slots][n], the tokens drafted (node 0's: the last accepted one);
+ * sampled [n_slots][n], the token drawn at each node (stage_sample of its logits
+ * row).  From node 0 the walk goes to the first child whose token is the one
+ * sampled at the node, until there is none.  All device memory:
+ *   count_out [n_slots]    nodes walked (at least 1: node 0)
+ *   path_out  [n_slots][n] their indices, then -1
+ *   next_out  [n_slots]    the token sampled at the last of them
+ *   keep_out  uint8 [n_slots][n] 1 for the nodes walked: the rows that later
+ *                          forwards keep in their mask
+ * Errors: INVALID (NULL, n_slots < 1), CAPACITY (n), HIP. */
+int stage_tree_accept(Stage* stage, const int32_t* parents, const int32_t* tokens, const int32_t* sampled, int n_slots, int n,
+                      int32_t* count_out, int32_t* path_out, int32_t* next_out, uint8_t* keep_out, void* stream);
 
 /* ------------------------------------------------------------------------
  * First-stage role ("Per-Stage Export Pipeline": the first shard also holds

@@ -12,11 +12,13 @@ ERRORS = {
     -1: "STAGE_E_INVALID", -2: "STAGE_E_SHAPE", -3: "STAGE_E_CAPACITY", -4: "STAGE_E_OOM",
     -5: "STAGE_E_HIP", -6: "STAGE_E_STATE_MISMATCH", -7: "STAGE_E_UNSUPPORTED", -8: "STAGE_E_DEVICE",
 }
+DTYPE_F32 = 0
 DTYPE_F16 = 1
 DTYPE_BF16 = 2
 MAX_ROWS = 64
 STATIC_SCRATCH_BYTES = 64 << 20   # STAGE_STATIC_SCRATCH_BYTES
 MAX_PREFILL = 8192                # STAGE_MAX_PREFILL
+MAX_VOCAB = 1 << 20               # STAGE_MAX_VOCAB
 
 # Every function that include/stage.h declares.
 EXPORTS = (
@@ -27,6 +29,8 @@ EXPORTS = (
     "stage_debug_attn_arm", "stage_debug_attn_read",
     "kv_compact", "kv_capture_size", "kv_capture", "kv_restore", "kv_capture_noalloc",
     "stage_head_attach", "stage_head_top1", "stage_prefill", "stage_embed_attach", "stage_embed",
+    "stage_mx4_quantize", "stage_mx4_dequantize", "stage_mx4_create", "stage_mx4_free", "stage_mx4_product",
+    "stage_head_attach_mx4", "stage_sample", "stage_head_sample", "stage_tree_accept",
 )
 KERNEL_CLASSES = {"qkv": 0, "attn": 1, "oproj": 2, "gateup": 3, "down": 4, "persistent": 5}
 
@@ -59,6 +63,11 @@ class StageRequest(ctypes.Structure):
     ]
 
 
+class StageSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -71,7 +80,7 @@ def load() -> ctypes.CDLL:
         raise ImportError(f"{LIB_PATH} is missing: build it with __graft_entry__.build() "
                           "(python -m paper_2608_19147_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
-    P, I, V = ctypes.POINTER, ctypes.c_int, ctypes.c_void_p
+    P, I, L, V = ctypes.POINTER, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
     sig = {
         "stage_create": (I, [P(StageConfig), P(LayerWeights), I, V, P(V)]),
         "stage_destroy": (I, [V]),
@@ -103,6 +112,15 @@ def load() -> ctypes.CDLL:
         "stage_prefill": (I, [V, V, I, V, V, V, V, V]),
         "stage_embed_attach": (I, [V, V, I, I, V]),
         "stage_embed": (I, [V, V, I, V, V]),
+        "stage_mx4_quantize": (I, [V, V, I, L, I, I, V, V, V]),
+        "stage_mx4_dequantize": (I, [V, V, V, I, I, V, I, L, V]),
+        "stage_mx4_create": (I, [V, V, V, I, I, I, V, P(V)]),
+        "stage_mx4_free": (I, [V]),
+        "stage_mx4_product": (I, [V, V, I, L, I, I, V, I, L, V]),
+        "stage_head_attach_mx4": (I, [V, V, V, V, I, I, V]),
+        "stage_sample": (I, [V, V, I, L, I, I, P(StageSampling), V, V, V, V]),
+        "stage_head_sample": (I, [V, V, I, P(StageSampling), V, V, V, V, V]),
+        "stage_tree_accept": (I, [V, V, V, V, I, I, V, V, V, V, V]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

@@ -340,6 +340,48 @@ hipError_t launch_table_identity(int16_t* table, int S, int cap, int n, hipStrea
 // 1 / sum over tiles of se * exp(max_t - max) (the softmax probability of it).
 hipError_t launch_top1_merge(const float4* part, int M, int ntiles, int32_t* token, float* p, float* logit, hipStream_t st);
 
+// ---- MXFP4 (mx4.hip)
+// W [n][k] in the packed form: 64-row groups, steps of 64 k (k padded to 256),
+//   w: [groups][steps][2 (j)][64 lanes] x 16 bytes: 32 codes of row 64 group + 2 (lane % 32) + j,
+//      k = 64 step + 32 (lane / 32) ..: what one lane feeds to a 32 x 32 x 64 product.  The rows of the two j
+//      alternate, so that a lane's results of both are neighbours in an output row;
+//   s: [groups][steps / 4][2][64 lanes] words: the E8M0 bytes of those codes for 4 steps.
+// Rows from n and columns from k on hold zero codes with scale 1.
+struct Mx4Mat {
+    uint8_t* w; uint32_t* s;
+    int n, k, groups, steps;
+};
+// Activation rows in product form: 32-row tiles, the steps of the matrix, `terms` E4M3 terms (0: one E2M1 term),
+//   a: [tiles][steps][term] fragments of 2 x 64 lanes x 16 bytes (E2M1: 64 x 16); s: [tiles][steps / 4][term][64] words.
+struct Mx4Act {
+    uint8_t* a; uint8_t* s;
+    int tiles, steps, terms;
+};
+hipError_t launch_mx4_quantize(const void* x, int dt, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales, hipStream_t st);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int m, int k, void* out, int dt, int64_t ld,
+                                 hipStream_t st);
+hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx4Mat& w, hipStream_t st);
+hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, int m, int k, hipStream_t st);
+hipError_t launch_mx4_gemm(const Mx4Mat& w, const Mx4Act& a, int m, void* out, int dt, int64_t ld, hipStream_t st);
+// out [m][H] fp16 = RMSNorm(row) * gamma.
+hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st);
+
+// ---- sampling and drafted trees (sample.hip)
+struct SampleRow {
+    double per_t;                                  // 32 / temperature
+    int top_k; float top_p, min_p;
+};
+struct SampleArgs {
+    const void* logits; int dt; size_t ld; int V;
+    const float* u;                                // [m], or null: 0, the first of the ranking
+    int32_t* token; float* p;
+    float* top;                                    // optional [m]: the largest logit
+    SampleRow rows[MAX_ROWS];
+};
+hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st);
+hipError_t launch_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* sampled, int S, int n, int32_t* count,
+                              int32_t* path, int32_t* next, uint8_t* keep, hipStream_t st);
+
 // Row m < n of out [n][H] = row ids[m] (device int32) of table [vocab][H]
 // (2-byte elements, copied bit for bit); an id outside [0, vocab) gives a zero
 // row and sets *err to 1.

@@ -9,7 +9,9 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -160,6 +162,13 @@ struct Stage {
     DevMat head;
     uint16_t* final_norm = nullptr;
     float4* top1_part = nullptr;                       // [MAX_ROWS][head tiles]
+    Mx4Matrix* head4 = nullptr;                        // or an MXFP4 head (stage_head_attach_mx4), freed with the stage
+    uint16_t* head_rows = nullptr;                     // its normalized input rows, fp16 [MAX_ROWS][H]
+    float *logits = nullptr, *head_p = nullptr;        // logits rows [MAX_ROWS][vocab] and [MAX_ROWS], on first need
+    int32_t* head_tok = nullptr;
+    // workspace of the MXFP4 products: activation fragments and their scales, grown on need
+    uint8_t *mx_a = nullptr, *mx_s = nullptr;
+    size_t mx_a_cap = 0, mx_s_cap = 0;
     // first-stage role: token embedding table [embed_vocab][H] in act dtype (stage_embed_attach)
     uint16_t* embed = nullptr;
     int embed_vocab = 0;
@@ -216,6 +225,8 @@ struct Stage {
         (void)hipSetDevice(device);
         (void)hipDeviceSynchronize();
         for (void* p : allocs) (void)hipFree(p);
+        for (void* p : {(void*)mx_a, (void*)mx_s})
+            if (p) (void)hipFree(p);
         if (meta_dev) (void)hipFree(meta_dev);
         for (int i = 0; i < META_RING; ++i) {
             if (meta_host[i]) (void)hipHostFree(meta_host[i]);
@@ -235,6 +246,11 @@ struct Stage {
         *p = (T*)q;
         return STAGE_OK;
     }
+};
+
+struct Mx4Matrix {
+    Stage* stage = nullptr;
+    Mx4Mat m{};
 };
 
 struct KVState {
@@ -487,6 +503,196 @@ std::vector<uint8_t> blob_header(const Stage* st, int S, int Pn, const std::vect
     std::memcpy(h.data(), &hd, sizeof(hd));
     std::memcpy(h.data() + sizeof(hd), lens.data(), 4 * (size_t)S);
     return h;
+}
+
+// ---------------------------------------------------------------- the last stage's answer
+
+// The current device of the calling thread, back when the call ends.
+struct DeviceGuard {
+    int prev = -1;
+    hipError_t err;
+    explicit DeviceGuard(int dev) {
+        err = hipGetDevice(&prev);
+        if (err == hipSuccess && prev != dev) err = hipSetDevice(dev);
+        else prev = -1;
+    }
+    ~DeviceGuard() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+// No C++ exception leaves a C entry.
+template <class F>
+int guarded(F f) noexcept {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        try { return fail(STAGE_E_OOM, "host allocation failed"); } catch (...) { return STAGE_E_OOM; }
+    } catch (...) {
+        try { return fail(STAGE_E_INVALID, "unexpected failure"); } catch (...) { return STAGE_E_INVALID; }
+    }
+}
+
+// A call that uses the stage's workspace cannot be captured: a replay would not be ordered with the stage's other calls.
+int not_captured(hipStream_t s) {
+    hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing(s, &c));
+    return c == hipStreamCaptureStatusNone ? STAGE_OK : fail(STAGE_E_UNSUPPORTED, "this call cannot be captured into a graph");
+}
+
+bool dtype_ok(int dt) { return dt == STAGE_DTYPE_F32 || dt == STAGE_DTYPE_F16 || dt == STAGE_DTYPE_BF16; }
+int any_dt(int dt) { return dt == STAGE_DTYPE_F32 ? (int)DT_F32 : dt_code(dt); }
+
+constexpr int64_t MX4_MAX_DIM = 1 << 24;
+constexpr int64_t MX4_MAX_VALUES = (int64_t)1 << 36;
+
+// Row and column counts of an MXFP4 call.
+int mx4_dims(int64_t rows, int64_t k) {
+    if (rows < 1 || k < 1) return fail(STAGE_E_INVALID, "rows and k must be positive");
+    if (rows > MX4_MAX_DIM || k > MX4_MAX_DIM || rows * k > MX4_MAX_VALUES) return fail(STAGE_E_CAPACITY, "matrix too large");
+    return STAGE_OK;
+}
+
+int grow(uint8_t** p, size_t* cap, size_t bytes) {
+    if (*cap >= bytes) return STAGE_OK;
+    HIP_TRY(hipDeviceSynchronize());                       // queued work may still read the old one
+    if (*p) HIP_TRY(hipFree(*p));
+    *p = nullptr;
+    *cap = 0;
+    if (hipMalloc(p, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        *p = nullptr;
+        return fail(STAGE_E_OOM, "product workspace allocation failed");
+    }
+    *cap = bytes;
+    return STAGE_OK;
+}
+
+// Packs a matrix into device memory of its own.
+int mx4_load(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int k, int on_device, hipStream_t s, Mx4Mat* out) {
+    Mx4Mat w{};
+    w.n = n;
+    w.k = k;
+    w.groups = (n + 63) / 64;
+    w.steps = (k + 255) / 256 * 4;
+    const size_t cb = (size_t)n * ((k + 1) / 2), sb = (size_t)n * ((k + 31) / 32);
+    void *tc = nullptr, *ts = nullptr;
+    auto undo = [&](int rc) {
+        for (void* p : {tc, ts, (void*)w.w, (void*)w.s})
+            if (p) (void)hipFree(p);
+        return rc;
+    };
+    if (hipMalloc(&w.w, (size_t)w.groups * w.steps * 2048) != hipSuccess ||
+        hipMalloc(&w.s, (size_t)w.groups * w.steps * 128) != hipSuccess ||
+        (!on_device && (hipMalloc(&tc, cb) != hipSuccess || hipMalloc(&ts, sb) != hipSuccess))) {
+        (void)hipGetLastError();
+        return undo(fail(STAGE_E_OOM, "MXFP4 matrix allocation failed"));
+    }
+    auto move = [&]() -> int {
+        if (!on_device) {
+            HIP_TRY(hipMemcpyAsync(tc, codes, cb, hipMemcpyHostToDevice, s));
+            HIP_TRY(hipMemcpyAsync(ts, scales, sb, hipMemcpyHostToDevice, s));
+        }
+        HIP_TRY(launch_mx4_pack(on_device ? codes : (const uint8_t*)tc, on_device ? scales : (const uint8_t*)ts, w, s));
+        HIP_TRY(hipStreamSynchronize(s));
+        return STAGE_OK;
+    };
+    const int rc = move();
+    if (rc) return undo(rc);
+    if (tc) (void)hipFree(tc);
+    if (ts) (void)hipFree(ts);
+    *out = w;
+    return STAGE_OK;
+}
+
+constexpr int MX4_PASS = 2048;                             // rows of one product pass
+
+// out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).
+int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
+            hipStream_t s) {
+    const size_t xb = dt == DT_F32 ? 4 : 2, ob = odt == DT_F32 ? 4 : 2;
+    for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
+        const int mm = std::min(MX4_PASS, m - m0);
+        Mx4Act a{};
+        a.terms = act == 4 ? 0 : dt == DT_BF16 ? 2 : 3;
+        a.tiles = (mm + 31) / 32;
+        a.steps = w.steps;
+        const size_t nt = a.terms ? a.terms : 1;
+        int rc = grow(&st->mx_a, &st->mx_a_cap, (size_t)a.tiles * a.steps * nt * (a.terms ? 2048 : 1024));
+        if (!rc) rc = grow(&st->mx_s, &st->mx_s_cap, (size_t)a.tiles * a.steps * nt * 64);
+        if (rc) return rc;
+        a.a = st->mx_a;
+        a.s = st->mx_s;
+        HIP_TRY(launch_mx4_prep(a, (const uint8_t*)x + (size_t)m0 * ldx * xb, dt, ldx, mm, w.k, s));
+        HIP_TRY(launch_mx4_gemm(w, a, mm, (uint8_t*)out + (size_t)m0 * ldo * ob, odt, ldo, s));
+    }
+    return STAGE_OK;
+}
+
+int check_sampling(const StageSampling* params, int M) {
+    for (int i = 0; i < M; ++i) {
+        const StageSampling& q = params[i];
+        const std::string who = "row " + std::to_string(i) + ": ";
+        if (!(q.temperature == 0.0f || (q.temperature >= 1e-3f && q.temperature <= 1e3f)))
+            return fail(STAGE_E_INVALID, who + "temperature must be 0 or in [1e-3, 1e3]");
+        if (q.top_k < 0) return fail(STAGE_E_INVALID, who + "top_k must not be negative");
+        if (!(q.top_p > 0.0f && q.top_p <= 1.0f)) return fail(STAGE_E_INVALID, who + "top_p must be in (0, 1]");
+        if (!(q.min_p >= 0.0f && q.min_p <= 1.0f)) return fail(STAGE_E_INVALID, who + "min_p must be in [0, 1]");
+    }
+    return STAGE_OK;
+}
+
+// params null: the whole softmax, and the first of the ranking (u null).
+int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, const StageSampling* params, const float* u,
+               int32_t* token, float* p, float* top, hipStream_t s) {
+    SampleArgs a{};
+    a.logits = logits;
+    a.dt = dt;
+    a.ld = (size_t)ld;
+    a.V = V;
+    a.u = u;
+    a.token = token;
+    a.p = p;
+    a.top = top;
+    for (int i = 0; i < M; ++i) {
+        a.rows[i] = SampleRow{32.0, 0, 1.0f, 0.0f};
+        if (!params) continue;
+        const StageSampling& q = params[i];
+        if (q.temperature == 0.0f) a.rows[i].top_k = 1;
+        else a.rows[i] = SampleRow{32.0 / (double)q.temperature, q.top_k, q.top_p, q.min_p};
+    }
+    HIP_TRY(launch_sample(a, M, s));
+    return STAGE_OK;
+}
+
+int ensure_logits(Stage* st) {
+    if (st->logits) return STAGE_OK;
+    float* l = nullptr;
+    int rc = st->head_p ? STAGE_OK : st->alloc(&st->head_p, MAX_ROWS);
+    if (!rc && !st->head_tok) rc = st->alloc(&st->head_tok, MAX_ROWS);
+    if (!rc) rc = st->alloc(&l, (size_t)MAX_ROWS * st->vocab);
+    if (!rc) st->logits = l;
+    return rc;
+}
+
+// RMSNorm, the MXFP4 head and, per row, a token: params and u as in sample_run.
+int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params, const float* u, int32_t* token, float* p,
+              float* top, float* logits_out, void* stream) {
+    if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
+    const StageConfig& c = st->cfg;
+    DeviceGuard dev(st->device);
+    HIP_TRY(dev.err);
+    hipStream_t s = (hipStream_t)stream;
+    int rc = not_captured(s);
+    if (!rc && !logits_out) rc = ensure_logits(st);
+    if (rc) return rc;
+    float* lg = logits_out ? logits_out : st->logits;
+    HIP_TRY(order_on(st, s));
+    HIP_TRY(launch_rms_rows(hidden, dt_code(c.act_dtype), st->final_norm, M, c.hidden, c.rms_eps, st->head_rows, s));
+    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F16, c.hidden, M, 16, lg, DT_F32, st->vocab, s))) return rc;
+    if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s))) return rc;
+    HIP_TRY(mark_done(st, s));
+    return STAGE_OK;
 }
 
 }  // namespace
@@ -778,6 +984,7 @@ int stage_create(const StageConfig* cfg, const LayerWeights* layers, int weights
 
 int stage_destroy(Stage* stage) {
     if (!stage) return fail(STAGE_E_INVALID, "stage is NULL");
+    delete stage->head4;                                   // its buffers are the stage's
     delete stage;
     return STAGE_OK;
 }
@@ -1229,7 +1436,7 @@ int kv_restore(KVState* kv, const void* blob, int64_t blob_bytes, int blob_on_de
 
 int stage_head_attach(Stage* st, const uint16_t* final_norm, const QuantMatrix* lm_head, int weights_on_device, void* stream) {
     if (!st || !final_norm || !lm_head || !lm_head->q || !lm_head->scales) return fail(STAGE_E_INVALID, "NULL argument");
-    if (st->head_ok) return fail(STAGE_E_UNSUPPORTED, "the stage already has a head");
+    if (st->head_ok || st->head4) return fail(STAGE_E_UNSUPPORTED, "the stage already has a head");
     const StageConfig& c = st->cfg;
     const int H = c.hidden;
     if (lm_head->n < 1 || lm_head->k != H) return fail(STAGE_E_SHAPE, "lm_head must be [vocab >= 1, hidden]");
@@ -1317,6 +1524,7 @@ int stage_embed(Stage* st, const int32_t* ids, int n, void* hidden_out, void* st
 int stage_head_top1(Stage* st, const void* hidden, int M, int32_t* token_out, float* p_out, float* logit_out,
                     float* logits_out, void* stream) {
     if (!st || !hidden || !token_out || !p_out) return fail(STAGE_E_INVALID, "NULL argument");
+    if (st->head4) return head4_run(st, hidden, M, nullptr, nullptr, token_out, p_out, logit_out, logits_out, stream);
     if (!st->head_ok) return fail(STAGE_E_INVALID, "no head attached (stage_head_attach)");
     if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
     const StageConfig& c = st->cfg;
@@ -1347,6 +1555,177 @@ int stage_head_top1(Stage* st, const void* hidden, int M, int32_t* token_out, fl
     HIP_TRY(launch_top1_merge(st->top1_part, M, st->head.pm.ntiles, token_out, p_out, logit_out, s));
     HIP_TRY(mark_done(st, s));
     return STAGE_OK;
+}
+
+int stage_mx4_quantize(Stage* st, const void* x, int dtype, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales, void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !x || !codes || !scales) return fail(STAGE_E_INVALID, "NULL argument");
+        if (!dtype_ok(dtype)) return fail(STAGE_E_INVALID, "dtype must be F32, F16 or BF16");
+        int rc = mx4_dims(m, k);
+        if (rc) return rc;
+        if (ld < k) return fail(STAGE_E_SHAPE, "row stride below k");
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        HIP_TRY(launch_mx4_quantize(x, any_dt(dtype), ld, m, k, codes, scales, (hipStream_t)stream));
+        return STAGE_OK;
+    });
+}
+
+int stage_mx4_dequantize(Stage* st, const uint8_t* codes, const uint8_t* scales, int m, int k, void* out, int dtype, int64_t ld,
+                         void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !codes || !scales || !out) return fail(STAGE_E_INVALID, "NULL argument");
+        if (!dtype_ok(dtype)) return fail(STAGE_E_INVALID, "dtype must be F32, F16 or BF16");
+        int rc = mx4_dims(m, k);
+        if (rc) return rc;
+        if (ld < k) return fail(STAGE_E_SHAPE, "row stride below k");
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        HIP_TRY(launch_mx4_dequantize(codes, scales, m, k, out, any_dt(dtype), ld, (hipStream_t)stream));
+        return STAGE_OK;
+    });
+}
+
+int stage_mx4_create(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int k, int on_device, void* stream,
+                     Mx4Matrix** out) {
+    return guarded([&]() -> int {
+        if (!st || !codes || !scales || !out) return fail(STAGE_E_INVALID, "NULL argument");
+        *out = nullptr;
+        int rc = mx4_dims(n, k);
+        if (rc) return rc;
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        if ((rc = not_captured((hipStream_t)stream))) return rc;
+        Mx4Matrix* m = new Mx4Matrix();
+        m->stage = st;
+        if ((rc = mx4_load(st, codes, scales, n, k, on_device, (hipStream_t)stream, &m->m))) {
+            delete m;
+            return rc;
+        }
+        *out = m;
+        return STAGE_OK;
+    });
+}
+
+int stage_mx4_free(Mx4Matrix* m) {
+    return guarded([&]() -> int {
+        if (!m) return fail(STAGE_E_INVALID, "matrix is NULL");
+        DeviceGuard dev(m->stage->device);
+        (void)hipDeviceSynchronize();
+        (void)hipFree(m->m.w);
+        (void)hipFree(m->m.s);
+        delete m;
+        return STAGE_OK;
+    });
+}
+
+int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int m, int act_bits, void* out, int out_dtype,
+                      int64_t ldo, void* stream) {
+    return guarded([&]() -> int {
+        if (!w || !x || !out) return fail(STAGE_E_INVALID, "NULL argument");
+        if (!dtype_ok(x_dtype) || !dtype_ok(out_dtype)) return fail(STAGE_E_INVALID, "dtypes must be F32, F16 or BF16");
+        if (act_bits != 4 && act_bits != 16) return fail(STAGE_E_INVALID, "act_bits must be 4 or 16");
+        if (act_bits == 16 && x_dtype == STAGE_DTYPE_F32) return fail(STAGE_E_UNSUPPORTED, "F32 rows need act_bits 4");
+        if (m < 1 || m > STAGE_MAX_PREFILL) return fail(STAGE_E_CAPACITY, "m must be in [1, STAGE_MAX_PREFILL]");
+        if (ldx < w->m.k || ldo < w->m.n) return fail(STAGE_E_SHAPE, "row stride below the row length");
+        Stage* st = w->stage;
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        hipStream_t s = (hipStream_t)stream;
+        int rc = not_captured(s);
+        if (rc) return rc;
+        HIP_TRY(order_on(st, s));
+        rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s);
+        if (rc) return rc;
+        HIP_TRY(mark_done(st, s));
+        return STAGE_OK;
+    });
+}
+
+int stage_head_attach_mx4(Stage* st, const uint16_t* final_norm, const uint8_t* codes, const uint8_t* scales, int vocab,
+                          int weights_on_device, void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !final_norm || !codes || !scales) return fail(STAGE_E_INVALID, "NULL argument");
+        if (st->head_ok || st->head4) return fail(STAGE_E_UNSUPPORTED, "the stage already has a head");
+        if (vocab < 1) return fail(STAGE_E_SHAPE, "vocab must be >= 1");
+        if (vocab > STAGE_MAX_VOCAB) return fail(STAGE_E_CAPACITY, "vocab exceeds STAGE_MAX_VOCAB");
+        const int H = st->cfg.hidden;
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        hipStream_t s = (hipStream_t)stream;
+        int rc = not_captured(s);
+        if (rc) return rc;
+        HIP_TRY(order_on(st, s));
+        uint16_t *fn = nullptr, *rows = nullptr;
+        if ((rc = st->alloc(&fn, (size_t)H)) || (rc = st->alloc(&rows, (size_t)MAX_ROWS * H))) return rc;
+        HIP_TRY(hipMemcpyAsync(fn, final_norm, (size_t)H * 2, weights_on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice, s));
+        std::unique_ptr<Mx4Matrix> m(new Mx4Matrix());
+        m->stage = st;
+        if ((rc = mx4_load(st, codes, scales, vocab, H, weights_on_device, s, &m->m))) return rc;
+        st->allocs.push_back(m->m.w);
+        st->allocs.push_back(m->m.s);
+        st->weight_bytes += (int64_t)m->m.groups * m->m.steps * (2048 + 128) + 2 * (int64_t)H;
+        st->final_norm = fn;
+        st->head_rows = rows;
+        st->vocab = vocab;
+        st->head4 = m.release();
+        HIP_TRY(mark_done(st, s));
+        return STAGE_OK;
+    });
+}
+
+int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, int vocab, const StageSampling* params, const float* u,
+                 int32_t* token_out, float* p_out, void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !logits || !params || !u || !token_out || !p_out) return fail(STAGE_E_INVALID, "NULL argument");
+        if (!dtype_ok(dtype)) return fail(STAGE_E_INVALID, "dtype must be F32, F16 or BF16");
+        if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
+        if (vocab < 1) return fail(STAGE_E_SHAPE, "vocab must be >= 1");
+        if (vocab > STAGE_MAX_VOCAB) return fail(STAGE_E_CAPACITY, "vocab exceeds STAGE_MAX_VOCAB");
+        if (ld < vocab) return fail(STAGE_E_SHAPE, "row stride below vocab");
+        int rc = check_sampling(params, M);
+        if (rc) return rc;
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, (hipStream_t)stream);
+    });
+}
+
+int stage_head_sample(Stage* st, const void* hidden, int M, const StageSampling* params, const float* u, int32_t* token_out,
+                      float* p_out, float* logits_out, void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !hidden || !params || !u || !token_out || !p_out) return fail(STAGE_E_INVALID, "NULL argument");
+        if (!st->head_ok && !st->head4) return fail(STAGE_E_INVALID, "no head attached (stage_head_attach, stage_head_attach_mx4)");
+        if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
+        if (st->vocab > STAGE_MAX_VOCAB) return fail(STAGE_E_CAPACITY, "vocab exceeds STAGE_MAX_VOCAB");
+        int rc = check_sampling(params, M);
+        if (rc) return rc;
+        if (st->head4) return head4_run(st, hidden, M, params, u, token_out, p_out, nullptr, logits_out, stream);
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        hipStream_t s = (hipStream_t)stream;
+        if ((rc = not_captured(s)) || (rc = ensure_logits(st))) return rc;
+        float* lg = logits_out ? logits_out : st->logits;
+        if ((rc = stage_head_top1(st, hidden, M, st->head_tok, st->head_p, nullptr, lg, stream))) return rc;
+        if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token_out, p_out, nullptr, s))) return rc;
+        HIP_TRY(mark_done(st, s));
+        return STAGE_OK;
+    });
+}
+
+int stage_tree_accept(Stage* st, const int32_t* parents, const int32_t* tokens, const int32_t* sampled, int n_slots, int n,
+                      int32_t* count_out, int32_t* path_out, int32_t* next_out, uint8_t* keep_out, void* stream) {
+    return guarded([&]() -> int {
+        if (!st || !parents || !tokens || !sampled || !count_out || !path_out || !next_out || !keep_out)
+            return fail(STAGE_E_INVALID, "NULL argument");
+        if (n_slots < 1) return fail(STAGE_E_INVALID, "n_slots must be positive");
+        if (n < 1 || n > MAX_ROWS) return fail(STAGE_E_CAPACITY, "n must be in [1, STAGE_MAX_ROWS]");
+        DeviceGuard dev(st->device);
+        HIP_TRY(dev.err);
+        HIP_TRY(launch_tree_accept(parents, tokens, sampled, n_slots, n, count_out, path_out, next_out, keep_out,
+                                   (hipStream_t)stream));
+        return STAGE_OK;
+    });
 }
 
 int stage_prefill(Stage* st, KVState* kv, int n, const int32_t* positions, const uint8_t* past_mask, const void* hidden_in,

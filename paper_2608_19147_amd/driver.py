@@ -57,3 +57,37 @@ class VerifyDriver:
         keep = (np.arange(k + 1)[None, :] <= lead[:, None]).astype(np.uint8)
         self.valid = np.concatenate([self.valid, keep], axis=1)
         return 1 + lead
+
+    def tree_inputs(self, parents: np.ndarray, beam_idx: Optional[np.ndarray] = None):
+        """(positions [S, n], mask_rows [S, n, P + n], beam_idx) of the forward that
+        verifies a drafted tree per slot: parents [S, n], every node's parent before
+        it, node 0 (the last accepted token) the root.  A node sees the slot's valid
+        rows, its ancestors and itself; its position is the number of valid rows plus
+        its depth.  Applies the reorder to the valid masks first (it persists)."""
+        if beam_idx is not None:
+            beam_idx = np.asarray(beam_idx, np.int32)
+            self.valid = self.valid[beam_idx]
+        parents = np.asarray(parents)
+        s, n = parents.shape
+        if s != self.n_slots or n < 1 or (n > 1 and not ((parents[:, 1:] >= 0) & (parents[:, 1:] < np.arange(1, n))).all()):
+            raise ValueError("parents must be [slots, nodes], each node's parent before it")
+        see = np.zeros((s, n, n), np.uint8)
+        depth = np.zeros((s, n), np.int32)
+        slot = np.arange(s)
+        see[:, 0, 0] = 1
+        for i in range(1, n):
+            see[:, i] = see[slot, parents[:, i]]
+            see[:, i, i] = 1
+            depth[:, i] = depth[slot, parents[:, i]] + 1
+        past = np.broadcast_to(self.valid[:, None, :], (s, n, self.physical_len))
+        positions = self.valid.sum(axis=1).astype(np.int32)[:, None] + depth
+        return positions, np.concatenate([past, see], axis=2), beam_idx
+
+    def accept_tree(self, keep: np.ndarray) -> np.ndarray:
+        """Record which nodes of the last ``tree_inputs`` forward were accepted: keep
+        [S, n] of ``Stage.tree_accept``.  Returns the nodes kept per slot."""
+        keep = (np.asarray(keep) != 0).astype(np.uint8)
+        if keep.ndim != 2 or keep.shape[0] != self.n_slots:
+            raise ValueError("keep must be [slots, nodes]")
+        self.valid = np.concatenate([self.valid, keep], axis=1)
+        return keep.sum(axis=1).astype(np.int32)

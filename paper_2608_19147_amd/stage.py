@@ -22,17 +22,22 @@ _DT = {"f16": _lib.DTYPE_F16, "bf16": _lib.DTYPE_BF16}
 _TORCH = {"f16": torch.float16, "bf16": torch.bfloat16}
 
 
+_DT_OF = {torch.float32: _lib.DTYPE_F32, torch.float16: _lib.DTYPE_F16, torch.bfloat16: _lib.DTYPE_BF16}
+
 _LIVE_STATES: "weakref.WeakSet[KVState]" = weakref.WeakSet()
+_LIVE_MATRICES: "weakref.WeakSet[Mx4Matrix]" = weakref.WeakSet()
 _LIVE_STAGES: "weakref.WeakSet[Stage]" = weakref.WeakSet()
 
 
 def close_all() -> None:
-    """Free every live KV state, then every live stage.  Registered with
+    """Free every live KV state and MXFP4 matrix, then every live stage.  Registered with
     atexit, so the library's device synchronizations and frees run while the
     interpreter and the HIP runtime are both still whole, rather than from
     ``__del__`` during interpreter shutdown."""
     for kv in list(_LIVE_STATES):
         kv.free()
+    for m in list(_LIVE_MATRICES):
+        m.free()
     for st in list(_LIVE_STAGES):
         st.close()
 
@@ -50,6 +55,37 @@ def _ptr(a) -> int:
     if isinstance(a, torch.Tensor):
         return a.data_ptr()
     return a.ctypes.data
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """The row stride of a device [m, k] tensor of a float type whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _DT_OF:
+        raise ValueError(f"{name} must be a device [rows, columns] tensor in float32, float16 or bfloat16")
+    if t.shape[0] < 1 or t.shape[1] < 1:
+        raise ValueError(f"{name} is empty")
+    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}'s rows must be contiguous and must not overlap")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+
+
+def _ints(t: torch.Tensor, name: str, shape, device) -> int:
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+class _Call:
+    """The stream a call runs on, and the tensors made for it: they are allocated
+    in that stream's pool, so a later reuse of their memory is ordered behind it."""
+
+    def __init__(self, stream, device):
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self.device = device
+        self.ptr = ctypes.c_void_p(int(self.stream.cuda_stream))
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
 
 class Stage:
@@ -105,6 +141,9 @@ class Stage:
             for kv in list(_LIVE_STATES):
                 if kv.stage is self:
                     kv.free()
+            for m in list(_LIVE_MATRICES):
+                if m.stage is self:
+                    m.free()
             check(self.lib.stage_destroy(self.handle))
             self.handle = None
 
@@ -202,6 +241,102 @@ class Stage:
                                        ctypes.c_void_p(_stream_ptr(stream))))
         return tok, p, lg, full
 
+    def attach_head_mx4(self, final_norm: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+        """Final RMSNorm weight [H] (act dtype) and an MXFP4 LM head: codes uint8
+        [vocab, ceil(H/2)], scales uint8 [vocab, ceil(H/32)] (all on the host or
+        all on the device)."""
+        vocab = int(codes.shape[0])
+        if tuple(final_norm.shape) != (self.shape.hidden,) or final_norm.dtype != self.act_dtype:
+            raise ValueError("final_norm must be [hidden] in the activation dtype")
+        on_dev = _check_mx4(codes, scales, self.shape.hidden)
+        fn = final_norm.contiguous()
+        if fn.is_cuda != bool(on_dev):
+            raise ValueError("final_norm, codes and scales must be on one side")
+        call = _Call(stream, codes.device if on_dev else None)
+        check(self.lib.stage_head_attach_mx4(self.handle, ctypes.c_void_p(fn.data_ptr()), ctypes.c_void_p(codes.data_ptr()),
+                                             ctypes.c_void_p(scales.data_ptr()), vocab, on_dev, call.ptr))
+        self.vocab = vocab
+
+    def head_sample(self, hidden: torch.Tensor, params, u: torch.Tensor, with_logits: bool = False, stream=None):
+        """(token int32 [M], p fp32 [M], logits fp32 [M, vocab] or None): one token
+        drawn per row of ``hidden`` through the attached head; ``params`` and ``u``
+        as in ``sample``."""
+        if hidden.dim() != 2 or hidden.shape[1] != self.shape.hidden or hidden.dtype != self.act_dtype or not hidden.is_cuda \
+                or not hidden.is_contiguous():
+            raise ValueError("hidden must be a contiguous device [M, hidden] tensor in the activation dtype")
+        M = int(hidden.shape[0])
+        call = _Call(stream, hidden.device)
+        arr = _sampling(params, M)
+        _check_u(u, M, hidden.device)
+        tok, p = call.empty(M, torch.int32), call.empty(M, torch.float32)
+        full = call.empty((M, getattr(self, "vocab", 1)), torch.float32) if with_logits else None
+        check(self.lib.stage_head_sample(self.handle, ctypes.c_void_p(hidden.data_ptr()), M, arr, ctypes.c_void_p(u.data_ptr()),
+                                         ctypes.c_void_p(tok.data_ptr()), ctypes.c_void_p(p.data_ptr()),
+                                         ctypes.c_void_p(full.data_ptr() if full is not None else None), call.ptr))
+        return tok, p, full
+
+    def sample(self, logits: torch.Tensor, params, u: torch.Tensor, stream=None):
+        """(token int32 [M], p fp32 [M]): one token drawn per row of ``logits``
+        [M, vocab] (float32, float16 or bfloat16; rows may be part of wider ones)
+        by ``params`` (a ``Sampling``, or one per row) and ``u`` fp32 [M] in [0, 1)."""
+        ld = _rows(logits, "logits")
+        M, V = (int(v) for v in logits.shape)
+        call = _Call(stream, logits.device)
+        arr = _sampling(params, M)
+        _check_u(u, M, logits.device)
+        tok, p = call.empty(M, torch.int32), call.empty(M, torch.float32)
+        check(self.lib.stage_sample(self.handle, ctypes.c_void_p(logits.data_ptr()), _DT_OF[logits.dtype], ld, M, V, arr,
+                                    ctypes.c_void_p(u.data_ptr()), ctypes.c_void_p(tok.data_ptr()),
+                                    ctypes.c_void_p(p.data_ptr()), call.ptr))
+        return tok, p
+
+    def tree_accept(self, parents: torch.Tensor, tokens: torch.Tensor, sampled: torch.Tensor, stream=None):
+        """(count int32 [S], path int32 [S, n], next int32 [S], keep uint8 [S, n]) of
+        the walk of S drafted trees of n nodes: device int32 [S, n] parents (before
+        their children; node 0 is the root), drafted tokens and the tokens sampled
+        at the nodes.  ``path`` holds the walked nodes, then -1; ``keep`` marks them;
+        ``next`` is the token sampled at the last one."""
+        if parents.dim() != 2 or not parents.is_cuda:
+            raise ValueError("parents must be a device [slots, nodes] tensor")
+        S, n = (int(v) for v in parents.shape)
+        ptrs = [_ints(t, name, (S, n), parents.device)
+                for t, name in ((parents, "parents"), (tokens, "tokens"), (sampled, "sampled"))]
+        call = _Call(stream, parents.device)
+        count, path = call.empty(S, torch.int32), call.empty((S, n), torch.int32)
+        nxt, keep = call.empty(S, torch.int32), call.empty((S, n), torch.uint8)
+        check(self.lib.stage_tree_accept(self.handle, *(ctypes.c_void_p(v) for v in ptrs), S, n,
+                                         *(ctypes.c_void_p(t.data_ptr()) for t in (count, path, nxt, keep)), call.ptr))
+        return count, path, nxt, keep
+
+    def mx4_quantize(self, x: torch.Tensor, stream=None):
+        """(codes uint8 [m, ceil(k/2)], scales uint8 [m, ceil(k/32)]): the rows of a
+        device [m, k] tensor (float32, float16 or bfloat16) in MXFP4."""
+        ld = _rows(x, "x")
+        m, k = (int(v) for v in x.shape)
+        call = _Call(stream, x.device)
+        codes, scales = call.empty((m, (k + 1) // 2), torch.uint8), call.empty((m, (k + 31) // 32), torch.uint8)
+        check(self.lib.stage_mx4_quantize(self.handle, ctypes.c_void_p(x.data_ptr()), _DT_OF[x.dtype], ld, m, k,
+                                          ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()), call.ptr))
+        return codes, scales
+
+    def mx4_dequantize(self, codes: torch.Tensor, scales: torch.Tensor, k: int, out_dtype=torch.float32, stream=None) -> torch.Tensor:
+        """The values [m, k] that device codes and scales stand for."""
+        if not _check_mx4(codes, scales, k):
+            raise ValueError("codes and scales must be device tensors")
+        if out_dtype not in _DT_OF:
+            raise ValueError("out_dtype must be float32, float16 or bfloat16")
+        m = int(codes.shape[0])
+        call = _Call(stream, codes.device)
+        out = call.empty((m, k), out_dtype)
+        check(self.lib.stage_mx4_dequantize(self.handle, ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()),
+                                            m, int(k), ctypes.c_void_p(out.data_ptr()), _DT_OF[out_dtype], int(k), call.ptr))
+        return out
+
+    def mx4_matrix(self, codes: torch.Tensor, scales: torch.Tensor, k: int, stream=None) -> "Mx4Matrix":
+        """A weight matrix [n, k] in MXFP4 for products, packed once: codes uint8
+        [n, ceil(k/2)] and scales uint8 [n, ceil(k/32)], on the host or the device."""
+        return Mx4Matrix(self, codes, scales, k, stream)
+
     def attach_embedding(self, table: torch.Tensor, on_device: bool = False, stream=None) -> None:
         """Token embedding table [vocab, H] in the act dtype (first-stage role)."""
         t = table.contiguous() if on_device else table.detach().cpu().contiguous()
@@ -276,6 +411,93 @@ class Stage:
         check(self.lib.stage_forward(self.handle, arr, len(requests), ctypes.c_void_p(hidden_in.data_ptr()),
                                      ctypes.c_void_p(hidden_out.data_ptr()), ctypes.c_void_p(_stream_ptr(stream))))
         return hidden_out
+
+
+def _check_mx4(codes: torch.Tensor, scales: torch.Tensor, k: int) -> int:
+    """1 if the MXFP4 pair of rows of k is on the device, 0 on the host."""
+    ok = codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 2 and scales.dim() == 2 and k >= 1 \
+        and tuple(codes.shape) == (scales.shape[0], (k + 1) // 2) and scales.shape[1] == (k + 31) // 32 and codes.shape[0] >= 1
+    if not ok:
+        raise ValueError(f"codes and scales must be uint8 [rows, {(k + 1) // 2}] and [rows, {(k + 31) // 32}]")
+    if codes.device != scales.device or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("codes and scales must be contiguous and on one device")
+    return int(codes.is_cuda)
+
+
+def _check_u(u: torch.Tensor, M: int, device) -> None:
+    if u.dtype != torch.float32 or tuple(u.shape) != (M,) or u.device != device or not u.is_contiguous():
+        raise ValueError(f"u must be a contiguous float32 [{M}] tensor on {device}")
+
+
+@dataclass(frozen=True)
+class Sampling:
+    """How a row's token is drawn: weights exp((logit - max) / temperature) over
+    the tokens ranked highest logit first (lowest index first among equals), of
+    which top_k keeps the first (0: all), top_p the shortest run that holds its
+    share of their weight (1: all), min_p those of at least min_p of the largest
+    weight (0: all).  Temperature 0 takes the first."""
+
+    temperature: float = 1.0
+    top_k: int = 0
+    top_p: float = 1.0
+    min_p: float = 0.0
+
+
+def _sampling(params, M: int):
+    ps = [params] * M if isinstance(params, Sampling) else list(params)
+    if len(ps) != M:
+        raise ValueError(f"{len(ps)} sampling parameters for {M} rows")
+    arr = (_lib.StageSampling * max(1, M))()
+    for a, q in zip(arr, ps):
+        a.temperature, a.top_k, a.top_p, a.min_p = float(q.temperature), int(q.top_k), float(q.top_p), float(q.min_p)
+    return arr
+
+
+class Mx4Matrix:
+    """A weight matrix W [n, k] in MXFP4, packed for products (``Stage.mx4_matrix``)."""
+
+    def __init__(self, stage: Stage, codes: torch.Tensor, scales: torch.Tensor, k: int, stream=None):
+        on_dev = _check_mx4(codes, scales, k)
+        self.stage, self.lib = stage, stage.lib
+        self.n, self.k = int(codes.shape[0]), int(k)
+        call = _Call(stream, codes.device if on_dev else None)
+        h = ctypes.c_void_p()
+        check(self.lib.stage_mx4_create(stage.handle, ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()),
+                                        self.n, self.k, on_dev, call.ptr, ctypes.byref(h)))
+        self.handle = h
+        _LIVE_MATRICES.add(self)
+
+    def free(self) -> None:
+        if getattr(self, "handle", None):
+            check(self.lib.stage_mx4_free(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    def product(self, x: torch.Tensor, act_bits: int = 16, out_dtype: Optional[torch.dtype] = None,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """x W^T [m, n] of device rows x [m, k]: 16-bit rows as they are (``act_bits``
+        16) or rounded to MXFP4 first (4, also float32 rows), in ``out_dtype``
+        (x's by default) or into ``out`` [m, n], whose rows may be part of wider ones."""
+        ldx = _rows(x, "x")
+        m = int(x.shape[0])
+        if x.shape[1] != self.k:
+            raise ValueError(f"x has {x.shape[1]} columns, the matrix {self.k}")
+        call = _Call(stream, x.device)
+        if out is None:
+            if (out_dtype or x.dtype) not in _DT_OF:
+                raise ValueError("out_dtype must be float32, float16 or bfloat16")
+            out = call.empty((m, self.n), out_dtype or x.dtype)
+        elif tuple(out.shape) != (m, self.n) or out.device != x.device or out_dtype not in (None, out.dtype):
+            raise ValueError(f"out must be a [{m}, {self.n}] tensor on {x.device}")
+        ldo = _rows(out, "out")
+        check(self.lib.stage_mx4_product(self.handle, ctypes.c_void_p(x.data_ptr()), _DT_OF[x.dtype], ldx, m, int(act_bits),
+                                         ctypes.c_void_p(out.data_ptr()), _DT_OF[out.dtype], ldo, call.ptr))
+        return out
 
 
 @dataclass
