@@ -63,11 +63,6 @@ class StageRequest(ctypes.Structure):
     ]
 
 
-class StageSampling(ctypes.Structure):
-    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
-                ("min_p", ctypes.c_float)]
-
-
 _lib = None
 
 
@@ -118,8 +113,8 @@ def load() -> ctypes.CDLL:
         "stage_mx4_free": (I, [V]),
         "stage_mx4_product": (I, [V, V, I, L, I, I, V, I, L, V]),
         "stage_head_attach_mx4": (I, [V, V, V, V, I, I, V]),
-        "stage_sample": (I, [V, V, I, L, I, I, P(StageSampling), V, V, V, V]),
-        "stage_head_sample": (I, [V, V, I, P(StageSampling), V, V, V, V, V]),
+        "stage_sample": (I, [V, V, I, L, I, I, V, V, V, V, V]),
+        "stage_head_sample": (I, [V, V, I, V, V, V, V, V, V]),
         "stage_tree_accept": (I, [V, V, V, V, I, I, V, V, V, V, V]),
     }
     for name, (res, args) in sig.items():

@@ -9,12 +9,19 @@
 // Products: out[m][n] = sum_k x[m][k] W[n][k], W in MXFP4.  The scaled matrix
 // instruction takes E2M1 codes with their scale bytes as they are, so weights
 // are never unpacked.  Activations of 16 bits go in as sums of E4M3 terms, each
-// with its own block scale: t1 = E4M3(x), t2 = E4M3(x - t1), ...  An E4M3 value
-// has 4 significant bits and the rounding error of one is at most half its last
-// place, a number of 4 fewer bits with its sign, so two terms hold bf16's 8 bits
-// and three f16's 11 bits exactly (down to 2^-14 of the block's largest value;
-// below that the error is at most 2^-18 of it after the first term and shrinks
-// by 2^4 with each further one).  Activations of 4 bits are one E2M1 term.
+// with its own block scales: t1 = E4M3(x), t2 = E4M3(x - t1), ...  Measured on
+// the instruction: the 8 products of neighbouring elements are added in units of
+// 2^-13 of the largest one's power of two, what is below is cut off; groups of 8
+// and the accumulator are added as fp32.  A term is therefore scaled to a largest
+// magnitude in [1, 2): E4M3's smallest step is 2^-9, so that every product is a
+// multiple of 2^-10 and below 12, and nothing is cut.  (Scaled to E4M3's full
+// range instead, results of 32 bits were 1e-5 off.)  What a term leaves of x is
+// at most 2^-4 of x and of a block at most 2^-4 of its largest magnitude (half
+// the last of 4 bits), or 2^-10 where E4M3's smallest step decides: two terms
+// come within 2^-14 of a block's largest magnitude, three within 2^-18, and the
+// larger elements of bf16 (8 significant bits) and f16 (11) are exact in two and
+// three terms.  Two terms are taken for bf16 rows with 16-bit results, three
+// otherwise.  Activations of 4 bits are one E2M1 term.
 #include "device.h"
 
 namespace stg {
@@ -178,8 +185,9 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
         *(u32x2*)(a + frag + (b * 32 + r) * 16 + (p & 1) * 8) = o;
         if (!(p & 1)) as[sc] = (uint8_t)byte;
     } else {
-        int byte = (int)block_byte(top, 7);                        // largest scaled magnitude in [2^7, 2^8)
-        const bool bad = byte == 255;
+        int byte = (int)block_byte(top, 0);                        // largest scaled magnitude in [1, 2)
+        const bool bad = top >= 0x7f800000u;
+        byte = min(byte, 252);
         const float inv = bad ? 0.0f : e8m0_inv((uint32_t)byte);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = bad ? 0.0f : v[i] * inv;
@@ -204,7 +212,7 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
             if (!(p & 1)) as[sc + (size_t)t * 256] = (uint8_t)(bad ? 255 : byte);
             if (t + 1 < NT) {
                 rest = max(rest, (uint32_t)__shfl_xor((int)rest, 1));
-                int e = rest ? (int)(rest >> 23) - 134 : 0;        // the rest's largest magnitude to [2^7, 2^8)
+                int e = rest ? (int)(rest >> 23) - 127 : 0;        // the rest's largest magnitude to [1, 2)
                 e = max(e, max(-byte, -127));
                 byte += e;
                 const float up = __uint_as_float((uint32_t)(127 - e) << 23);

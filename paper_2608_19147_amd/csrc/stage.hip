@@ -614,7 +614,7 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
     for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
         const int mm = std::min(MX4_PASS, m - m0);
         Mx4Act a{};
-        a.terms = act == 4 ? 0 : dt == DT_BF16 ? 2 : 3;
+        a.terms = act == 4 ? 0 : dt == DT_BF16 && odt != DT_F32 ? 2 : 3;
         a.tiles = (mm + 31) / 32;
         a.steps = w.steps;
         const size_t nt = a.terms ? a.terms : 1;
@@ -632,12 +632,13 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
 int check_sampling(const StageSampling* params, int M) {
     for (int i = 0; i < M; ++i) {
         const StageSampling& q = params[i];
-        const std::string who = "row " + std::to_string(i) + ": ";
+        const char* bad = nullptr;
         if (!(q.temperature == 0.0f || (q.temperature >= 1e-3f && q.temperature <= 1e3f)))
-            return fail(STAGE_E_INVALID, who + "temperature must be 0 or in [1e-3, 1e3]");
-        if (q.top_k < 0) return fail(STAGE_E_INVALID, who + "top_k must not be negative");
-        if (!(q.top_p > 0.0f && q.top_p <= 1.0f)) return fail(STAGE_E_INVALID, who + "top_p must be in (0, 1]");
-        if (!(q.min_p >= 0.0f && q.min_p <= 1.0f)) return fail(STAGE_E_INVALID, who + "min_p must be in [0, 1]");
+            bad = "temperature must be 0 or in [1e-3, 1e3]";
+        else if (q.top_k < 0) bad = "top_k must not be negative";
+        else if (!(q.top_p > 0.0f && q.top_p <= 1.0f)) bad = "top_p must be in (0, 1]";
+        else if (!(q.min_p >= 0.0f && q.min_p <= 1.0f)) bad = "min_p must be in [0, 1]";
+        if (bad) return fail(STAGE_E_INVALID, "row " + std::to_string(i) + ": " + bad);
     }
     return STAGE_OK;
 }

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import atexit
 import ctypes
+import struct
 import weakref
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -16,6 +17,9 @@ import torch
 
 from . import _lib
 from ._lib import check
+
+# the current stream's handle of a device (what torch.cuda.current_stream(i).cuda_stream holds, without its objects)
+from torch._C import _cuda_getCurrentRawStream as _raw_stream
 
 MATRIX_NAMES = ("wq", "wk", "wv", "wo", "wg", "wu", "wd")
 _DT = {"f16": _lib.DTYPE_F16, "bf16": _lib.DTYPE_BF16}
@@ -61,31 +65,27 @@ def _rows(t: torch.Tensor, name: str) -> int:
     """The row stride of a device [m, k] tensor of a float type whose rows are contiguous."""
     if t.dim() != 2 or not t.is_cuda or t.dtype not in _DT_OF:
         raise ValueError(f"{name} must be a device [rows, columns] tensor in float32, float16 or bfloat16")
-    if t.shape[0] < 1 or t.shape[1] < 1:
+    m, k = t.shape
+    if m < 1 or k < 1:
         raise ValueError(f"{name} is empty")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    ld, step = t.stride()
+    if k > 1 and step != 1 or m > 1 and ld < k:
         raise ValueError(f"{name}'s rows must be contiguous and must not overlap")
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+    return max(ld, k)
 
 
-def _ints(t: torch.Tensor, name: str, shape, device) -> int:
-    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
-    return t.data_ptr()
+def _on(stream, device):
+    """(stream handle, maker of tensors) of a call on ``device``: the tensors come
+    from the pool of the stream that writes them, so that a later use of their
+    memory is ordered behind it."""
+    if stream is None:
+        return _raw_stream(device.index), torch.empty
 
+    def empty(shape, dtype, device):
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
 
-class _Call:
-    """The stream a call runs on, and the tensors made for it: they are allocated
-    in that stream's pool, so a later reuse of their memory is ordered behind it."""
-
-    def __init__(self, stream, device):
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        self.device = device
-        self.ptr = ctypes.c_void_p(int(self.stream.cuda_stream))
-
-    def empty(self, shape, dtype) -> torch.Tensor:
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+    return int(stream.cuda_stream), empty
 
 
 class Stage:
@@ -243,19 +243,16 @@ class Stage:
 
     def attach_head_mx4(self, final_norm: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
         """Final RMSNorm weight [H] (act dtype) and an MXFP4 LM head: codes uint8
-        [vocab, ceil(H/2)], scales uint8 [vocab, ceil(H/32)] (all on the host or
-        all on the device)."""
-        vocab = int(codes.shape[0])
-        if tuple(final_norm.shape) != (self.shape.hidden,) or final_norm.dtype != self.act_dtype:
-            raise ValueError("final_norm must be [hidden] in the activation dtype")
+        [vocab, ceil(H/2)], scales uint8 [vocab, ceil(H/32)], all on the host or
+        all on the device."""
         on_dev = _check_mx4(codes, scales, self.shape.hidden)
-        fn = final_norm.contiguous()
-        if fn.is_cuda != bool(on_dev):
-            raise ValueError("final_norm, codes and scales must be on one side")
-        call = _Call(stream, codes.device if on_dev else None)
-        check(self.lib.stage_head_attach_mx4(self.handle, ctypes.c_void_p(fn.data_ptr()), ctypes.c_void_p(codes.data_ptr()),
-                                             ctypes.c_void_p(scales.data_ptr()), vocab, on_dev, call.ptr))
-        self.vocab = vocab
+        if tuple(final_norm.shape) != (self.shape.hidden,) or final_norm.dtype != self.act_dtype or not final_norm.is_contiguous():
+            raise ValueError("final_norm must be a contiguous [hidden] tensor in the activation dtype")
+        if final_norm.device != codes.device:
+            raise ValueError("final_norm, codes and scales must be on one device")
+        check(self.lib.stage_head_attach_mx4(self.handle, final_norm.data_ptr(), codes.data_ptr(), scales.data_ptr(),
+                                             codes.shape[0], on_dev, _stream_ptr(stream)))
+        self.vocab = int(codes.shape[0])
 
     def head_sample(self, hidden: torch.Tensor, params, u: torch.Tensor, with_logits: bool = False, stream=None):
         """(token int32 [M], p fp32 [M], logits fp32 [M, vocab] or None): one token
@@ -264,15 +261,14 @@ class Stage:
         if hidden.dim() != 2 or hidden.shape[1] != self.shape.hidden or hidden.dtype != self.act_dtype or not hidden.is_cuda \
                 or not hidden.is_contiguous():
             raise ValueError("hidden must be a contiguous device [M, hidden] tensor in the activation dtype")
-        M = int(hidden.shape[0])
-        call = _Call(stream, hidden.device)
-        arr = _sampling(params, M)
-        _check_u(u, M, hidden.device)
-        tok, p = call.empty(M, torch.int32), call.empty(M, torch.float32)
-        full = call.empty((M, getattr(self, "vocab", 1)), torch.float32) if with_logits else None
-        check(self.lib.stage_head_sample(self.handle, ctypes.c_void_p(hidden.data_ptr()), M, arr, ctypes.c_void_p(u.data_ptr()),
-                                         ctypes.c_void_p(tok.data_ptr()), ctypes.c_void_p(p.data_ptr()),
-                                         ctypes.c_void_p(full.data_ptr() if full is not None else None), call.ptr))
+        M, dev = hidden.shape[0], hidden.device
+        packed = _sampling(params, M)
+        _check_u(u, M, dev)
+        sp, empty = _on(stream, dev)
+        tok, p = empty(M, dtype=torch.int32, device=dev), empty(M, dtype=torch.float32, device=dev)
+        full = empty((M, getattr(self, "vocab", 1)), dtype=torch.float32, device=dev) if with_logits else None
+        check(self.lib.stage_head_sample(self.handle, hidden.data_ptr(), M, packed, u.data_ptr(), tok.data_ptr(), p.data_ptr(),
+                                         full.data_ptr() if full is not None else None, sp))
         return tok, p, full
 
     def sample(self, logits: torch.Tensor, params, u: torch.Tensor, stream=None):
@@ -280,14 +276,14 @@ class Stage:
         [M, vocab] (float32, float16 or bfloat16; rows may be part of wider ones)
         by ``params`` (a ``Sampling``, or one per row) and ``u`` fp32 [M] in [0, 1)."""
         ld = _rows(logits, "logits")
-        M, V = (int(v) for v in logits.shape)
-        call = _Call(stream, logits.device)
-        arr = _sampling(params, M)
-        _check_u(u, M, logits.device)
-        tok, p = call.empty(M, torch.int32), call.empty(M, torch.float32)
-        check(self.lib.stage_sample(self.handle, ctypes.c_void_p(logits.data_ptr()), _DT_OF[logits.dtype], ld, M, V, arr,
-                                    ctypes.c_void_p(u.data_ptr()), ctypes.c_void_p(tok.data_ptr()),
-                                    ctypes.c_void_p(p.data_ptr()), call.ptr))
+        M, V = logits.shape
+        dev = logits.device
+        packed = _sampling(params, M)
+        _check_u(u, M, dev)
+        sp, empty = _on(stream, dev)
+        tok, p = empty(M, dtype=torch.int32, device=dev), empty(M, dtype=torch.float32, device=dev)
+        check(self.lib.stage_sample(self.handle, logits.data_ptr(), _DT_OF[logits.dtype], ld, M, V, packed, u.data_ptr(),
+                                    tok.data_ptr(), p.data_ptr(), sp))
         return tok, p
 
     def tree_accept(self, parents: torch.Tensor, tokens: torch.Tensor, sampled: torch.Tensor, stream=None):
@@ -298,25 +294,29 @@ class Stage:
         ``next`` is the token sampled at the last one."""
         if parents.dim() != 2 or not parents.is_cuda:
             raise ValueError("parents must be a device [slots, nodes] tensor")
-        S, n = (int(v) for v in parents.shape)
-        ptrs = [_ints(t, name, (S, n), parents.device)
-                for t, name in ((parents, "parents"), (tokens, "tokens"), (sampled, "sampled"))]
-        call = _Call(stream, parents.device)
-        count, path = call.empty(S, torch.int32), call.empty((S, n), torch.int32)
-        nxt, keep = call.empty(S, torch.int32), call.empty((S, n), torch.uint8)
-        check(self.lib.stage_tree_accept(self.handle, *(ctypes.c_void_p(v) for v in ptrs), S, n,
-                                         *(ctypes.c_void_p(t.data_ptr()) for t in (count, path, nxt, keep)), call.ptr))
+        shape, dev = parents.shape, parents.device
+        for t, name in ((parents, "parents"), (tokens, "tokens"), (sampled, "sampled")):
+            if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {dev}")
+        S, n = shape
+        sp, empty = _on(stream, dev)
+        count, path = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.int32, device=dev)
+        nxt, keep = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.uint8, device=dev)
+        check(self.lib.stage_tree_accept(self.handle, parents.data_ptr(), tokens.data_ptr(), sampled.data_ptr(), S, n,
+                                         count.data_ptr(), path.data_ptr(), nxt.data_ptr(), keep.data_ptr(), sp))
         return count, path, nxt, keep
 
     def mx4_quantize(self, x: torch.Tensor, stream=None):
         """(codes uint8 [m, ceil(k/2)], scales uint8 [m, ceil(k/32)]): the rows of a
         device [m, k] tensor (float32, float16 or bfloat16) in MXFP4."""
         ld = _rows(x, "x")
-        m, k = (int(v) for v in x.shape)
-        call = _Call(stream, x.device)
-        codes, scales = call.empty((m, (k + 1) // 2), torch.uint8), call.empty((m, (k + 31) // 32), torch.uint8)
-        check(self.lib.stage_mx4_quantize(self.handle, ctypes.c_void_p(x.data_ptr()), _DT_OF[x.dtype], ld, m, k,
-                                          ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()), call.ptr))
+        m, k = x.shape
+        dev = x.device
+        sp, empty = _on(stream, dev)
+        codes = empty((m, (k + 1) // 2), dtype=torch.uint8, device=dev)
+        scales = empty((m, (k + 31) // 32), dtype=torch.uint8, device=dev)
+        check(self.lib.stage_mx4_quantize(self.handle, x.data_ptr(), _DT_OF[x.dtype], ld, m, k, codes.data_ptr(),
+                                          scales.data_ptr(), sp))
         return codes, scales
 
     def mx4_dequantize(self, codes: torch.Tensor, scales: torch.Tensor, k: int, out_dtype=torch.float32, stream=None) -> torch.Tensor:
@@ -325,11 +325,11 @@ class Stage:
             raise ValueError("codes and scales must be device tensors")
         if out_dtype not in _DT_OF:
             raise ValueError("out_dtype must be float32, float16 or bfloat16")
-        m = int(codes.shape[0])
-        call = _Call(stream, codes.device)
-        out = call.empty((m, k), out_dtype)
-        check(self.lib.stage_mx4_dequantize(self.handle, ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()),
-                                            m, int(k), ctypes.c_void_p(out.data_ptr()), _DT_OF[out_dtype], int(k), call.ptr))
+        m, dev = codes.shape[0], codes.device
+        sp, empty = _on(stream, dev)
+        out = empty((m, k), dtype=out_dtype, device=dev)
+        check(self.lib.stage_mx4_dequantize(self.handle, codes.data_ptr(), scales.data_ptr(), m, k, out.data_ptr(),
+                                            _DT_OF[out_dtype], k, sp))
         return out
 
     def mx4_matrix(self, codes: torch.Tensor, scales: torch.Tensor, k: int, stream=None) -> "Mx4Matrix":
@@ -442,15 +442,17 @@ class Sampling:
     top_p: float = 1.0
     min_p: float = 0.0
 
+    def __post_init__(self):
+        # the C struct StageSampling, made once for every call that takes this object
+        object.__setattr__(self, "packed", struct.pack("=fiff", self.temperature, self.top_k, self.top_p, self.min_p))
 
-def _sampling(params, M: int):
-    ps = [params] * M if isinstance(params, Sampling) else list(params)
-    if len(ps) != M:
-        raise ValueError(f"{len(ps)} sampling parameters for {M} rows")
-    arr = (_lib.StageSampling * max(1, M))()
-    for a, q in zip(arr, ps):
-        a.temperature, a.top_k, a.top_p, a.min_p = float(q.temperature), int(q.top_k), float(q.top_p), float(q.min_p)
-    return arr
+
+def _sampling(params, M: int) -> bytes:
+    if isinstance(params, Sampling):
+        return params.packed * M
+    if len(params) != M:
+        raise ValueError(f"{len(params)} sampling parameters for {M} rows")
+    return b"".join([q.packed for q in params])
 
 
 class Mx4Matrix:
@@ -460,10 +462,9 @@ class Mx4Matrix:
         on_dev = _check_mx4(codes, scales, k)
         self.stage, self.lib = stage, stage.lib
         self.n, self.k = int(codes.shape[0]), int(k)
-        call = _Call(stream, codes.device if on_dev else None)
         h = ctypes.c_void_p()
-        check(self.lib.stage_mx4_create(stage.handle, ctypes.c_void_p(codes.data_ptr()), ctypes.c_void_p(scales.data_ptr()),
-                                        self.n, self.k, on_dev, call.ptr, ctypes.byref(h)))
+        check(self.lib.stage_mx4_create(stage.handle, codes.data_ptr(), scales.data_ptr(), self.n, self.k, on_dev,
+                                        _stream_ptr(stream), ctypes.byref(h)))
         self.handle = h
         _LIVE_MATRICES.add(self)
 
@@ -484,19 +485,22 @@ class Mx4Matrix:
         16) or rounded to MXFP4 first (4, also float32 rows), in ``out_dtype``
         (x's by default) or into ``out`` [m, n], whose rows may be part of wider ones."""
         ldx = _rows(x, "x")
-        m = int(x.shape[0])
-        if x.shape[1] != self.k:
-            raise ValueError(f"x has {x.shape[1]} columns, the matrix {self.k}")
-        call = _Call(stream, x.device)
+        m, k = x.shape
+        if k != self.k:
+            raise ValueError(f"x has {k} columns, the matrix {self.k}")
+        dev = x.device
+        sp, empty = _on(stream, dev)
         if out is None:
-            if (out_dtype or x.dtype) not in _DT_OF:
+            out_dtype = out_dtype or x.dtype
+            if out_dtype not in _DT_OF:
                 raise ValueError("out_dtype must be float32, float16 or bfloat16")
-            out = call.empty((m, self.n), out_dtype or x.dtype)
-        elif tuple(out.shape) != (m, self.n) or out.device != x.device or out_dtype not in (None, out.dtype):
-            raise ValueError(f"out must be a [{m}, {self.n}] tensor on {x.device}")
-        ldo = _rows(out, "out")
-        check(self.lib.stage_mx4_product(self.handle, ctypes.c_void_p(x.data_ptr()), _DT_OF[x.dtype], ldx, m, int(act_bits),
-                                         ctypes.c_void_p(out.data_ptr()), _DT_OF[out.dtype], ldo, call.ptr))
+            out, ldo = empty((m, self.n), dtype=out_dtype, device=dev), self.n
+        else:
+            if tuple(out.shape) != (m, self.n) or out.device != dev or out_dtype not in (None, out.dtype):
+                raise ValueError(f"out must be a [{m}, {self.n}] tensor on {dev}")
+            ldo = _rows(out, "out")
+        check(self.lib.stage_mx4_product(self.handle, x.data_ptr(), _DT_OF[x.dtype], ldx, m, act_bits, out.data_ptr(),
+                                         _DT_OF[out.dtype], ldo, sp))
         return out
 
 
