@@ -356,9 +356,9 @@ int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out,
  *   scales : uint8 [m][ceil(k/32)].
  * Tensors are device memory unless said otherwise; row strides `ld` count
  * elements and may exceed the row length; no alignment beyond the element's is
- * needed.  stage_mx4_quantize, stage_mx4_dequantize, stage_sample and
- * stage_tree_accept use no memory of the stage: calls on different streams are
- * independent and may be captured into a graph.  The other calls use the
+ * needed.  stage_mx4_quantize, stage_mx4_dequantize and stage_tree_accept use no
+ * memory of the stage: calls on different streams are independent and may be
+ * captured into a graph.  The other calls use the
  * stage's workspace, are ordered with the stage's calls like a forward and
  * refuse a capturing stream (STAGE_E_UNSUPPORTED).  The calling thread's current
  * device is left as it was.
@@ -435,8 +435,10 @@ typedef struct StageSampling {
  * [M]; u: device fp32 [M] in [0, 1) (values outside are taken as the nearest
  * inside).  A row without a ranked token gives token -1 and p 0.
  * 1 <= M <= STAGE_MAX_ROWS.  The result does not depend on the other rows.
+ * Allocates a workspace on first use above 8192 tokens (kept, grown when a larger
+ * vocabulary comes).
  * Errors: INVALID (NULL, dtype, params), SHAPE (vocab, ld), CAPACITY (M, vocab),
- * HIP. */
+ * UNSUPPORTED (capturing stream), OOM, HIP. */
 int stage_sample(Stage* stage, const void* logits, int dtype, int64_t ld, int M, int vocab, const StageSampling* params,
                  const float* u, int32_t* token_out, float* p_out, void* stream);
 

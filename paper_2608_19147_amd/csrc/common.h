@@ -371,14 +371,23 @@ struct SampleRow {
     double per_t;                                  // 32 / temperature
     int top_k; float top_p, min_p;
 };
+constexpr int SAMPLE_SLICE = 8192;                 // tokens one workgroup counts
+constexpr int SAMPLE_MAX_SLICES = 128;             // 2^20 tokens
+constexpr size_t SAMPLE_ROW_BYTES = 46080;         // workspace of a row (RowSpace)
 struct SampleArgs {
     const void* logits; int dt; size_t ld; int V;
+    int vec;                                       // rows start on 16 bytes
+    int slices;                                    // of a row, 0 for one; with more, the rows' and slices' workspace:
+    uint8_t* rows_ws;                              // [MAX_ROWS] x SAMPLE_ROW_BYTES
+    void* heads; unsigned long long* bins;         // [m][slices], [m][slices][bins]
     const float* u;                                // [m], or null: 0, the first of the ranking
     int32_t* token; float* p;
     float* top;                                    // optional [m]: the largest logit
     SampleRow rows[MAX_ROWS];
 };
 hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st);
+size_t sample_slice_bytes(int slices);             // of MAX_ROWS rows' heads (16 bytes each) and, behind them, bins
+hipError_t launch_sample_clear(uint8_t* rows_ws, hipStream_t st);   // once, on a new rows' workspace
 hipError_t launch_tree_accept(const int32_t* parents, const int32_t* tokens, const int32_t* sampled, int S, int n, int32_t* count,
                               int32_t* path, int32_t* next, uint8_t* keep, hipStream_t st);
 

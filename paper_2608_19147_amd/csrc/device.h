@@ -124,6 +124,13 @@ __device__ __forceinline__ float load_coherent(const float* p) {
     return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+__device__ __forceinline__ void store_coherent(unsigned long long* p, unsigned long long v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long load_coherent(const unsigned long long* p) {
+    return __hip_atomic_load(const_cast<unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // Returns true in exactly one workgroup: the last of `n` to arrive at counter *c,
 // which it resets.  Every thread of the workgroup must call it.
 __device__ __forceinline__ bool last_arrival(unsigned* c, unsigned n, int* flag) {

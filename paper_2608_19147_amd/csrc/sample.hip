@@ -6,24 +6,30 @@
 // drawn is the first whose running weight passes u times the kept weight.  Every
 // step is then a search for a place in the ranking by count, by weight or by
 // value, and none needs the row sorted: a histogram over bins of the scaled
-// logit says which bin holds the place, and only that bin's tokens are ranked.
+// logit says which bins hold the places, and only those bins' tokens are ranked.
 //
 // Bins: x = logit * 32 / T, q = floor(x), bin = q_max - q, weight exp((x - x_max)
-// / 32) up to a common factor: exp(d) E[bin], d = (x - q) / 32, E[b] = exp(-b / 32).
-// exp(d) goes into a bin's sum as an integer in units of 2^-43 (sums are then
-// the same in any order, below 2^64 for 2^20 tokens), the bins' sums are joined
-// in 64-bit floating point.  Bins from 1024 on (weights below e^-31.97 of the
-// largest, together less than 2^20 e^-31.97 = 1.4e-8 of the kept weight) are left
-// out: neither u nor top_p, 24-bit numbers below 1, come nearer to 1 than 6e-8,
-// so no draw and no cut falls there.
+// / 32), up to a common factor exp(d) E[bin] with d = (x - q) / 32 - 1 / 64 and
+// E[b] = exp(-b / 32).  The grid does not move with the row's largest logit, so
+// slices of a row are counted apart and joined by shifting whole bins.  exp(d)
+// is summed as an integer in units of 2^-36 (any order of addition gives the same
+// sum; below 2^57 for 2^20 tokens), the bins' sums are joined in 64-bit floating
+// point.  Bins from 1024 on (weights below e^-31.9 of the largest, together less
+// than 2^20 e^-31.9 = 1.5e-8 of the kept weight) are left out: neither u nor
+// top_p, 24-bit numbers below 1, comes nearer to 1 than 6e-8, so no draw and no
+// cut falls there.
 #include "device.h"
 
 namespace stg {
 
 constexpr int SB_BINS = 1024;        // bins of 1/32 of a unit of logit / T
-constexpr int SB_CAP = 2048;         // tokens of one bin that are ranked in LDS
-constexpr int SB_THREADS = 1024;
-constexpr double SB_UNIT = 8796093022208.0;        // 2^43
+constexpr int SB_CAP = 4096;         // tokens of the bins that matter that are gathered
+constexpr int SB_RANK = 256;         // tokens that are ranked by counting larger ones
+constexpr int SB_RANGES = 4;         // runs of bins that are gathered
+constexpr int SB_THREADS = 512;      // of a workgroup
+constexpr int SB_PER = SB_BINS / SB_THREADS;       // bins a thread, neighbours
+constexpr int SL_LEN = SAMPLE_SLICE; // tokens of a slice: a bin's count fits the 14 bits below its sum
+static_assert(SL_LEN == 16 * SB_THREADS && SL_LEN < (1 << 14), "slice");
 
 // Order of finite logits as unsigned integers; NaN and -inf are not ranked (0), +inf ranks as the largest finite value, -0 as 0.
 __device__ __forceinline__ uint32_t rank_key(float l) {
@@ -33,17 +39,17 @@ __device__ __forceinline__ uint32_t rank_key(float l) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-// exp(d) 2^43 as an integer, d in [0, 1/32]: Taylor to d^7, the rest below 3e-17.
+// exp(d - 1/64) in units of 2^-36, d in [0, 1/32]: Taylor around 1/64 to the 5th power, the rest below 2.1e-14, a
+// third of half a unit.  Added to 2^52, the units are the low bits of the sum.
 __device__ __forceinline__ unsigned long long exp_units(double d) {
-    double p = 1.0 / 5040.0;
-    p = fma(p, d, 1.0 / 720.0);
-    p = fma(p, d, 1.0 / 120.0);
-    p = fma(p, d, 1.0 / 24.0);
-    p = fma(p, d, 1.0 / 6.0);
-    p = fma(p, d, 0.5);
-    p = fma(p, d, 1.0);
-    p = fma(p, d, 1.0);
-    return (unsigned long long)(p * SB_UNIT + 0.5);
+    const double c = d - 1.0 / 64.0;
+    double p = 1.0 / 120.0;
+    p = fma(p, c, 1.0 / 24.0);
+    p = fma(p, c, 1.0 / 6.0);
+    p = fma(p, c, 0.5);
+    p = fma(p, c, 1.0);
+    p = fma(p, c, 1.0);
+    return (unsigned long long)__double_as_longlong(fma(p, 68719476736.0, 4503599627370496.0)) & 0xfffffffffffffull;
 }
 
 struct RowBins {                      // the scaled logit of a row's tokens
@@ -53,6 +59,111 @@ struct RowBins {                      // the scaled logit of a row's tokens
     __device__ __forceinline__ double bin(double xv) const { return qmax - floor(xv); }
     __device__ __forceinline__ unsigned long long units(double xv) const { return exp_units((xv - floor(xv)) * (1.0 / 32.0)); }
 };
+
+struct RowArgs {
+    const void* logits; int dt; size_t base; int V;
+    int vec;                          // rows start on 16 bytes
+};
+
+// Keys of tokens i .. i + 7 (i a multiple of 8); 0 past the row's end.
+__device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)[8]) {
+    float v[8];
+    if (r.vec && i + 8 <= r.V) {
+        if (r.dt == DT_F32) {
+            const u32x4* p = (const u32x4*)((const float*)r.logits + r.base + i);
+            const u32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { v[j] = __uint_as_float(a[j]); v[4 + j] = __uint_as_float(b[j]); }
+        } else {
+            const u32x4 a = *(const u32x4*)((const uint16_t*)r.logits + r.base + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 1] >> (16 * (j & 1))), r.dt);
+        }
+    } else {
+        size_t off[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) off[j] = r.base + min(i + j, r.V - 1);
+        load_vals<8>(r.logits, r.dt, off, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i + j < r.V ? v[j] : -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = rank_key(v[j]);
+}
+
+// One slice of a row: its largest token; its bins, counted from that one's
+// (sum << 14 | count), stand apart.
+struct SliceHead { double q; uint32_t top; uint32_t pad; };
+
+template <int NW>
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    uint32_t t = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) t = max(t, buf[w]);
+    return t;
+}
+
+__device__ __forceinline__ void count_keys(const uint32_t (&k)[8], const RowBins& rb, unsigned long long* hist) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (!k[j]) continue;
+        const double x = rb.x(k[j]), b = rb.bin(x);
+        if (b < (double)SB_BINS) atomicAdd(&hist[(int)b], rb.units(x) << 14 | 1ull);
+    }
+}
+
+// Keys of a thread's 16 tokens of slice `slice`: i0 + 0 .. 7 and i0 + SL_LEN / 2 + 0 .. 7.
+__device__ __forceinline__ int load_slice(const RowArgs& r, int slice, uint32_t (&k)[2][8]) {
+    const int i0 = slice * SL_LEN + threadIdx.x * 8;
+    load_keys(r, i0, k[0]);
+    load_keys(r, i0 + SL_LEN / 2, k[1]);
+    return i0;
+}
+
+// The largest key of the workgroup's, and hist[] of its tokens counted from it.
+__device__ __forceinline__ uint32_t count_slice(const uint32_t (&k)[2][8], RowBins& rb, unsigned long long* hist, uint32_t* buf) {
+    for (int i = threadIdx.x; i < SB_BINS; i += SB_THREADS) hist[i] = 0ull;
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, max(k[0][j], k[1][j]));
+    top = block_max<SB_THREADS / 64>(top, buf);
+    rb.qmax = floor(rb.x(top));
+    if (top) {
+        count_keys(k[0], rb, hist);
+        count_keys(k[1], rb, hist);
+    }
+    __syncthreads();
+    return top;
+}
+
+// What the counts of a row say before any token is ranked.
+struct RowPlan {
+    double qmax, all, thr;            // floor(x) of the largest; the row's weight; min_p's least units in bin 0
+    unsigned long long units0;        // units of bin 0
+    uint32_t top;                     // key of the largest, 0: nothing to draw from
+    unsigned nall, n;                 // tokens; those of the runs of bins in which the places can be
+    unsigned slices;                  // slices that hold some of the latter
+    int kbin, vbin;                   // bins of top_k's cut and of min_p's (SB_BINS: none)
+    int lo[SB_RANGES], hi[SB_RANGES]; // the runs (lo = SB_BINS: none)
+    uint32_t klo[SB_RANGES], khi[SB_RANGES];   // their keys
+    unsigned touched[SAMPLE_MAX_SLICES / 32];  // the slices, one bit each
+};
+
+// Workspace of one row of a sampled batch: SAMPLE_ROW_BYTES, then the slices' heads and bins.
+struct RowSpace {
+    unsigned long long list[SB_CAP];  // gathered tokens, key << 32 | ~index
+    double cum[SB_BINS];              // weight of the bins up to and with this one
+    unsigned cumc[SB_BINS];           // their tokens
+    RowPlan plan;
+    unsigned arrived, drawn;          // slices that are counted, gathered: zero between calls
+    unsigned fill;                    // tokens in the list
+};
+static_assert(sizeof(RowSpace) <= SAMPLE_ROW_BYTES, "row workspace");
 
 // Tokens of one row with lo <= key <= hi in bin `bin`: a part of the ranking
 // without gaps.
@@ -67,311 +178,777 @@ enum Want : int { BY_COUNT = 0, BY_MASS = 1, BY_VALUE = 2 };
 struct Place { int count; unsigned long long units; uint32_t key; int index; };   // the first `count` of a part: their units, the last one
 
 struct SampleShared {
-    unsigned long long list[SB_CAP];           // key << 32 | ~index
-    unsigned long long mass[SB_BINS];
-    unsigned cnt[SB_BINS];
+    unsigned long long hist[SB_BINS];          // units << 14 | count
+    double cum[SB_BINS];                       // weight of the bins up to and with this one
+    unsigned cumc[SB_BINS];                    // their tokens
+    union {
+        unsigned pieces[SB_BINS];              // tokens of the buckets of a part too large for the list
+        struct {
+            unsigned long long ranked[SB_RANK];    // tokens in order
+            unsigned long long pre[SB_RANK];       // units of ranked[] up to and with each
+        };
+    };
+    unsigned rank[SB_RANK];
+    int shift[SAMPLE_MAX_SLICES];              // bins from the row's largest to the slice's, or -1: nothing there
+    unsigned touched[SAMPLE_MAX_SLICES / 32];
     unsigned long long wave_u[SB_THREADS / 64];
     unsigned wave_c[SB_THREADS / 64];
     double wave_d[SB_THREADS / 64];
     uint32_t klo, khi;
     unsigned fill;
-    unsigned bin_c0;
-    int found;
-    unsigned long long bin_u0;
+    unsigned c0;
+    int found, flag;
+    unsigned long long u0;
     Place place;
 };
 
-struct RowArgs {
-    const void* logits; int dt; size_t base; int V;
-};
-
-// Inclusive sums over the workgroup's threads, in thread order.
+// Inclusive sum over the wave's lanes by lane permutes within the vector unit
+// (__shfl goes through LDS, several times the latency).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp_u(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned long long dpp_u(unsigned long long v) {
+    return (unsigned long long)dpp_u<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | dpp_u<CTRL, ROWS>((unsigned)v);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_u(double v) {
+    return __longlong_as_double((long long)dpp_u<CTRL, ROWS>((unsigned long long)__double_as_longlong(v)));
+}
 template <class S>
-__device__ __forceinline__ S scan_block(S v, S* wave, S* total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const S u = __shfl_up(v, o);
-        if (lane >= o) v += u;
-    }
-    __syncthreads();                            // earlier readers of wave[] are done
-    if (lane == 63) wave[w] = v;
+__device__ __forceinline__ S scan_wave(S v) {
+    v += dpp_u<0x111, 0xF>(v);                  // row_shr 1, 2, 4, 8: within 16 lanes
+    v += dpp_u<0x112, 0xF>(v);
+    v += dpp_u<0x114, 0xF>(v);
+    v += dpp_u<0x118, 0xF>(v);
+    v += dpp_u<0x142, 0xA>(v);                  // the last lane of rows 0 and 2 to rows 1 and 3
+    v += dpp_u<0x143, 0xC>(v);                  // and that of row 1 to rows 2 and 3
+    return v;
+}
+
+// Inclusive sums of two values over the workgroup's threads, in thread order, and the totals.
+template <class A, class B>
+__device__ __forceinline__ void scan_block(A& a, B& b, A* wa, B* wb, A* ta, B* tb) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    a = scan_wave(a);
+    b = scan_wave(b);
+    __syncthreads();                            // earlier readers of the waves' sums are done
+    if (lane == 63) { wa[w] = a; wb[w] = b; }
     __syncthreads();
-    S b = S(0), t = S(0);
-    for (int i = 0; i < nw; ++i) {
-        if (i < w) b += wave[i];
-        t += wave[i];
+    const A pa = lane < SB_THREADS / 64 ? wa[lane] : A(0);
+    const B pb = lane < SB_THREADS / 64 ? wb[lane] : B(0);
+    A sa = scan_wave(pa);
+    B sb = scan_wave(pb);
+    *ta = __shfl(sa, SB_THREADS / 64 - 1);
+    *tb = __shfl(sb, SB_THREADS / 64 - 1);
+    sa = __shfl(sa, w ? w - 1 : 0);
+    sb = __shfl(sb, w ? w - 1 : 0);
+    if (w) { a += sa; b += sb; }
+}
+
+// The first i < n <= 4096 for which pred holds (it holds for all later ones), or
+// n: 64 places at once, then the places between two of them.  Every wave finds
+// it for itself, without a barrier.
+template <class F>
+__device__ __forceinline__ int wave_search(int n, F pred) {
+    const int lane = threadIdx.x & 63, step = (n + 63) >> 6;
+    const int i = lane * step + step - 1;
+    const unsigned long long a = __ballot(pred(i < n ? i : n - 1));
+    if (!a) return n;
+    const int j = (__ffsll(a) - 1) * step + lane;
+    const unsigned long long b = __ballot(lane < step && j < n && pred(j < n ? j : n - 1));
+    return j - lane + __ffsll(b) - 1;
+}
+
+// hist[] of n tokens was filled: the first bucket with which the part reaches t
+// (else the last one that holds any), and what is ahead of it.  c0, u0 and n
+// become those of the bucket.
+__device__ __forceinline__ int find_bucket(Want want, unsigned long long t, int& c0, unsigned long long& u0, int& n, SampleShared& sh) {
+    const int tid = threadIdx.x;
+    unsigned own[SB_PER], c = 0, tc;
+    unsigned long long ownu[SB_PER], u = 0, tu;
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        const unsigned long long h = sh.hist[SB_PER * tid + j];
+        own[j] = (unsigned)h & 16383u;
+        ownu[j] = h >> 14;
+        c += own[j];
+        u += ownu[j];
     }
-    *total = t;
-    return v + b;
+    if (tid == 0) sh.found = SB_BINS;
+    unsigned upc = c;
+    unsigned long long upu = u;
+    scan_block(upc, upu, sh.wave_c, sh.wave_u, &tc, &tu);
+    upc -= c;
+    upu -= u;
+    int mine = SB_BINS;
+    unsigned ac = upc;
+    unsigned long long au = upu;
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        const unsigned c1 = upc + own[j];
+        const unsigned long long u1 = upu + ownu[j];
+        const bool here = own[j] != 0u && ((want == BY_COUNT ? (unsigned long long)(c0 + (int)c1) >= t : u0 + u1 >= t) || c1 == tc);
+        if (here && mine == SB_BINS) { mine = SB_PER * tid + j; ac = upc; au = upu; }
+        upc = c1;
+        upu = u1;
+    }
+    if (mine < SB_BINS) atomicMin(&sh.found, mine);
+    __syncthreads();
+    const int s = sh.found;
+    if (mine == s) { sh.c0 = (unsigned)c0 + ac; sh.u0 = u0 + au; sh.fill = (unsigned)sh.hist[s] & 16383u; }
+    __syncthreads();
+    c0 = (int)sh.c0;
+    u0 = sh.u0;
+    n = (int)sh.fill;
+    return s;
+}
+
+// ranked[0..n) sorted downwards (n <= SB_RANK) and summed: each token's rank is
+// the number of larger ones, counted by four threads a token.
+__device__ __forceinline__ void rank_tokens(int n, const RowBins& rb, SampleShared& sh) {
+    const int tid = threadIdx.x, e = tid & (SB_RANK - 1), q = tid / SB_RANK;
+    constexpr int PARTS = SB_THREADS / SB_RANK;
+    if (tid < SB_RANK) sh.rank[tid] = 0u;
+    __syncthreads();
+    const unsigned long long v = e < n ? sh.ranked[e] : 0ull;
+    unsigned larger = 0;
+    if (e < n)
+        for (int i = q; i < n; i += PARTS) larger += sh.ranked[i] > v;
+    if (larger) atomicAdd(&sh.rank[e], larger);
+    __syncthreads();
+    const unsigned at = sh.rank[e];
+    __syncthreads();
+    if (q == 0 && e < n) sh.ranked[at] = v;
+    __syncthreads();
+    unsigned long long u = tid < n ? rb.units(rb.x((uint32_t)(sh.ranked[tid] >> 32))) : 0ull, tu;
+    unsigned zero = 0, tz;
+    scan_block(u, zero, sh.wave_u, sh.wave_c, &tu, &tz);
+    if (tid < SB_RANK) sh.pre[tid] = u;
+    __syncthreads();
+}
+
+// The place among ranked tokens at .. at + n - 1, with c0 tokens of u0 units of their part ahead.
+__device__ __forceinline__ Place place_in_ranked(int at, int n, int c0, unsigned long long u0, Want want, unsigned long long t,
+                                                 const RowBins& rb, const SampleShared& sh) {
+    const unsigned long long base = at ? sh.pre[at - 1] : 0ull;
+    int lo;                                     // the fewest that do (BY_VALUE: the first that does not)
+    if (want == BY_COUNT) {
+        const unsigned long long c = t - (unsigned)c0;
+        lo = c < (unsigned)n ? (int)c : n;
+    } else if (want == BY_MASS) {
+        lo = min(n, wave_search(n, [&](int i) { return u0 + (sh.pre[at + i] - base) >= t; }) + 1);
+    } else {
+        lo = wave_search(n, [&](int i) { return rb.units(rb.x((uint32_t)(sh.ranked[at + i] >> 32))) < t; });
+    }
+    if (lo == 0) return Place{c0, u0, 0u, -1};
+    const unsigned long long v = sh.ranked[at + lo - 1];
+    return Place{c0 + lo, u0 + (sh.pre[at + lo - 1] - base), (uint32_t)(v >> 32), (int)~(uint32_t)v};
 }
 
 // The place in `part` that `want` asks for: its first `t` tokens (BY_COUNT), the
 // fewest whose units together reach `t`, all of them if none do (BY_MASS), or
-// those of at least `t` units each (BY_VALUE).  Whole workgroup; every thread
-// gets the result.
-__device__ Place find_place(const RowArgs& r, const RowBins& rb, Part part, Want want, unsigned long long t, SampleShared& sh) {
+// those of at least `t` units each (BY_VALUE, which names no token).  listed > 0:
+// the part's tokens stand among the list's first `listed`.  Otherwise, above
+// SB_CAP of them, passes over the row narrow the part to a bucket of its keys' range (or
+// find a token of equal ones by index), then gather it.  The list is narrowed
+// the same way, in registers, until SB_RANK tokens are left, which are ranked.
+// Whole workgroup; every thread gets the result.  (One loop over the row serves
+// every kind of pass, and the caller calls this in one place: a row is one
+// workgroup's work once, so instructions come from memory, not from the cache.)
+__device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb, Part part, unsigned long long* list, int listed, Want want,
+                                            unsigned long long t, SampleShared& sh) {
+    enum Pass : int { RANGE, PIECES, COUNT, PICK, VALUE, GATHER };
     const int tid = threadIdx.x;
     int c0 = 0;                                 // tokens and units of the part ahead of the piece looked at
     unsigned long long u0 = 0;
-    auto key_of = [&](int i) {
-        const uint32_t k = rank_key(load_val(r.logits, r.dt, r.base + i));
-        return k != 0u && k >= part.lo && k <= part.hi && rb.bin(rb.x(k)) == (double)part.bin ? k : 0u;
-    };
-    while (part.n > SB_CAP) {
-        // the keys' range, then a histogram over it
-        if (tid == 0) { sh.klo = 0xffffffffu; sh.khi = 0u; }
-        for (int i = tid; i < SB_BINS; i += SB_THREADS) { sh.mass[i] = 0; sh.cnt[i] = 0; }
-        __syncthreads();
-        uint32_t lo = 0xffffffffu, hi = 0u;
-        for (int i = tid; i < r.V; i += SB_THREADS) {
-            const uint32_t k = key_of(i);
-            if (k) { lo = min(lo, k); hi = max(hi, k); }
+    if (listed <= 0) {
+        const int run = ((r.V + SB_THREADS - 1) / SB_THREADS + 7) / 8 * 8;   // COUNT, PICK: neighbours of one thread
+        int shift = 0, kth = 0;
+        unsigned upto = 0, mine = 0;
+        Pass pass = part.n <= SB_CAP ? GATHER : want == BY_VALUE ? VALUE : RANGE;
+        for (;;) {
+            __syncthreads();
+            if (tid == 0) { sh.klo = 0xffffffffu; sh.khi = 0u; sh.fill = 0u; sh.place = Place{0, 0ull, 0u, -1}; }
+            if (pass == RANGE)
+                for (int i = tid; i < SB_BINS; i += SB_THREADS) { sh.pieces[i] = 0u; sh.hist[i] = 0ull; }
+            __syncthreads();
+            uint32_t lo = 0xffffffffu, hi = 0u;
+            unsigned long long sum = 0;
+            const unsigned ahead = upto - mine;
+            unsigned n = 0;
+            const bool runs = pass == COUNT || pass == PICK;
+            const int first = runs ? min(r.V, tid * run) : tid * 8, end = runs ? min(r.V, first + run) : r.V, by = runs ? 8 : SB_THREADS * 8;
+            for (int i = first; i < end; i += by) {
+                uint32_t k[8];
+                load_keys(r, i, k);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (k[j] == 0u || k[j] < part.lo || k[j] > part.hi) continue;
+                    const double x = rb.x(k[j]);
+                    if (rb.bin(x) != (double)part.bin) continue;
+                    if (pass == RANGE) {
+                        lo = min(lo, k[j]);
+                        hi = max(hi, k[j]);
+                    } else if (pass == PIECES) {
+                        const uint32_t s = (part.hi - k[j]) >> shift;
+                        atomicAdd(&sh.pieces[s], 1u);
+                        atomicAdd(&sh.hist[s], rb.units(x));
+                    } else if (pass == VALUE) {
+                        const unsigned long long e = rb.units(x);
+                        if (e >= t) { ++n; sum += e; }
+                    } else if (runs) {
+                        ++n;
+                        if (pass == PICK && ahead + n == (unsigned)kth) sh.place.index = i + j;
+                    } else {
+                        const unsigned f = atomicAdd(&sh.fill, 1u);
+                        if (f < (unsigned)SB_CAP) store_coherent(&list[f], ((unsigned long long)k[j] << 32) | (uint32_t)~(i + j));
+                    }
+                }
+            }
+            if (pass == RANGE && hi) { atomicMin(&sh.klo, lo); atomicMax(&sh.khi, hi); }
+            if (pass == GATHER) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the list is read by other waves
+            __syncthreads();
+            if (pass == GATHER) break;
+            if (pass == RANGE) {
+                part.lo = sh.klo;
+                part.hi = sh.khi;
+                shift = 0;
+                while (((part.hi - part.lo) >> shift) >= (uint32_t)SB_BINS) ++shift;
+                pass = part.lo == part.hi ? COUNT : PIECES;
+            } else if (pass == PIECES) {
+                if (tid == 0) {                 // the first piece that holds the place, else the last one
+                    int last = 0, cc = c0, lc = c0;
+                    unsigned long long uu = u0, lu = u0;
+                    for (int s = 0; s < SB_BINS; ++s) {
+                        if (!sh.pieces[s]) continue;
+                        last = s; lc = cc; lu = uu;
+                        cc += (int)sh.pieces[s];
+                        uu += sh.hist[s];
+                        if (want == BY_COUNT ? (unsigned long long)cc >= t : uu >= t) break;
+                    }
+                    sh.found = last;
+                    sh.c0 = (unsigned)lc;
+                    sh.u0 = lu;
+                }
+                __syncthreads();
+                const int s = sh.found;
+                const uint32_t nhi = part.hi - ((uint32_t)s << shift), span = (1u << shift) - 1u;
+                part.lo = max(part.lo, nhi >= span ? nhi - span : 0u);
+                part.hi = nhi;
+                part.n = (int)sh.pieces[s];
+                c0 = (int)sh.c0;
+                u0 = sh.u0;
+                pass = part.n > SB_CAP ? RANGE : GATHER;
+            } else if (pass == VALUE) {
+                unsigned tc;
+                unsigned long long tu;
+                scan_block(n, sum, sh.wave_c, sh.wave_u, &tc, &tu);
+                return Place{(int)tc, tu, 0u, -1};
+            } else if (pass == COUNT) {         // all equal: the kth-th by index
+                const unsigned long long e = rb.units(rb.x(part.lo));
+                unsigned long long q, none = 0, tn;
+                if (want == BY_COUNT) q = t - (unsigned)c0;
+                else q = t > u0 ? (t - u0 + e - 1) / e : 1u;
+                kth = q < (unsigned)part.n ? (int)q : part.n;
+                unsigned tot;
+                upto = mine = n;
+                scan_block(upto, none, sh.wave_c, sh.wave_u, &tot, &tn);
+                pass = PICK;
+            } else {
+                return Place{c0 + kth, u0 + (unsigned long long)kth * rb.units(rb.x(part.lo)), part.lo, sh.place.index};
+            }
         }
+        listed = part.n;
+    }
+    // at most SB_CAP tokens in the list: a few a thread
+    constexpr int PER = SB_CAP / SB_THREADS;
+    unsigned long long e[PER];
+    unsigned alive = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = tid + j * SB_THREADS;
+        e[j] = i < listed ? load_coherent(&list[i]) : 0ull;
+        const uint32_t k = (uint32_t)(e[j] >> 32);
+        if (k >= part.lo && k <= part.hi && k && rb.bin(rb.x(k)) == (double)part.bin) alive |= 1u << j;
+    }
+    if (want == BY_VALUE) {
+        unsigned n = 0, tc;
+        unsigned long long sum = 0, tu;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const unsigned long long v = alive >> j & 1u ? rb.units(rb.x((uint32_t)(e[j] >> 32))) : 0ull;
+            if (v >= t && v) { ++n; sum += v; }
+        }
+        scan_block(n, sum, sh.wave_c, sh.wave_u, &tc, &tu);
+        return Place{(int)tc, tu, 0u, -1};
+    }
+    int n = part.n;
+    while (n > SB_RANK) {
+        // buckets of the keys' range, highest first; of the index where all keys are equal
+        uint32_t lo = 0xffffffffu, hi = 0u;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint32_t k = (uint32_t)(e[j] >> 32);
+            if (alive >> j & 1u) { lo = min(lo, k); hi = max(hi, k); }
+        }
+        __syncthreads();
+        for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
+        if (tid == 0) { sh.klo = 0xffffffffu; sh.khi = 0u; }
+        __syncthreads();
         if (hi) { atomicMin(&sh.klo, lo); atomicMax(&sh.khi, hi); }
         __syncthreads();
-        part.lo = sh.klo;
-        part.hi = sh.khi;
-        if (part.lo == part.hi) {               // all equal: ranked by index alone
-            const unsigned long long e = rb.units(rb.x(part.lo));
-            unsigned long long q;
-            if (want == BY_COUNT) q = t - (unsigned)c0;
-            else if (want == BY_VALUE) q = e >= t ? (unsigned)part.n : 0u;
-            else q = t > u0 ? (t - u0 + e - 1) / e : 1u;
-            const int k = q < (unsigned)part.n ? (int)q : part.n;
-            // the k-th by index: each thread counts a run of the row
-            const int run = (r.V + SB_THREADS - 1) / SB_THREADS, b = min(r.V, tid * run), e1 = min(r.V, b + run);
-            unsigned mine = 0, tot;
-            for (int i = b; i < e1; ++i) mine += key_of(i) != 0u;
-            const unsigned upto = scan_block<unsigned>(mine, sh.wave_c, &tot);
-            if (tid == 0) sh.place.index = -1;
-            __syncthreads();
-            if (k > 0 && upto >= (unsigned)k && upto - mine < (unsigned)k) {
-                unsigned at = upto - mine;
-                for (int i = b; i < e1; ++i)
-                    if (key_of(i) != 0u && ++at == (unsigned)k) { sh.place.index = i; break; }
-            }
-            __syncthreads();
-            const Place p{c0 + k, u0 + (unsigned long long)k * e, part.lo, sh.place.index};
-            __syncthreads();
-            return p;
-        }
-        int shift = 0;
-        while (((part.hi - part.lo) >> shift) >= (uint32_t)SB_BINS) ++shift;
-        for (int i = tid; i < r.V; i += SB_THREADS) {
-            const uint32_t k = key_of(i);
-            if (k) {
-                const uint32_t s = (part.hi - k) >> shift;
-                atomicAdd(&sh.cnt[s], 1u);
-                atomicAdd(&sh.mass[s], rb.units(rb.x(k)));
-            }
-        }
-        __syncthreads();
-        if (tid == 0) {                         // the first piece that holds the place, else the last one
-            int s = 0, last = 0;
-            int cc = c0, lc = c0;
-            unsigned long long uu = u0, lu = u0;
-            for (; s < SB_BINS; ++s) {
-                if (!sh.cnt[s]) continue;
-                last = s; lc = cc; lu = uu;
-                const int c1 = cc + (int)sh.cnt[s];
-                const unsigned long long u1 = uu + sh.mass[s];
-                bool here;
-                if (want == BY_COUNT) here = (unsigned long long)c1 >= t;
-                else if (want == BY_MASS) here = u1 >= t;
-                else here = rb.units(rb.x(max(part.lo, part.hi - (((uint32_t)s + 1) << shift) + 1))) < t;   // its least token fails
-                if (here) break;
-                cc = c1;
-                uu = u1;
-            }
-            sh.found = last;
-            sh.bin_c0 = (unsigned)lc;
-            sh.bin_u0 = lu;
-        }
-        __syncthreads();
-        const int s = sh.found;
-        const uint32_t nhi = part.hi - ((uint32_t)s << shift);
-        const uint32_t span = (1u << shift) - 1u;
-        part.lo = max(part.lo, nhi >= span ? nhi - span : 0u);
-        part.hi = nhi;
-        part.n = (int)sh.cnt[s];
-        c0 = (int)sh.bin_c0;
-        u0 = sh.bin_u0;
-        __syncthreads();
-    }
-    // few enough: into LDS, ranked, summed
-    if (tid == 0) sh.fill = 0;
-    int n2 = 64;
-    while (n2 < part.n) n2 <<= 1;
-    for (int i = tid; i < n2; i += SB_THREADS) sh.list[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < r.V; i += SB_THREADS) {
-        const uint32_t k = key_of(i);
-        if (k) {
-            const unsigned at = atomicAdd(&sh.fill, 1u);
-            if (at < SB_CAP) sh.list[at] = ((unsigned long long)k << 32) | (uint32_t)~i;
-        }
-    }
-    __syncthreads();
-    for (int size = 2; size <= n2; size <<= 1)
-        for (int step = size >> 1; step > 0; step >>= 1) {
-            for (int i = tid; i < n2 / 2; i += SB_THREADS) {
-                const int a = 2 * i - (i & (step - 1)), b = a + step;
-                const bool down = (a & size) == 0;
-                const unsigned long long va = sh.list[a], vb = sh.list[b];
-                if ((va < vb) == down) { sh.list[a] = vb; sh.list[b] = va; }
-            }
-            __syncthreads();
-        }
-    constexpr int PER = SB_CAP / SB_THREADS;    // neighbours in rank a thread
-    unsigned long long e[PER], mine = 0, tot;
+        lo = sh.klo;
+        hi = sh.khi;
+        const uint32_t range = lo == hi ? (uint32_t)r.V - 1u : hi - lo;
+        const int shift = max(0, 22 - (int)__clz(range | 1u));       // range >> shift < 1024
+        auto bucket = [&](unsigned long long v) { return (lo == hi ? ~(uint32_t)v : hi - (uint32_t)(v >> 32)) >> shift; };
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int i = tid * PER + j;
-        e[j] = i < part.n && i < n2 ? rb.units(rb.x((uint32_t)(sh.list[i] >> 32))) : 0ull;
-        mine += e[j];
-    }
-    if (tid == 0) sh.place.count = 0;
-    const unsigned long long upto = scan_block<unsigned long long>(mine, sh.wave_u, &tot);
-    unsigned long long run = upto - mine;
+        for (int j = 0; j < PER; ++j)
+            if (alive >> j & 1u) atomicAdd(&sh.hist[bucket(e[j])], rb.units(rb.x((uint32_t)(e[j] >> 32))) << 14 | 1ull);
+        __syncthreads();
+        const uint32_t s = (uint32_t)find_bucket(want, t, c0, u0, n, sh);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int i = tid * PER + j;
-        const unsigned long long was = run;
-        run += e[j];
-        if (i >= part.n) continue;
-        bool here;                              // true at one i: the last of the place
-        if (want == BY_COUNT) here = (unsigned long long)(c0 + i + 1) == t || (i == part.n - 1 && (unsigned long long)(c0 + part.n) < t);
-        else if (want == BY_MASS) here = (u0 + run >= t || i == part.n - 1) && (u0 + was < t || i == 0);
-        else here = e[j] >= t && (i == part.n - 1 || rb.units(rb.x((uint32_t)(sh.list[i + 1] >> 32))) < t);
-        if (here) sh.place = Place{c0 + i + 1, u0 + run, (uint32_t)(sh.list[i] >> 32), (int)~(uint32_t)sh.list[i]};
+        for (int j = 0; j < PER; ++j)
+            if (bucket(e[j]) != s) alive &= ~(1u << j);
     }
     __syncthreads();
-    Place p = sh.place;
-    if (p.count == 0) p = Place{c0, u0, 0u, -1};   // BY_VALUE: none
+    if (tid == 0) sh.fill = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (alive >> j & 1u) sh.ranked[atomicAdd(&sh.fill, 1u)] = e[j];
+    __syncthreads();
+    rank_tokens(n, rb, sh);
+    const Place p = place_in_ranked(0, n, c0, u0, want, t, rb, sh);
     __syncthreads();
     return p;
 }
 
-// One workgroup a row.
-__global__ __launch_bounds__(SB_THREADS) void sample_kernel(SampleArgs a) {
-    __shared__ SampleShared sh;
-    __shared__ double cum[SB_BINS];             // weight of the bins up to and with this one
-    __shared__ unsigned cumc[SB_BINS];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
+// From a thread's SB_PER bins (tokens bc, units bu) to the row's running sums, in
+// sh.cum and sh.cumc, and its plan: the runs of bins in which cuts and draw can fall.
+__device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const RowBins& rb, uint32_t top, const unsigned (&bc)[SB_PER],
+                                             const unsigned long long (&bu)[SB_PER], SampleShared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    double all, upw = 0.0, wj[SB_PER];
+    unsigned nall, upc = 0;
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        wj[j] = (double)bu[j] * exp((double)(SB_PER * tid + j) * (-1.0 / 32.0));
+        upw += wj[j];
+        upc += bc[j];
+    }
+    const double w = upw;
+    const unsigned c = upc;
+    if (tid == 0) sh.u0 = bu[0];
+    scan_block(upw, upc, sh.wave_d, sh.wave_c, &all, &nall);
+    upc -= c;
+    double run = upw - w;
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        // a thread's last bin takes the scan's own sum, so that the running weight never falls from one bin to the next
+        run += wj[j];
+        upc += bc[j];
+        sh.cum[SB_PER * tid + j] = j == SB_PER - 1 ? upw : fmin(run, upw);
+        sh.cumc[SB_PER * tid + j] = upc;
+    }
+    __syncthreads();
+    auto before = [&](int b) { return b ? sh.cum[b - 1] : 0.0; };
+    auto cbefore = [&](int b) { return b ? sh.cumc[b - 1] : 0u; };
+    auto bin_reaching = [&](double t) { return wave_search(SB_BINS, [&](int i) { return sh.cum[i] >= t; }); };
+    auto bin_of_count = [&](unsigned n) { return wave_search(SB_BINS, [&](int i) { return sh.cumc[i] >= n; }); };
+    const bool by_k = p.top_k > 0 && (unsigned)p.top_k < nall, by_p = p.top_p < 1.0f;
+    RowPlan pl;
+    pl.qmax = rb.qmax;
+    pl.all = all;
+    pl.thr = (double)p.min_p * (double)rb.units(rb.x(top));    // exp(d) E[bin] >= min_p exp(d_max)
+    pl.units0 = sh.u0;
+    pl.top = top;
+    pl.nall = nall;
+    pl.kbin = bin_of_count(by_k ? (unsigned)p.top_k : nall);
+    pl.vbin = SB_BINS;
+    if (p.min_p > 0.0f) {
+        // the first bin with tokens whose least weight fails min_p may hold some that pass, those behind it none;
+        // log and exp agree to far less than a bin, and one bin more than needed does no harm: its tokens are compared
+        const double least = (double)exp_units(0.0);
+        const int b = max(0, (int)fmin((double)SB_BINS, floor(-32.0 * log(pl.thr / least))) - 1);
+        const int f = b + wave_search(SB_BINS - b, [&](int i) { return exp((double)(b + i) * (-1.0 / 32.0)) * least < pl.thr; });
+        if (f < SB_BINS) pl.vbin = bin_of_count(cbefore(f) + 1u);
+    }
+    // The places, whatever the tokens of the cut bins are: the kept weight lies between what is ahead of a cut's bin
+    // and what is up to it.
+    int lo[SB_RANGES] = {by_k ? pl.kbin : SB_BINS, SB_BINS, pl.vbin, SB_BINS}, hi[SB_RANGES] = {pl.kbin, 0, pl.vbin, 0};
+    {
+        double wlo = by_k ? before(pl.kbin) : all, whi = sh.cum[pl.kbin];
+        int end = pl.kbin;                      // no later place is behind it
+        if (by_p) {
+            const double tlo = (double)p.top_p * wlo, thi = (double)p.top_p * whi;
+            lo[1] = min(end, bin_reaching(tlo));
+            hi[1] = min(end, bin_reaching(thi));
+            wlo = fmax(tlo, before(lo[1]));
+            whi = fmin(whi, sh.cum[hi[1]]);
+            end = hi[1];
+        }
+        if (pl.vbin <= end) {
+            wlo = fmin(wlo, before(pl.vbin));
+            whi = fmin(whi, sh.cum[pl.vbin]);
+            end = pl.vbin;
+        }
+        const double thi = (double)u * whi;
+        lo[3] = min(end, bin_reaching((double)u * wlo));
+        hi[3] = min(end, wave_search(SB_BINS, [&](int i) { return sh.cum[i] > thi; }));
+    }
+    // in order and apart: a run that starts in or right behind an earlier one is joined to it
+#pragma unroll
+    for (int i = 0; i < SB_RANGES; ++i)
+#pragma unroll
+        for (int j = 0; j < SB_RANGES - 1 - i; ++j)
+            if (lo[j + 1] < lo[j]) {
+                const int l = lo[j], h = hi[j];
+                lo[j] = lo[j + 1]; hi[j] = hi[j + 1];
+                lo[j + 1] = l; hi[j + 1] = h;
+            }
+#pragma unroll
+    for (int i = SB_RANGES - 1; i > 0; --i)
+        if (lo[i] < SB_BINS && lo[i] <= hi[i - 1] + 1) {
+            hi[i - 1] = max(hi[i - 1], hi[i]);
+            lo[i] = SB_BINS;
+        }
+    // The least key whose bin is b or less, for the ends of the runs: x rises with the key, so a logit next to q / per_t
+    // is where floor(x) comes to q, to be found among 8 keys by 8 lanes; where the rounding of a large x leaves it
+    // outside of them, by halving.  Lanes 0-7: the first run's low keys, 8-15: the end of its high ones, ...
+    const int g = lane >> 4;
+    const int b = (lane & 8) ? (g == 0 ? lo[0] : g == 1 ? lo[1] : g == 2 ? lo[2] : lo[3]) - 1
+                             : (g == 0 ? hi[0] : g == 1 ? hi[1] : g == 2 ? hi[2] : hi[3]);
+    const uint32_t near = max(rank_key((float)((rb.qmax - (double)b) / rb.per_t)), 0x00800004u) - 4u;
+    const unsigned mask = (unsigned)(__ballot(rb.bin(rb.x(near + (lane & 7))) <= (double)b) >> (lane & 56)) & 255u;
+    uint32_t key = near + (mask ? __ffs(mask) - 1 : 8);
+    if (mask == 0u || mask == 255u) {
+        uint32_t kl = 0x00800000u, kh = 0xff800000u;           // the finite numbers' keys
+        while (kl < kh) {
+            const uint32_t mid = kl + (kh - kl) / 2;
+            if (rb.bin(rb.x(mid)) <= (double)b) kh = mid;
+            else kl = mid + 1;
+        }
+        key = kl;
+    }
+    pl.n = 0;
+#pragma unroll
+    for (int i = 0; i < SB_RANGES; ++i) {
+        pl.lo[i] = lo[i];
+        pl.hi[i] = hi[i];
+        pl.klo[i] = 1u;
+        pl.khi[i] = 0u;
+        if (lo[i] >= SB_BINS) continue;
+        pl.klo[i] = (uint32_t)__builtin_amdgcn_readlane((int)key, 16 * i);
+        pl.khi[i] = lo[i] ? (uint32_t)__builtin_amdgcn_readlane((int)key, 16 * i + 8) - 1u : top;
+        pl.n += sh.cumc[hi[i]] - cbefore(lo[i]);
+    }
+    pl.slices = 0u;
+    return pl;
+}
+
+// The tokens of the plan's runs among a lane's 16 go into the list; a wave asks
+// once for their places.
+template <class Put>
+__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t (&k)[2][8], int i0, unsigned* fill, Put put) {
+    unsigned m = 0;
+#pragma unroll
+    for (int q = 0; q < SB_RANGES; ++q) {
+        if (pl.klo[q] > pl.khi[q]) continue;
+        const uint32_t klo = pl.klo[q], span = pl.khi[q] - klo;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) m |= k[j >> 3][j & 7] - klo <= span ? 1u << j : 0u;
+    }
+    if (!__ballot(m != 0u)) return;
+    const unsigned mine = (unsigned)__popc(m), upto = scan_wave(mine);
+    unsigned at = 0;
+    if ((threadIdx.x & 63) == 63) at = atomicAdd(fill, upto);
+    at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + upto - mine;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (m >> j & 1u) {
+            const uint32_t index = (uint32_t)(i0 + (j >> 3) * (SL_LEN / 2) + (j & 7));
+            if (at < (unsigned)SB_CAP) put(at, ((unsigned long long)k[j >> 3][j & 7] << 32) | (uint32_t)~index);
+            ++at;
+        }
+}
+
+// The cuts and the draw of a row, by one workgroup: its running sums in sh.cum
+// and sh.cumc, the tokens of the plan's runs in the list (unless they are more
+// than SB_CAP: then the row is read again, place by place).
+__device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const RowArgs& r, const RowPlan& plan, float u,
+                                         unsigned long long* list, SampleShared& sh) {
+    const int tid = threadIdx.x;
     const SampleRow p = a.rows[row];
-    // the largest
-    if (tid == 0) sh.khi = 0u;
-    __syncthreads();
-    uint32_t top = 0;
-    for (int i = tid; i < r.V; i += SB_THREADS) top = max(top, rank_key(load_val(r.logits, r.dt, r.base + i)));
-    atomicMax(&sh.khi, top);
-    __syncthreads();
-    top = sh.khi;
-    if (!top) {                                 // nothing to draw from
-        if (tid == 0) {
-            a.token[row] = -1;
-            a.p[row] = 0.0f;
-            if (a.top) a.top[row] = -INFINITY;
-        }
-        return;
+    const RowBins rb{p.per_t, plan.qmax};
+    const double all = plan.all;
+    const unsigned nall = plan.nall;
+    const bool by_k = p.top_k > 0 && (unsigned)p.top_k < nall, by_p = p.top_p < 1.0f;
+    auto before = [&](int b) { return b ? sh.cum[b - 1] : 0.0; };
+    auto cbefore = [&](int b) { return b ? sh.cumc[b - 1] : 0u; };
+    auto E = [&](int b) { return exp((double)b * (-1.0 / 32.0)); };
+    bool listed = plan.n <= (unsigned)SB_CAP, ranked = plan.n <= (unsigned)SB_RANK;
+    if (ranked) {                               // few: ranked together, bin behind bin
+        if (tid < (int)plan.n) sh.ranked[tid] = load_coherent(&list[tid]);
+        __syncthreads();
+        rank_tokens((int)plan.n, rb, sh);
     }
-    RowBins rb{p.per_t, 0.0};
-    const double xtop = rb.x(top);
-    rb.qmax = floor(xtop);
-    for (int i = tid; i < SB_BINS; i += SB_THREADS) { sh.mass[i] = 0; sh.cnt[i] = 0; }
-    __syncthreads();
-    for (int i = tid; i < r.V; i += SB_THREADS) {
-        const uint32_t k = rank_key(load_val(r.logits, r.dt, r.base + i));
-        if (!k) continue;
-        const double x = rb.x(k), b = rb.bin(x);
-        if (b < (double)SB_BINS) {
-            atomicAdd(&sh.cnt[(int)b], 1u);
-            atomicAdd(&sh.mass[(int)b], rb.units(x));
+    // where bin b's tokens start among all of the runs', or -1
+    auto start = [&](int b) {
+        int at = -1;
+        unsigned base = 0;
+#pragma unroll
+        for (int i = 0; i < SB_RANGES; ++i) {
+            if (plan.lo[i] >= SB_BINS) continue;
+            if (b >= plan.lo[i] && b <= plan.hi[i]) at = (int)(base + cbefore(b) - cbefore(plan.lo[i]));
+            base += sh.cumc[plan.hi[i]] - cbefore(plan.lo[i]);
         }
-    }
-    __syncthreads();
-    // E[b] and the bins' sums; one bin a thread
-    const double E = exp((double)tid * (-1.0 / 32.0));
-    double all;
-    unsigned nall;
-    const unsigned bc = sh.cnt[tid];
-    const unsigned long long bu = sh.mass[tid];
-    cum[tid] = scan_block<double>((double)bu * E, sh.wave_d, &all);
-    cumc[tid] = scan_block<unsigned>(bc, sh.wave_c, &nall);
-    __shared__ unsigned bins_c[SB_BINS];
-    __shared__ unsigned long long bins_u[SB_BINS];
-    bins_c[tid] = bc;
-    bins_u[tid] = bu;
-    __syncthreads();
-    auto before = [&](int b) { return b ? cum[b - 1] : 0.0; };
-    auto cbefore = [&](int b) { return b ? cumc[b - 1] : 0u; };
-    auto E_of = [&](int b) { return exp((double)b * (-1.0 / 32.0)); };
-    // first bin with pred, by the lowest thread that has it
-    auto first_bin = [&](bool pred) {
-        __syncthreads();
-        if (tid == 0) sh.found = SB_BINS;
-        __syncthreads();
-        if (pred) atomicMin(&sh.found, tid);
-        __syncthreads();
-        return sh.found;
+        return at;
     };
-    auto part_of = [&](int b) { return Part{b, 0u, 0xffffffffu, (int)bins_c[b]}; };
     // kept: the first C tokens, of weight W; W0: the units of those in bin 0, where the largest is (E[0] = 1)
     int C = (int)nall;
     double W = all;
-    unsigned long long W0 = bins_u[0];
-    auto cut = [&](int b, const Place& pl) {
-        const int c = (int)cbefore(b) + pl.count;
-        if (c >= C) return;
-        C = c;
-        W = before(b) + (double)pl.units * E_of(b);
-        if (b == 0) W0 = pl.units;
-    };
+    unsigned long long W0 = plan.units0;
     // share * kept weight, in units of bin b and less what is ahead of it, rounded down or up.  Where all that is
     // kept is in bin 0 the product is exact: equal logits have no other way to agree with u or top_p times their number.
     auto target = [&](float share, int b, bool up) {
-        if (C <= (int)cumc[0]) {
+        if (C <= (int)sh.cumc[0]) {
             const unsigned long long f = (unsigned long long)((double)share * 18446744073709551616.0);
             return __umul64hi(W0, f) + (up && W0 * f != 0ull ? 1ull : 0ull);
         }
-        const double t = fmax(0.0, ((double)share * W - before(b)) / E_of(b));
+        const double t = fmax(0.0, ((double)share * W - before(b)) / E(b));
         return (unsigned long long)(up ? ceil(t) : floor(t));
     };
-    auto bin_of = [&](float share) {            // the bin in which the running weight reaches share * W
-        const double t = (double)share * W;
-        const int b = first_bin(bc != 0u && cum[tid] >= t), last = first_bin(bc != 0u && cumc[tid] >= (unsigned)C);
-        return C <= (int)cumc[0] ? 0 : min(b, last);
-    };
-    if (p.top_k > 0 && (unsigned)p.top_k < nall) {
-        const int b = first_bin(cumc[tid] >= (unsigned)p.top_k);
-        cut(b, find_place(r, rb, part_of(b), BY_COUNT, (unsigned)p.top_k - cbefore(b), sh));
+    Place pl{0, 0ull, 0u, -1};
+    int b = 0;
+#pragma unroll 1
+    for (int step = 0; step < 5; ++step) {      // the three cuts, the draw, and the draw again where it came behind the last cut
+        Want want = BY_MASS;
+        unsigned long long t;
+        if (step == 0) {
+            if (!by_k) continue;
+            b = plan.kbin;
+            want = BY_COUNT;
+            t = (unsigned)p.top_k - cbefore(b);
+        } else if (step == 2) {
+            if (plan.vbin >= SB_BINS || cbefore(plan.vbin) >= (unsigned)C) continue;
+            b = plan.vbin;
+            want = BY_VALUE;
+            t = (unsigned long long)ceil(plan.thr / E(b));
+        } else if (step == 4) {
+            if ((int)cbefore(b) + pl.count <= C) continue;
+            want = BY_COUNT;
+            t = (unsigned)C - cbefore(b);
+        } else {
+            if (step == 1 && !by_p) continue;
+            // the bin in which the running weight reaches top_p of what is kept, or passes u of it
+            const float share = step == 1 ? p.top_p : u;
+            const double goal = (double)share * W;
+            const int to = wave_search(SB_BINS, [&](int i) { return step == 3 ? sh.cum[i] > goal : sh.cum[i] >= goal; });
+            b = C <= (int)sh.cumc[0] ? 0 : min(to, wave_search(SB_BINS, [&](int i) { return sh.cumc[i] >= (unsigned)C; }));
+            t = target(share, b, step == 1) + (step == 3 ? 1ull : 0ull);
+        }
+        const int at = start(b), cnt = (int)(sh.cumc[b] - cbefore(b));
+        if (ranked && at >= 0) pl = place_in_ranked(at, cnt, 0, 0ull, want, t, rb, sh);
+        else {
+            pl = find_place(r, rb, Part{b, 0u, 0xffffffffu, cnt}, list, listed && at >= 0 ? (int)plan.n : 0, want, t, sh);
+            listed = listed && at >= 0;         // find_place took the list's memory
+            ranked = false;                     // and that of the ranked ones
+        }
+        const int c = (int)cbefore(b) + pl.count;
+        if (step < 3 && c < C) {
+            C = c;
+            W = before(b) + (double)pl.units * E(b);
+            if (b == 0) W0 = pl.units;
+        }
     }
-    if (p.top_p < 1.0f) {
-        const int b = bin_of(p.top_p);
-        cut(b, find_place(r, rb, part_of(b), BY_MASS, target(p.top_p, b, true), sh));
-    }
-    if (p.min_p > 0.0f) {
-        // exp(d) E[bin] >= min_p exp(d_max), exp(d) in [1, e^(1/32)): the first bin whose least weight fails may hold
-        // some that pass, those behind it none
-        const double thr = (double)p.min_p * (double)rb.units(xtop);
-        const int b = first_bin(bc != 0u && E * SB_UNIT < thr);
-        if (b < SB_BINS) cut(b, find_place(r, rb, part_of(b), BY_VALUE, (unsigned long long)ceil(thr / E_of(b)), sh));
-    }
-    const float u = a.u ? fminf(fmaxf(a.u[row], 0.0f), 0.99999994f) : 0.0f;
-    const int b = bin_of(u);
-    Place pl = find_place(r, rb, part_of(b), BY_MASS, target(u, b, false) + 1ull, sh);
-    if ((int)cbefore(b) + pl.count > C) pl = find_place(r, rb, part_of(b), BY_COUNT, (unsigned)C - cbefore(b), sh);
     if (tid == 0) {
         a.token[row] = pl.index;
-        a.p[row] = (float)((double)rb.units(rb.x(pl.key)) * E_of(b) / W);
-        if (a.top) a.top[row] = key_logit(top);
+        a.p[row] = (float)((double)rb.units(rb.x(pl.key)) * E(b) / W);
+        if (a.top) a.top[row] = key_logit(plan.top);
     }
 }
 
+__device__ __forceinline__ void draw_nothing(const SampleArgs& a, int row) {
+    if (threadIdx.x == 0) {
+        a.token[row] = -1;
+        a.p[row] = 0.0f;
+        if (a.top) a.top[row] = -INFINITY;
+    }
+}
+
+__device__ __forceinline__ float row_u(const SampleArgs& a, int row) { return a.u ? fminf(fmaxf(a.u[row], 0.0f), 0.99999994f) : 0.0f; }
+
+// A row of one slice, by one workgroup.
+__global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) {
+    __shared__ SampleShared sh;
+    __shared__ unsigned long long list[SB_CAP];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    RowBins rb{a.rows[row].per_t, 0.0};
+    const float u = row_u(a, row);
+    uint32_t k[2][8];
+    const int i0 = load_slice(r, 0, k);
+    if (tid == 0) sh.fill = 0u;
+    const uint32_t top = count_slice(k, rb, sh.hist, sh.wave_c);
+    if (!top) return draw_nothing(a, row);
+    unsigned bc[SB_PER];
+    unsigned long long bu[SB_PER];
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        bc[j] = (unsigned)sh.hist[SB_PER * tid + j] & 16383u;
+        bu[j] = sh.hist[SB_PER * tid + j] >> 14;
+    }
+    const RowPlan plan = make_plan(a.rows[row], u, rb, top, bc, bu, sh);
+    if (plan.n <= (unsigned)SB_CAP) take_tokens(plan, k, i0, &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
+    __syncthreads();
+    draw_row(a, row, r, plan, u, list, sh);
+}
+
+// Counts one slice of a row; the row's last workgroup to end joins the counts and makes the plan.
+__global__ __launch_bounds__(SB_THREADS, 4) void sample_count_kernel(SampleArgs a) {
+    __shared__ SampleShared sh;
+    const int slice = blockIdx.x, row = blockIdx.y, ns = gridDim.x, tid = threadIdx.x;
+    RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
+    SliceHead* heads = (SliceHead*)a.heads + (size_t)row * ns;
+    unsigned long long* bins = a.bins + (size_t)row * ns * SB_BINS;
+    RowBins rb{a.rows[row].per_t, 0.0};
+    {
+        const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+        uint32_t k[2][8];
+        load_slice(r, slice, k);
+        const uint32_t top = count_slice(k, rb, sh.hist, sh.wave_c);
+        if (tid == 0) {
+            store_coherent((unsigned long long*)&heads[slice].q, (unsigned long long)__double_as_longlong(rb.qmax));
+            store_coherent((unsigned long long*)&heads[slice].top, (unsigned long long)top);
+        }
+        for (int i = tid; i < SB_BINS; i += SB_THREADS) store_coherent(&bins[(size_t)slice * SB_BINS + i], sh.hist[i]);
+    }
+    if (!last_arrival(&ws->arrived, (unsigned)ns, &sh.flag)) return;
+    uint32_t top = 0;
+    double q = 0.0;
+    if (tid < ns) {
+        q = __longlong_as_double((long long)load_coherent((unsigned long long*)&heads[tid].q));
+        top = (uint32_t)load_coherent((unsigned long long*)&heads[tid].top);
+    }
+    const uint32_t mytop = top;
+    top = block_max<SB_THREADS / 64>(top, sh.wave_c);
+    rb.qmax = floor(rb.x(top));
+    if (tid < SAMPLE_MAX_SLICES) {
+        const double d = rb.qmax - q;
+        sh.shift[tid] = mytop != 0u && d < (double)SB_BINS ? (int)d : -1;
+    }
+    if (tid < SAMPLE_MAX_SLICES / 32) sh.touched[tid] = 0u;
+    __syncthreads();
+    if (!top) {
+        if (tid == 0) ws->plan.top = 0u;
+        return;
+    }
+    unsigned bc[SB_PER] = {};
+    unsigned long long bu[SB_PER] = {}, in_lo = 0, in_hi = 0;  // this thread's bins, and the slices that have tokens in them
+    for (int s0 = 0; s0 < ns; s0 += 8) {
+        unsigned long long v[8][SB_PER];
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const int s = s0 + g, d = s < ns ? sh.shift[s] : -1;
+#pragma unroll
+            for (int j = 0; j < SB_PER; ++j) {
+                const int i = SB_PER * tid + j - d;
+                v[g][j] = d >= 0 && i >= 0 ? load_coherent(&bins[(size_t)s * SB_BINS + i]) : 0ull;
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            unsigned long long some = 0;
+#pragma unroll
+            for (int j = 0; j < SB_PER; ++j) {
+                bc[j] += (unsigned)v[g][j] & 16383u;
+                bu[j] += v[g][j] >> 14;
+                some |= v[g][j];
+            }
+            const unsigned long long bit = some ? 1ull << ((s0 + g) & 63) : 0ull;
+            if (s0 < 64) in_lo |= bit;
+            else in_hi |= bit;
+        }
+    }
+    RowPlan plan = make_plan(a.rows[row], row_u(a, row), rb, top, bc, bu, sh);
+    bool mine = false;
+#pragma unroll
+    for (int i = 0; i < SB_RANGES; ++i)
+        mine |= plan.lo[i] < SB_BINS && SB_PER * tid + SB_PER > plan.lo[i] && SB_PER * tid <= plan.hi[i];
+    if (mine) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            if ((unsigned)(in_lo >> (32 * w))) atomicOr(&sh.touched[w], (unsigned)(in_lo >> (32 * w)));
+            if ((unsigned)(in_hi >> (32 * w))) atomicOr(&sh.touched[2 + w], (unsigned)(in_hi >> (32 * w)));
+        }
+    }
+    for (int i = tid; i < SB_BINS; i += SB_THREADS) {
+        ws->cum[i] = sh.cum[i];
+        ws->cumc[i] = sh.cumc[i];
+    }
+    __syncthreads();
+    if (tid == 0) {
+        // more tokens than the list takes: the row's first workgroup draws alone
+#pragma unroll
+        for (int w = 0; w < SAMPLE_MAX_SLICES / 32; ++w) {
+            plan.touched[w] = plan.n <= (unsigned)SB_CAP ? sh.touched[w] : w == 0 ? 1u : 0u;
+            plan.slices += (unsigned)__popc(plan.touched[w]);
+        }
+        ws->plan = plan;
+        ws->fill = 0u;
+    }
+}
+
+// Gathers one slice's tokens of the plan's runs; the row's last workgroup to end draws.
+__global__ __launch_bounds__(SB_THREADS, 4) void sample_draw_kernel(SampleArgs a) {
+    __shared__ SampleShared sh;
+    const int slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
+    const RowPlan plan = ws->plan;
+    if (!plan.top) {
+        if (slice == 0) draw_nothing(a, row);
+        return;
+    }
+    if (!(ws->plan.touched[slice >> 5] >> (slice & 31) & 1u)) return;
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    if (plan.n <= (unsigned)SB_CAP) {
+        uint32_t k[2][8];
+        const int i0 = load_slice(r, slice, k);
+        take_tokens(plan, k, i0, &ws->fill, [&](unsigned at, unsigned long long v) { store_coherent(&ws->list[at], v); });
+    }
+    if (!last_arrival(&ws->drawn, plan.slices, &sh.flag)) return;
+    for (int i = tid; i < SB_BINS; i += SB_THREADS) {
+        sh.cum[i] = ws->cum[i];
+        sh.cumc[i] = ws->cumc[i];
+    }
+    __syncthreads();
+    draw_row(a, row, r, plan, row_u(a, row), ws->list, sh);
+}
+
 hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st) {
-    sample_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), 0, st>>>(a);
+    if (!a.slices) {
+        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const dim3 g((unsigned)a.slices, (unsigned)m);
+    sample_count_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
+    sample_draw_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+size_t sample_slice_bytes(int slices) { return (size_t)MAX_ROWS * slices * (sizeof(SliceHead) + 8 * SB_BINS); }
+
+// The counters of every row's workspace, once.
+__global__ void sample_clear_kernel(uint8_t* rows) {
+    RowSpace* ws = (RowSpace*)(rows + (size_t)threadIdx.x * SAMPLE_ROW_BYTES);
+    ws->arrived = 0u;
+    ws->drawn = 0u;
+    ws->fill = 0u;
+}
+
+hipError_t launch_sample_clear(uint8_t* rows, hipStream_t st) {
+    sample_clear_kernel<<<dim3(1), dim3(MAX_ROWS), 0, st>>>(rows);
     return hipGetLastError();
 }
 

@@ -169,6 +169,9 @@ struct Stage {
     // workspace of the MXFP4 products: activation fragments and their scales, grown on need
     uint8_t *mx_a = nullptr, *mx_s = nullptr;
     size_t mx_a_cap = 0, mx_s_cap = 0;
+    // workspace of the sampling calls: the slices' counts, grown on need
+    uint8_t *smp = nullptr, *smp_rows = nullptr;
+    size_t smp_cap = 0;
     // first-stage role: token embedding table [embed_vocab][H] in act dtype (stage_embed_attach)
     uint16_t* embed = nullptr;
     int embed_vocab = 0;
@@ -225,7 +228,7 @@ struct Stage {
         (void)hipSetDevice(device);
         (void)hipDeviceSynchronize();
         for (void* p : allocs) (void)hipFree(p);
-        for (void* p : {(void*)mx_a, (void*)mx_s})
+        for (void* p : {(void*)mx_a, (void*)mx_s, (void*)smp})
             if (p) (void)hipFree(p);
         if (meta_dev) (void)hipFree(meta_dev);
         for (int i = 0; i < META_RING; ++i) {
@@ -562,7 +565,7 @@ int grow(uint8_t** p, size_t* cap, size_t bytes) {
     if (hipMalloc(p, bytes) != hipSuccess) {
         (void)hipGetLastError();
         *p = nullptr;
-        return fail(STAGE_E_OOM, "product workspace allocation failed");
+        return fail(STAGE_E_OOM, "workspace allocation failed");
     }
     *cap = bytes;
     return STAGE_OK;
@@ -655,6 +658,22 @@ int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, 
     a.token = token;
     a.p = p;
     a.top = top;
+    const size_t es = dt == DT_F32 ? 4 : 2;
+    a.vec = ((uintptr_t)logits & 15) == 0 && (M == 1 || (size_t)ld * es % 16 == 0);
+    if (V > SAMPLE_SLICE) {
+        a.slices = (V + SAMPLE_SLICE - 1) / SAMPLE_SLICE;
+        int rc = grow(&st->smp, &st->smp_cap, sample_slice_bytes(a.slices));
+        if (rc) return rc;
+        if (!st->smp_rows) {
+            uint8_t* rows = nullptr;
+            if ((rc = st->alloc(&rows, MAX_ROWS * SAMPLE_ROW_BYTES))) return rc;
+            HIP_TRY(launch_sample_clear(rows, s));
+            st->smp_rows = rows;
+        }
+        a.rows_ws = st->smp_rows;
+        a.heads = st->smp;
+        a.bins = (unsigned long long*)(st->smp + (size_t)MAX_ROWS * a.slices * 16);
+    }
     for (int i = 0; i < M; ++i) {
         a.rows[i] = SampleRow{32.0, 0, 1.0f, 0.0f};
         if (!params) continue;
@@ -1688,7 +1707,13 @@ int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, in
         if (rc) return rc;
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
-        return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, (hipStream_t)stream);
+        hipStream_t s = (hipStream_t)stream;
+        if ((rc = not_captured(s))) return rc;
+        HIP_TRY(order_on(st, s));
+        rc = sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);
+        if (rc) return rc;
+        HIP_TRY(mark_done(st, s));
+        return STAGE_OK;
     });
 }
 
