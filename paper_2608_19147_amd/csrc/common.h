@@ -362,7 +362,18 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, in
                                  hipStream_t st);
 hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx4Mat& w, hipStream_t st);
 hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, int m, int k, hipStream_t st);
-hipError_t launch_mx4_gemm(const Mx4Mat& w, const Mx4Act& a, int m, void* out, int dt, int64_t ld, hipStream_t st);
+struct Mx4Gemm {
+    Mx4Mat w; Mx4Act a;
+    int m;
+    void* out; int dt; size_t ld;
+    int pairs;                                     // two neighbouring outputs may be stored at once
+    int split, steps_per;                          // splits of K, steps of each (a multiple of 4)
+    float* part; int part_ld;                      // split > 1: their sums [split][m][part_ld]
+    int mtiles;                                    // set by the launcher
+};
+// Splits of K that fill the device.
+int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus);
+hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st);
 // out [m][H] fp16 = RMSNorm(row) * gamma.
 hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st);
 

@@ -31,13 +31,17 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 // ------------------------------------------------------------------ E2M1, E4M3
 
-// Code of a value scaled to [0, 8) in magnitude: nearest, ties to even, at most 6.
-__device__ __forceinline__ uint32_t e2m1(float v) {
-    const float a = fabsf(v);
-    const float inv = a < 2.0f ? 2.0f : a < 4.0f ? 1.0f : 0.5f;    // steps of 0.5, 1 and 2
-    const float r = rintf(a * inv);                                // 0..4, 2..4, 2..4 steps
-    const uint32_t c = (uint32_t)r + (a < 2.0f ? 0u : a < 4.0f ? 2u : 4u);
-    return (c > 7u ? 7u : c) | ((__float_as_uint(v) >> 28) & 8u);
+// Codes of eight values times `inv` (then below 8 in magnitude): nearest, ties
+// to even, at most 6; the first value in the low bits.  The conversion does all
+// of that; its scale operand is left at 1 and the power of two multiplied in
+// before, exactly, also where it is subnormal.
+__device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8], float inv) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * inv, v[1] * inv, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * inv, v[3] * inv, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * inv, v[5] * inv, 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * inv, v[7] * inv, 1.0f, 3);
+    return w;
 }
 
 __device__ __forceinline__ float e2m1_value(uint32_t c) {
@@ -65,50 +69,126 @@ __device__ __forceinline__ uint32_t absbits(float v) { return __float_as_uint(v)
 
 // ------------------------------------------------------------------ quantize
 
-__global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, int dt, size_t ld, int m, int k,
+// Eight values of a row a thread, four neighbouring threads a block: their
+// largest magnitude is shared by lane exchanges, each writes 4 bytes of codes.
+// VEC: rows start on 16 bytes and hold a multiple of 8 values (codes then start
+// on 4 bytes).  Bound by memory: 2 bytes a value read (16 bits), 17/32 written.
+template <int DT, bool VEC>
+__global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, size_t ld, int m, int k, int chunks,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    const int nb = (k + 31) / 32;
-    const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;     // one block of 32 a thread
-    if (idx >= (size_t)m * nb) return;
-    const int r = (int)(idx / nb), b = (int)(idx % nb);
-    const int n = min(32, k - 32 * b);
+    // chunks: of 8 values in a row, a multiple of 4
+    const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
+    if (idx >= (size_t)m * chunks) return;                         // whole blocks of 32 leave together
+    const bool small = (size_t)m * chunks < ((size_t)1 << 32);
+    const size_t r = small ? (size_t)((uint32_t)idx / (uint32_t)chunks) : idx / chunks;
+    const int c = (int)(idx - r * chunks), i0 = 8 * c;
+    float v[8];
+    if (VEC && i0 + 8 <= k) {
+        if constexpr (DT == DT_F32) {
+            const u32x4* p = (const u32x4*)((const float*)x + r * ld + i0);
+            const u32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { v[j] = __uint_as_float(a[j]); v[4 + j] = __uint_as_float(b[j]); }
+        } else {
+            const u32x4 a = *(const u32x4*)((const uint16_t*)x + r * ld + i0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 1] >> (16 * (j & 1))), DT);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i0 + j < k ? load_val(x, DT, r * ld + i0 + j) : 0.0f;
+    }
     uint32_t top = 0;
-    float v[32];
-    for (int i = 0; i < 32; ++i) {
-        v[i] = i < n ? load_val(x, dt, r * ld + 32 * (size_t)b + i) : 0.0f;
-        top = max(top, absbits(v[i]));
-    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, absbits(v[j]));
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));   // lane ^ 2
+    if (i0 >= k) return;
     const uint32_t byte = block_byte(top, 2);
-    const float inv = byte == 255u ? 0.0f : e8m0_inv(byte);
-    uint8_t* c = codes + (size_t)r * ((k + 1) / 2) + 16 * (size_t)b;
-    for (int i = 0; i < n; i += 2) {
-        const uint32_t lo = byte == 255u ? 0u : e2m1(v[i] * inv), hi = byte == 255u ? 0u : e2m1(v[i + 1] * inv);
-        c[i / 2] = (uint8_t)(lo | (hi << 4));
+    const uint32_t w = byte == 255u ? 0u : e2m1x8(v, e8m0_inv(byte));
+    uint8_t* o = codes + r * ((size_t)(k + 1) / 2) + i0 / 2;
+    if (VEC) {
+        *(uint32_t*)o = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + 2 * j < k) o[j] = (uint8_t)(w >> (8 * j));
     }
-    scales[(size_t)r * nb + b] = (uint8_t)byte;
+    if ((c & 3) == 0) scales[r * (size_t)(chunks / 4) + c / 4] = (uint8_t)byte;
 }
 
 hipError_t launch_mx4_quantize(const void* x, int dt, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales, hipStream_t st) {
-    const size_t n = (size_t)m * ((k + 31) / 32);
-    mx4_quantize_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(x, dt, (size_t)ld, m, k, codes, scales);
+    const int chunks = (k + 31) / 32 * 4;
+    const size_t n = (size_t)m * chunks;
+    const dim3 g((unsigned)((n + 255) / 256)), b(256);
+    const size_t es = dt == DT_F32 ? 4 : 2;
+    const bool vec = k % 8 == 0 && ((uintptr_t)x & 15) == 0 && (m == 1 || (size_t)ld * es % 16 == 0) && ((uintptr_t)codes & 3) == 0;
+#define MX4_Q(DT, VEC) mx4_quantize_kernel<DT, VEC><<<g, b, 0, st>>>(x, (size_t)ld, m, k, chunks, codes, scales)
+    if (dt == DT_F32) vec ? MX4_Q(DT_F32, true) : MX4_Q(DT_F32, false);
+    else if (dt == DT_F16) vec ? MX4_Q(DT_F16, true) : MX4_Q(DT_F16, false);
+    else vec ? MX4_Q(DT_BF16, true) : MX4_Q(DT_BF16, false);
+#undef MX4_Q
     return hipGetLastError();
 }
 
+// Eight values a thread.  VEC: codes start on 4 bytes, rows of out on 16, k is a multiple of 8.
+template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                             int m, int k, void* __restrict__ out, int dt, size_t ld) {
+                                                             int m, int k, int chunks, void* __restrict__ out, size_t ld) {
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
-    if (idx >= (size_t)m * k) return;
-    const size_t r = idx / k, c = idx % k;
-    const uint32_t code = (codes[r * ((k + 1) / 2) + c / 2] >> (4 * (c & 1))) & 15u;
-    const float v = e2m1_value(code) * e8m0(scales[r * ((k + 31) / 32) + c / 32]);
-    if (dt == DT_F32) ((float*)out)[r * ld + c] = v;
-    else ((uint16_t*)out)[r * ld + c] = to_half_bits(v, dt);
+    if (idx >= (size_t)m * chunks) return;
+    const bool small = (size_t)m * chunks < ((size_t)1 << 32);
+    const size_t r = small ? (size_t)((uint32_t)idx / (uint32_t)chunks) : idx / chunks;
+    const int c = (int)(idx - r * chunks), i0 = 8 * c;
+    const uint8_t* p = codes + r * ((size_t)(k + 1) / 2) + i0 / 2;
+    uint32_t w = 0;
+    if (VEC) {
+        w = *(const uint32_t*)p;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + 2 * j < k) w |= (uint32_t)p[j] << (8 * j);
+    }
+    const float s = e8m0(scales[r * (size_t)((k + 31) / 32) + c / 4]);
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = e2m1_value(w >> (4 * j)) * s;
+    const size_t at = r * ld + i0;
+    if constexpr (DT == DT_F32) {
+        if (VEC) {
+            ((float4*)((float*)out + at))[0] = float4{v[0], v[1], v[2], v[3]};
+            ((float4*)((float*)out + at))[1] = float4{v[4], v[5], v[6], v[7]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i0 + j < k) ((float*)out)[at + j] = v[j];
+        }
+    } else {
+        if (VEC) {
+            u32x4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = (uint32_t)to_half_bits(v[2 * j], DT) | (uint32_t)to_half_bits(v[2 * j + 1], DT) << 16;
+            *(u32x4*)((uint16_t*)out + at) = o;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i0 + j < k) ((uint16_t*)out)[at + j] = to_half_bits(v[j], DT);
+        }
+    }
 }
 
 hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int m, int k, void* out, int dt, int64_t ld,
                                  hipStream_t st) {
-    const size_t n = (size_t)m * k;
-    mx4_dequantize_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(codes, scales, m, k, out, dt, (size_t)ld);
+    const int chunks = (k + 7) / 8;
+    const size_t n = (size_t)m * chunks;
+    const dim3 g((unsigned)((n + 255) / 256)), b(256);
+    const size_t es = dt == DT_F32 ? 4 : 2;
+    const bool vec = k % 8 == 0 && ((uintptr_t)out & 15) == 0 && (m == 1 || (size_t)ld * es % 16 == 0) && ((uintptr_t)codes & 3) == 0;
+#define MX4_D(DT, VEC) mx4_dequantize_kernel<DT, VEC><<<g, b, 0, st>>>(codes, scales, m, k, chunks, out, (size_t)ld)
+    if (dt == DT_F32) vec ? MX4_D(DT_F32, true) : MX4_D(DT_F32, false);
+    else if (dt == DT_F16) vec ? MX4_D(DT_F16, true) : MX4_D(DT_F16, false);
+    else vec ? MX4_D(DT_BF16, true) : MX4_D(DT_BF16, false);
+#undef MX4_D
     return hipGetLastError();
 }
 
@@ -148,27 +228,46 @@ hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx
 
 // ------------------------------------------------------------------ activations
 
+// Values at .. at + 15 of x, zero from `left` on.  vec: at is a multiple of 16 bytes into x.
+__device__ __forceinline__ void load16(const void* x, int dt, int vec, size_t at, int left, float (&v)[16]) {
+    if (vec && left >= 16) {
+        if (dt == DT_F32) {
+            const u32x4* p = (const u32x4*)((const float*)x + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const u32x4 a = p[q];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * q + j] = __uint_as_float(a[j]);
+            }
+        } else {
+            const u32x4* p = (const u32x4*)((const uint16_t*)x + at);
+            const u32x4 a[2] = {p[0], p[1]};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 3][(j >> 1) & 3] >> (16 * (j & 1))), dt);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = j < left ? load_val(x, dt, at + j) : 0.0f;
+    }
+}
+
 // 16 values of one row (half a block) a thread; the two threads of a block are
-// neighbours and share its largest magnitude.  Rows from m and columns from k
-// on are zero.  T terms of E4M3 (T = 0: one E2M1 term).
+// neighbours and share its largest magnitude.  A workgroup takes 32 rows by two
+// steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
+// m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).
 template <int T>
-__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, int dt, size_t ld, int m, int k, int steps,
-                                                       int tiles, uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
+__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, int dt, int vec, size_t ld, int m, int k, int steps,
+                                                       uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1;
-    const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
-    if (idx >= (size_t)tiles * 32 * steps * 4) return;             // whole waves: a block's two threads stay together
-    const int p = (int)(idx & 3);                                  // quarter of the step of 64
-    const size_t rs = idx >> 2;
-    const int s = (int)(rs % steps), row = (int)(rs / steps);
+    const int p = threadIdx.x & 3;                                 // quarter of the step of 64
+    const int s = 2 * blockIdx.x + (threadIdx.x >> 7), row = 32 * blockIdx.y + ((threadIdx.x >> 2) & 31);
     const int k0 = 64 * s + 16 * p;
     float v[16];
+    load16(x, dt, vec, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        v[i] = row < m && k0 + i < k ? load_val(x, dt, row * ld + k0 + i) : 0.0f;
-        top = max(top, absbits(v[i]));
-    }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    for (int i = 0; i < 16; ++i) top = max(top, absbits(v[i]));
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
     const size_t tile = row >> 5;
     const int r = row & 31, b = p >> 1;
     const size_t frag = (tile * steps + s) * (size_t)(NT * U) * 1024;
@@ -176,12 +275,10 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
     if constexpr (T == 0) {
         const uint32_t byte = block_byte(top, 2);
         const float inv = byte == 255u ? 0.0f : e8m0_inv(byte);
-        u32x2 o = {0u, 0u};
+        float h[2][8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t c = byte == 255u ? 0u : e2m1(v[i] * inv);
-            o[i >> 3] |= c << (4 * (i & 7));
-        }
+        for (int i = 0; i < 16; ++i) h[i >> 3][i & 7] = byte == 255u ? 0.0f : v[i];
+        const u32x2 o = {e2m1x8(h[0], inv), e2m1x8(h[1], inv)};
         *(u32x2*)(a + frag + (b * 32 + r) * 16 + (p & 1) * 8) = o;
         if (!(p & 1)) as[sc] = (uint8_t)byte;
     } else {
@@ -211,7 +308,7 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
             *(u32x4*)(a + frag + ((size_t)t * 2 + b) * 1024 + ((p & 1) * 32 + r) * 16) = o;
             if (!(p & 1)) as[sc + (size_t)t * 256] = (uint8_t)(bad ? 255 : byte);
             if (t + 1 < NT) {
-                rest = max(rest, (uint32_t)__shfl_xor((int)rest, 1));
+                rest = max(rest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rest, 0xB1, 0xF, 0xF, false));
                 int e = rest ? (int)(rest >> 23) - 127 : 0;        // the rest's largest magnitude to [1, 2)
                 e = max(e, max(-byte, -127));
                 byte += e;
@@ -224,12 +321,12 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
 }
 
 hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, int m, int k, hipStream_t st) {
-    const size_t n = (size_t)a.tiles * 32 * a.steps * 4;
-    const dim3 g((unsigned)((n + 255) / 256)), b(256);
+    const int vec = ((uintptr_t)x & 15) == 0 && (m == 1 || (size_t)ld * (dt == DT_F32 ? 4 : 2) % 16 == 0);
+    const dim3 g((unsigned)(a.steps / 2), (unsigned)a.tiles), b(256);
     switch (a.terms) {
-        case 0: mx4_prep_kernel<0><<<g, b, 0, st>>>(x, dt, (size_t)ld, m, k, a.steps, a.tiles, a.a, a.s); break;
-        case 2: mx4_prep_kernel<2><<<g, b, 0, st>>>(x, dt, (size_t)ld, m, k, a.steps, a.tiles, a.a, a.s); break;
-        case 3: mx4_prep_kernel<3><<<g, b, 0, st>>>(x, dt, (size_t)ld, m, k, a.steps, a.tiles, a.a, a.s); break;
+        case 0: mx4_prep_kernel<0><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
+        case 2: mx4_prep_kernel<2><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
+        case 3: mx4_prep_kernel<3><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -237,49 +334,236 @@ hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, i
 
 // ------------------------------------------------------------------ product
 
-__device__ __forceinline__ void store_out(void* out, int dt, size_t i, float v) {
-    if (dt == DT_F32) ((float*)out)[i] = v;
-    else ((uint16_t*)out)[i] = to_half_bits(v, dt);
-}
-
-// One 32 x 32 tile a wave.
-template <int T>
-__global__ __launch_bounds__(64) void mx4_gemm_kernel(Mx4Mat w, const uint8_t* __restrict__ a, const uint8_t* __restrict__ as,
-                                                      int m, void* __restrict__ out, int dt, size_t ld) {
-    constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
-    const int lane = threadIdx.x, g = blockIdx.x >> 1, j = blockIdx.x & 1;
-    const size_t tile = blockIdx.y;
-    v16f acc = {};
-    for (int s = 0; s < w.steps; ++s) {
-        const u32x4 wf = ((const u32x4*)w.w)[(((size_t)g * w.steps + s) * 2 + j) * 64 + lane];
-        const uint32_t ws = w.s[(((size_t)g * (w.steps / 4) + s / 4) * 2 + j) * 64 + lane] >> (8 * (s & 3));
-        const v8i b = {(int)wf[0], (int)wf[1], (int)wf[2], (int)wf[3], 0, 0, 0, 0};
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const u32x4* f = (const u32x4*)(a + ((tile * w.steps + s) * NT + t) * (size_t)(U * 1024));
-            const uint32_t sa = ((const uint32_t*)as)[((tile * (w.steps / 4) + s / 4) * NT + t) * 64 + lane] >> (8 * (s & 3));
-            const u32x4 lo = f[lane], hi = U == 2 ? f[64 + lane] : u32x4{0u, 0u, 0u, 0u};
-            const v8i av = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, b, acc, FMT, 4, 0, (int)sa, 0, (int)ws);
+// Outputs of row `row` at p.out: columns col (even) and col + 1, as far as they exist.
+template <int DT>
+__device__ __forceinline__ void store_pair(const Mx4Gemm& p, int row, int col, bool fast, float a, float b) {
+    const size_t at = (size_t)row * p.ld + col;
+    if constexpr (DT == DT_F32) {
+        float* o = (float*)p.out + at;
+        if (fast) *(float2*)o = float2{a, b};
+        else {
+            o[0] = a;
+            if (col + 1 < p.w.n) o[1] = b;
+        }
+    } else {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        uint16_t* o = (uint16_t*)p.out + at;
+        const uint32_t h = DT == DT_BF16 ? __builtin_bit_cast(uint32_t, bf2{(__bf16)a, (__bf16)b}) : pack_f16x2(a, b);
+        if (fast) *(uint32_t*)o = h;
+        else {
+            o[0] = (uint16_t)h;
+            if (col + 1 < p.w.n) o[1] = (uint16_t)(h >> 16);
         }
     }
-    const int col = 64 * g + 2 * (lane & 31) + j;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int row = (int)tile * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-        if (row < m && col < w.n) store_out(out, dt, row * ld + col, acc[r]);
+}
+
+// The product of a fragment pair; the scale bytes are byte `step` (0..3) of their words.
+template <int FMT>
+__device__ __forceinline__ v16f mx4_mfma(v8i a, v8i b, v16f c, int step, uint32_t sa, uint32_t sb) {
+    switch (step) {                                                // a constant where this is used
+        case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FMT, 4, 0, (int)sa, 0, (int)sb);
+        case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FMT, 4, 1, (int)sa, 1, (int)sb);
+        case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FMT, 4, 2, (int)sa, 2, (int)sb);
+        default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, FMT, 4, 3, (int)sa, 3, (int)sb);
     }
 }
 
-hipError_t launch_mx4_gemm(const Mx4Mat& w, const Mx4Act& a, int m, void* out, int dt, int64_t ld, hipStream_t st) {
-    const dim3 g((unsigned)(2 * w.groups), (unsigned)((m + 31) / 32)), b(64);
-    switch (a.terms) {
-        case 0: mx4_gemm_kernel<0><<<g, b, 0, st>>>(w, a.a, a.s, m, out, dt, (size_t)ld); break;
-        case 2: mx4_gemm_kernel<2><<<g, b, 0, st>>>(w, a.a, a.s, m, out, dt, (size_t)ld); break;
-        case 3: mx4_gemm_kernel<3><<<g, b, 0, st>>>(w, a.a, a.s, m, out, dt, (size_t)ld); break;
+// One workgroup: 32 MT rows of x by 256 outputs, one 64-row group of W a wave,
+// over steps_per = a multiple of 4 steps of K (blockIdx.z: the split).  The
+// activations' fragments are shared by the four waves through LDS, double
+// buffered; W's go from memory to the registers that the product reads, each
+// used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.
+//
+// split > 1: fp32 sums to part [split][m][n], joined by mx4_reduce_kernel.
+template <int T, int MT, int KS>
+__global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
+    constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
+    constexpr int PIECES = MT * KS * NT * U;                       // kilobytes of a buffer
+    constexpr int PW = PIECES / 4;                                 // loaded by a wave
+    static_assert(PIECES % 4 == 0 && 4 % KS == 0, "buffer");
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    u32x4* lds = (u32x4*)smem;                                     // [2][PIECES * 64]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // neighbouring workgroups go to different XCDs: give each XCD a run of tiles, row tiles first, so that its L2
+    // holds the weights of few groups and every tile of them
+    int bid = blockIdx.x;
+    {
+        const int nwg = gridDim.x, per = nwg >> 3, more = nwg & 7, x = bid & 7, at = bid >> 3;
+        bid = x * per + min(x, more) + at;
+    }
+    const int mt0 = (bid % p.mtiles) * MT;
+    int g = (bid / p.mtiles) * 4 + wave;
+    const bool off = g >= p.w.groups;                              // a wave without outputs keeps step with the others
+    if (off) g = p.w.groups - 1;
+    const int steps = p.w.steps, s0 = blockIdx.z * p.steps_per, s1 = min(steps, s0 + p.steps_per);
+    const u32x4* wp = (const u32x4*)p.w.w + (size_t)g * steps * 128 + lane;
+    const uint32_t* wsp = p.w.s + (size_t)g * (steps / 4) * 128 + lane;
+    const uint32_t* asp = (const uint32_t*)p.a.s + (size_t)mt0 * (steps / 4) * NT * 64 + lane;
+    // this wave's pieces of a buffer: piece q of tile q / (KS NT U); tiles past the last are the last one again
+    const u32x4* ap[PW];
+#pragma unroll
+    for (int q = 0; q < PW; ++q) {
+        const int i = wave * PW + q, tile = min(mt0 + i / (KS * NT * U), p.a.tiles - 1);
+        ap[q] = (const u32x4*)p.a.a + ((size_t)tile * steps * (NT * U) + i % (KS * NT * U)) * 64 + lane;
+    }
+    int as_off[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) as_off[t] = (min(mt0 + t, p.a.tiles - 1) - mt0) * (steps / 4) * NT * 64;
+    v16f acc[MT][2] = {};
+    u32x4 ar[PW], wr[2][KS][2];
+    uint32_t wsc[2], asc[MT][NT], wsn[2], asn[MT][NT];
+    auto load_a = [&](int s) {
+#pragma unroll
+        for (int q = 0; q < PW; ++q) ar[q] = ap[q][(size_t)s * (NT * U * 64)];
+    };
+    auto load_w = [&](int s, u32x4 (&r)[KS][2]) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) r[i][j] = wp[(size_t)(s + i) * 128 + j * 64];
+    };
+    auto load_s = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) wsn[j] = wsp[(size_t)(s / 4) * 128 + j * 64];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) asn[t][n] = asp[as_off[t] + ((s / 4) * NT + n) * 64];
+    };
+    load_s(s0);
+    load_a(s0);
+    load_w(s0, wr[0]);
+#pragma unroll
+    for (int q = 0; q < PW; ++q) lds[(wave * PW + q) * 64 + lane] = ar[q];
+    for (int s = s0; s < s1; s += 4) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) wsc[j] = wsn[j];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) asc[t][n] = asn[t][n];
+        const int s_next = s + 4 < s1 ? s + 4 : s;
+#pragma unroll
+        for (int h = 0; h < 4 / KS; ++h) {
+            constexpr int PAR = (4 / KS) & 1;                      // buffers alternate; with one a round, by rounds
+            const int cur = PAR ? ((s - s0) >> 2) & 1 : h & 1;
+            __syncthreads();                                       // this buffer is written, the other one read
+            const int sn = h + 1 < 4 / KS ? s + (h + 1) * KS : s_next;
+            load_a(sn);
+            load_w(sn, wr[1]);
+            if (h == 4 / KS - 1) load_s(s_next);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                v8i b[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const u32x4 f = wr[0][i][j];
+                    b[j] = v8i{(int)f[0], (int)f[1], (int)f[2], (int)f[3], 0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const u32x4* f = &lds[cur * PIECES * 64 + (((t * KS + i) * NT + n) * U) * 64 + lane];
+                        const u32x4 lo = f[0], hi = U == 2 ? f[64] : u32x4{0u, 0u, 0u, 0u};
+                        const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) acc[t][j] = mx4_mfma<FMT>(a, b[j], acc[t][j], h * KS + i, asc[t][n], wsc[j]);
+                    }
+            }
+#pragma unroll
+            for (int q = 0; q < PW; ++q) lds[(cur ^ 1) * PIECES * 64 + (wave * PW + q) * 64 + lane] = ar[q];
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) wr[0][i][j] = wr[1][i][j];
+        }
+    }
+    if (off) return;
+    // lane l holds outputs 64 g + 2 (l mod 32) + j of rows 8 (r / 4) + 4 (l / 32) + r mod 4
+    const int col = 64 * g + 2 * (lane & 31);
+    const bool fast = p.pairs && col + 1 < p.w.n;
+    auto each = [&](auto put) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = (mt0 + t) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+                if (row < p.m) put(row, acc[t][0][r], acc[t][1][r]);
+            }
+    };
+    if (p.split > 1) {
+        float* part = p.part + (size_t)blockIdx.z * p.m * p.part_ld + col;
+        each([&](int row, float a, float b) { *(float2*)(part + (size_t)row * p.part_ld) = float2{a, b}; });
+    } else if (col < p.w.n) {
+        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, fast, a, b); });
+        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, fast, a, b); });
+        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, fast, a, b); });
+    }
+}
+
+// out = the sum of the splits, in their order.
+__global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
+    const int pairs = (p.w.n + 1) / 2;
+    const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
+    if (idx >= (size_t)p.m * pairs) return;
+    const int row = (int)(idx / pairs), col = 2 * (int)(idx % pairs);
+    float a = 0.0f, b = 0.0f;
+    for (int z = 0; z < p.split; ++z) {
+        const float2 v = *(const float2*)(p.part + ((size_t)z * p.m + row) * p.part_ld + col);
+        a += v.x;
+        b += v.y;
+    }
+    const bool fast = p.pairs && col + 1 < p.w.n;
+    if (p.dt == DT_F32) store_pair<DT_F32>(p, row, col, fast, a, b);
+    else if (p.dt == DT_F16) store_pair<DT_F16>(p, row, col, fast, a, b);
+    else store_pair<DT_BF16>(p, row, col, fast, a, b);
+}
+
+template <int T, int MT, int KS>
+hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
+    p.mtiles = (p.a.tiles + MT - 1) / MT;
+    const int ntiles = (p.w.groups + 3) / 4;
+    constexpr int LDS = 2 * MT * KS * (T ? 2 * T : 1) * 1024;
+    hipError_t e = hipSuccess;
+    if (LDS > 65536) e = hipFuncSetAttribute((const void*)mx4_gemm_kernel<T, MT, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (e != hipSuccess) return e;
+    mx4_gemm_kernel<T, MT, KS><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), LDS, st>>>(p);
+    e = hipGetLastError();
+    if (e == hipSuccess && p.split > 1) {
+        const size_t n = (size_t)p.m * ((p.w.n + 1) / 2);
+        mx4_reduce_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(p);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// Row tiles of 32 that a workgroup takes.
+static int gemm_mt(int terms, int tiles) { return tiles >= 5 ? (terms ? 4 : 8) : tiles >= 3 ? 4 : tiles; }
+
+// Splits of K: enough workgroups for every CU, at least 4 rounds of 256 k each.
+int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus) {
+    const int mt = gemm_mt(terms, tiles), wgs = (tiles + mt - 1) / mt * ((w.groups + 3) / 4), rounds = w.steps / 4;
+    int split = 1;
+    while (wgs * (split + 1) <= n_cus && rounds / (split + 1) >= 2) ++split;
+    return split;
+}
+
+hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
+    const int mt = gemm_mt(p.a.terms, p.a.tiles);
+    switch (p.a.terms * 10 + mt) {
+        case 1: return run_gemm<0, 1, 4>(p, st);
+        case 2: return run_gemm<0, 2, 4>(p, st);
+        case 4: return run_gemm<0, 4, 4>(p, st);
+        case 8: return run_gemm<0, 8, 4>(p, st);
+        case 21: return run_gemm<2, 1, 4>(p, st);
+        case 22: return run_gemm<2, 2, 2>(p, st);
+        case 24: return run_gemm<2, 4, 2>(p, st);
+        case 31: return run_gemm<3, 1, 4>(p, st);
+        case 32: return run_gemm<3, 2, 2>(p, st);
+        case 34: return run_gemm<3, 4, 2>(p, st);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 // out[m][H] = fp16(RMSNorm(row) * gamma): the input of an MXFP4 head.

@@ -167,8 +167,9 @@ struct Stage {
     float *logits = nullptr, *head_p = nullptr;        // logits rows [MAX_ROWS][vocab] and [MAX_ROWS], on first need
     int32_t* head_tok = nullptr;
     // workspace of the MXFP4 products: activation fragments and their scales, grown on need
-    uint8_t *mx_a = nullptr, *mx_s = nullptr;
-    size_t mx_a_cap = 0, mx_s_cap = 0;
+    // and the sums of split products
+    uint8_t *mx_a = nullptr, *mx_s = nullptr, *mx_p = nullptr;
+    size_t mx_a_cap = 0, mx_s_cap = 0, mx_p_cap = 0;
     // workspace of the sampling calls: the slices' counts, grown on need
     uint8_t *smp = nullptr, *smp_rows = nullptr;
     size_t smp_cap = 0;
@@ -228,7 +229,7 @@ struct Stage {
         (void)hipSetDevice(device);
         (void)hipDeviceSynchronize();
         for (void* p : allocs) (void)hipFree(p);
-        for (void* p : {(void*)mx_a, (void*)mx_s, (void*)smp})
+        for (void* p : {(void*)mx_a, (void*)mx_s, (void*)mx_p, (void*)smp})
             if (p) (void)hipFree(p);
         if (meta_dev) (void)hipFree(meta_dev);
         for (int i = 0; i < META_RING; ++i) {
@@ -627,7 +628,23 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         a.a = st->mx_a;
         a.s = st->mx_s;
         HIP_TRY(launch_mx4_prep(a, (const uint8_t*)x + (size_t)m0 * ldx * xb, dt, ldx, mm, w.k, s));
-        HIP_TRY(launch_mx4_gemm(w, a, mm, (uint8_t*)out + (size_t)m0 * ldo * ob, odt, ldo, s));
+        Mx4Gemm p{};
+        p.w = w;
+        p.a = a;
+        p.m = mm;
+        p.out = (uint8_t*)out + (size_t)m0 * ldo * ob;
+        p.dt = odt;
+        p.ld = (size_t)ldo;
+        p.pairs = ((uintptr_t)p.out & (2 * ob - 1)) == 0 && (mm == 1 || ldo % 2 == 0);
+        p.split = mx4_split(w, a.terms, a.tiles, st->n_cus);
+        p.steps_per = (w.steps / 4 + p.split - 1) / p.split * 4;
+        p.split = (w.steps + p.steps_per - 1) / p.steps_per;
+        p.part_ld = 64 * w.groups;
+        if (p.split > 1) {
+            if ((rc = grow(&st->mx_p, &st->mx_p_cap, (size_t)p.split * mm * p.part_ld * 4))) return rc;
+            p.part = (float*)st->mx_p;
+        }
+        HIP_TRY(launch_mx4_gemm(p, s));
     }
     return STAGE_OK;
 }
