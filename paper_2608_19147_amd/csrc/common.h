@@ -345,14 +345,15 @@ hipError_t launch_top1_merge(const float4* part, int M, int ntiles, int32_t* tok
 //   w: [groups][steps][2 (j)][64 lanes] x 16 bytes: 32 codes of row 64 group + 2 (lane % 32) + j,
 //      k = 64 step + 32 (lane / 32) ..: what one lane feeds to a 32 x 32 x 64 product.  The rows of the two j
 //      alternate, so that a lane's results of both are neighbours in an output row;
-//   s: [groups][steps / 4][2][64 lanes] words: the E8M0 bytes of those codes for 4 steps.
+//   s: [groups][steps / 4][64 lanes][2] words: the E8M0 bytes of those codes for 4 steps.
 // Rows from n and columns from k on hold zero codes with scale 1.
 struct Mx4Mat {
     uint8_t* w; uint32_t* s;
     int n, k, groups, steps;
 };
 // Activation rows in product form: 32-row tiles, the steps of the matrix, `terms` E4M3 terms (0: one E2M1 term),
-//   a: [tiles][steps][term] fragments of 2 x 64 lanes x 16 bytes (E2M1: 64 x 16); s: [tiles][steps / 4][term][64] words.
+//   a: [tiles][steps][term] fragments of 2 x 64 lanes x 16 bytes (E2M1: 64 x 16);
+//   s: [groups of 4 tiles][steps / 4][term][64 lanes][4 tiles] words, as for W.
 struct Mx4Act {
     uint8_t* a; uint8_t* s;
     int tiles, steps, terms;

@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
     u32x4 o;
     for (int i = 0; i < 4; ++i) o[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | (uint32_t)c[4 * i + 3] << 24;
     ((u32x4*)w.w)[idx] = o;
-    ((uint8_t*)w.s)[((((size_t)g * (w.steps / 4) + s / 4) * 2 + j) * 64 + lane) * 4 + (s & 3)] = byte;
+    ((uint8_t*)w.s)[((((size_t)g * (w.steps / 4) + s / 4) * 64 + lane) * 2 + j) * 4 + (s & 3)] = byte;
 }
 
 hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx4Mat& w, hipStream_t st) {
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
     const size_t tile = row >> 5;
     const int r = row & 31, b = p >> 1;
     const size_t frag = (tile * steps + s) * (size_t)(NT * U) * 1024;
-    const size_t sc = ((tile * (steps / 4) + s / 4) * NT * 64 + b * 32 + r) * 4 + (s & 3);
+    const size_t sc = ((((tile >> 2) * (steps / 4) + s / 4) * NT * 64 + b * 32 + r) * 4 + (tile & 3)) * 4 + (s & 3);
     if constexpr (T == 0) {
         const uint32_t byte = block_byte(top, 2);
         const float inv = byte == 255u ? 0.0f : e8m0_inv(byte);
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
             }
             // element e of lane 32 g + r: k = 16 g + e for the first 16, 32 + 16 g + e - 16 for the others
             *(u32x4*)(a + frag + ((size_t)t * 2 + b) * 1024 + ((p & 1) * 32 + r) * 16) = o;
-            if (!(p & 1)) as[sc + (size_t)t * 256] = (uint8_t)(bad ? 255 : byte);
+            if (!(p & 1)) as[sc + (size_t)t * 1024] = (uint8_t)(bad ? 255 : byte);
             if (t + 1 < NT) {
                 rest = max(rest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rest, 0xB1, 0xF, 0xF, false));
                 int e = rest ? (int)(rest >> 23) - 127 : 0;        // the rest's largest magnitude to [1, 2)
@@ -368,6 +368,75 @@ __device__ __forceinline__ v16f mx4_mfma(v8i a, v8i b, v16f c, int step, uint32_
     }
 }
 
+// The outputs of a wave: MT row tiles from mt0, group g.  Lane l holds outputs
+// 64 g + 2 (l mod 32) + j of rows 8 (r / 4) + 4 (l / 32) + r mod 4.
+template <int MT>
+__device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, const v16f (&acc)[MT][2]) {
+    const int lane = threadIdx.x & 63;
+    const int col = 64 * g + 2 * (lane & 31);
+    const bool fast = p.pairs && col + 1 < p.w.n;
+    auto each = [&](auto put) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = (mt0 + t) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+                if (row < p.m) put(row, acc[t][0][r], acc[t][1][r]);
+            }
+    };
+    if (p.split > 1) {
+        float* part = p.part + (size_t)blockIdx.z * p.m * p.part_ld + col;
+        each([&](int row, float a, float b) { *(float2*)(part + (size_t)row * p.part_ld) = float2{a, b}; });
+    } else if (col < p.w.n) {
+        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, fast, a, b); });
+        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, fast, a, b); });
+        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, fast, a, b); });
+    }
+}
+
+// Scale words of MT row tiles and a group of W, four steps at once.
+template <int NT, int MT>
+struct ScaleLoad {
+    const uint32_t* a[(MT + 3) / 4];
+    const u32x2* w;
+    __device__ __forceinline__ ScaleLoad(const Mx4Gemm& p, int mt0, int g, int lane) {
+        const int quads = p.w.steps / 4, groups = (p.a.tiles + 3) / 4;
+#pragma unroll
+        for (int q = 0; q < (MT + 3) / 4; ++q)
+            a[q] = (const uint32_t*)p.a.s + ((size_t)min(mt0 / 4 + q, groups - 1) * quads * NT * 64 + lane) * 4 + (MT < 4 ? mt0 % 4 : 0);
+        w = (const u32x2*)p.w.s + (size_t)g * quads * 64 + lane;
+    }
+    __device__ __forceinline__ void load(int quad, uint32_t (&as)[MT][NT], uint32_t (&ws)[2]) const {
+        const u32x2 v = w[(size_t)quad * 64];
+        ws[0] = v[0];
+        ws[1] = v[1];
+#pragma unroll
+        for (int q = 0; q < (MT + 3) / 4; ++q)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t* s = a[q] + ((size_t)quad * NT + n) * 256;
+                if constexpr (MT == 1) as[0][n] = s[0];
+                else if constexpr (MT == 2) {
+                    const u32x2 t = *(const u32x2*)s;
+                    as[0][n] = t[0];
+                    as[1][n] = t[1];
+                } else {
+                    const u32x4 t = *(const u32x4*)s;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) as[4 * q + i][n] = t[i];
+                }
+            }
+    }
+};
+
+// Neighbouring workgroups go to different XCDs: gives each XCD a run of tiles,
+// row tiles first, so that its L2 holds the weights of few groups and every tile
+// of them.
+__device__ __forceinline__ int xcd_run(int bid, int nwg) {
+    const int per = nwg >> 3, more = nwg & 7, x = bid & 7;
+    return x * per + min(x, more) + (bid >> 3);
+}
+
 // One workgroup: 32 MT rows of x by 256 outputs, one 64-row group of W a wave,
 // over steps_per = a multiple of 4 steps of K (blockIdx.z: the split).  The
 // activations' fragments are shared by the four waves through LDS, double
@@ -380,25 +449,19 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
     constexpr int PIECES = MT * KS * NT * U;                       // kilobytes of a buffer
     constexpr int PW = PIECES / 4;                                 // loaded by a wave
+    constexpr int FRAGS = MT * KS * NT, DEPTH = FRAGS < 4 ? FRAGS : T ? 2 : 4;
     static_assert(PIECES % 4 == 0 && 4 % KS == 0, "buffer");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     u32x4* lds = (u32x4*)smem;                                     // [2][PIECES * 64]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // neighbouring workgroups go to different XCDs: give each XCD a run of tiles, row tiles first, so that its L2
-    // holds the weights of few groups and every tile of them
-    int bid = blockIdx.x;
-    {
-        const int nwg = gridDim.x, per = nwg >> 3, more = nwg & 7, x = bid & 7, at = bid >> 3;
-        bid = x * per + min(x, more) + at;
-    }
+    const int bid = xcd_run(blockIdx.x, gridDim.x);
     const int mt0 = (bid % p.mtiles) * MT;
     int g = (bid / p.mtiles) * 4 + wave;
     const bool off = g >= p.w.groups;                              // a wave without outputs keeps step with the others
     if (off) g = p.w.groups - 1;
     const int steps = p.w.steps, s0 = blockIdx.z * p.steps_per, s1 = min(steps, s0 + p.steps_per);
     const u32x4* wp = (const u32x4*)p.w.w + (size_t)g * steps * 128 + lane;
-    const uint32_t* wsp = p.w.s + (size_t)g * (steps / 4) * 128 + lane;
-    const uint32_t* asp = (const uint32_t*)p.a.s + (size_t)mt0 * (steps / 4) * NT * 64 + lane;
+    const ScaleLoad<NT, MT> sl(p, mt0, g, lane);
     // this wave's pieces of a buffer: piece q of tile q / (KS NT U); tiles past the last are the last one again
     const u32x4* ap[PW];
 #pragma unroll
@@ -406,9 +469,6 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
         const int i = wave * PW + q, tile = min(mt0 + i / (KS * NT * U), p.a.tiles - 1);
         ap[q] = (const u32x4*)p.a.a + ((size_t)tile * steps * (NT * U) + i % (KS * NT * U)) * 64 + lane;
     }
-    int as_off[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) as_off[t] = (min(mt0 + t, p.a.tiles - 1) - mt0) * (steps / 4) * NT * 64;
     v16f acc[MT][2] = {};
     u32x4 ar[PW], wr[2][KS][2];
     uint32_t wsc[2], asc[MT][NT], wsn[2], asn[MT][NT];
@@ -422,14 +482,7 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) r[i][j] = wp[(size_t)(s + i) * 128 + j * 64];
     };
-    auto load_s = [&](int s) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) wsn[j] = wsp[(size_t)(s / 4) * 128 + j * 64];
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) asn[t][n] = asp[as_off[t] + ((s / 4) * NT + n) * 64];
-    };
+    auto load_s = [&](int s) { sl.load(s / 4, asn, wsn); };
     load_s(s0);
     load_a(s0);
     load_w(s0, wr[0]);
@@ -452,24 +505,31 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
             load_a(sn);
             load_w(sn, wr[1]);
             if (h == 4 / KS - 1) load_s(s_next);
+            // fragments in the order of use, read DEPTH ahead of their products; the scheduling barriers keep the loads
+            // above in front (the compiler had sunk them behind the products that cover them) and the reads ahead
+            const u32x4* buf = lds + cur * PIECES * 64 + lane;
+            u32x4 fr[DEPTH + 1][U];
+            auto read = [&](int e) {
+                const int i = e / (MT * NT), t = e / NT % MT, n = e % NT;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                v8i b[2];
+                for (int u = 0; u < U; ++u) fr[e % (DEPTH + 1)][u] = buf[(((t * KS + i) * NT + n) * U + u) * 64];
+            };
+#pragma unroll
+            for (int e = 0; e < DEPTH; ++e) read(e);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int e = 0; e < FRAGS; ++e) {
+                const int i = e / (MT * NT), t = e / NT % MT, n = e % NT;
+                if (e + DEPTH < FRAGS) read(e + DEPTH);
+                const u32x4 lo = fr[e % (DEPTH + 1)][0], hi = U == 2 ? fr[e % (DEPTH + 1)][U - 1] : u32x4{0u, 0u, 0u, 0u};
+                const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const u32x4 f = wr[0][i][j];
-                    b[j] = v8i{(int)f[0], (int)f[1], (int)f[2], (int)f[3], 0, 0, 0, 0};
+                    const v8i b = {(int)f[0], (int)f[1], (int)f[2], (int)f[3], 0, 0, 0, 0};
+                    acc[t][j] = mx4_mfma<FMT>(a, b, acc[t][j], h * KS + i, asc[t][n], wsc[j]);
                 }
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const u32x4* f = &lds[cur * PIECES * 64 + (((t * KS + i) * NT + n) * U) * 64 + lane];
-                        const u32x4 lo = f[0], hi = U == 2 ? f[64] : u32x4{0u, 0u, 0u, 0u};
-                        const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) acc[t][j] = mx4_mfma<FMT>(a, b[j], acc[t][j], h * KS + i, asc[t][n], wsc[j]);
-                    }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int q = 0; q < PW; ++q) lds[(cur ^ 1) * PIECES * 64 + (wave * PW + q) * 64 + lane] = ar[q];
@@ -480,26 +540,116 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
         }
     }
     if (off) return;
-    // lane l holds outputs 64 g + 2 (l mod 32) + j of rows 8 (r / 4) + 4 (l / 32) + r mod 4
-    const int col = 64 * g + 2 * (lane & 31);
-    const bool fast = p.pairs && col + 1 < p.w.n;
-    auto each = [&](auto put) {
+    store_tiles<MT>(p, mt0, g, acc);
+}
+
+// The same product for many rows, where the matrix cores are to be the bound.
+// A step of 64 k is 2 MT NT products of 32 or 64 cycles a wave, one wave a SIMD,
+// which issues in order: whatever the wave waits for or cannot issue leaves the
+// matrix core idle.  So
+//  - loads run D steps ahead in registers, W's fragments to their use, the
+//    activations' (a wave loads a quarter of a step's) into one of two LDS
+//    buffers;
+//  - memory instructions stand one by one between the products (four waves that
+//    each issue six at a time had the products wait for 35% of the cycles);
+//  - fragments are read AHEAD of their products, across the step's end: the
+//    barrier that frees one buffer and opens the other stands where the first
+//    fragment of the next step is read, under the products in between.
+// Everything is unrolled over D steps (a divisor of the step count), so that the
+// rings are registers.
+template <int T, int MT, int D>
+__global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
+    constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
+    constexpr int PIECES = MT * NT * U, PW = PIECES / 4;           // kilobytes of a step's fragments; loaded by a wave
+    constexpr int FRAGS = MT * NT;                                 // of a step
+    constexpr int AHEAD = 3, RING = AHEAD + 1;                     // fragments read before their products
+    constexpr int QUADS = D / 4, OPEN = FRAGS - AHEAD;             // OPEN: the fragment before whose products the barrier stands
+    static_assert(PIECES % 4 == 0 && D % 4 == 0 && FRAGS % RING == 0 && PW <= OPEN && PW + 2 <= FRAGS, "rings");
+    __shared__ u32x4 lds[2][PIECES * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int bid = xcd_run(blockIdx.x, gridDim.x);
+    const int mt0 = (bid % p.mtiles) * MT;
+    int g = (bid / p.mtiles) * 4 + wave;
+    const bool off = g >= p.w.groups;                              // a wave without outputs keeps step with the others
+    if (off) g = p.w.groups - 1;
+    const int steps = p.w.steps, s0 = blockIdx.z * p.steps_per, s1 = min(steps, s0 + p.steps_per), last = s1 - 1;
+    const u32x4* wp = (const u32x4*)p.w.w + (size_t)g * steps * 128 + lane;
+    const ScaleLoad<NT, MT> sl(p, mt0, g, lane);
+    const u32x4* ap[PW];                                           // tiles past the last are the last one again
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = (mt0 + t) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-                if (row < p.m) put(row, acc[t][0][r], acc[t][1][r]);
-            }
-    };
-    if (p.split > 1) {
-        float* part = p.part + (size_t)blockIdx.z * p.m * p.part_ld + col;
-        each([&](int row, float a, float b) { *(float2*)(part + (size_t)row * p.part_ld) = float2{a, b}; });
-    } else if (col < p.w.n) {
-        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, fast, a, b); });
-        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, fast, a, b); });
-        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, fast, a, b); });
+    for (int q = 0; q < PW; ++q) {
+        const int i = wave * PW + q, tile = min(mt0 + i / (NT * U), p.a.tiles - 1);
+        ap[q] = (const u32x4*)p.a.a + ((size_t)tile * steps * (NT * U) + i % (NT * U)) * 64 + lane;
     }
+    v16f acc[MT][2] = {};
+    u32x4 ar[D][PW], wr[D][2], fr[RING][U];
+    uint32_t ws[QUADS][2], as[QUADS][MT][NT], wsn[2], asn[MT][NT];
+    auto load_a = [&](int slot, int q, int s) { ar[slot][q] = ap[q][(size_t)min(s, last) * (NT * U * 64)]; };
+    auto load_w = [&](int slot, int j, int s) { wr[slot][j] = wp[(size_t)min(s, last) * 128 + j * 64]; };
+    auto write_a = [&](int slot, int q, int buf) { lds[buf][(wave * PW + q) * 64 + lane] = ar[slot][q]; };
+    auto read = [&](int ring, int buf, int f) {                    // fragment f (tile, term) of a step
+#pragma unroll
+        for (int u = 0; u < U; ++u) fr[ring][u] = lds[buf][(f * U + u) * 64 + lane];
+    };
+    // steps s0 .. s0 + D - 1 of both operands; step s0 to LDS, and its first fragments to registers
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) sl.load(min(s0 + 4 * q, last) / 4, as[q], ws[q]);
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+#pragma unroll
+        for (int q = 0; q < PW; ++q) load_a(d, q, s0 + d);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) load_w(d, j, s0 + d);
+    }
+#pragma unroll
+    for (int q = 0; q < PW; ++q) {
+        write_a(0, q, 0);
+        load_a(0, q, s0 + D);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) read(f, 0, f);
+    for (int s = s0; s < s1; s += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            // step s + d stands in buffer d mod 2; step s + d + 1 goes into the other one, which the last barrier freed
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) {
+                if (f == OPEN) __syncthreads();                    // step s + d + 1 is written, and step s + d read
+                if (f < OPEN) read((f + AHEAD) % RING, d & 1, f + AHEAD);
+                else read((f + AHEAD) % RING, (d + 1) & 1, f - OPEN);
+                if (f < PW) {
+                    write_a((d + 1) % D, f, (d + 1) & 1);
+                    load_a((d + 1) % D, f, s + d + 1 + D);
+                } else if (f < PW + 2) {
+                    load_w((d + D - 1) % D, f - PW, s + d - 1 + D);     // the step before is done with its own
+                } else if (f == PW + 2 && d % 4 == 0) {
+                    // the four steps before are done with their scales; where there is one set, the next one waits
+                    if constexpr (QUADS > 1) sl.load(min(s + d - 4 + D, last) / 4, as[(d / 4 + QUADS - 1) % QUADS], ws[(d / 4 + QUADS - 1) % QUADS]);
+                    else sl.load(min(s + 4, last) / 4, asn, wsn);
+                }
+                const u32x4 lo = fr[f % RING][0], hi = U == 2 ? fr[f % RING][U - 1] : u32x4{0u, 0u, 0u, 0u};
+                const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const u32x4 w = wr[d][j];
+                    const v8i b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+                    acc[f / NT][j] = mx4_mfma<FMT>(a, b, acc[f / NT][j], d & 3, as[d / 4][f / NT][f % NT], ws[d / 4][j]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (QUADS == 1) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) ws[0][j] = wsn[j];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) as[0][t][n] = asn[t][n];
+        }
+    }
+    if (off) return;
+    store_tiles<MT>(p, mt0, g, acc);
 }
 
 // out = the sum of the splits, in their order.
@@ -520,6 +670,12 @@ __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
     else store_pair<DT_BF16>(p, row, col, fast, a, b);
 }
 
+static hipError_t run_reduce(const Mx4Gemm& p, hipStream_t st) {
+    const size_t n = (size_t)p.m * ((p.w.n + 1) / 2);
+    mx4_reduce_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(p);
+    return hipGetLastError();
+}
+
 template <int T, int MT, int KS>
 hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
     p.mtiles = (p.a.tiles + MT - 1) / MT;
@@ -530,12 +686,16 @@ hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
     if (e != hipSuccess) return e;
     mx4_gemm_kernel<T, MT, KS><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), LDS, st>>>(p);
     e = hipGetLastError();
-    if (e == hipSuccess && p.split > 1) {
-        const size_t n = (size_t)p.m * ((p.w.n + 1) / 2);
-        mx4_reduce_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(p);
-        e = hipGetLastError();
-    }
-    return e;
+    return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
+}
+
+template <int T, int MT, int D>
+hipError_t run_pipe(Mx4Gemm p, hipStream_t st) {
+    p.mtiles = (p.a.tiles + MT - 1) / MT;
+    const int ntiles = (p.w.groups + 3) / 4;
+    mx4_pipe_kernel<T, MT, D><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), 0, st>>>(p);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
 }
 
 // Row tiles of 32 that a workgroup takes.
@@ -551,11 +711,16 @@ int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus) {
 
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
     const int mt = gemm_mt(p.a.terms, p.a.tiles);
+    if (p.steps_per % 8 == 0 && p.w.steps % 8 == 0) switch (p.a.terms * 10 + mt) {
+        case 8: return run_pipe<0, 8, 8>(p, st);
+        case 24: return run_pipe<2, 4, 4>(p, st);
+        case 34: return run_pipe<3, 4, 4>(p, st);
+    }
     switch (p.a.terms * 10 + mt) {
         case 1: return run_gemm<0, 1, 4>(p, st);
         case 2: return run_gemm<0, 2, 4>(p, st);
         case 4: return run_gemm<0, 4, 4>(p, st);
-        case 8: return run_gemm<0, 8, 4>(p, st);
+        case 8: return run_gemm<0, 8, 2>(p, st);
         case 21: return run_gemm<2, 1, 4>(p, st);
         case 22: return run_gemm<2, 2, 2>(p, st);
         case 24: return run_gemm<2, 4, 2>(p, st);

@@ -579,6 +579,7 @@ int mx4_load(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int 
     w.k = k;
     w.groups = (n + 63) / 64;
     w.steps = (k + 255) / 256 * 4;
+    if (k >= 2048) w.steps = (k + 511) / 512 * 8;          // the many-row product takes 8 steps at a time
     const size_t cb = (size_t)n * ((k + 1) / 2), sb = (size_t)n * ((k + 31) / 32);
     void *tc = nullptr, *ts = nullptr;
     auto undo = [&](int rc) {
@@ -623,7 +624,7 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         a.steps = w.steps;
         const size_t nt = a.terms ? a.terms : 1;
         int rc = grow(&st->mx_a, &st->mx_a_cap, (size_t)a.tiles * a.steps * nt * (a.terms ? 2048 : 1024));
-        if (!rc) rc = grow(&st->mx_s, &st->mx_s_cap, (size_t)a.tiles * a.steps * nt * 64);
+        if (!rc) rc = grow(&st->mx_s, &st->mx_s_cap, (size_t)(a.tiles + 3) / 4 * 4 * a.steps * nt * 64);
         if (rc) return rc;
         a.a = st->mx_a;
         a.s = st->mx_s;
@@ -637,7 +638,8 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         p.ld = (size_t)ldo;
         p.pairs = ((uintptr_t)p.out & (2 * ob - 1)) == 0 && (mm == 1 || ldo % 2 == 0);
         p.split = mx4_split(w, a.terms, a.tiles, st->n_cus);
-        p.steps_per = (w.steps / 4 + p.split - 1) / p.split * 4;
+        const int unit = w.steps % 8 == 0 ? 8 : 4;
+        p.steps_per = (w.steps / unit + p.split - 1) / p.split * unit;
         p.split = (w.steps + p.steps_per - 1) / p.steps_per;
         p.part_ld = 64 * w.groups;
         if (p.split > 1) {
