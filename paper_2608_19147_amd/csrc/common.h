@@ -375,6 +375,9 @@ struct Mx4Gemm {
 // Splits of K that fill the device.
 int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus);
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st);
+// A product of few rows that prepares them itself and needs no workspace (p.a: only terms).
+bool mx4_rows_direct(const Mx4Mat& w, int m);
+hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st);
 // out [m][H] fp16 = RMSNorm(row) * gamma.
 hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st);
 

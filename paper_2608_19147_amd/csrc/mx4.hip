@@ -251,6 +251,38 @@ __device__ __forceinline__ void load16(const void* x, int dt, int vec, size_t at
     }
 }
 
+// One E4M3 term of 16 values: 16 bytes; v keeps what is left.
+__device__ __forceinline__ u32x4 take_term(float (&v)[16]) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], w, true);
+        o[i] = (uint32_t)w;
+        v[4 * i] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
+        v[4 * i + 1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
+        v[4 * i + 2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
+        v[4 * i + 3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
+    }
+    return o;
+}
+
+// The first term's scale byte of a block: largest scaled magnitude in [1, 2).
+__device__ __forceinline__ int term_byte(uint32_t top) { return min((int)block_byte(top, 0), 252); }
+// The next one's, from what is left (scaled by the last one's), and the power of two between them.
+__device__ __forceinline__ int next_byte(int byte, uint32_t rest, float* up) {
+    int e = rest ? (int)(rest >> 23) - 127 : 0;
+    e = max(e, max(-byte, -127));
+    *up = __uint_as_float((uint32_t)(127 - e) << 23);
+    return byte + e;
+}
+__device__ __forceinline__ uint32_t top16(const float (&v)[16]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, absbits(v[i]));
+    return top;
+}
+
 // 16 values of one row (half a block) a thread; the two threads of a block are
 // neighbours and share its largest magnitude.  A workgroup takes 32 rows by two
 // steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
@@ -264,9 +296,7 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
     const int k0 = 64 * s + 16 * p;
     float v[16];
     load16(x, dt, vec, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, absbits(v[i]));
+    uint32_t top = top16(v);
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
     const size_t tile = row >> 5;
     const int r = row & 31, b = p >> 1;
@@ -282,37 +312,21 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
         *(u32x2*)(a + frag + (b * 32 + r) * 16 + (p & 1) * 8) = o;
         if (!(p & 1)) as[sc] = (uint8_t)byte;
     } else {
-        int byte = (int)block_byte(top, 0);                        // largest scaled magnitude in [1, 2)
         const bool bad = top >= 0x7f800000u;
-        byte = min(byte, 252);
+        int byte = bad ? 0 : term_byte(top);
         const float inv = bad ? 0.0f : e8m0_inv((uint32_t)byte);
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = bad ? 0.0f : v[i] * inv;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            u32x4 o;
-            uint32_t rest = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], w, true);
-                o[i] = (uint32_t)w;
-                v[4 * i] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
-                v[4 * i + 1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
-                v[4 * i + 2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
-                v[4 * i + 3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) rest = max(rest, absbits(v[4 * i + q]));
-            }
             // element e of lane 32 g + r: k = 16 g + e for the first 16, 32 + 16 g + e - 16 for the others
-            *(u32x4*)(a + frag + ((size_t)t * 2 + b) * 1024 + ((p & 1) * 32 + r) * 16) = o;
+            *(u32x4*)(a + frag + ((size_t)t * 2 + b) * 1024 + ((p & 1) * 32 + r) * 16) = take_term(v);
             if (!(p & 1)) as[sc + (size_t)t * 1024] = (uint8_t)(bad ? 255 : byte);
             if (t + 1 < NT) {
+                uint32_t rest = top16(v);
                 rest = max(rest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rest, 0xB1, 0xF, 0xF, false));
-                int e = rest ? (int)(rest >> 23) - 127 : 0;        // the rest's largest magnitude to [1, 2)
-                e = max(e, max(-byte, -127));
-                byte += e;
-                const float up = __uint_as_float((uint32_t)(127 - e) << 23);
+                float up;
+                byte = next_byte(byte, rest, &up);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] *= up;
             }
@@ -650,6 +664,128 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
     }
     if (off) return;
     store_tiles<MT>(p, mt0, g, acc);
+}
+
+// At most 16 rows of x, in one launch and without a workspace: 16 outputs a
+// workgroup (every second row of a group, so that their fragments are the packed
+// ones), K over its eight waves, 128 k at a time on the 16 x 16 x 128 product.
+// The wave's weights are on their way while it turns its part of x into terms;
+// the waves' sums meet in LDS, in their order.  Bound by the latency of one read
+// (4096 x 4096: 8.9 MB in about 3 us) and, above some 16k outputs, by the terms
+// that every workgroup makes for itself: there the rows are prepared once
+// (mx4_rows_direct).
+constexpr int ROW_WAVES = 8, ROW_BATCH = 4;
+template <int T>
+__global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, int xdt, int vec, size_t ldx) {
+    constexpr int NT = T ? T : 1, FMT = T ? 0 : 4;
+    typedef float v4f __attribute__((ext_vector_type(4)));
+    __shared__ float part[ROW_WAVES][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kb = lane >> 4;
+    const int g = blockIdx.x >> 2, j = blockIdx.x & 1, h = (blockIdx.x >> 1) & 1;
+    const int steps = p.w.steps, chunks = steps / 2, per = (chunks + ROW_WAVES - 1) / ROW_WAVES;
+    const int c0 = wave * per, c1 = min(chunks, c0 + per);
+    // lane: row 16 h + r16 of the tile j, block kb of the chunk
+    const int at = (kb & 1) * 32 + 16 * h + r16;
+    const u32x4* wp = (const u32x4*)p.w.w + ((size_t)g * steps * 2 + j) * 64 + at;
+    const uint32_t* sp = p.w.s + ((size_t)g * (steps / 4) * 64 + at) * 2 + j;
+    v4f acc = {};
+    for (int c = c0; c < c1; c += ROW_BATCH) {
+        u32x4 w[ROW_BATCH];
+        uint32_t ws[ROW_BATCH];
+#pragma unroll
+        for (int i = 0; i < ROW_BATCH; ++i) {
+            const int s = 2 * min(c + i, c1 - 1) + (kb >> 1);
+            w[i] = wp[(size_t)s * 128];
+            ws[i] = sp[(size_t)(s / 4) * 128] >> (8 * (s & 3));
+        }
+#pragma unroll
+        for (int i = 0; i < ROW_BATCH; ++i) {
+            if (c + i >= c1) break;
+            const v8i b = {(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3], 0, 0, 0, 0};
+            // values of row r16: E4M3 terms take k = 16 kb + 0..15 and 64 + 16 kb + 0..15 of the chunk, E2M1 32 kb + 0..31
+            const int k0 = 128 * (c + i) + (T ? 16 : 32) * kb, k1 = k0 + (T ? 64 : 16);
+            float v[2][16];
+            load16(x, xdt, vec, (size_t)r16 * ldx + k0, r16 < p.m ? p.w.k - k0 : 0, v[0]);
+            load16(x, xdt, vec, (size_t)r16 * ldx + k1, r16 < p.m ? p.w.k - k1 : 0, v[1]);
+            uint32_t top[2] = {top16(v[0]), top16(v[1])};
+            if constexpr (T == 0) {
+                const uint32_t byte = block_byte(max(top[0], top[1]), 2);
+                const bool bad = byte == 255u;
+                const float inv = bad ? 0.0f : e8m0_inv(byte);
+                v8i a = {};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float e[8];
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) e[n] = bad ? 0.0f : v[q >> 1][8 * (q & 1) + n];
+                    a[q] = (int)e2m1x8(e, inv);
+                }
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, FMT, 4, 0, (int)byte, 0, (int)ws[i]);
+            } else {
+                // a block is the same half of two lanes 16 apart
+                int byte[2];
+                bool bad[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    top[q] = max(top[q], (uint32_t)__shfl_xor((int)top[q], 16));
+                    bad[q] = top[q] >= 0x7f800000u;
+                    byte[q] = bad[q] ? 0 : term_byte(top[q]);
+                    const float inv = bad[q] ? 0.0f : e8m0_inv((uint32_t)byte[q]);
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) v[q][n] = bad[q] ? 0.0f : v[q][n] * inv;
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const u32x4 lo = take_term(v[0]), hi = take_term(v[1]);
+                    const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                    // the product takes block b's byte from lanes 16 b: blocks 0 and 1 are first halves of lanes 0 and 32
+                    const int both = (bad[0] ? 255 : byte[0]) | (bad[1] ? 255 : byte[1]) << 8;
+                    const int sa = __shfl(both, 32 * (kb & 1) + r16) >> (8 * (kb >> 1));
+                    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, FMT, 4, 0, sa, 0, (int)ws[i]);
+                    if (t + 1 < NT) {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t rest = top16(v[q]);
+                            rest = max(rest, (uint32_t)__shfl_xor((int)rest, 16));
+                            float up;
+                            byte[q] = next_byte(byte[q], rest, &up);
+#pragma unroll
+                            for (int n = 0; n < 16; ++n) v[q][n] *= up;
+                        }
+                    }
+                }
+            }
+        }
+    }
+    // lane l holds output l mod 16 of rows 4 (l / 16) + r
+#pragma unroll
+    for (int r = 0; r < 4; ++r) part[wave][(4 * kb + r) * 16 + r16] = acc[r];
+    __syncthreads();
+    const int tid = threadIdx.x;
+    if (tid >= 256) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < ROW_WAVES; ++w) sum += part[w][tid];
+    const int row = tid >> 4, col = 64 * g + 2 * (16 * h + (tid & 15)) + j;
+    if (row < p.m && col < p.w.n) {
+        const size_t o = (size_t)row * p.ld + col;
+        if (p.dt == DT_F32) ((float*)p.out)[o] = sum;
+        else ((uint16_t*)p.out)[o] = to_half_bits(sum, p.dt);
+    }
+}
+
+bool mx4_rows_direct(const Mx4Mat& w, int m) { return m <= 16 && w.groups <= 256; }
+
+hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st) {
+    const int vec = ((uintptr_t)x & 15) == 0 && (p.m == 1 || (size_t)ldx * (dt == DT_F32 ? 4 : 2) % 16 == 0);
+    const dim3 g((unsigned)(4 * p.w.groups)), b(64 * ROW_WAVES);
+    switch (p.a.terms) {
+        case 0: mx4_rows_kernel<0><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
+        case 2: mx4_rows_kernel<2><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
+        case 3: mx4_rows_kernel<3><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
 }
 
 // out = the sum of the splits, in their order.

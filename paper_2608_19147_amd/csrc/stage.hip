@@ -612,6 +612,8 @@ int mx4_load(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int 
 
 constexpr int MX4_PASS = 2048;                             // rows of one product pass
 
+int mx4_terms(int dt, int act, int odt) { return act == 4 ? 0 : dt == DT_BF16 && odt != DT_F32 ? 2 : 3; }
+
 // out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).
 int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
             hipStream_t s) {
@@ -619,7 +621,7 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
     for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
         const int mm = std::min(MX4_PASS, m - m0);
         Mx4Act a{};
-        a.terms = act == 4 ? 0 : dt == DT_BF16 && odt != DT_F32 ? 2 : 3;
+        a.terms = mx4_terms(dt, act, odt);
         a.tiles = (mm + 31) / 32;
         a.steps = w.steps;
         const size_t nt = a.terms ? a.terms : 1;
@@ -1671,6 +1673,17 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
+        if (mx4_rows_direct(w->m, m)) {                    // no workspace: nothing to order
+            Mx4Gemm p{};
+            p.w = w->m;
+            p.a.terms = mx4_terms(any_dt(x_dtype), act_bits, any_dt(out_dtype));
+            p.m = m;
+            p.out = out;
+            p.dt = any_dt(out_dtype);
+            p.ld = (size_t)ldo;
+            HIP_TRY(launch_mx4_rows(p, x, any_dt(x_dtype), ldx, s));
+            return STAGE_OK;
+        }
         int rc = not_captured(s);
         if (rc) return rc;
         HIP_TRY(order_on(st, s));
@@ -1727,6 +1740,8 @@ int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, in
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
+        if (vocab <= SAMPLE_SLICE)                         // one slice a row: no workspace, nothing to order
+            return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);
         if ((rc = not_captured(s))) return rc;
         HIP_TRY(order_on(st, s));
         rc = sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);

@@ -252,26 +252,31 @@ def test_product_streams(stage):
 
 
 def test_capture(stage):
-    """Rounding uses no memory of the stage and can be captured; a product refuses and leaves the capture whole."""
+    """Rounding and products of few rows use no memory of the stage and can be captured; a larger product refuses and
+    leaves the capture whole."""
     codes, scales = _weights(64, 64, 19)
     mat = stage.mx4_matrix(torch.from_numpy(mx4_pack(codes)), torch.from_numpy(scales), 64)
-    x = _rows(9, 64, 20, "bf16").cuda()
+    x, many = _rows(9, 64, 20, "bf16").cuda(), _rows(17, 64, 20, "bf16").cuda()
     mat.product(x)
+    mat.product(many)
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         c, s = stage.mx4_quantize(x)
         v = stage.mx4_dequantize(c, s, 64, torch.bfloat16)
+        o = mat.product(x, out_dtype=torch.float32)
         with pytest.raises(StageError) as ei:
-            mat.product(x)
+            mat.product(many)
         assert ei.value.code == -7
     for i in range(3):
         x.copy_(_rows(9, 64, 21 + i, "bf16"))
-        mat.product(x)
+        mat.product(many)
         g.replay()
+        eager = mat.product(x, out_dtype=torch.float32)
         torch.cuda.synchronize()
         ref = mx4_values(*mx4_encode(x.double().cpu().numpy()))
         assert np.array_equal(v.double().cpu().numpy(), ref)
+        assert torch.equal(o, eager)
     mat.free()
 
 
