@@ -229,25 +229,34 @@ hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx
 // ------------------------------------------------------------------ activations
 
 // Values at .. at + 15 of x, zero from `left` on.  vec: at is a multiple of 16 bytes into x.
-__device__ __forceinline__ void load16(const void* x, int dt, int vec, size_t at, int left, float (&v)[16]) {
-    if (vec && left >= 16) {
-        if (dt == DT_F32) {
-            const u32x4* p = (const u32x4*)((const float*)x + at);
+template <int DT>
+__device__ __forceinline__ void load16(const void* x, int vec, size_t at, int left, float (&v)[16]) {
+    if constexpr (DT == DT_F32) {
+        const float* f = (const float*)x + at;
+        if (vec && left >= 16) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const u32x4 a = p[q];
+                const u32x4 a = ((const u32x4*)f)[q];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[4 * q + j] = __uint_as_float(a[j]);
             }
         } else {
-            const u32x4* p = (const u32x4*)((const uint16_t*)x + at);
-            const u32x4 a[2] = {p[0], p[1]};
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 3][(j >> 1) & 3] >> (16 * (j & 1))), dt);
+            for (int j = 0; j < 16; ++j) v[j] = j < left ? f[j] : 0.0f;
         }
     } else {
+        const uint16_t* f = (const uint16_t*)x + at;
+        u32x4 a[2];
+        if (vec && left >= 16) {
+            a[0] = ((const u32x4*)f)[0];
+            a[1] = ((const u32x4*)f)[1];
+        } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = j < left ? load_val(x, dt, at + j) : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                a[j >> 2][j & 3] = (2 * j < left ? (uint32_t)f[2 * j] : 0u) | (2 * j + 1 < left ? (uint32_t)f[2 * j + 1] << 16 : 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 3][(j >> 1) & 3] >> (16 * (j & 1))), DT);
     }
 }
 
@@ -287,15 +296,15 @@ __device__ __forceinline__ uint32_t top16(const float (&v)[16]) {
 // neighbours and share its largest magnitude.  A workgroup takes 32 rows by two
 // steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
 // m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).
-template <int T>
-__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, int dt, int vec, size_t ld, int m, int k, int steps,
+template <int T, int DT>
+__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, int vec, size_t ld, int m, int k, int steps,
                                                        uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1;
     const int p = threadIdx.x & 3;                                 // quarter of the step of 64
     const int s = 2 * blockIdx.x + (threadIdx.x >> 7), row = 32 * blockIdx.y + ((threadIdx.x >> 2) & 31);
     const int k0 = 64 * s + 16 * p;
     float v[16];
-    load16(x, dt, vec, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
+    load16<DT>(x, vec, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
     uint32_t top = top16(v);
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
     const size_t tile = row >> 5;
@@ -337,12 +346,17 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
 hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, int m, int k, hipStream_t st) {
     const int vec = ((uintptr_t)x & 15) == 0 && (m == 1 || (size_t)ld * (dt == DT_F32 ? 4 : 2) % 16 == 0);
     const dim3 g((unsigned)(a.steps / 2), (unsigned)a.tiles), b(256);
-    switch (a.terms) {
-        case 0: mx4_prep_kernel<0><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
-        case 2: mx4_prep_kernel<2><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
-        case 3: mx4_prep_kernel<3><<<g, b, 0, st>>>(x, dt, vec, (size_t)ld, m, k, a.steps, a.a, a.s); break;
+#define MX4_PREP(T, DT) mx4_prep_kernel<T, DT><<<g, b, 0, st>>>(x, vec, (size_t)ld, m, k, a.steps, a.a, a.s)
+    switch (a.terms * 4 + dt) {
+        case DT_F32: MX4_PREP(0, DT_F32); break;
+        case DT_F16: MX4_PREP(0, DT_F16); break;
+        case DT_BF16: MX4_PREP(0, DT_BF16); break;
+        case 8 + DT_BF16: MX4_PREP(2, DT_BF16); break;
+        case 12 + DT_F16: MX4_PREP(3, DT_F16); break;
+        case 12 + DT_BF16: MX4_PREP(3, DT_BF16); break;
         default: return hipErrorInvalidValue;
     }
+#undef MX4_PREP
     return hipGetLastError();
 }
 
@@ -669,105 +683,116 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
 // At most 16 rows of x, in one launch and without a workspace: 16 outputs a
 // workgroup (every second row of a group, so that their fragments are the packed
 // ones), K over its eight waves, 128 k at a time on the 16 x 16 x 128 product.
-// The wave's weights are on their way while it turns its part of x into terms;
-// the waves' sums meet in LDS, in their order.  Bound by the latency of one read
-// (4096 x 4096: 8.9 MB in about 3 us) and, above some 16k outputs, by the terms
+// The workgroup turns x into terms in LDS, a segment of K at a time, while its
+// first weights are on their way; the waves' sums meet in LDS, in their order.
+// Bound by the latency of one read after a launch and by fetching the code, so
+// there is one copy of the conversion; and, above some 16k outputs, by the terms
 // that every workgroup makes for itself: there the rows are prepared once
 // (mx4_rows_direct).
-constexpr int ROW_WAVES = 8, ROW_BATCH = 4;
-template <int T>
-__global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, int xdt, int vec, size_t ldx) {
-    constexpr int NT = T ? T : 1, FMT = T ? 0 : 4;
+constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
+template <int T, int DT>
+__global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, int vec, size_t ldx, int seg) {
+    constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
     typedef float v4f __attribute__((ext_vector_type(4)));
+    // fragments [chunk][term][half][block or quarter kb][row]; scales [chunk][term][row] words of 4 blocks; sums
+    __shared__ __attribute__((aligned(16))) uint8_t frags[ROW_LDS];
+    __shared__ uint32_t scales[T ? ROW_LDS / 128 : ROW_LDS / 64];  // a word for the 128 or 64 bytes of a chunk's row
     __shared__ float part[ROW_WAVES][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, kb = lane >> 4;
-    const int g = blockIdx.x >> 2, j = blockIdx.x & 1, h = (blockIdx.x >> 1) & 1;
-    const int steps = p.w.steps, chunks = steps / 2, per = (chunks + ROW_WAVES - 1) / ROW_WAVES;
-    const int c0 = wave * per, c1 = min(chunks, c0 + per);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, kb = lane >> 4;
+    const int g = blockIdx.x >> 2, j = blockIdx.x & 1, h = (blockIdx.x >> 1) & 1, m = p.m;
+    const int steps = p.w.steps, chunks = steps / 2;
     // lane: row 16 h + r16 of the tile j, block kb of the chunk
     const int at = (kb & 1) * 32 + 16 * h + r16;
     const u32x4* wp = (const u32x4*)p.w.w + ((size_t)g * steps * 2 + j) * 64 + at;
     const uint32_t* sp = p.w.s + ((size_t)g * (steps / 4) * 64 + at) * 2 + j;
     v4f acc = {};
-    for (int c = c0; c < c1; c += ROW_BATCH) {
+#pragma unroll 1
+    for (int k0 = 0; k0 < 64 * steps; k0 += seg) {                 // seg: a multiple of 128
+        const int n = min(seg / 128, chunks - k0 / 128);           // chunks of the segment; a run of them is the wave's
+        const int per = (n + ROW_WAVES - 1) / ROW_WAVES, c0 = min(n, wave * per), c1 = min(n, c0 + per);
         u32x4 w[ROW_BATCH];
         uint32_t ws[ROW_BATCH];
+        auto load = [&](int c) {
 #pragma unroll
-        for (int i = 0; i < ROW_BATCH; ++i) {
-            const int s = 2 * min(c + i, c1 - 1) + (kb >> 1);
-            w[i] = wp[(size_t)s * 128];
-            ws[i] = sp[(size_t)(s / 4) * 128] >> (8 * (s & 3));
-        }
-#pragma unroll
-        for (int i = 0; i < ROW_BATCH; ++i) {
-            if (c + i >= c1) break;
-            const v8i b = {(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3], 0, 0, 0, 0};
-            // values of row r16: E4M3 terms take k = 16 kb + 0..15 and 64 + 16 kb + 0..15 of the chunk, E2M1 32 kb + 0..31
-            const int k0 = 128 * (c + i) + (T ? 16 : 32) * kb, k1 = k0 + (T ? 64 : 16);
-            float v[2][16];
-            load16(x, xdt, vec, (size_t)r16 * ldx + k0, r16 < p.m ? p.w.k - k0 : 0, v[0]);
-            load16(x, xdt, vec, (size_t)r16 * ldx + k1, r16 < p.m ? p.w.k - k1 : 0, v[1]);
-            uint32_t top[2] = {top16(v[0]), top16(v[1])};
+            for (int i = 0; i < ROW_BATCH; ++i) {
+                const int s = k0 / 64 + 2 * min(c + i, n - 1) + (kb >> 1);
+                w[i] = wp[(size_t)s * 128];
+                ws[i] = sp[(size_t)(s / 4) * 128] >> (8 * (s & 3));
+            }
+        };
+        load(c0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+        for (int i = tid; i < m * 8 * n; i += 64 * ROW_WAVES) {    // 16 values; neighbours share a block
+            const int q = i & 7, rc = i >> 3, row = rc / n, c = rc - row * n, k = k0 + 128 * c + 16 * q;
+            float v[16];
+            load16<DT>(x, vec, (size_t)row * ldx + k, p.w.k - k, v);
+            uint32_t top = top16(v);
+            top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
+            const bool bad = top >= 0x7f800000u;
             if constexpr (T == 0) {
-                const uint32_t byte = block_byte(max(top[0], top[1]), 2);
-                const bool bad = byte == 255u;
+                const uint32_t byte = block_byte(top, 2);
                 const float inv = bad ? 0.0f : e8m0_inv(byte);
-                v8i a = {};
+                float e[2][8];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float e[8];
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) e[n] = bad ? 0.0f : v[q >> 1][8 * (q & 1) + n];
-                    a[q] = (int)e2m1x8(e, inv);
-                }
-                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, FMT, 4, 0, (int)byte, 0, (int)ws[i]);
+                for (int z = 0; z < 16; ++z) e[z >> 3][z & 7] = bad ? 0.0f : v[z];
+                *(u32x2*)(frags + ((size_t)(c * 4 + (q >> 1)) * m + row) * 16 + (q & 1) * 8) = u32x2{e2m1x8(e[0], inv), e2m1x8(e[1], inv)};
+                ((uint8_t*)scales)[(c * m + row) * 4 + (q >> 1)] = (uint8_t)byte;
             } else {
-                // a block is the same half of two lanes 16 apart
-                int byte[2];
-                bool bad[2];
+                // element e of lane 16 kb + r: k = 16 kb + e for the first 16, 64 + 16 kb + e - 16 for the others
+                int byte = bad ? 0 : term_byte(top);
+                const float inv = bad ? 0.0f : e8m0_inv((uint32_t)byte);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    top[q] = max(top[q], (uint32_t)__shfl_xor((int)top[q], 16));
-                    bad[q] = top[q] >= 0x7f800000u;
-                    byte[q] = bad[q] ? 0 : term_byte(top[q]);
-                    const float inv = bad[q] ? 0.0f : e8m0_inv((uint32_t)byte[q]);
-#pragma unroll
-                    for (int n = 0; n < 16; ++n) v[q][n] = bad[q] ? 0.0f : v[q][n] * inv;
-                }
+                for (int z = 0; z < 16; ++z) v[z] = bad ? 0.0f : v[z] * inv;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const u32x4 lo = take_term(v[0]), hi = take_term(v[1]);
-                    const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-                    // the product takes block b's byte from lanes 16 b: blocks 0 and 1 are first halves of lanes 0 and 32
-                    const int both = (bad[0] ? 255 : byte[0]) | (bad[1] ? 255 : byte[1]) << 8;
-                    const int sa = __shfl(both, 32 * (kb & 1) + r16) >> (8 * (kb >> 1));
-                    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, FMT, 4, 0, sa, 0, (int)ws[i]);
+                    *(u32x4*)(frags + ((size_t)((c * NT + t) * 8 + q) * m + row) * 16) = take_term(v);
+                    ((uint8_t*)scales)[((c * NT + t) * m + row) * 4 + (q >> 1)] = (uint8_t)(bad ? 255 : byte);
                     if (t + 1 < NT) {
+                        uint32_t rest = top16(v);
+                        rest = max(rest, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rest, 0xB1, 0xF, 0xF, false));
+                        float up;
+                        byte = next_byte(byte, rest, &up);
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t rest = top16(v[q]);
-                            rest = max(rest, (uint32_t)__shfl_xor((int)rest, 16));
-                            float up;
-                            byte[q] = next_byte(byte[q], rest, &up);
-#pragma unroll
-                            for (int n = 0; n < 16; ++n) v[q][n] *= up;
-                        }
+                        for (int z = 0; z < 16; ++z) v[z] *= up;
                     }
                 }
             }
         }
+        __syncthreads();
+#pragma unroll 1
+        for (int c = c0; c < c1; c += ROW_BATCH) {
+            if (c != c0) load(c);
+#pragma unroll
+            for (int i = 0; i < ROW_BATCH; ++i) {
+                if (c + i >= c1) break;
+                const v8i b = {(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3], 0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    u32x4 f[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
+                    uint32_t sa = 0x7f7f7f7fu;
+                    if (r16 < m) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) f[u] = *(const u32x4*)(frags + ((size_t)(((c + i) * NT + t) * 4 * U + 4 * u + kb) * m + r16) * 16);
+                        sa = scales[((c + i) * NT + t) * m + r16] >> (8 * kb);
+                    }
+                    const v8i a = {(int)f[0][0], (int)f[0][1], (int)f[0][2], (int)f[0][3], (int)f[1][0], (int)f[1][1], (int)f[1][2], (int)f[1][3]};
+                    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, FMT, 4, 0, (int)sa, 0, (int)ws[i]);
+                }
+            }
+        }
+        __syncthreads();
     }
     // lane l holds output l mod 16 of rows 4 (l / 16) + r
 #pragma unroll
     for (int r = 0; r < 4; ++r) part[wave][(4 * kb + r) * 16 + r16] = acc[r];
     __syncthreads();
-    const int tid = threadIdx.x;
     if (tid >= 256) return;
     float sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < ROW_WAVES; ++w) sum += part[w][tid];
     const int row = tid >> 4, col = 64 * g + 2 * (16 * h + (tid & 15)) + j;
-    if (row < p.m && col < p.w.n) {
+    if (row < m && col < p.w.n) {
         const size_t o = (size_t)row * p.ld + col;
         if (p.dt == DT_F32) ((float*)p.out)[o] = sum;
         else ((uint16_t*)p.out)[o] = to_half_bits(sum, p.dt);
@@ -779,12 +804,21 @@ bool mx4_rows_direct(const Mx4Mat& w, int m) { return m <= 16 && w.groups <= 256
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st) {
     const int vec = ((uintptr_t)x & 15) == 0 && (p.m == 1 || (size_t)ldx * (dt == DT_F32 ? 4 : 2) % 16 == 0);
     const dim3 g((unsigned)(4 * p.w.groups)), b(64 * ROW_WAVES);
-    switch (p.a.terms) {
-        case 0: mx4_rows_kernel<0><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
-        case 2: mx4_rows_kernel<2><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
-        case 3: mx4_rows_kernel<3><<<g, b, 0, st>>>(p, x, dt, vec, (size_t)ldx); break;
+    // the longest segment of K that LDS holds, the same number of chunks for each wave
+    const int per_k = p.m * (p.a.terms ? 2 * p.a.terms : 1);       // half bytes
+    int seg = ROW_LDS * 2 / per_k / ROW_SEG * ROW_SEG;
+    if (seg > 64 * p.w.steps) seg = 64 * p.w.steps;
+#define MX4_ROWS(T, DT) mx4_rows_kernel<T, DT><<<g, b, 0, st>>>(p, x, vec, (size_t)ldx, seg)
+    switch (p.a.terms * 4 + dt) {
+        case DT_F32: MX4_ROWS(0, DT_F32); break;
+        case DT_F16: MX4_ROWS(0, DT_F16); break;
+        case DT_BF16: MX4_ROWS(0, DT_BF16); break;
+        case 8 + DT_BF16: MX4_ROWS(2, DT_BF16); break;
+        case 12 + DT_F16: MX4_ROWS(3, DT_F16); break;
+        case 12 + DT_BF16: MX4_ROWS(3, DT_BF16); break;
         default: return hipErrorInvalidValue;
     }
+#undef MX4_ROWS
     return hipGetLastError();
 }
 
