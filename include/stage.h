@@ -359,8 +359,9 @@ int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out,
  * needed.  stage_mx4_quantize, stage_mx4_dequantize, stage_tree_accept, and
  * stage_sample of up to 8192 tokens use no memory of the stage: calls on
  * different streams are independent and may be captured into a graph.  So does a
- * stage_mx4_product of few rows (up to 16, up to 16384 outputs).  The other calls
- * use the stage's workspace, are ordered with the stage's calls like a forward
+ * stage_mx4_product of up to 16 rows and 16384 outputs, or of up to 64 rows of at
+ * most 2048 columns and 16384 / ceil(rows / 16) outputs.  The other calls use the
+ * stage's workspace, are ordered with the stage's calls like a forward
  * and refuse a capturing stream (STAGE_E_UNSUPPORTED).  The calling thread's current
  * device is left as it was.
  * ------------------------------------------------------------------------ */

@@ -680,15 +680,15 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
     store_tiles<MT>(p, mt0, g, acc);
 }
 
-// At most 16 rows of x, in one launch and without a workspace: 16 outputs a
+// Few rows of x, in one launch and without a workspace: 16 of them by 16 outputs a
 // workgroup (every second row of a group, so that their fragments are the packed
 // ones), K over its eight waves, 128 k at a time on the 16 x 16 x 128 product.
 // The workgroup turns x into terms in LDS, a segment of K at a time, while its
 // first weights are on their way; the waves' sums meet in LDS, in their order.
 // Bound by the latency of one read after a launch and by fetching the code, so
-// there is one copy of the conversion; and, above some 16k outputs, by the terms
-// that every workgroup makes for itself: there the rows are prepared once
-// (mx4_rows_direct).
+// there is one copy of the conversion; where many outputs or long rows make the
+// terms that every workgroup makes for itself the larger part, the rows are
+// prepared once instead (mx4_rows_direct).
 constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
 __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, int vec, size_t ldx, int seg) {
@@ -699,7 +699,8 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, con
     __shared__ uint32_t scales[T ? ROW_LDS / 128 : ROW_LDS / 64];  // a word for the 128 or 64 bytes of a chunk's row
     __shared__ float part[ROW_WAVES][256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, kb = lane >> 4;
-    const int g = blockIdx.x >> 2, j = blockIdx.x & 1, h = (blockIdx.x >> 1) & 1, m = p.m;
+    const int g = blockIdx.x >> 2, j = blockIdx.x & 1, h = (blockIdx.x >> 1) & 1;
+    const int row0 = 16 * blockIdx.y, m = min(16, p.m - row0);
     const int steps = p.w.steps, chunks = steps / 2;
     // lane: row 16 h + r16 of the tile j, block kb of the chunk
     const int at = (kb & 1) * 32 + 16 * h + r16;
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, con
         for (int i = tid; i < m * 8 * n; i += 64 * ROW_WAVES) {    // 16 values; neighbours share a block
             const int q = i & 7, rc = i >> 3, row = rc / n, c = rc - row * n, k = k0 + 128 * c + 16 * q;
             float v[16];
-            load16<DT>(x, vec, (size_t)row * ldx + k, p.w.k - k, v);
+            load16<DT>(x, vec, (size_t)(row0 + row) * ldx + k, p.w.k - k, v);
             uint32_t top = top16(v);
             top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
             const bool bad = top >= 0x7f800000u;
@@ -793,19 +794,25 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, con
     for (int w = 0; w < ROW_WAVES; ++w) sum += part[w][tid];
     const int row = tid >> 4, col = 64 * g + 2 * (16 * h + (tid & 15)) + j;
     if (row < m && col < p.w.n) {
-        const size_t o = (size_t)row * p.ld + col;
+        const size_t o = (size_t)(row0 + row) * p.ld + col;
         if (p.dt == DT_F32) ((float*)p.out)[o] = sum;
         else ((uint16_t*)p.out)[o] = to_half_bits(sum, p.dt);
     }
 }
 
-bool mx4_rows_direct(const Mx4Mat& w, int m) { return m <= 16 && w.groups <= 256; }
+// One launch for a few rows, where making the terms in every workgroup costs less than a launch that prepares them
+// (3-4 us, and its event): one tile of 16 rows up to 16384 outputs; up to four of at most 2048 columns, while the
+// workgroups are at most four a CU.
+bool mx4_rows_direct(const Mx4Mat& w, int m) {
+    const int tiles = (m + 15) / 16;
+    return tiles == 1 ? w.groups <= 256 : tiles <= 4 && w.k <= 2048 && w.groups * tiles <= 256;
+}
 
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st) {
     const int vec = ((uintptr_t)x & 15) == 0 && (p.m == 1 || (size_t)ldx * (dt == DT_F32 ? 4 : 2) % 16 == 0);
-    const dim3 g((unsigned)(4 * p.w.groups)), b(64 * ROW_WAVES);
+    const dim3 g((unsigned)(4 * p.w.groups), (unsigned)((p.m + 15) / 16)), b(64 * ROW_WAVES);
     // the longest segment of K that LDS holds, the same number of chunks for each wave
-    const int per_k = p.m * (p.a.terms ? 2 * p.a.terms : 1);       // half bytes
+    const int per_k = (p.m < 16 ? p.m : 16) * (p.a.terms ? 2 * p.a.terms : 1);       // half bytes
     int seg = ROW_LDS * 2 / per_k / ROW_SEG * ROW_SEG;
     if (seg > 64 * p.w.steps) seg = 64 * p.w.steps;
 #define MX4_ROWS(T, DT) mx4_rows_kernel<T, DT><<<g, b, 0, st>>>(p, x, vec, (size_t)ldx, seg)

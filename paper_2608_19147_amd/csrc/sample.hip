@@ -52,6 +52,51 @@ __device__ __forceinline__ unsigned long long exp_units(double d) {
     return (unsigned long long)__double_as_longlong(fma(p, 68719476736.0, 4503599627370496.0)) & 0xfffffffffffffull;
 }
 
+// exp(-b / 32) and its inverse for b = 32 q + r, as products of exp(-q) and exp(-r / 32): correctly rounded values, so that
+// a product is within 2 units in the last place.
+__constant__ const double EXP_Q[32] = {
+    0x1.0000000000000p+0, 0x1.78b56362cef38p-2, 0x1.152aaa3bf81ccp-3, 0x1.97db0ccceb0afp-5,
+    0x1.2c155b8213cf4p-6, 0x1.b993fe00d5376p-8, 0x1.44e51f113d4d6p-9, 0x1.de16b9c24a98fp-11,
+    0x1.5fc21041027adp-12, 0x1.02cf22526545ap-13, 0x1.7cd79b5647c9bp-15, 0x1.18354238f6764p-16,
+    0x1.9c54c3b43bc8bp-18, 0x1.2f6053b981d98p-19, 0x1.be6c6fdb01612p-21, 0x1.4875ca227ec38p-22,
+    0x1.e355bbaee85cbp-24, 0x1.639e3175a689dp-25, 0x1.05a628c699fa1p-26, 0x1.81056ff2c5772p-28,
+    0x1.1b48655f37267p-29, 0x1.a0db0d0ddb3ecp-31, 0x1.32b48bf117da2p-32, 0x1.c3527e433fab1p-34,
+    0x1.4c1078fe9228ap-35, 0x1.e8a37a45fc32ep-37, 0x1.67852a7007e42p-38, 0x1.0885298767e9ap-39,
+    0x1.853f01d6d53bap-41, 0x1.1e642baeb84a0p-42, 0x1.a56e0c2ac7f75p-44, 0x1.36121e24d3bbap-45,
+};
+__constant__ const double EXP_R[32] = {
+    0x1.0000000000000p+0, 0x1.f03f56a88b5d8p-1, 0x1.e0fabfbc702a4p-1, 0x1.d22e6a0197c03p-1,
+    0x1.c3d6a24ed8222p-1, 0x1.b5efd29f24c26p-1, 0x1.a876812c0877cp-1, 0x1.9b674f8f2f3d8p-1,
+    0x1.8ebef9eac820bp-1, 0x1.827a561889716p-1, 0x1.769652df22f7ep-1, 0x1.6b0ff72deb89dp-1,
+    0x1.5fe4615e98e8fp-1, 0x1.5510c67cd2591p-1, 0x1.4a9271936fd09p-1, 0x1.4066c2ff39127p-1,
+    0x1.368b2fc6f960ap-1, 0x1.2cfd40f8bdcaep-1, 0x1.23ba930c1568bp-1, 0x1.1ac0d5492c0dcp-1,
+    0x1.120dc934993e8p-1, 0x1.099f41ffbe580p-1, 0x1.017323fd90020p-1, 0x1.f30ec8375038bp-2,
+    0x1.e3b40ebefcd7ep-2, 0x1.d4d244cf4ea9ep-2, 0x1.c665b1e1f1e0dp-2, 0x1.b86ababeef8dfp-2,
+    0x1.aadde095dad4bp-2, 0x1.9dbbc01e18268p-2, 0x1.910110be06976p-2, 0x1.84aaa3b8d514ep-2,
+};
+__constant__ const double INV_Q[32] = {
+    0x1.0000000000000p+0, 0x1.5bf0a8b145769p+1, 0x1.d8e64b8d4ddaep+2, 0x1.415e5bf6fb106p+4,
+    0x1.b4c902e273a58p+5, 0x1.28d389970338fp+7, 0x1.936dc5690c08fp+8, 0x1.122885aaeddaap+10,
+    0x1.749ea7d470c6ep+11, 0x1.fa7157c470f82p+12, 0x1.5829dcf950560p+14, 0x1.d3c4488ee4f7fp+15,
+    0x1.3de1654d37c9ap+17, 0x1.b00b5916ac955p+18, 0x1.259ac48bf05d7p+20, 0x1.8f0ccafad2a87p+21,
+    0x1.0f2ebd0a80020p+23, 0x1.709348c0ea4f9p+24, 0x1.f4f22091940bdp+25, 0x1.546d8f9ed26e1p+27,
+    0x1.ceb088b68e804p+28, 0x1.3a6e1fd9eecfdp+30, 0x1.ab5adb9c43600p+31, 0x1.226af33b1fdc1p+33,
+    0x1.8ab7fb5475fb7p+34, 0x1.0c3d3920962c9p+36, 0x1.6c932696a6b5dp+37, 0x1.ef822f7f6731dp+38,
+    0x1.50bba3796379ap+40, 0x1.c9aae4631c056p+41, 0x1.370470aec28edp+43, 0x1.a6b765d8cdf6dp+44,
+};
+__constant__ const double INV_R[32] = {
+    0x1.0000000000000p+0, 0x1.08205601127edp+0, 0x1.1082b577d34edp+0, 0x1.192937074e0cdp+0,
+    0x1.2216045b6f5cdp+0, 0x1.2b4b58b372c79p+0, 0x1.34cb8170b5835p+0, 0x1.3e98deaa11dccp+0,
+    0x1.48b5e3c3e8186p+0, 0x1.5325180cfacf7p+0, 0x1.5de9176045ff5p+0, 0x1.690492cbf9433p+0,
+    0x1.747a513dbef6ap+0, 0x1.804d30347b546p+0, 0x1.8c802477b0010p+0, 0x1.99163ad4b1dccp+0,
+    0x1.a61298e1e069cp+0, 0x1.b3787dc80f95fp+0, 0x1.c14b431256446p+0, 0x1.cf8e5d84758a9p+0,
+    0x1.de455df80e3c0p+0, 0x1.ed73f240dc142p+0, 0x1.fd1de6182f8c9p+0, 0x1.06a39207f0a09p+1,
+    0x1.0ef9db467dcf8p+1, 0x1.1793e4652cc50p+1, 0x1.2073d3f1bd518p+1, 0x1.299be1f3e7f1cp+1,
+    0x1.330e587b62b28p+1, 0x1.3ccd9432682b4p+1, 0x1.46dc04f4e5338p+1, 0x1.513c2e6c731d7p+1,
+};
+__device__ __forceinline__ double bin_weight(int b) { return EXP_Q[b >> 5] * EXP_R[b & 31]; }
+__device__ __forceinline__ double bin_inverse(int b) { return INV_Q[b >> 5] * INV_R[b & 31]; }
+
 struct RowBins {                      // the scaled logit of a row's tokens
     double per_t;                     // 32 / T
     double qmax;                      // floor(x) of the largest
@@ -93,7 +138,7 @@ __device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)
 
 // One slice of a row: its largest token; its bins, counted from that one's
 // (sum << 14 | count), stand apart.
-struct SliceHead { double q; uint32_t top; uint32_t pad; };
+struct SliceHead { double q; uint32_t top; uint32_t used; };   // used: bins up to the last that holds any
 
 template <int NW>
 __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
@@ -108,37 +153,36 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
     return t;
 }
 
-__device__ __forceinline__ void count_keys(const uint32_t (&k)[8], const RowBins& rb, unsigned long long* hist) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (!k[j]) continue;
-        const double x = rb.x(k[j]), b = rb.bin(x);
-        if (b < (double)SB_BINS) atomicAdd(&hist[(int)b], rb.units(x) << 14 | 1ull);
-    }
-}
-
-// Keys of a thread's 16 tokens of slice `slice`: i0 + 0 .. 7 and i0 + SL_LEN / 2 + 0 .. 7.
-__device__ __forceinline__ int load_slice(const RowArgs& r, int slice, uint32_t (&k)[2][8]) {
-    const int i0 = slice * SL_LEN + threadIdx.x * 8;
-    load_keys(r, i0, k[0]);
-    load_keys(r, i0 + SL_LEN / 2, k[1]);
-    return i0;
-}
-
-// The largest key of the workgroup's, and hist[] of its tokens counted from it.
-__device__ __forceinline__ uint32_t count_slice(const uint32_t (&k)[2][8], RowBins& rb, unsigned long long* hist, uint32_t* buf) {
-    for (int i = threadIdx.x; i < SB_BINS; i += SB_THREADS) hist[i] = 0ull;
+// The keys of a slice into LDS, in the order of the tokens; the largest one.
+// (Loops over a thread's 16 tokens stay loops: a workgroup runs this code once,
+// and fetching instructions costs it about 0.9 us a kilobyte.)
+__device__ __forceinline__ uint32_t load_slice(const RowArgs& r, int slice, uint32_t* keys, uint32_t* buf) {
     uint32_t top = 0;
+#pragma unroll 1
+    for (int i = threadIdx.x * 8; i < SL_LEN; i += SB_THREADS * 8) {
+        uint32_t k[8];
+        load_keys(r, slice * SL_LEN + i, k);
+        *(u32x4*)(keys + i) = u32x4{k[0], k[1], k[2], k[3]};
+        *(u32x4*)(keys + i + 4) = u32x4{k[4], k[5], k[6], k[7]};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, max(k[0][j], k[1][j]));
-    top = block_max<SB_THREADS / 64>(top, buf);
-    rb.qmax = floor(rb.x(top));
-    if (top) {
-        count_keys(k[0], rb, hist);
-        count_keys(k[1], rb, hist);
+        for (int j = 0; j < 8; ++j) top = max(top, k[j]);
     }
+    return block_max<SB_THREADS / 64>(top, buf);               // and a barrier: the keys are written
+}
+
+__device__ __forceinline__ void count_key(uint32_t k, const RowBins& rb, unsigned long long* hist) {
+    const double x = rb.x(k), b = rb.bin(x);
+    if (k && b < (double)SB_BINS) atomicAdd(&hist[(int)b], rb.units(x) << 14 | 1ull);
+}
+
+// hist[] of the slice's tokens, counted from rb.qmax.
+__device__ __forceinline__ void count_slice(const uint32_t* keys, const RowBins& rb, unsigned long long* hist) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < SB_BINS; i += SB_THREADS) hist[i] = 0ull;
     __syncthreads();
-    return top;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < SL_LEN; i += SB_THREADS) count_key(keys[i], rb, hist);
+    __syncthreads();
 }
 
 // What the counts of a row say before any token is ranked.
@@ -147,11 +191,10 @@ struct RowPlan {
     unsigned long long units0;        // units of bin 0
     uint32_t top;                     // key of the largest, 0: nothing to draw from
     unsigned nall, n;                 // tokens; those of the runs of bins in which the places can be
-    unsigned slices;                  // slices that hold some of the latter
     int kbin, vbin;                   // bins of top_k's cut and of min_p's (SB_BINS: none)
     int lo[SB_RANGES], hi[SB_RANGES]; // the runs (lo = SB_BINS: none)
-    uint32_t klo[SB_RANGES], khi[SB_RANGES];   // their keys
-    unsigned touched[SAMPLE_MAX_SLICES / 32];  // the slices, one bit each
+    uint32_t klo[SB_RANGES], span[SB_RANGES];  // their least keys, and how many keys there are from it
+    unsigned touched[SAMPLE_MAX_SLICES / 32];  // slices that hold some of those, one bit each
 };
 
 // Workspace of one row of a sampled batch: SAMPLE_ROW_BYTES, then the slices' heads and bins.
@@ -160,7 +203,7 @@ struct RowSpace {
     double cum[SB_BINS];              // weight of the bins up to and with this one
     unsigned cumc[SB_BINS];           // their tokens
     RowPlan plan;
-    unsigned arrived, drawn;          // slices that are counted, gathered: zero between calls
+    unsigned arrived;                 // slices that are counted: zero between calls
     unsigned fill;                    // tokens in the list
 };
 static_assert(sizeof(RowSpace) <= SAMPLE_ROW_BYTES, "row workspace");
@@ -189,7 +232,8 @@ struct SampleShared {
         };
     };
     unsigned rank[SB_RANK];
-    int shift[SAMPLE_MAX_SLICES];              // bins from the row's largest to the slice's, or -1: nothing there
+    int shift[SAMPLE_MAX_SLICES];              // bins from the row's largest to the slice's (SB_BINS: nothing there)
+    int used[SAMPLE_MAX_SLICES];               // and how many bins the slice has
     unsigned touched[SAMPLE_MAX_SLICES / 32];
     unsigned long long wave_u[SB_THREADS / 64];
     unsigned wave_c[SB_THREADS / 64];
@@ -350,13 +394,13 @@ __device__ __forceinline__ Place place_in_ranked(int at, int n, int c0, unsigned
 // those of at least `t` units each (BY_VALUE, which names no token).  listed > 0:
 // the part's tokens stand among the list's first `listed`.  Otherwise, above
 // SB_CAP of them, passes over the row narrow the part to a bucket of its keys' range (or
-// find a token of equal ones by index), then gather it.  The list is narrowed
-// the same way, in registers, until SB_RANK tokens are left, which are ranked.
+// find a token of equal ones by index), then gather it.  The part's tokens are
+// narrowed the same way, in LDS (sel), until SB_RANK are left, which are ranked.
 // Whole workgroup; every thread gets the result.  (One loop over the row serves
 // every kind of pass, and the caller calls this in one place: a row is one
 // workgroup's work once, so instructions come from memory, not from the cache.)
 __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb, Part part, unsigned long long* list, int listed, Want want,
-                                            unsigned long long t, SampleShared& sh) {
+                                            unsigned long long t, unsigned long long* sel, SampleShared& sh) {
     enum Pass : int { RANGE, PIECES, COUNT, PICK, VALUE, GATHER };
     const int tid = threadIdx.x;
     int c0 = 0;                                 // tokens and units of the part ahead of the piece looked at
@@ -460,63 +504,69 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
         }
         listed = part.n;
     }
-    // at most SB_CAP tokens in the list: a few a thread
-    constexpr int PER = SB_CAP / SB_THREADS;
-    unsigned long long e[PER];
-    unsigned alive = 0;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int i = tid + j * SB_THREADS;
-        e[j] = i < listed ? load_coherent(&list[i]) : 0ull;
-        const uint32_t k = (uint32_t)(e[j] >> 32);
-        if (k >= part.lo && k <= part.hi && k && rb.bin(rb.x(k)) == (double)part.bin) alive |= 1u << j;
-    }
-    if (want == BY_VALUE) {
-        unsigned n = 0, tc;
-        unsigned long long sum = 0, tu;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const unsigned long long v = alive >> j & 1u ? rb.units(rb.x((uint32_t)(e[j] >> 32))) : 0ull;
-            if (v >= t && v) { ++n; sum += v; }
-        }
-        scan_block(n, sum, sh.wave_c, sh.wave_u, &tc, &tu);
-        return Place{(int)tc, tu, 0u, -1};
-    }
-    int n = part.n;
-    while (n > SB_RANK) {
-        // buckets of the keys' range, highest first; of the index where all keys are equal
-        uint32_t lo = 0xffffffffu, hi = 0u;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const uint32_t k = (uint32_t)(e[j] >> 32);
-            if (alive >> j & 1u) { lo = min(lo, k); hi = max(hi, k); }
-        }
-        __syncthreads();
-        for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
-        if (tid == 0) { sh.klo = 0xffffffffu; sh.khi = 0u; }
-        __syncthreads();
-        if (hi) { atomicMin(&sh.klo, lo); atomicMax(&sh.khi, hi); }
-        __syncthreads();
-        lo = sh.klo;
-        hi = sh.khi;
-        const uint32_t range = lo == hi ? (uint32_t)r.V - 1u : hi - lo;
-        const int shift = max(0, 22 - (int)__clz(range | 1u));       // range >> shift < 1024
-        auto bucket = [&](unsigned long long v) { return (lo == hi ? ~(uint32_t)v : hi - (uint32_t)(v >> 32)) >> shift; };
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (alive >> j & 1u) atomicAdd(&sh.hist[bucket(e[j])], rb.units(rb.x((uint32_t)(e[j] >> 32))) << 14 | 1ull);
-        __syncthreads();
-        const uint32_t s = (uint32_t)find_bucket(want, t, c0, u0, n, sh);
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (bucket(e[j]) != s) alive &= ~(1u << j);
-    }
+    // the part's tokens among the list's into LDS; by value, they are counted and summed at once
     __syncthreads();
     if (tid == 0) sh.fill = 0u;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-        if (alive >> j & 1u) sh.ranked[atomicAdd(&sh.fill, 1u)] = e[j];
+    unsigned cnt = 0, tc;
+    unsigned long long sum = 0, tu;
+#pragma unroll 1
+    for (int i = tid; i < listed; i += SB_THREADS) {
+        const unsigned long long v = load_coherent(&list[i]);
+        const uint32_t k = (uint32_t)(v >> 32);
+        if (k < part.lo || k > part.hi) continue;
+        const double x = rb.x(k);
+        if (rb.bin(x) != (double)part.bin) continue;
+        if (want == BY_VALUE) {
+            const unsigned long long e = rb.units(x);
+            if (e >= t) { ++cnt; sum += e; }
+        } else {
+            sel[atomicAdd(&sh.fill, 1u)] = v;
+        }
+    }
+    if (want == BY_VALUE) {
+        scan_block(cnt, sum, sh.wave_c, sh.wave_u, &tc, &tu);
+        return Place{(int)tc, tu, 0u, -1};
+    }
+    int n = part.n;
+#pragma unroll 1
+    while (n > SB_RANK) {
+        // buckets of the keys' range, highest first; of the index where all keys are equal
+        __syncthreads();
+        uint32_t lo = 0xffffffffu, hi = 0u;
+#pragma unroll 1
+        for (int i = tid; i < n; i += SB_THREADS) {
+            const uint32_t k = (uint32_t)(sel[i] >> 32);
+            lo = min(lo, k);
+            hi = max(hi, k);
+        }
+#pragma unroll 1
+        for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
+        hi = block_max<SB_THREADS / 64>(hi, sh.wave_c);
+        lo = ~block_max<SB_THREADS / 64>(~lo, sh.wave_c);
+        const uint32_t range = lo == hi ? (uint32_t)r.V - 1u : hi - lo;
+        const int shift = max(0, 22 - (int)__clz(range | 1u));       // range >> shift < 1024
+        auto bucket = [&](unsigned long long v) { return (lo == hi ? ~(uint32_t)v : hi - (uint32_t)(v >> 32)) >> shift; };
+#pragma unroll 1
+        for (int i = tid; i < n; i += SB_THREADS) {
+            const unsigned long long v = sel[i];
+            atomicAdd(&sh.hist[bucket(v)], rb.units(rb.x((uint32_t)(v >> 32))) << 14 | 1ull);
+        }
+        __syncthreads();
+        const int was = n;
+        const uint32_t s = (uint32_t)find_bucket(want, t, c0, u0, n, sh);
+        __syncthreads();
+        if (tid == 0) sh.fill = 0u;
+#pragma unroll 1
+        for (int i0 = 0; i0 < was; i0 += SB_THREADS) {               // what stays moves down, behind what has been read
+            const unsigned long long v = i0 + tid < was ? sel[i0 + tid] : 0ull;
+            __syncthreads();
+            if (v && bucket(v) == s) sel[atomicAdd(&sh.fill, 1u)] = v;
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < n; i += SB_THREADS) sh.ranked[i] = sel[i];
     __syncthreads();
     rank_tokens(n, rb, sh);
     const Place p = place_in_ranked(0, n, c0, u0, want, t, rb, sh);
@@ -533,7 +583,7 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
     unsigned nall, upc = 0;
 #pragma unroll
     for (int j = 0; j < SB_PER; ++j) {
-        wj[j] = (double)bu[j] * exp((double)(SB_PER * tid + j) * (-1.0 / 32.0));
+        wj[j] = (double)bu[j] * bin_weight(SB_PER * tid + j);
         upw += wj[j];
         upc += bc[j];
     }
@@ -567,11 +617,9 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
     pl.kbin = bin_of_count(by_k ? (unsigned)p.top_k : nall);
     pl.vbin = SB_BINS;
     if (p.min_p > 0.0f) {
-        // the first bin with tokens whose least weight fails min_p may hold some that pass, those behind it none;
-        // log and exp agree to far less than a bin, and one bin more than needed does no harm: its tokens are compared
+        // the first bin with tokens whose least weight fails min_p may hold some that pass, those behind it none
         const double least = (double)exp_units(0.0);
-        const int b = max(0, (int)fmin((double)SB_BINS, floor(-32.0 * log(pl.thr / least))) - 1);
-        const int f = b + wave_search(SB_BINS - b, [&](int i) { return exp((double)(b + i) * (-1.0 / 32.0)) * least < pl.thr; });
+        const int f = wave_search(SB_BINS, [&](int i) { return bin_weight(i) * least < pl.thr; });
         if (f < SB_BINS) pl.vbin = bin_of_count(cbefore(f) + 1u);
     }
     // The places, whatever the tokens of the cut bins are: the kept weight lies between what is ahead of a cut's bin
@@ -636,48 +684,47 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
     for (int i = 0; i < SB_RANGES; ++i) {
         pl.lo[i] = lo[i];
         pl.hi[i] = hi[i];
-        pl.klo[i] = 1u;
-        pl.khi[i] = 0u;
+        pl.klo[i] = pl.span[i] = 0u;
         if (lo[i] >= SB_BINS) continue;
         pl.klo[i] = (uint32_t)__builtin_amdgcn_readlane((int)key, 16 * i);
-        pl.khi[i] = lo[i] ? (uint32_t)__builtin_amdgcn_readlane((int)key, 16 * i + 8) - 1u : top;
+        pl.span[i] = (lo[i] ? (uint32_t)__builtin_amdgcn_readlane((int)key, 16 * i + 8) : top + 1u) - pl.klo[i];
         pl.n += sh.cumc[hi[i]] - cbefore(lo[i]);
     }
-    pl.slices = 0u;
     return pl;
 }
 
-// The tokens of the plan's runs among a lane's 16 go into the list; a wave asks
-// once for their places.
+// The slice's tokens of the plan's runs go into the list; a wave asks once for
+// their places.
 template <class Put>
-__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t (&k)[2][8], int i0, unsigned* fill, Put put) {
+__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* keys, int slice, unsigned* fill, Put put) {
+    const int tid = threadIdx.x;
     unsigned m = 0;
+#pragma unroll 2
+    for (int i = 0; i < SL_LEN / SB_THREADS; ++i) {
+        const uint32_t k = keys[i * SB_THREADS + tid];
+        bool in = false;
 #pragma unroll
-    for (int q = 0; q < SB_RANGES; ++q) {
-        if (pl.klo[q] > pl.khi[q]) continue;
-        const uint32_t klo = pl.klo[q], span = pl.khi[q] - klo;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) m |= k[j >> 3][j & 7] - klo <= span ? 1u << j : 0u;
+        for (int q = 0; q < SB_RANGES; ++q) in |= k - pl.klo[q] < pl.span[q];
+        m |= in ? 1u << i : 0u;
     }
     if (!__ballot(m != 0u)) return;
     const unsigned mine = (unsigned)__popc(m), upto = scan_wave(mine);
     unsigned at = 0;
-    if ((threadIdx.x & 63) == 63) at = atomicAdd(fill, upto);
+    if ((tid & 63) == 63) at = atomicAdd(fill, upto);
     at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + upto - mine;
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (m >> j & 1u) {
-            const uint32_t index = (uint32_t)(i0 + (j >> 3) * (SL_LEN / 2) + (j & 7));
-            if (at < (unsigned)SB_CAP) put(at, ((unsigned long long)k[j >> 3][j & 7] << 32) | (uint32_t)~index);
-            ++at;
-        }
+    while (m) {
+        const int i = (__ffs(m) - 1) * SB_THREADS + tid;
+        if (at < (unsigned)SB_CAP) put(at, ((unsigned long long)keys[i] << 32) | (uint32_t)~(slice * SL_LEN + i));
+        ++at;
+        m &= m - 1u;
+    }
 }
 
 // The cuts and the draw of a row, by one workgroup: its running sums in sh.cum
 // and sh.cumc, the tokens of the plan's runs in the list (unless they are more
 // than SB_CAP: then the row is read again, place by place).
 __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const RowArgs& r, const RowPlan& plan, float u,
-                                         unsigned long long* list, SampleShared& sh) {
+                                         unsigned long long* list, unsigned long long* sel, SampleShared& sh) {
     const int tid = threadIdx.x;
     const SampleRow p = a.rows[row];
     const RowBins rb{p.per_t, plan.qmax};
@@ -686,10 +733,9 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
     const bool by_k = p.top_k > 0 && (unsigned)p.top_k < nall, by_p = p.top_p < 1.0f;
     auto before = [&](int b) { return b ? sh.cum[b - 1] : 0.0; };
     auto cbefore = [&](int b) { return b ? sh.cumc[b - 1] : 0u; };
-    auto E = [&](int b) { return exp((double)b * (-1.0 / 32.0)); };
     bool listed = plan.n <= (unsigned)SB_CAP, ranked = plan.n <= (unsigned)SB_RANK;
     if (ranked) {                               // few: ranked together, bin behind bin
-        if (tid < (int)plan.n) sh.ranked[tid] = load_coherent(&list[tid]);
+        if (tid < (int)plan.n) sh.ranked[tid] = list[tid];
         __syncthreads();
         rank_tokens((int)plan.n, rb, sh);
     }
@@ -716,11 +762,11 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
             const unsigned long long f = (unsigned long long)((double)share * 18446744073709551616.0);
             return __umul64hi(W0, f) + (up && W0 * f != 0ull ? 1ull : 0ull);
         }
-        const double t = fmax(0.0, ((double)share * W - before(b)) / E(b));
+        const double t = fmax(0.0, ((double)share * W - before(b)) * bin_inverse(b));
         return (unsigned long long)(up ? ceil(t) : floor(t));
     };
     Place pl{0, 0ull, 0u, -1};
-    int b = 0;
+    int b = 0, end = plan.kbin;                 // end: the bin of the last token kept
 #pragma unroll 1
     for (int step = 0; step < 5; ++step) {      // the three cuts, the draw, and the draw again where it came behind the last cut
         Want want = BY_MASS;
@@ -734,7 +780,7 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
             if (plan.vbin >= SB_BINS || cbefore(plan.vbin) >= (unsigned)C) continue;
             b = plan.vbin;
             want = BY_VALUE;
-            t = (unsigned long long)ceil(plan.thr / E(b));
+            t = (unsigned long long)ceil(plan.thr * bin_inverse(b));
         } else if (step == 4) {
             if ((int)cbefore(b) + pl.count <= C) continue;
             want = BY_COUNT;
@@ -744,27 +790,27 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
             // the bin in which the running weight reaches top_p of what is kept, or passes u of it
             const float share = step == 1 ? p.top_p : u;
             const double goal = (double)share * W;
-            const int to = wave_search(SB_BINS, [&](int i) { return step == 3 ? sh.cum[i] > goal : sh.cum[i] >= goal; });
-            b = C <= (int)sh.cumc[0] ? 0 : min(to, wave_search(SB_BINS, [&](int i) { return sh.cumc[i] >= (unsigned)C; }));
+            b = C <= (int)sh.cumc[0] ? 0 : min(end, wave_search(SB_BINS, [&](int i) { return step == 3 ? sh.cum[i] > goal : sh.cum[i] >= goal; }));
             t = target(share, b, step == 1) + (step == 3 ? 1ull : 0ull);
         }
         const int at = start(b), cnt = (int)(sh.cumc[b] - cbefore(b));
         if (ranked && at >= 0) pl = place_in_ranked(at, cnt, 0, 0ull, want, t, rb, sh);
         else {
-            pl = find_place(r, rb, Part{b, 0u, 0xffffffffu, cnt}, list, listed && at >= 0 ? (int)plan.n : 0, want, t, sh);
+            pl = find_place(r, rb, Part{b, 0u, 0xffffffffu, cnt}, list, listed && at >= 0 ? (int)plan.n : 0, want, t, sel, sh);
             listed = listed && at >= 0;         // find_place took the list's memory
             ranked = false;                     // and that of the ranked ones
         }
         const int c = (int)cbefore(b) + pl.count;
         if (step < 3 && c < C) {
             C = c;
-            W = before(b) + (double)pl.units * E(b);
+            W = before(b) + (double)pl.units * bin_weight(b);
             if (b == 0) W0 = pl.units;
+            end = pl.count ? b : wave_search(SB_BINS, [&](int i) { return sh.cumc[i] >= (unsigned)C; });
         }
     }
     if (tid == 0) {
         a.token[row] = pl.index;
-        a.p[row] = (float)((double)rb.units(rb.x(pl.key)) * E(b) / W);
+        a.p[row] = (float)((double)rb.units(rb.x(pl.key)) * bin_weight(b) / W);
         if (a.top) a.top[row] = key_logit(plan.top);
     }
 }
@@ -780,17 +826,25 @@ __device__ __forceinline__ void draw_nothing(const SampleArgs& a, int row) {
 __device__ __forceinline__ float row_u(const SampleArgs& a, int row) { return a.u ? fminf(fmaxf(a.u[row], 0.0f), 0.99999994f) : 0.0f; }
 
 // A row of one slice, by one workgroup.
+struct SmallShared {
+    uint32_t keys[SL_LEN];
+    unsigned long long list[SB_CAP];
+    SampleShared sh;
+};
 __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) {
-    __shared__ SampleShared sh;
-    __shared__ unsigned long long list[SB_CAP];
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    SmallShared& all = *(SmallShared*)smem;
+    SampleShared& sh = all.sh;
+    uint32_t* keys = all.keys;
+    unsigned long long* list = all.list;
     const int row = blockIdx.x, tid = threadIdx.x;
     const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
     RowBins rb{a.rows[row].per_t, 0.0};
     const float u = row_u(a, row);
-    uint32_t k[2][8];
-    const int i0 = load_slice(r, 0, k);
     if (tid == 0) sh.fill = 0u;
-    const uint32_t top = count_slice(k, rb, sh.hist, sh.wave_c);
+    const uint32_t top = load_slice(r, 0, keys, sh.wave_c);
+    rb.qmax = floor(rb.x(top));
+    count_slice(keys, rb, sh.hist);
     if (!top) return draw_nothing(a, row);
     unsigned bc[SB_PER];
     unsigned long long bu[SB_PER];
@@ -800,13 +854,13 @@ __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) 
         bu[j] = sh.hist[SB_PER * tid + j] >> 14;
     }
     const RowPlan plan = make_plan(a.rows[row], u, rb, top, bc, bu, sh);
-    if (plan.n <= (unsigned)SB_CAP) take_tokens(plan, k, i0, &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
+    if (plan.n <= (unsigned)SB_CAP) take_tokens(plan, keys, 0, &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
     __syncthreads();
-    draw_row(a, row, r, plan, u, list, sh);
+    draw_row(a, row, r, plan, u, list, (unsigned long long*)keys, sh);
 }
 
 // Counts one slice of a row; the row's last workgroup to end joins the counts and makes the plan.
-__global__ __launch_bounds__(SB_THREADS, 4) void sample_count_kernel(SampleArgs a) {
+__global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
     const int slice = blockIdx.x, row = blockIdx.y, ns = gridDim.x, tid = threadIdx.x;
     RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
@@ -815,28 +869,56 @@ __global__ __launch_bounds__(SB_THREADS, 4) void sample_count_kernel(SampleArgs 
     RowBins rb{a.rows[row].per_t, 0.0};
     {
         const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
-        uint32_t k[2][8];
-        load_slice(r, slice, k);
-        const uint32_t top = count_slice(k, rb, sh.hist, sh.wave_c);
+        // keys in registers: without them in LDS four workgroups share a CU
+        uint32_t k[2][8], top = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_keys(r, slice * SL_LEN + h * (SL_LEN / 2) + tid * 8, k[h]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, k[h][j]);
+        }
+#pragma unroll 1
+        for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
+        top = block_max<SB_THREADS / 64>(top, sh.wave_c);
+        rb.qmax = floor(rb.x(top));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) count_key(k[h][j], rb, sh.hist);
+        __syncthreads();
+        if (tid == 0) sh.found = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = tid; i < SB_BINS; i += SB_THREADS) {
+            const unsigned long long some = __ballot(sh.hist[i] != 0ull);
+            if (some && (tid & 63) == 0) atomicMax(&sh.found, i + 64 - __clzll(some));
+        }
+        __syncthreads();
+        const int used = sh.found;
+#pragma unroll 1
+        for (int i = tid; i < used; i += SB_THREADS) store_coherent(&bins[(size_t)slice * SB_BINS + i], sh.hist[i]);
         if (tid == 0) {
             store_coherent((unsigned long long*)&heads[slice].q, (unsigned long long)__double_as_longlong(rb.qmax));
-            store_coherent((unsigned long long*)&heads[slice].top, (unsigned long long)top);
+            store_coherent((unsigned long long*)&heads[slice].top, (unsigned long long)used << 32 | top);
         }
-        for (int i = tid; i < SB_BINS; i += SB_THREADS) store_coherent(&bins[(size_t)slice * SB_BINS + i], sh.hist[i]);
     }
     if (!last_arrival(&ws->arrived, (unsigned)ns, &sh.flag)) return;
     uint32_t top = 0;
     double q = 0.0;
+    int used = 0;
     if (tid < ns) {
         q = __longlong_as_double((long long)load_coherent((unsigned long long*)&heads[tid].q));
-        top = (uint32_t)load_coherent((unsigned long long*)&heads[tid].top);
+        const unsigned long long v = load_coherent((unsigned long long*)&heads[tid].top);
+        top = (uint32_t)v;
+        used = (int)(v >> 32);
     }
     const uint32_t mytop = top;
     top = block_max<SB_THREADS / 64>(top, sh.wave_c);
     rb.qmax = floor(rb.x(top));
     if (tid < SAMPLE_MAX_SLICES) {
         const double d = rb.qmax - q;
-        sh.shift[tid] = mytop != 0u && d < (double)SB_BINS ? (int)d : -1;
+        sh.shift[tid] = mytop != 0u && d < (double)SB_BINS ? (int)d : SB_BINS;
+        sh.used[tid] = used;
     }
     if (tid < SAMPLE_MAX_SLICES / 32) sh.touched[tid] = 0u;
     __syncthreads();
@@ -846,15 +928,16 @@ __global__ __launch_bounds__(SB_THREADS, 4) void sample_count_kernel(SampleArgs 
     }
     unsigned bc[SB_PER] = {};
     unsigned long long bu[SB_PER] = {}, in_lo = 0, in_hi = 0;  // this thread's bins, and the slices that have tokens in them
+#pragma unroll 1
     for (int s0 = 0; s0 < ns; s0 += 8) {
         unsigned long long v[8][SB_PER];
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
-            const int s = s0 + g, d = s < ns ? sh.shift[s] : -1;
+            const int s = min(s0 + g, ns - 1), d = sh.shift[s], end = s0 + g < ns ? sh.used[s] : 0;
 #pragma unroll
             for (int j = 0; j < SB_PER; ++j) {
                 const int i = SB_PER * tid + j - d;
-                v[g][j] = d >= 0 && i >= 0 ? load_coherent(&bins[(size_t)s * SB_BINS + i]) : 0ull;
+                v[g][j] = i >= 0 && i < end ? load_coherent(&bins[(size_t)s * SB_BINS + i]) : 0ull;
             }
         }
 #pragma unroll
@@ -889,51 +972,57 @@ __global__ __launch_bounds__(SB_THREADS, 4) void sample_count_kernel(SampleArgs 
     }
     __syncthreads();
     if (tid == 0) {
-        // more tokens than the list takes: the row's first workgroup draws alone
 #pragma unroll
-        for (int w = 0; w < SAMPLE_MAX_SLICES / 32; ++w) {
-            plan.touched[w] = plan.n <= (unsigned)SB_CAP ? sh.touched[w] : w == 0 ? 1u : 0u;
-            plan.slices += (unsigned)__popc(plan.touched[w]);
-        }
+        for (int w = 0; w < SAMPLE_MAX_SLICES / 32; ++w) plan.touched[w] = sh.touched[w];
         ws->plan = plan;
         ws->fill = 0u;
     }
 }
 
-// Gathers one slice's tokens of the plan's runs; the row's last workgroup to end draws.
-__global__ __launch_bounds__(SB_THREADS, 4) void sample_draw_kernel(SampleArgs a) {
+// Gathers one slice's tokens of the plan's runs.
+__global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a) {
+    __shared__ __attribute__((aligned(16))) uint32_t keys[SL_LEN];
+    __shared__ uint32_t buf[SB_THREADS / 64];
+    const int slice = blockIdx.x, row = blockIdx.y;
+    RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
+    const RowPlan& plan = ws->plan;
+    if (!plan.top || plan.n > (unsigned)SB_CAP || !(plan.touched[slice >> 5] >> (slice & 31) & 1u)) return;
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    load_slice(r, slice, keys, buf);
+    take_tokens(plan, keys, slice, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
+}
+
+// The cuts and the draw, one workgroup a row.
+__global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
-    const int slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    __shared__ unsigned long long sel[SB_CAP];
+    const int row = blockIdx.x, tid = threadIdx.x;
     RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
     const RowPlan plan = ws->plan;
-    if (!plan.top) {
-        if (slice == 0) draw_nothing(a, row);
-        return;
-    }
-    if (!(ws->plan.touched[slice >> 5] >> (slice & 31) & 1u)) return;
+    if (!plan.top) return draw_nothing(a, row);
     const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
-    if (plan.n <= (unsigned)SB_CAP) {
-        uint32_t k[2][8];
-        const int i0 = load_slice(r, slice, k);
-        take_tokens(plan, k, i0, &ws->fill, [&](unsigned at, unsigned long long v) { store_coherent(&ws->list[at], v); });
-    }
-    if (!last_arrival(&ws->drawn, plan.slices, &sh.flag)) return;
-    for (int i = tid; i < SB_BINS; i += SB_THREADS) {
-        sh.cum[i] = ws->cum[i];
-        sh.cumc[i] = ws->cumc[i];
+#pragma unroll
+    for (int j = 0; j < SB_PER; ++j) {
+        sh.cum[j * SB_THREADS + tid] = ws->cum[j * SB_THREADS + tid];
+        sh.cumc[j * SB_THREADS + tid] = ws->cumc[j * SB_THREADS + tid];
     }
     __syncthreads();
-    draw_row(a, row, r, plan, row_u(a, row), ws->list, sh);
+    draw_row(a, row, r, plan, row_u(a, row), ws->list, sel, sh);
 }
 
 hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st) {
     if (!a.slices) {
-        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), 0, st>>>(a);
+        // on every launch: the attribute belongs to the device that is current
+        const hipError_t e = hipFuncSetAttribute((const void*)sample_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 sizeof(SmallShared));
+        if (e != hipSuccess) return e;
+        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), sizeof(SmallShared), st>>>(a);
         return hipGetLastError();
     }
     const dim3 g((unsigned)a.slices, (unsigned)m);
     sample_count_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
-    sample_draw_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
+    sample_gather_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
+    sample_draw_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -943,7 +1032,6 @@ size_t sample_slice_bytes(int slices) { return (size_t)MAX_ROWS * slices * (size
 __global__ void sample_clear_kernel(uint8_t* rows) {
     RowSpace* ws = (RowSpace*)(rows + (size_t)threadIdx.x * SAMPLE_ROW_BYTES);
     ws->arrived = 0u;
-    ws->drawn = 0u;
     ws->fill = 0u;
 }
 

@@ -256,7 +256,7 @@ def test_capture(stage):
     leaves the capture whole."""
     codes, scales = _weights(64, 64, 19)
     mat = stage.mx4_matrix(torch.from_numpy(mx4_pack(codes)), torch.from_numpy(scales), 64)
-    x, many = _rows(9, 64, 20, "bf16").cuda(), _rows(17, 64, 20, "bf16").cuda()
+    x, many = _rows(9, 64, 20, "bf16").cuda(), _rows(65, 64, 20, "bf16").cuda()
     mat.product(x)
     mat.product(many)
     torch.cuda.synchronize()
