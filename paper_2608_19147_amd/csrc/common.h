@@ -367,7 +367,6 @@ struct Mx4Gemm {
     Mx4Mat w; Mx4Act a;
     int m;
     void* out; int dt; size_t ld;
-    int pairs;                                     // two neighbouring outputs may be stored at once
     int split, steps_per;                          // splits of K, steps of each (a multiple of 4)
     float* part; int part_ld;                      // split > 1: their sums [split][m][part_ld]
     int mtiles;                                    // set by the launcher
@@ -391,7 +390,6 @@ constexpr int SAMPLE_MAX_SLICES = 128;             // 2^20 tokens
 constexpr size_t SAMPLE_ROW_BYTES = 46080;         // workspace of a row (RowSpace)
 struct SampleArgs {
     const void* logits; int dt; size_t ld; int V;
-    int vec;                                       // rows start on 16 bytes
     int slices;                                    // of a row, 0 for one; with more, the rows' and slices' workspace:
     uint8_t* rows_ws;                              // [MAX_ROWS] x SAMPLE_ROW_BYTES
     void* heads; unsigned long long* bins;         // [m][slices], [m][slices][bins]

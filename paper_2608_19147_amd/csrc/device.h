@@ -9,6 +9,10 @@ namespace stg {
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+// The same at any address: global memory takes wide accesses at every byte.
+typedef u32x4 __attribute__((aligned(1))) u32x4_any;
+typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+typedef uint32_t __attribute__((aligned(1))) u32_any;
 
 // ------------------------------------------------------------------ conversions
 

@@ -71,9 +71,8 @@ __device__ __forceinline__ uint32_t absbits(float v) { return __float_as_uint(v)
 
 // Eight values of a row a thread, four neighbouring threads a block: their
 // largest magnitude is shared by lane exchanges, each writes 4 bytes of codes.
-// VEC: rows start on 16 bytes and hold a multiple of 8 values (codes then start
-// on 4 bytes).  Bound by memory: 2 bytes a value read (16 bits), 17/32 written.
-template <int DT, bool VEC>
+// Bound by memory: 2 bytes a value read (16 bits), 17/32 written.
+template <int DT>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, size_t ld, int m, int k, int chunks,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     // chunks: of 8 values in a row, a multiple of 4
@@ -83,14 +82,14 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
     const size_t r = small ? (size_t)((uint32_t)idx / (uint32_t)chunks) : idx / chunks;
     const int c = (int)(idx - r * chunks), i0 = 8 * c;
     float v[8];
-    if (VEC && i0 + 8 <= k) {
+    if (i0 + 8 <= k) {
         if constexpr (DT == DT_F32) {
-            const u32x4* p = (const u32x4*)((const float*)x + r * ld + i0);
+            const u32x4_any* p = (const u32x4_any*)((const float*)x + r * ld + i0);
             const u32x4 a = p[0], b = p[1];
 #pragma unroll
             for (int j = 0; j < 4; ++j) { v[j] = __uint_as_float(a[j]); v[4 + j] = __uint_as_float(b[j]); }
         } else {
-            const u32x4 a = *(const u32x4*)((const uint16_t*)x + r * ld + i0);
+            const u32x4 a = *(const u32x4_any*)((const uint16_t*)x + r * ld + i0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 1] >> (16 * (j & 1))), DT);
         }
@@ -107,8 +106,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restric
     const uint32_t byte = block_byte(top, 2);
     const uint32_t w = byte == 255u ? 0u : e2m1x8(v, e8m0_inv(byte));
     uint8_t* o = codes + r * ((size_t)(k + 1) / 2) + i0 / 2;
-    if (VEC) {
-        *(uint32_t*)o = w;
+    if (i0 + 8 <= k) {
+        *(u32_any*)o = w;
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -121,18 +120,16 @@ hipError_t launch_mx4_quantize(const void* x, int dt, int64_t ld, int m, int k, 
     const int chunks = (k + 31) / 32 * 4;
     const size_t n = (size_t)m * chunks;
     const dim3 g((unsigned)((n + 255) / 256)), b(256);
-    const size_t es = dt == DT_F32 ? 4 : 2;
-    const bool vec = k % 8 == 0 && ((uintptr_t)x & 15) == 0 && (m == 1 || (size_t)ld * es % 16 == 0) && ((uintptr_t)codes & 3) == 0;
-#define MX4_Q(DT, VEC) mx4_quantize_kernel<DT, VEC><<<g, b, 0, st>>>(x, (size_t)ld, m, k, chunks, codes, scales)
-    if (dt == DT_F32) vec ? MX4_Q(DT_F32, true) : MX4_Q(DT_F32, false);
-    else if (dt == DT_F16) vec ? MX4_Q(DT_F16, true) : MX4_Q(DT_F16, false);
-    else vec ? MX4_Q(DT_BF16, true) : MX4_Q(DT_BF16, false);
+#define MX4_Q(DT) mx4_quantize_kernel<DT><<<g, b, 0, st>>>(x, (size_t)ld, m, k, chunks, codes, scales)
+    if (dt == DT_F32) MX4_Q(DT_F32);
+    else if (dt == DT_F16) MX4_Q(DT_F16);
+    else MX4_Q(DT_BF16);
 #undef MX4_Q
     return hipGetLastError();
 }
 
-// Eight values a thread.  VEC: codes start on 4 bytes, rows of out on 16, k is a multiple of 8.
-template <int DT, bool VEC>
+// Eight values a thread.
+template <int DT>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                              int m, int k, int chunks, void* __restrict__ out, size_t ld) {
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
@@ -142,8 +139,9 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __re
     const int c = (int)(idx - r * chunks), i0 = 8 * c;
     const uint8_t* p = codes + r * ((size_t)(k + 1) / 2) + i0 / 2;
     uint32_t w = 0;
-    if (VEC) {
-        w = *(const uint32_t*)p;
+    const bool whole = i0 + 8 <= k;
+    if (whole) {
+        w = *(const u32_any*)p;
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -155,20 +153,22 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __re
     for (int j = 0; j < 8; ++j) v[j] = e2m1_value(w >> (4 * j)) * s;
     const size_t at = r * ld + i0;
     if constexpr (DT == DT_F32) {
-        if (VEC) {
-            ((float4*)((float*)out + at))[0] = float4{v[0], v[1], v[2], v[3]};
-            ((float4*)((float*)out + at))[1] = float4{v[4], v[5], v[6], v[7]};
+        if (whole) {
+            u32x4_any* o = (u32x4_any*)((float*)out + at);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                o[j] = u32x4{__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])};
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (i0 + j < k) ((float*)out)[at + j] = v[j];
         }
     } else {
-        if (VEC) {
+        if (whole) {
             u32x4 o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = (uint32_t)to_half_bits(v[2 * j], DT) | (uint32_t)to_half_bits(v[2 * j + 1], DT) << 16;
-            *(u32x4*)((uint16_t*)out + at) = o;
+            *(u32x4_any*)((uint16_t*)out + at) = o;
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -182,12 +182,10 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, in
     const int chunks = (k + 7) / 8;
     const size_t n = (size_t)m * chunks;
     const dim3 g((unsigned)((n + 255) / 256)), b(256);
-    const size_t es = dt == DT_F32 ? 4 : 2;
-    const bool vec = k % 8 == 0 && ((uintptr_t)out & 15) == 0 && (m == 1 || (size_t)ld * es % 16 == 0) && ((uintptr_t)codes & 3) == 0;
-#define MX4_D(DT, VEC) mx4_dequantize_kernel<DT, VEC><<<g, b, 0, st>>>(codes, scales, m, k, chunks, out, (size_t)ld)
-    if (dt == DT_F32) vec ? MX4_D(DT_F32, true) : MX4_D(DT_F32, false);
-    else if (dt == DT_F16) vec ? MX4_D(DT_F16, true) : MX4_D(DT_F16, false);
-    else vec ? MX4_D(DT_BF16, true) : MX4_D(DT_BF16, false);
+#define MX4_D(DT) mx4_dequantize_kernel<DT><<<g, b, 0, st>>>(codes, scales, m, k, chunks, out, (size_t)ld)
+    if (dt == DT_F32) MX4_D(DT_F32);
+    else if (dt == DT_F16) MX4_D(DT_F16);
+    else MX4_D(DT_BF16);
 #undef MX4_D
     return hipGetLastError();
 }
@@ -228,15 +226,15 @@ hipError_t launch_mx4_pack(const uint8_t* codes, const uint8_t* scales, const Mx
 
 // ------------------------------------------------------------------ activations
 
-// Values at .. at + 15 of x, zero from `left` on.  vec: at is a multiple of 16 bytes into x.
+// Values at .. at + 15 of x, zero from `left` on.
 template <int DT>
-__device__ __forceinline__ void load16(const void* x, int vec, size_t at, int left, float (&v)[16]) {
+__device__ __forceinline__ void load16(const void* x, size_t at, int left, float (&v)[16]) {
     if constexpr (DT == DT_F32) {
         const float* f = (const float*)x + at;
-        if (vec && left >= 16) {
+        if (left >= 16) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const u32x4 a = ((const u32x4*)f)[q];
+                const u32x4 a = ((const u32x4_any*)f)[q];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[4 * q + j] = __uint_as_float(a[j]);
             }
@@ -247,9 +245,9 @@ __device__ __forceinline__ void load16(const void* x, int vec, size_t at, int le
     } else {
         const uint16_t* f = (const uint16_t*)x + at;
         u32x4 a[2];
-        if (vec && left >= 16) {
-            a[0] = ((const u32x4*)f)[0];
-            a[1] = ((const u32x4*)f)[1];
+        if (left >= 16) {
+            a[0] = ((const u32x4_any*)f)[0];
+            a[1] = ((const u32x4_any*)f)[1];
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -297,14 +295,14 @@ __device__ __forceinline__ uint32_t top16(const float (&v)[16]) {
 // steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
 // m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).
 template <int T, int DT>
-__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, int vec, size_t ld, int m, int k, int steps,
+__global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, size_t ld, int m, int k, int steps,
                                                        uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1;
     const int p = threadIdx.x & 3;                                 // quarter of the step of 64
     const int s = 2 * blockIdx.x + (threadIdx.x >> 7), row = 32 * blockIdx.y + ((threadIdx.x >> 2) & 31);
     const int k0 = 64 * s + 16 * p;
     float v[16];
-    load16<DT>(x, vec, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
+    load16<DT>(x, (size_t)row * ld + k0, row < m ? k - k0 : 0, v);
     uint32_t top = top16(v);
     top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
     const size_t tile = row >> 5;
@@ -344,9 +342,8 @@ __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ 
 }
 
 hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, int m, int k, hipStream_t st) {
-    const int vec = ((uintptr_t)x & 15) == 0 && (m == 1 || (size_t)ld * (dt == DT_F32 ? 4 : 2) % 16 == 0);
     const dim3 g((unsigned)(a.steps / 2), (unsigned)a.tiles), b(256);
-#define MX4_PREP(T, DT) mx4_prep_kernel<T, DT><<<g, b, 0, st>>>(x, vec, (size_t)ld, m, k, a.steps, a.a, a.s)
+#define MX4_PREP(T, DT) mx4_prep_kernel<T, DT><<<g, b, 0, st>>>(x, (size_t)ld, m, k, a.steps, a.a, a.s)
     switch (a.terms * 4 + dt) {
         case DT_F32: MX4_PREP(0, DT_F32); break;
         case DT_F16: MX4_PREP(0, DT_F16); break;
@@ -364,24 +361,18 @@ hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, i
 
 // Outputs of row `row` at p.out: columns col (even) and col + 1, as far as they exist.
 template <int DT>
-__device__ __forceinline__ void store_pair(const Mx4Gemm& p, int row, int col, bool fast, float a, float b) {
+__device__ __forceinline__ void store_pair(const Mx4Gemm& p, int row, int col, float a, float b) {
     const size_t at = (size_t)row * p.ld + col;
     if constexpr (DT == DT_F32) {
         float* o = (float*)p.out + at;
-        if (fast) *(float2*)o = float2{a, b};
-        else {
-            o[0] = a;
-            if (col + 1 < p.w.n) o[1] = b;
-        }
+        if (col + 1 < p.w.n) *(u32x2_any*)o = u32x2{__float_as_uint(a), __float_as_uint(b)};
+        else o[0] = a;
     } else {
         typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
         uint16_t* o = (uint16_t*)p.out + at;
         const uint32_t h = DT == DT_BF16 ? __builtin_bit_cast(uint32_t, bf2{(__bf16)a, (__bf16)b}) : pack_f16x2(a, b);
-        if (fast) *(uint32_t*)o = h;
-        else {
-            o[0] = (uint16_t)h;
-            if (col + 1 < p.w.n) o[1] = (uint16_t)(h >> 16);
-        }
+        if (col + 1 < p.w.n) *(u32_any*)o = h;
+        else o[0] = (uint16_t)h;
     }
 }
 
@@ -402,7 +393,6 @@ template <int MT>
 __device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, const v16f (&acc)[MT][2]) {
     const int lane = threadIdx.x & 63;
     const int col = 64 * g + 2 * (lane & 31);
-    const bool fast = p.pairs && col + 1 < p.w.n;
     auto each = [&](auto put) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
@@ -416,9 +406,9 @@ __device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, co
         float* part = p.part + (size_t)blockIdx.z * p.m * p.part_ld + col;
         each([&](int row, float a, float b) { *(float2*)(part + (size_t)row * p.part_ld) = float2{a, b}; });
     } else if (col < p.w.n) {
-        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, fast, a, b); });
-        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, fast, a, b); });
-        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, fast, a, b); });
+        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, a, b); });
+        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, a, b); });
+        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, a, b); });
     }
 }
 
@@ -691,7 +681,7 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
 // prepared once instead (mx4_rows_direct).
 constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
-__global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, int vec, size_t ldx, int seg) {
+__global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, size_t ldx, int seg) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
     typedef float v4f __attribute__((ext_vector_type(4)));
     // fragments [chunk][term][half][block or quarter kb][row]; scales [chunk][term][row] words of 4 blocks; sums
@@ -727,7 +717,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, con
         for (int i = tid; i < m * 8 * n; i += 64 * ROW_WAVES) {    // 16 values; neighbours share a block
             const int q = i & 7, rc = i >> 3, row = rc / n, c = rc - row * n, k = k0 + 128 * c + 16 * q;
             float v[16];
-            load16<DT>(x, vec, (size_t)(row0 + row) * ldx + k, p.w.k - k, v);
+            load16<DT>(x, (size_t)(row0 + row) * ldx + k, p.w.k - k, v);
             uint32_t top = top16(v);
             top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));   // lane ^ 1
             const bool bad = top >= 0x7f800000u;
@@ -809,13 +799,12 @@ bool mx4_rows_direct(const Mx4Mat& w, int m) {
 }
 
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st) {
-    const int vec = ((uintptr_t)x & 15) == 0 && (p.m == 1 || (size_t)ldx * (dt == DT_F32 ? 4 : 2) % 16 == 0);
     const dim3 g((unsigned)(4 * p.w.groups), (unsigned)((p.m + 15) / 16)), b(64 * ROW_WAVES);
     // the longest segment of K that LDS holds, the same number of chunks for each wave
     const int per_k = (p.m < 16 ? p.m : 16) * (p.a.terms ? 2 * p.a.terms : 1);       // half bytes
     int seg = ROW_LDS * 2 / per_k / ROW_SEG * ROW_SEG;
     if (seg > 64 * p.w.steps) seg = 64 * p.w.steps;
-#define MX4_ROWS(T, DT) mx4_rows_kernel<T, DT><<<g, b, 0, st>>>(p, x, vec, (size_t)ldx, seg)
+#define MX4_ROWS(T, DT) mx4_rows_kernel<T, DT><<<g, b, 0, st>>>(p, x, (size_t)ldx, seg)
     switch (p.a.terms * 4 + dt) {
         case DT_F32: MX4_ROWS(0, DT_F32); break;
         case DT_F16: MX4_ROWS(0, DT_F16); break;
@@ -841,10 +830,9 @@ __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
         a += v.x;
         b += v.y;
     }
-    const bool fast = p.pairs && col + 1 < p.w.n;
-    if (p.dt == DT_F32) store_pair<DT_F32>(p, row, col, fast, a, b);
-    else if (p.dt == DT_F16) store_pair<DT_F16>(p, row, col, fast, a, b);
-    else store_pair<DT_BF16>(p, row, col, fast, a, b);
+    if (p.dt == DT_F32) store_pair<DT_F32>(p, row, col, a, b);
+    else if (p.dt == DT_F16) store_pair<DT_F16>(p, row, col, a, b);
+    else store_pair<DT_BF16>(p, row, col, a, b);
 }
 
 static hipError_t run_reduce(const Mx4Gemm& p, hipStream_t st) {

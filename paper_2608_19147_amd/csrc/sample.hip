@@ -107,20 +107,19 @@ struct RowBins {                      // the scaled logit of a row's tokens
 
 struct RowArgs {
     const void* logits; int dt; size_t base; int V;
-    int vec;                          // rows start on 16 bytes
 };
 
 // Keys of tokens i .. i + 7 (i a multiple of 8); 0 past the row's end.
 __device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)[8]) {
     float v[8];
-    if (r.vec && i + 8 <= r.V) {
+    if (i + 8 <= r.V) {
         if (r.dt == DT_F32) {
-            const u32x4* p = (const u32x4*)((const float*)r.logits + r.base + i);
+            const u32x4_any* p = (const u32x4_any*)((const float*)r.logits + r.base + i);
             const u32x4 a = p[0], b = p[1];
 #pragma unroll
             for (int j = 0; j < 4; ++j) { v[j] = __uint_as_float(a[j]); v[4 + j] = __uint_as_float(b[j]); }
         } else {
-            const u32x4 a = *(const u32x4*)((const uint16_t*)r.logits + r.base + i);
+            const u32x4 a = *(const u32x4_any*)((const uint16_t*)r.logits + r.base + i);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = half_bits_to_f32((uint16_t)(a[j >> 1] >> (16 * (j & 1))), r.dt);
         }
@@ -838,7 +837,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) 
     uint32_t* keys = all.keys;
     unsigned long long* list = all.list;
     const int row = blockIdx.x, tid = threadIdx.x;
-    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
     RowBins rb{a.rows[row].per_t, 0.0};
     const float u = row_u(a, row);
     if (tid == 0) sh.fill = 0u;
@@ -868,7 +867,7 @@ __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs 
     unsigned long long* bins = a.bins + (size_t)row * ns * SB_BINS;
     RowBins rb{a.rows[row].per_t, 0.0};
     {
-        const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+        const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
         // keys in registers: without them in LDS four workgroups share a CU
         uint32_t k[2][8], top = 0;
 #pragma unroll
@@ -987,7 +986,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a)
     RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
     const RowPlan& plan = ws->plan;
     if (!plan.top || plan.n > (unsigned)SB_CAP || !(plan.touched[slice >> 5] >> (slice & 31) & 1u)) return;
-    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
     load_slice(r, slice, keys, buf);
     take_tokens(plan, keys, slice, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
 }
@@ -1000,7 +999,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
     RowSpace* ws = (RowSpace*)(a.rows_ws + (size_t)row * SAMPLE_ROW_BYTES);
     const RowPlan plan = ws->plan;
     if (!plan.top) return draw_nothing(a, row);
-    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V, a.vec};
+    const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
 #pragma unroll
     for (int j = 0; j < SB_PER; ++j) {
         sh.cum[j * SB_THREADS + tid] = ws->cum[j * SB_THREADS + tid];

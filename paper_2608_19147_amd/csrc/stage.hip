@@ -638,7 +638,6 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         p.out = (uint8_t*)out + (size_t)m0 * ldo * ob;
         p.dt = odt;
         p.ld = (size_t)ldo;
-        p.pairs = ((uintptr_t)p.out & (2 * ob - 1)) == 0 && (mm == 1 || ldo % 2 == 0);
         p.split = mx4_split(w, a.terms, a.tiles, st->n_cus);
         const int unit = w.steps % 8 == 0 ? 8 : 4;
         p.steps_per = (w.steps / unit + p.split - 1) / p.split * unit;
@@ -679,8 +678,6 @@ int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, 
     a.token = token;
     a.p = p;
     a.top = top;
-    const size_t es = dt == DT_F32 ? 4 : 2;
-    a.vec = ((uintptr_t)logits & 15) == 0 && (M == 1 || (size_t)ld * es % 16 == 0);
     if (V > SAMPLE_SLICE) {
         a.slices = (V + SAMPLE_SLICE - 1) / SAMPLE_SLICE;
         int rc = grow(&st->smp, &st->smp_cap, sample_slice_bytes(a.slices));
