@@ -367,15 +367,17 @@ struct Mx4Gemm {
     Mx4Mat w; Mx4Act a;
     int m;
     void* out; int dt; size_t ld;
-    int split, steps_per;                          // splits of K, steps of each (a multiple of 4)
-    float* part; int part_ld;                      // split > 1: their sums [split][m][part_ld]
+    int mt, split, steps_per;                      // row tiles a workgroup; splits of K, steps of each (a multiple of 4)
+    float* part; int part_ld;                      // split > 1: their sums [split][32 a.tiles][part_ld]
     int mtiles;                                    // set by the launcher
 };
-// Splits of K that fill the device.
-int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus);
+// Sets mt, split and steps_per for p.w and p.a; the time that they should take, in us.
+float mx4_plan(Mx4Gemm& p, int n_cus);
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st);
-// A product of few rows that prepares them itself and needs no workspace (p.a: only terms).
-bool mx4_rows_direct(const Mx4Mat& w, int m);
+// A product of up to MX4_ROWS_MAX rows that prepares them itself and needs no workspace (p.a: only terms), and whether
+// that is the faster way.
+constexpr int MX4_ROWS_MAX = 64;
+bool mx4_rows_direct(const Mx4Gemm& p, int n_cus);
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st);
 // out [m][H] fp16 = RMSNorm(row) * gamma.
 hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st);

@@ -359,20 +359,36 @@ hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, i
 
 // ------------------------------------------------------------------ product
 
-// Outputs of row `row` at p.out: columns col (even) and col + 1, as far as they exist.
-template <int DT>
-__device__ __forceinline__ void store_pair(const Mx4Gemm& p, int row, int col, float a, float b) {
-    const size_t at = (size_t)row * p.ld + col;
+// Outputs v of row `row`, columns col .. col + N - 1 (N 4 or 8), as far as the n columns go.
+template <int DT, int N>
+__device__ __forceinline__ void store_run(void* out, size_t ld, int n, int row, int col, const float (&v)[N]) {
+    const size_t at = (size_t)row * ld + col;
     if constexpr (DT == DT_F32) {
-        float* o = (float*)p.out + at;
-        if (col + 1 < p.w.n) *(u32x2_any*)o = u32x2{__float_as_uint(a), __float_as_uint(b)};
-        else o[0] = a;
+        float* o = (float*)out + at;
+        if (col + N <= n) {
+#pragma unroll
+            for (int j = 0; j < N; j += 4)
+                *(u32x4_any*)(o + j) = u32x4{__float_as_uint(v[j]), __float_as_uint(v[j + 1]), __float_as_uint(v[j + 2]), __float_as_uint(v[j + 3])};
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (col + j < n) o[j] = v[j];
+        }
     } else {
         typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-        uint16_t* o = (uint16_t*)p.out + at;
-        const uint32_t h = DT == DT_BF16 ? __builtin_bit_cast(uint32_t, bf2{(__bf16)a, (__bf16)b}) : pack_f16x2(a, b);
-        if (col + 1 < p.w.n) *(u32_any*)o = h;
-        else o[0] = (uint16_t)h;
+        uint16_t* o = (uint16_t*)out + at;
+        uint32_t h[N / 2];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j)
+            h[j] = DT == DT_BF16 ? __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2 * j], (__bf16)v[2 * j + 1]}) : pack_f16x2(v[2 * j], v[2 * j + 1]);
+        if (col + N <= n) {
+            if constexpr (N == 8) *(u32x4_any*)o = u32x4{h[0], h[1], h[2], h[3]};
+            else *(u32x2_any*)o = u32x2{h[0], h[1]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (col + j < n) o[j] = (uint16_t)(h[j / 2] >> (16 * (j & 1)));
+        }
     }
 }
 
@@ -388,27 +404,95 @@ __device__ __forceinline__ v16f mx4_mfma(v8i a, v8i b, v16f c, int step, uint32_
 }
 
 // The outputs of a wave: MT row tiles from mt0, group g.  Lane l holds outputs
-// 64 g + 2 (l mod 32) + j of rows 8 (r / 4) + 4 (l / 32) + r mod 4.
-template <int MT>
-__device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, const v16f (&acc)[MT][2]) {
-    const int lane = threadIdx.x & 63;
-    const int col = 64 * g + 2 * (lane & 31);
-    auto each = [&](auto put) {
+// 64 g + 2 (l mod 32) + j of rows 8 (r / 4) + 4 (l / 32) + r mod 4.  Sums of a split
+// go straight to their rows, which are whole tiles, a group's even outputs ahead of
+// its odd ones (as pairs they would have to be moved to neighbouring registers first).
+// Results go through LDS of the wave's own, two tiles at a time, so that short loops
+// store their rows, 16 or 32 bytes a lane: stores straight from the registers were
+// 20 KB of instructions for MT = 8, and fetching them took most of 12 us a workgroup.
+constexpr int STORE_LD = 72;                                       // rows 4 apart lie in other banks
+constexpr int store_lds(int mt) { return 4 * (mt < 2 ? 1 : 2) * 32 * STORE_LD * 4; }
+// LDS accesses of a wave's lanes on either side keep their order (the unit takes a wave's in order).
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_rows(const float* buf, const Mx4Gemm& p, int row0, int rows, int col0) {
+    const int lane = threadIdx.x & 63, c = 8 * (lane & 7);
+    const bool whole = col0 + c + 8 <= p.w.n;
+#pragma unroll 1
+    for (int i0 = 0; i0 < rows; i0 += 32) {
+        float4 a[4], b[4];
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int q = 0; q < 4; ++q) {
+            const float* f = buf + (i0 + 8 * q + (lane >> 3)) * STORE_LD + c / 2;
+            a[q] = *(const float4*)f;
+            b[q] = *(const float4*)(f + 32);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int i = i0 + 8 * q + (lane >> 3);
+            const float v[8] = {a[q].x, b[q].x, a[q].y, b[q].y, a[q].z, b[q].z, a[q].w, b[q].w};
+            if (i >= rows) break;
+            if (whole) {
+                if constexpr (WIDE) store_run<DT_F32, 8>(p.out, p.ld, p.w.n, row0 + i, col0 + c, v);
+                else if (p.dt == DT_F16) store_run<DT_F16, 8>(p.out, p.ld, p.w.n, row0 + i, col0 + c, v);
+                else store_run<DT_BF16, 8>(p.out, p.ld, p.w.n, row0 + i, col0 + c, v);
+            }
+        }
+    }
+    if (whole) return;
+#pragma unroll 1
+    for (int i = lane >> 3; i < rows; i += 8)
+#pragma unroll 1
+        for (int j = c; col0 + j < p.w.n; ++j) {
+            const float f = buf[i * STORE_LD + (j & 1) * 32 + j / 2];
+            const size_t at = (size_t)(row0 + i) * p.ld + col0 + j;
+            if constexpr (WIDE) ((float*)p.out)[at] = f;
+            else ((uint16_t*)p.out)[at] = to_half_bits(f, p.dt);
+        }
+}
+template <int MT>
+__device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, const v16f (&acc)[MT][2], uint8_t* lds) {
+    constexpr int PASS = MT < 2 ? 1 : 2;
+    const int lane = threadIdx.x & 63;
+    const int tiles = min(MT, p.a.tiles - mt0);
+    if (p.split > 1) {
+        g = __builtin_amdgcn_readfirstlane(g);
+        float* part = p.part + ((size_t)blockIdx.z * p.a.tiles + mt0) * 32 * p.part_ld + 64 * g;
+        const uint32_t at = 4 * (lane >> 5) * p.part_ld + (lane & 31);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (t >= tiles) return;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = (mt0 + t) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-                if (row < p.m) put(row, acc[t][0][r], acc[t][1][r]);
+                float* o = part + (size_t)(32 * t + 8 * (r >> 2) + (r & 3)) * p.part_ld;
+                o[at] = acc[t][0][r];
+                o[at + 32] = acc[t][1][r];
             }
-    };
-    if (p.split > 1) {
-        float* part = p.part + (size_t)blockIdx.z * p.m * p.part_ld + col;
-        each([&](int row, float a, float b) { *(float2*)(part + (size_t)row * p.part_ld) = float2{a, b}; });
-    } else if (col < p.w.n) {
-        if (p.dt == DT_F32) each([&](int row, float a, float b) { store_pair<DT_F32>(p, row, col, a, b); });
-        else if (p.dt == DT_F16) each([&](int row, float a, float b) { store_pair<DT_F16>(p, row, col, a, b); });
-        else each([&](int row, float a, float b) { store_pair<DT_BF16>(p, row, col, a, b); });
+        }
+        return;
+    }
+    float* buf = (float*)lds + PASS * 32 * STORE_LD * (threadIdx.x >> 6);
+    float* own = buf + 4 * (lane >> 5) * STORE_LD + (lane & 31);
+#pragma unroll
+    for (int t0 = 0; t0 < MT; t0 += PASS) {
+        if (t0 >= tiles) return;
+#pragma unroll
+        for (int t = t0; t < t0 + PASS; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float* o = own + ((t - t0) * 32 + 8 * (r >> 2) + (r & 3)) * STORE_LD;
+                o[0] = acc[t][0][r];
+                o[32] = acc[t][1][r];
+            }
+        wave_lds_order();
+        const int row0 = (mt0 + t0) * 32, rows = min(32 * PASS, p.m - row0);
+        if (p.dt == DT_F32) store_rows<true>(buf, p, row0, rows, 64 * g);
+        else store_rows<false>(buf, p, row0, rows, 64 * g);
+        wave_lds_order();
     }
 }
 
@@ -461,7 +545,7 @@ __device__ __forceinline__ int xcd_run(int bid, int nwg) {
 // buffered; W's go from memory to the registers that the product reads, each
 // used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.
 //
-// split > 1: fp32 sums to part [split][m][n], joined by mx4_reduce_kernel.
+// split > 1: fp32 sums to part [split][tiles of 32 rows][n], joined by mx4_reduce_kernel.
 template <int T, int MT, int KS>
 __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
@@ -557,8 +641,9 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
                 for (int j = 0; j < 2; ++j) wr[0][i][j] = wr[1][i][j];
         }
     }
+    __syncthreads();                                               // the buffers are read
     if (off) return;
-    store_tiles<MT>(p, mt0, g, acc);
+    store_tiles<MT>(p, mt0, g, acc, smem);
 }
 
 // The same product for many rows, where the matrix cores are to be the bound.
@@ -583,7 +668,9 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
     constexpr int AHEAD = 3, RING = AHEAD + 1;                     // fragments read before their products
     constexpr int QUADS = D / 4, OPEN = FRAGS - AHEAD;             // OPEN: the fragment before whose products the barrier stands
     static_assert(PIECES % 4 == 0 && D % 4 == 0 && FRAGS % RING == 0 && PW <= OPEN && PW + 2 <= FRAGS, "rings");
-    __shared__ u32x4 lds[2][PIECES * 64];
+    constexpr int BUF = PIECES * 1024;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * BUF > store_lds(MT) ? 2 * BUF : store_lds(MT)];
+    u32x4* const lds[2] = {(u32x4*)smem, (u32x4*)(smem + BUF)};
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int bid = xcd_run(blockIdx.x, gridDim.x);
     const int mt0 = (bid % p.mtiles) * MT;
@@ -666,8 +753,9 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
                 for (int n = 0; n < NT; ++n) as[0][t][n] = asn[t][n];
         }
     }
+    __syncthreads();                                               // the buffers are read
     if (off) return;
-    store_tiles<MT>(p, mt0, g, acc);
+    store_tiles<MT>(p, mt0, g, acc, smem);
 }
 
 // Few rows of x, in one launch and without a workspace: 16 of them by 16 outputs a
@@ -678,7 +766,7 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
 // Bound by the latency of one read after a launch and by fetching the code, so
 // there is one copy of the conversion; where many outputs or long rows make the
 // terms that every workgroup makes for itself the larger part, the rows are
-// prepared once instead (mx4_rows_direct).
+// prepared once instead (mx4_rows_direct below).
 constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
 __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, size_t ldx, int seg) {
@@ -790,14 +878,6 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, con
     }
 }
 
-// One launch for a few rows, where making the terms in every workgroup costs less than a launch that prepares them
-// (3-4 us, and its event): one tile of 16 rows up to 16384 outputs; up to four of at most 2048 columns, while the
-// workgroups are at most four a CU.
-bool mx4_rows_direct(const Mx4Mat& w, int m) {
-    const int tiles = (m + 15) / 16;
-    return tiles == 1 ? w.groups <= 256 : tiles <= 4 && w.k <= 2048 && w.groups * tiles <= 256;
-}
-
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st) {
     const dim3 g((unsigned)(4 * p.w.groups), (unsigned)((p.m + 15) / 16)), b(64 * ROW_WAVES);
     // the longest segment of K that LDS holds, the same number of chunks for each wave
@@ -818,25 +898,38 @@ hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx,
     return hipGetLastError();
 }
 
-// out = the sum of the splits, in their order.
+// out = the sum of the splits, in their order: four outputs a thread, and eight
+// splits' on their way at a time (other XCDs wrote them: a read takes over a us).
 __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
-    const int pairs = (p.w.n + 1) / 2;
+    const int quads = (p.w.n + 3) / 4;
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
-    if (idx >= (size_t)p.m * pairs) return;
-    const int row = (int)(idx / pairs), col = 2 * (int)(idx % pairs);
-    float a = 0.0f, b = 0.0f;
-    for (int z = 0; z < p.split; ++z) {
-        const float2 v = *(const float2*)(p.part + ((size_t)z * p.m + row) * p.part_ld + col);
-        a += v.x;
-        b += v.y;
+    if (idx >= (size_t)p.m * quads) return;
+    const int row = (int)(idx / quads), col = 4 * (int)(idx % quads);
+    // two of a group's even outputs and two of its odd ones
+    const float2* part = (const float2*)(p.part + (size_t)row * p.part_ld + (col & ~63) + (col & 63) / 2);
+    const size_t step = (size_t)p.a.tiles * 16 * p.part_ld;        // a split's rows are whole tiles
+    float v[4] = {};
+    for (int z0 = 0; z0 < p.split; z0 += 8) {
+        float2 a[8], b[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const float2* at = part + (size_t)min(z0 + z, p.split - 1) * step;
+            a[z] = at[0];
+            b[z] = at[16];
+        }
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            if (z0 + z >= p.split) break;
+            v[0] += a[z].x; v[1] += b[z].x; v[2] += a[z].y; v[3] += b[z].y;
+        }
     }
-    if (p.dt == DT_F32) store_pair<DT_F32>(p, row, col, a, b);
-    else if (p.dt == DT_F16) store_pair<DT_F16>(p, row, col, a, b);
-    else store_pair<DT_BF16>(p, row, col, a, b);
+    if (p.dt == DT_F32) store_run<DT_F32, 4>(p.out, p.ld, p.w.n, row, col, v);
+    else if (p.dt == DT_F16) store_run<DT_F16, 4>(p.out, p.ld, p.w.n, row, col, v);
+    else store_run<DT_BF16, 4>(p.out, p.ld, p.w.n, row, col, v);
 }
 
 static hipError_t run_reduce(const Mx4Gemm& p, hipStream_t st) {
-    const size_t n = (size_t)p.m * ((p.w.n + 1) / 2);
+    const size_t n = (size_t)p.m * ((p.w.n + 3) / 4);
     mx4_reduce_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(p);
     return hipGetLastError();
 }
@@ -845,7 +938,7 @@ template <int T, int MT, int KS>
 hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
     p.mtiles = (p.a.tiles + MT - 1) / MT;
     const int ntiles = (p.w.groups + 3) / 4;
-    constexpr int LDS = 2 * MT * KS * (T ? 2 * T : 1) * 1024;
+    constexpr int BUFS = 2 * MT * KS * (T ? 2 * T : 1) * 1024, LDS = BUFS > store_lds(MT) ? BUFS : store_lds(MT);
     hipError_t e = hipSuccess;
     if (LDS > 65536) e = hipFuncSetAttribute((const void*)mx4_gemm_kernel<T, MT, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return e;
@@ -863,29 +956,71 @@ hipError_t run_pipe(Mx4Gemm p, hipStream_t st) {
     return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
 }
 
-// Row tiles of 32 that a workgroup takes.
-static int gemm_mt(int terms, int tiles) { return tiles >= 5 ? (terms ? 4 : 8) : tiles >= 3 ? 4 : tiles; }
+// Row tiles of 32 a workgroup (MT) and splits of K: the pair of least time by what
+// the parts cost, measured from 16 x 4096 x 4096 to 2048 x 28672 x 8192 (the picks are
+// within 1% of the best pair on average, 7% at worst).  A workgroup's step of 64 k
+// costs STEP (us), and a CU's workgroups take turns: larger tiles read less per
+// product, so they win once every CU has work (2048 x 4096 x 4096: 75, 65 and 60 us
+// with MT 1, 2 and 4).  START is what a tile's code and stores add, which is why small
+// products take small tiles (300 x 300 x 300 with 4-bit rows: 13, 15, 21 and 32 us with
+// MT 1, 2, 4 and 8); from MT 4 on a CU holds one workgroup and each round pays it.
+// Splits cost a launch and their sums' way to memory and back (33 x 256 x 14336: 64 us
+// unsplit, 20 in 16 splits; 700 x 2048 x 700: 15 and 21 in two).
+float mx4_plan(Mx4Gemm& p, int n_cus) {
+    constexpr int MTS[4] = {1, 2, 4, 8};
+    constexpr float START[4] = {0.0f, 1.8f, 6.5f, 15.0f};
+    constexpr float STEP[3][4] = {{0.15f, 0.185f, 0.25f, 0.36f}, {0.25f, 0.40f, 0.52f, 0.0f}, {0.35f, 0.55f, 0.75f, 0.0f}};   // terms 0, 2, 3
+    constexpr float BASE = 11.0f, JOIN = 4.0f, RATE = 7e6f;        // launches; the sums' launch; bytes a us
+    constexpr int MAX_SPLIT = 24;
+    const int unit = p.w.steps % 8 == 0 ? 8 : 4, units = p.w.steps / unit;
+    const float* step = STEP[p.a.terms ? p.a.terms - 1 : 0];
+    const float sums = (float)p.a.tiles * 32.0f * (float)p.w.groups * 64.0f * 8.0f / RATE;
+    float least = 3.4e38f;
+    for (int i = 0; i < (p.a.terms || unit == 4 ? 3 : 4); ++i) {   // MT 8 has the long form only
+        const float wgs = (float)((p.a.tiles + MTS[i] - 1) / MTS[i]) * (float)((p.w.groups + 3) / 4);
+        for (int s = 1; s <= MAX_SPLIT && s <= units; ++s) {
+            const int per = (units + s - 1) / s, split = (units + per - 1) / per;
+            if (split != s) continue;
+            const float rounds = fmaxf(1.0f, ceilf(wgs * (float)s / (float)n_cus));
+            const float us = BASE + rounds * (float)(per * unit) * step[i] + (MTS[i] >= 4 ? rounds : 1.0f) * START[i] + (s > 1 ? JOIN + (float)s * sums : 0.0f);
+            if (us < least) {
+                least = us;
+                p.mt = MTS[i];
+                p.split = s;
+                p.steps_per = per * unit;
+            }
+        }
+    }
+    return least;
+}
 
-// Splits of K: enough workgroups for every CU, at least 4 rounds of 256 k each.
-int mx4_split(const Mx4Mat& w, int terms, int tiles, int n_cus) {
-    const int mt = gemm_mt(terms, tiles), wgs = (tiles + mt - 1) / mt * ((w.groups + 3) / 4), rounds = w.steps / 4;
-    int split = 1;
-    while (wgs * (split + 1) <= n_cus && rounds / (split + 1) >= 2) ++split;
-    return split;
+// Whether up to 64 rows go through mx4_rows_kernel: its workgroups share CUs, each
+// makes the terms of 16 rows for itself (TERMS, us for 1000 values) after START, and
+// reads weights.  16 x 4096 x 4096 in two terms: 14.5 us so, 17 through the plan's three
+// launches; 16 x 14336 x 4096: 40 and 19; one row of 14336 x 14336: 26 and 30.
+bool mx4_rows_direct(const Mx4Gemm& rows, int n_cus) {
+    constexpr float BASE = 6.0f, SHARE = 0.65f, RATE = 16e6f;
+    constexpr float START[3] = {0.8f, 1.0f, 2.0f}, TERMS[3] = {0.06f, 0.15f, 0.21f};
+    Mx4Gemm p = rows;
+    if (p.m > MX4_ROWS_MAX) return false;
+    const int t = p.a.terms ? p.a.terms - 1 : 0;
+    const float wgs = 4.0f * (float)p.w.groups * (float)((p.m + 15) / 16);
+    const float own = START[t] + TERMS[t] * (float)(p.m < 16 ? p.m : 16) * (float)p.w.k * 1e-3f;
+    const float us = BASE + fmaxf(1.0f, SHARE * wgs / (float)n_cus) * own + (float)p.w.n * (float)p.w.k * 0.53f / RATE;
+    p.a.tiles = (p.m + 31) / 32;
+    return us < mx4_plan(p, n_cus);
 }
 
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
-    const int mt = gemm_mt(p.a.terms, p.a.tiles);
-    if (p.steps_per % 8 == 0 && p.w.steps % 8 == 0) switch (p.a.terms * 10 + mt) {
+    if (p.steps_per % 8 == 0 && p.w.steps % 8 == 0) switch (p.a.terms * 10 + p.mt) {
         case 8: return run_pipe<0, 8, 8>(p, st);
         case 24: return run_pipe<2, 4, 4>(p, st);
         case 34: return run_pipe<3, 4, 4>(p, st);
     }
-    switch (p.a.terms * 10 + mt) {
+    switch (p.a.terms * 10 + p.mt) {
         case 1: return run_gemm<0, 1, 4>(p, st);
         case 2: return run_gemm<0, 2, 4>(p, st);
         case 4: return run_gemm<0, 4, 4>(p, st);
-        case 8: return run_gemm<0, 8, 2>(p, st);
         case 21: return run_gemm<2, 1, 4>(p, st);
         case 22: return run_gemm<2, 2, 2>(p, st);
         case 24: return run_gemm<2, 4, 2>(p, st);

@@ -538,10 +538,16 @@ int guarded(F f) noexcept {
 }
 
 // A call that uses the stage's workspace cannot be captured: a replay would not be ordered with the stage's other calls.
-int not_captured(hipStream_t s) {
+int captured(hipStream_t s, bool& yes) {
     hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
     HIP_TRY(hipStreamIsCapturing(s, &c));
-    return c == hipStreamCaptureStatusNone ? STAGE_OK : fail(STAGE_E_UNSUPPORTED, "this call cannot be captured into a graph");
+    yes = c != hipStreamCaptureStatusNone;
+    return STAGE_OK;
+}
+int not_captured(hipStream_t s) {
+    bool yes = false;
+    const int rc = captured(s, yes);
+    return rc ? rc : yes ? fail(STAGE_E_UNSUPPORTED, "this call cannot be captured into a graph") : STAGE_OK;
 }
 
 bool dtype_ok(int dt) { return dt == STAGE_DTYPE_F32 || dt == STAGE_DTYPE_F16 || dt == STAGE_DTYPE_BF16; }
@@ -638,13 +644,10 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         p.out = (uint8_t*)out + (size_t)m0 * ldo * ob;
         p.dt = odt;
         p.ld = (size_t)ldo;
-        p.split = mx4_split(w, a.terms, a.tiles, st->n_cus);
-        const int unit = w.steps % 8 == 0 ? 8 : 4;
-        p.steps_per = (w.steps / unit + p.split - 1) / p.split * unit;
-        p.split = (w.steps + p.steps_per - 1) / p.steps_per;
+        mx4_plan(p, st->n_cus);
         p.part_ld = 64 * w.groups;
         if (p.split > 1) {
-            if ((rc = grow(&st->mx_p, &st->mx_p_cap, (size_t)p.split * mm * p.part_ld * 4))) return rc;
+            if ((rc = grow(&st->mx_p, &st->mx_p_cap, (size_t)p.split * a.tiles * 32 * p.part_ld * 4))) return rc;
             p.part = (float*)st->mx_p;
         }
         HIP_TRY(launch_mx4_gemm(p, s));
@@ -1670,21 +1673,25 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
-        if (mx4_rows_direct(w->m, m)) {                    // no workspace: nothing to order
-            Mx4Gemm p{};
-            p.w = w->m;
-            p.a.terms = mx4_terms(any_dt(x_dtype), act_bits, any_dt(out_dtype));
-            p.m = m;
-            p.out = out;
-            p.dt = any_dt(out_dtype);
-            p.ld = (size_t)ldo;
+        Mx4Gemm p{};
+        p.w = w->m;
+        p.a.terms = mx4_terms(any_dt(x_dtype), act_bits, any_dt(out_dtype));
+        p.m = m;
+        p.out = out;
+        p.dt = any_dt(out_dtype);
+        p.ld = (size_t)ldo;
+        // few rows need no workspace: nothing to order, and a graph can hold them
+        bool direct = mx4_rows_direct(p, st->n_cus), graph = false;
+        if (!direct) {
+            if (int rc = captured(s, graph)) return rc;
+            if (graph && m > MX4_ROWS_MAX) return not_captured(s);
+        }
+        if (direct || graph) {
             HIP_TRY(launch_mx4_rows(p, x, any_dt(x_dtype), ldx, s));
             return STAGE_OK;
         }
-        int rc = not_captured(s);
-        if (rc) return rc;
         HIP_TRY(order_on(st, s));
-        rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s);
+        int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s);
         if (rc) return rc;
         HIP_TRY(mark_done(st, s));
         return STAGE_OK;

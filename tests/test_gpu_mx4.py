@@ -166,6 +166,66 @@ def test_product_large(stage, m, n, k, dtype, act, out):
     _check_product(stage, m, n, k, dtype, act, out)
 
 
+# Row tiles of every size, K whole and split, with the short and the long form of the loop.
+TILES = {"bf16": [(1521, 20251, 65), (1459, 64, 14310), (237, 24956, 1092), (132, 26514, 2033), (1160, 1679, 4147)],
+         "f16": [(622, 24412, 66), (1755, 68, 9007), (131, 27946, 1752), (651, 9662, 796), (1672, 261, 10981)],
+         "4 bits": [(1526, 9690, 65), (1157, 118, 13128), (568, 7255, 2176), (76, 11101, 12573), (1803, 7009, 2326)]}
+
+
+@pytest.mark.parametrize("kind,m,n,k", [(kind, *size) for kind, sizes in TILES.items() for size in sizes])
+def test_product_tiles(stage, kind, m, n, k):
+    """Every output against 64 bits, on the device for its speed; rows of x and of the result inside wider ones."""
+    act, dtype, out = (4, torch.bfloat16, torch.bfloat16) if kind == "4 bits" else (16, DT[kind], DT[kind])
+    g = torch.Generator(device="cuda").manual_seed(m * 7 + k)
+    nb = -(-k // BLOCK)
+    codes = torch.randint(0, 16, (n, k), device="cuda", generator=g, dtype=torch.uint8)
+    scales = torch.randint(110, 124, (n, nb), device="cuda", generator=g, dtype=torch.uint8)
+    even = torch.nn.functional.pad(codes, (0, k % 2))
+    mat = stage.mx4_matrix(even[:, 0::2] | even[:, 1::2] << 4, scales, k)
+    x = (torch.randn((m, k + 3), device="cuda", generator=g) * torch.exp2(torch.randint(-3, 4, (m, k + 3), device="cuda", generator=g))).to(dtype)
+    x = x[:, :k]
+    got = mat.product(x, act, out).double()
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device="cuda")
+    w = torch.cat([grid, -grid])[codes.int()] * torch.exp2(scales.double() - 127).repeat_interleave(BLOCK, 1)[:, :k]
+    xd = x.double() if act == 16 else stage.mx4_dequantize(*stage.mx4_quantize(x), k, torch.float32).double()
+    top = torch.nn.functional.pad(xd.abs(), (0, nb * BLOCK - k)).view(m, nb, BLOCK).amax(2).repeat_interleave(BLOCK, 1)[:, :k]
+    terms, left = {"bf16": (2, 2.0 ** -14), "f16": (3, 2.0 ** -18), "4 bits": (1, 0.0)}[kind]
+    wt = w.t().contiguous()
+    ref = xd @ wt
+    tol = (left * top + 2.0 ** -23 * (terms * k / 8 + 8) * xd.abs()) @ wt.abs_()
+    f = torch.finfo(out)
+    tol += (ref.abs() + tol) * (f.eps / 2) + f.tiny * f.eps / 2
+    worst = float(((got - ref).abs() / tol).max())
+    print(f"{kind} m {m} n {n} k {k}: worst error {worst:.3f} of the tolerance")
+    assert worst <= 1.0
+    mat.free()
+
+
+@pytest.mark.parametrize("m", [20, 64])
+def test_capture_without_workspace(stage, m):
+    """Up to 64 rows are captured also where an eager call takes the stage's workspace, and need none of it on replay."""
+    n, k = 4200, 4100
+    codes, scales = _weights(n, k, 23)
+    mat = stage.mx4_matrix(torch.from_numpy(mx4_pack(codes)), torch.from_numpy(scales), k)
+    x = _rows(m, k, 24, "bf16").cuda()
+    mat.product(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o = mat.product(x)
+    for i in range(3):
+        new = _rows(m, k, 25 + i, "bf16")
+        x.copy_(new)
+        eager = mat.product(x).double().cpu().numpy()
+        g.replay()
+        mat.product(x.flip(0))
+        torch.cuda.synchronize()
+        ref, tol = _product(new, codes, scales, 16, torch.bfloat16)
+        assert (np.abs(o.double().cpu().numpy() - ref) <= tol).all()
+        assert (np.abs(eager - ref) <= tol).all()
+    mat.free()
+
+
 def test_product_passes(stage):
     """More rows than one pass takes: rows of the second pass equal the same rows on their own."""
     codes, scales = _weights(96, 160, 9)
