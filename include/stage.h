@@ -357,7 +357,7 @@ int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out,
  * Tensors are device memory unless said otherwise; row strides `ld` count
  * elements and may exceed the row length; no alignment beyond the element's is
  * needed.  stage_mx4_quantize, stage_mx4_dequantize, stage_tree_accept, and
- * stage_sample of up to 8192 tokens use no memory of the stage: calls on
+ * stage_sample of up to 24576 tokens use no memory of the stage: calls on
  * different streams are independent and may be captured into a graph.  The other
  * calls use the stage's workspace, are ordered with the stage's calls like a forward
  * and refuse a capturing stream (STAGE_E_UNSUPPORTED), but for stage_mx4_product of
@@ -438,7 +438,7 @@ typedef struct StageSampling {
  * [M]; u: device fp32 [M] in [0, 1) (values outside are taken as the nearest
  * inside).  A row without a ranked token gives token -1 and p 0.
  * 1 <= M <= STAGE_MAX_ROWS.  The result does not depend on the other rows.
- * Allocates a workspace on first use above 8192 tokens (kept, grown when a larger
+ * Allocates a workspace on first use above 24576 tokens (kept, grown when a larger
  * vocabulary comes).
  * Errors: INVALID (NULL, dtype, params), SHAPE (vocab, ld), CAPACITY (M, vocab),
  * UNSUPPORTED (capturing stream), OOM, HIP. */

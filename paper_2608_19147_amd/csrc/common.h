@@ -388,6 +388,7 @@ struct SampleRow {
     int top_k; float top_p, min_p;
 };
 constexpr int SAMPLE_SLICE = 8192;                 // tokens one workgroup counts
+constexpr int SAMPLE_SMALL = 3 * SAMPLE_SLICE;     // tokens of a row that one workgroup holds in LDS
 constexpr int SAMPLE_MAX_SLICES = 128;             // 2^20 tokens
 constexpr size_t SAMPLE_ROW_BYTES = 46080;         // workspace of a row (RowSpace)
 struct SampleArgs {

@@ -152,15 +152,15 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* buf) {
     return t;
 }
 
-// The keys of a slice into LDS, in the order of the tokens; the largest one.
-// (Loops over a thread's 16 tokens stay loops: a workgroup runs this code once,
-// and fetching instructions costs it about 0.9 us a kilobyte.)
-__device__ __forceinline__ uint32_t load_slice(const RowArgs& r, int slice, uint32_t* keys, uint32_t* buf) {
+// The keys of n tokens into LDS, from token `first` on in their order, and 0 up to
+// the next multiple of SB_THREADS; the largest one.  (Loops over a thread's tokens stay loops: a workgroup
+// runs this code once, and fetching instructions costs it about 0.9 us a kilobyte.)
+__device__ __forceinline__ uint32_t load_tokens(const RowArgs& r, int first, int n, uint32_t* keys, uint32_t* buf) {
     uint32_t top = 0;
 #pragma unroll 1
-    for (int i = threadIdx.x * 8; i < SL_LEN; i += SB_THREADS * 8) {
+    for (int i = threadIdx.x * 8; i < (n + SB_THREADS - 1) / SB_THREADS * SB_THREADS; i += SB_THREADS * 8) {
         uint32_t k[8];
-        load_keys(r, slice * SL_LEN + i, k);
+        load_keys(r, first + i, k);
         *(u32x4*)(keys + i) = u32x4{k[0], k[1], k[2], k[3]};
         *(u32x4*)(keys + i + 4) = u32x4{k[4], k[5], k[6], k[7]};
 #pragma unroll
@@ -174,13 +174,13 @@ __device__ __forceinline__ void count_key(uint32_t k, const RowBins& rb, unsigne
     if (k && b < (double)SB_BINS) atomicAdd(&hist[(int)b], rb.units(x) << 14 | 1ull);
 }
 
-// hist[] of the slice's tokens, counted from rb.qmax.
-__device__ __forceinline__ void count_slice(const uint32_t* keys, const RowBins& rb, unsigned long long* hist) {
+// hist[] of the slice's n tokens, counted from rb.qmax.
+__device__ __forceinline__ void count_slice(const uint32_t* keys, int n, const RowBins& rb, unsigned long long* hist) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < SB_BINS; i += SB_THREADS) hist[i] = 0ull;
     __syncthreads();
-#pragma unroll 2
-    for (int i = threadIdx.x; i < SL_LEN; i += SB_THREADS) count_key(keys[i], rb, hist);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += SB_THREADS) count_key(keys[i], rb, hist);
     __syncthreads();
 }
 
@@ -692,14 +692,14 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
     return pl;
 }
 
-// The slice's tokens of the plan's runs go into the list; a wave asks once for
-// their places.
+// The slice's tokens (n of them) of the plan's runs go into the list; a wave asks
+// once for their places.
 template <class Put>
-__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* keys, int slice, unsigned* fill, Put put) {
+__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* keys, int slice, int n, unsigned* fill, Put put) {
     const int tid = threadIdx.x;
     unsigned m = 0;
 #pragma unroll 2
-    for (int i = 0; i < SL_LEN / SB_THREADS; ++i) {
+    for (int i = 0; i < (n + SB_THREADS - 1) / SB_THREADS; ++i) {
         const uint32_t k = keys[i * SB_THREADS + tid];
         bool in = false;
 #pragma unroll
@@ -824,36 +824,46 @@ __device__ __forceinline__ void draw_nothing(const SampleArgs& a, int row) {
 
 __device__ __forceinline__ float row_u(const SampleArgs& a, int row) { return a.u ? fminf(fmaxf(a.u[row], 0.0f), 0.99999994f) : 0.0f; }
 
-// A row of one slice, by one workgroup.
+// A row of up to SAMPLE_SMALL tokens by one workgroup, in LDS: one launch, and no
+// workspace (16384 tokens, a row and 16 rows: 17 and 24 us, 23 and 31 through the three
+// kernels below; 24000 tokens: 22 and 28, 24 and 31).
 struct SmallShared {
-    uint32_t keys[SL_LEN];
-    unsigned long long list[SB_CAP];
     SampleShared sh;
+    alignas(16) unsigned long long list[SB_CAP];
+    alignas(16) uint32_t keys[SL_LEN];             // and those of the row's other slices behind them
 };
+static_assert(sizeof(SmallShared) + (SAMPLE_SMALL - SL_LEN) * 4 <= 160 * 1024 && SAMPLE_SMALL % SL_LEN == 0, "LDS");
 __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     SmallShared& all = *(SmallShared*)smem;
     SampleShared& sh = all.sh;
     uint32_t* keys = all.keys;
     unsigned long long* list = all.list;
-    const int row = blockIdx.x, tid = threadIdx.x;
+    const int row = blockIdx.x, tid = threadIdx.x, slices = (a.V + SL_LEN - 1) / SL_LEN;
     const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
     RowBins rb{a.rows[row].per_t, 0.0};
     const float u = row_u(a, row);
     if (tid == 0) sh.fill = 0u;
-    const uint32_t top = load_slice(r, 0, keys, sh.wave_c);
-    rb.qmax = floor(rb.x(top));
-    count_slice(keys, rb, sh.hist);
+    const uint32_t top = load_tokens(r, 0, a.V, keys, sh.wave_c);
     if (!top) return draw_nothing(a, row);
-    unsigned bc[SB_PER];
-    unsigned long long bu[SB_PER];
+    rb.qmax = floor(rb.x(top));
+    unsigned bc[SB_PER] = {};
+    unsigned long long bu[SB_PER] = {};
+#pragma unroll 1
+    for (int s = 0; s < slices; ++s) {             // a slice's counts at a time: they fit their bits
+        count_slice(keys + s * SL_LEN, min(SL_LEN, a.V - s * SL_LEN), rb, sh.hist);
 #pragma unroll
-    for (int j = 0; j < SB_PER; ++j) {
-        bc[j] = (unsigned)sh.hist[SB_PER * tid + j] & 16383u;
-        bu[j] = sh.hist[SB_PER * tid + j] >> 14;
+        for (int j = 0; j < SB_PER; ++j) {
+            bc[j] += (unsigned)sh.hist[SB_PER * tid + j] & 16383u;
+            bu[j] += sh.hist[SB_PER * tid + j] >> 14;
+        }
+        __syncthreads();
     }
     const RowPlan plan = make_plan(a.rows[row], u, rb, top, bc, bu, sh);
-    if (plan.n <= (unsigned)SB_CAP) take_tokens(plan, keys, 0, &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
+    if (plan.n <= (unsigned)SB_CAP)
+#pragma unroll 1
+        for (int s = 0; s < slices; ++s)
+            take_tokens(plan, keys + s * SL_LEN, s, min(SL_LEN, a.V - s * SL_LEN), &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
     __syncthreads();
     draw_row(a, row, r, plan, u, list, (unsigned long long*)keys, sh);
 }
@@ -987,8 +997,9 @@ __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a)
     const RowPlan& plan = ws->plan;
     if (!plan.top || plan.n > (unsigned)SB_CAP || !(plan.touched[slice >> 5] >> (slice & 31) & 1u)) return;
     const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
-    load_slice(r, slice, keys, buf);
-    take_tokens(plan, keys, slice, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
+    const int n = min(SL_LEN, a.V - slice * SL_LEN);
+    load_tokens(r, slice * SL_LEN, n, keys, buf);
+    take_tokens(plan, keys, slice, n, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
 }
 
 // The cuts and the draw, one workgroup a row.
@@ -1012,10 +1023,10 @@ __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
 hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st) {
     if (!a.slices) {
         // on every launch: the attribute belongs to the device that is current
-        const hipError_t e = hipFuncSetAttribute((const void*)sample_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 sizeof(SmallShared));
+        const int lds = (int)sizeof(SmallShared) + (a.V - 1) / SL_LEN * SL_LEN * 4;
+        const hipError_t e = hipFuncSetAttribute((const void*)sample_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
-        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), sizeof(SmallShared), st>>>(a);
+        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), lds, st>>>(a);
         return hipGetLastError();
     }
     const dim3 g((unsigned)a.slices, (unsigned)m);

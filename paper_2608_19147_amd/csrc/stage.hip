@@ -681,7 +681,7 @@ int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, 
     a.token = token;
     a.p = p;
     a.top = top;
-    if (V > SAMPLE_SLICE) {
+    if (V > SAMPLE_SMALL) {
         a.slices = (V + SAMPLE_SLICE - 1) / SAMPLE_SLICE;
         int rc = grow(&st->smp, &st->smp_cap, sample_slice_bytes(a.slices));
         if (rc) return rc;
@@ -1744,7 +1744,7 @@ int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, in
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
-        if (vocab <= SAMPLE_SLICE)                         // one slice a row: no workspace, nothing to order
+        if (vocab <= SAMPLE_SMALL)                         // no workspace, nothing to order
             return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);
         if ((rc = not_captured(s))) return rc;
         HIP_TRY(order_on(st, s));

@@ -63,6 +63,20 @@ def test_sample(stage, V, dtype):
     _check(stage, torch.from_numpy(_logits(M, V, 1)).to(DT[dtype]), MIX, u, near_ok=1)
 
 
+@pytest.mark.parametrize("V", [8191, 8192, 8193, 16384, 16391, 24576, 24577])
+def test_sample_slices(stage, V):
+    """Around the ends of the slices that are counted apart, and of the rows that one workgroup holds; at last equal logits,
+    which fill one bin of every slice."""
+    M = len(MIX)
+    u = np.random.default_rng(V + 1).random(M)
+    _check(stage, torch.from_numpy(_logits(M, V, 11)).float(), MIX, u, near_ok=1)
+    _check(stage, torch.from_numpy(_logits(M, V, 12, spread=0.3)).bfloat16(), MIX, u, near_ok=1)
+    us = [0.0, 0.5, 1 - 2.0 ** -24]
+    tok, p = stage.sample(torch.full((3, V), -1.5, device="cuda"), Sampling(), torch.tensor(us, dtype=torch.float32, device="cuda"))
+    assert tok.tolist() == [int(u * V) for u in us]
+    assert (p.double() - 1.0 / V).abs().max().item() <= 2.0 ** -24 / V
+
+
 @pytest.mark.parametrize("spread", [0.01, 0.3, 8.0, 100.0])
 def test_spreads(stage, spread):
     """From almost equal logits (every token in few bins) to ones far apart."""
