@@ -375,7 +375,7 @@ int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out,
  * values, ties to the even code, at most 6 times the scale.  A block of zeros has
  * byte 0, one with a NaN or an infinity byte 255 and zero codes.
  * Errors: INVALID (NULL, dtype, m or k < 1), SHAPE (ld < k), CAPACITY (m or k
- * above 2^24, m * k above 2^36), HIP. */
+ * above 2^24, m * k above 2^34), HIP. */
 int stage_mx4_quantize(Stage* stage, const void* x, int dtype, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales,
                        void* stream);
 
@@ -465,7 +465,7 @@ int stage_head_sample(Stage* stage, const void* hidden, int M, const StageSampli
  *   next_out  [n_slots]    the token sampled at the last of them
  *   keep_out  uint8 [n_slots][n] 1 for the nodes walked: the rows that later
  *                          forwards keep in their mask
- * Errors: INVALID (NULL, n_slots < 1), CAPACITY (n), HIP. */
+ * Errors: INVALID (NULL, n_slots < 1), CAPACITY (n; n_slots above 2^24), HIP. */
 int stage_tree_accept(Stage* stage, const int32_t* parents, const int32_t* tokens, const int32_t* sampled, int n_slots, int n,
                       int32_t* count_out, int32_t* path_out, int32_t* next_out, uint8_t* keep_out, void* stream);
 

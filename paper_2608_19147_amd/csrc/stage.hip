@@ -553,8 +553,9 @@ int not_captured(hipStream_t s) {
 bool dtype_ok(int dt) { return dt == STAGE_DTYPE_F32 || dt == STAGE_DTYPE_F16 || dt == STAGE_DTYPE_BF16; }
 int any_dt(int dt) { return dt == STAGE_DTYPE_F32 ? (int)DT_F32 : dt_code(dt); }
 
+constexpr int TREE_MAX_SLOTS = 1 << 24;
 constexpr int64_t MX4_MAX_DIM = 1 << 24;
-constexpr int64_t MX4_MAX_VALUES = (int64_t)1 << 36;
+constexpr int64_t MX4_MAX_VALUES = (int64_t)1 << 34;      // a launch has fewer than 2^32 threads, of 8 values
 
 // Row and column counts of an MXFP4 call.
 int mx4_dims(int64_t rows, int64_t k) {
@@ -1784,6 +1785,7 @@ int stage_tree_accept(Stage* st, const int32_t* parents, const int32_t* tokens, 
             return fail(STAGE_E_INVALID, "NULL argument");
         if (n_slots < 1) return fail(STAGE_E_INVALID, "n_slots must be positive");
         if (n < 1 || n > MAX_ROWS) return fail(STAGE_E_CAPACITY, "n must be in [1, STAGE_MAX_ROWS]");
+        if (n_slots > TREE_MAX_SLOTS) return fail(STAGE_E_CAPACITY, "n_slots must be at most 2^24");
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         HIP_TRY(launch_tree_accept(parents, tokens, sampled, n_slots, n, count_out, path_out, next_out, keep_out,

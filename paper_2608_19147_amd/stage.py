@@ -74,12 +74,16 @@ def _rows(t: torch.Tensor, name: str) -> int:
     return max(ld, k)
 
 
-def _on(stream, device):
-    """(stream handle, maker of tensors) of a call on ``device``: the tensors come
-    from the pool of the stream that writes them, so that a later use of their
-    memory is ordered behind it."""
+def _on(stage, stream, device):
+    """(stream handle, maker of tensors) of a call on the tensors' ``device``, which
+    has to be the stage's: the results come from the pool of the stream that writes
+    them, so that a later use of their memory is ordered behind it."""
+    if device.index != stage.device_index:
+        raise ValueError(f"the stage is on cuda:{stage.device_index}, the tensors on {device}")
     if stream is None:
         return _raw_stream(device.index), torch.empty
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
 
     def empty(shape, dtype, device):
         with torch.cuda.stream(stream):
@@ -98,6 +102,8 @@ class Stage:
     ``scales`` (float16 [N, K/G]), ``n``, ``k`` — host numpy arrays or device
     torch tensors (``on_device=True``).
     """
+
+    device_index = 0
 
     def __init__(self, shape, layers: Sequence, on_device: bool = False, stream=None):
         self.lib = _lib.load()
@@ -127,6 +133,7 @@ class Stage:
                 keep += [q, s]
                 setattr(arr[l], name, _lib.QuantMatrix(q=_ptr(q), scales=_ptr(s), n=m.n, k=m.k))
         h = ctypes.c_void_p()
+        self.device_index = torch.cuda.current_device()
         check(self.lib.stage_create(ctypes.byref(cfg), arr, int(on_device), ctypes.c_void_p(_stream_ptr(stream)),
                                     ctypes.byref(h)))
         self.handle = h
@@ -246,6 +253,8 @@ class Stage:
         [vocab, ceil(H/2)], scales uint8 [vocab, ceil(H/32)], all on the host or
         all on the device."""
         on_dev = _check_mx4(codes, scales, self.shape.hidden)
+        if on_dev:
+            _on(self, None, codes.device)
         if tuple(final_norm.shape) != (self.shape.hidden,) or final_norm.dtype != self.act_dtype or not final_norm.is_contiguous():
             raise ValueError("final_norm must be a contiguous [hidden] tensor in the activation dtype")
         if final_norm.device != codes.device:
@@ -264,7 +273,7 @@ class Stage:
         M, dev = hidden.shape[0], hidden.device
         packed = _sampling(params, M)
         _check_u(u, M, dev)
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self, stream, dev)
         tok, p = empty(M, dtype=torch.int32, device=dev), empty(M, dtype=torch.float32, device=dev)
         full = empty((M, getattr(self, "vocab", 1)), dtype=torch.float32, device=dev) if with_logits else None
         check(self.lib.stage_head_sample(self.handle, hidden.data_ptr(), M, packed, u.data_ptr(), tok.data_ptr(), p.data_ptr(),
@@ -280,7 +289,7 @@ class Stage:
         dev = logits.device
         packed = _sampling(params, M)
         _check_u(u, M, dev)
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self, stream, dev)
         tok, p = empty(M, dtype=torch.int32, device=dev), empty(M, dtype=torch.float32, device=dev)
         check(self.lib.stage_sample(self.handle, logits.data_ptr(), _DT_OF[logits.dtype], ld, M, V, packed, u.data_ptr(),
                                     tok.data_ptr(), p.data_ptr(), sp))
@@ -299,7 +308,7 @@ class Stage:
             if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {dev}")
         S, n = shape
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self, stream, dev)
         count, path = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.int32, device=dev)
         nxt, keep = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.uint8, device=dev)
         check(self.lib.stage_tree_accept(self.handle, parents.data_ptr(), tokens.data_ptr(), sampled.data_ptr(), S, n,
@@ -312,7 +321,7 @@ class Stage:
         ld = _rows(x, "x")
         m, k = x.shape
         dev = x.device
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self, stream, dev)
         codes = empty((m, (k + 1) // 2), dtype=torch.uint8, device=dev)
         scales = empty((m, (k + 31) // 32), dtype=torch.uint8, device=dev)
         check(self.lib.stage_mx4_quantize(self.handle, x.data_ptr(), _DT_OF[x.dtype], ld, m, k, codes.data_ptr(),
@@ -326,7 +335,7 @@ class Stage:
         if out_dtype not in _DT_OF:
             raise ValueError("out_dtype must be float32, float16 or bfloat16")
         m, dev = codes.shape[0], codes.device
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self, stream, dev)
         out = empty((m, k), dtype=out_dtype, device=dev)
         check(self.lib.stage_mx4_dequantize(self.handle, codes.data_ptr(), scales.data_ptr(), m, k, out.data_ptr(),
                                             _DT_OF[out_dtype], k, sp))
@@ -460,6 +469,8 @@ class Mx4Matrix:
 
     def __init__(self, stage: Stage, codes: torch.Tensor, scales: torch.Tensor, k: int, stream=None):
         on_dev = _check_mx4(codes, scales, k)
+        if on_dev:
+            _on(stage, None, codes.device)
         self.stage, self.lib = stage, stage.lib
         self.n, self.k = int(codes.shape[0]), int(k)
         h = ctypes.c_void_p()
@@ -483,13 +494,14 @@ class Mx4Matrix:
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """x W^T [m, n] of device rows x [m, k]: 16-bit rows as they are (``act_bits``
         16) or rounded to MXFP4 first (4, also float32 rows), in ``out_dtype``
-        (x's by default) or into ``out`` [m, n], whose rows may be part of wider ones."""
+        (x's by default) or into ``out`` [m, n], whose rows may be part of wider ones
+        and must not overlap x."""
         ldx = _rows(x, "x")
         m, k = x.shape
         if k != self.k:
             raise ValueError(f"x has {k} columns, the matrix {self.k}")
         dev = x.device
-        sp, empty = _on(stream, dev)
+        sp, empty = _on(self.stage, stream, dev)
         if out is None:
             out_dtype = out_dtype or x.dtype
             if out_dtype not in _DT_OF:

@@ -133,6 +133,13 @@ def test_tree_inputs():
     assert pos.tolist() == [[5], [5]] and beam.tolist() == [1, 1]
 
 
+def test_largest_launches(lib):
+    """Sizes whose launch would not fit are refused before anything is read."""
+    assert lib.stage_tree_accept(P, P, P, P, (1 << 24) + 1, 4, P, P, P, P, None) == -3
+    assert lib.stage_mx4_quantize(P, P, F32, 1 << 18, 1 << 17, 1 << 18, P, P, None) == -3
+    assert lib.stage_mx4_dequantize(P, P, P, 1 << 18, 1 << 17, P, F32, 1 << 17, None) == -3
+
+
 def test_tree_inputs_refused():
     d = VerifyDriver(1, 2)
     for bad in (np.array([[-1, 1]]), np.array([[-1, 0, 2]]), np.array([[-1, -1]]), np.zeros((2, 3), int), np.zeros((1, 0), int)):

@@ -231,3 +231,30 @@ def test_head_sample_int4():
     got, _ = _check(p.gpu, lg.cpu(), MIX, u, near_ok=1)
     assert np.array_equal(got, tok.cpu().numpy())
     p.close()
+
+
+def test_largest_vocabulary(stage):
+    """2^20 tokens: every slice, and equal logits in all of them."""
+    V = 1 << 20
+    M = 6
+    u = np.random.default_rng(71).random(M)
+    _check(stage, torch.from_numpy(_logits(M, V, 72)).float(), MIX[:M], u, near_ok=1)
+    us = [0.0, 0.3125, 1 - 2.0 ** -20]
+    tok, p = stage.sample(torch.zeros((3, V), device="cuda", dtype=torch.bfloat16), Sampling(), torch.tensor(us, device="cuda"))
+    assert tok.tolist() == [int(v * V) for v in us] and p.tolist() == [2.0 ** -20] * 3
+
+
+def test_other_device_refused(stage, monkeypatch):
+    """Tensors on a device that is not the stage's (the stage is made to say that its own is another)."""
+    z, u = torch.zeros((1, 10), device="cuda"), torch.zeros(1, device="cuda")
+    t = torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    codes, scales = stage.mx4_quantize(torch.ones((2, 32), device="cuda"))
+    mat = stage.mx4_matrix(codes, scales, 32)
+    monkeypatch.setattr(stage, "device_index", stage.device_index + 1)
+    for call in (lambda: stage.sample(z, Sampling(), u), lambda: stage.tree_accept(t, t, t), lambda: stage.mx4_quantize(z),
+                 lambda: stage.mx4_dequantize(codes, scales, 32), lambda: stage.mx4_matrix(codes, scales, 32),
+                 lambda: mat.product(torch.ones((1, 32), device="cuda"), 4),
+                 lambda: stage.head_sample(torch.zeros((1, synth.TINY.hidden), dtype=stage.act_dtype, device="cuda"), Sampling(), u)):
+        with pytest.raises(ValueError, match="the stage is on"):
+            call()
+    mat.free()
