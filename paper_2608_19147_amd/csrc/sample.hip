@@ -39,17 +39,16 @@ __device__ __forceinline__ uint32_t rank_key(float l) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-// exp(d - 1/64) in units of 2^-36, d in [0, 1/32]: Taylor around 1/64 to the 5th power, the rest below 2.1e-14, a
-// third of half a unit.  Added to 2^52, the units are the low bits of the sum.
-__device__ __forceinline__ unsigned long long exp_units(double d) {
-    const double c = d - 1.0 / 64.0;
-    double p = 1.0 / 120.0;
-    p = fma(p, c, 1.0 / 24.0);
-    p = fma(p, c, 1.0 / 6.0);
-    p = fma(p, c, 0.5);
-    p = fma(p, c, 1.0);
-    p = fma(p, c, 1.0);
-    return (unsigned long long)__double_as_longlong(fma(p, 68719476736.0, 4503599627370496.0)) & 0xfffffffffffffull;
+// exp((f - 1/2) / 32) in units of 2^-36, f in [0, 1]: Taylor around f = 1/2 to the 5th power, the rest below 2.1e-14,
+// 0.0015 of a unit, with the coefficients 2^36 / (32^n n!).  Added to 2^52, the units are the low bits of the sum.
+__device__ __forceinline__ unsigned long long exp_units(double f) {
+    const double c = f - 0.5;
+    double p = 2048.0 / 120.0;
+    p = fma(p, c, 65536.0 / 24.0);
+    p = fma(p, c, 2097152.0 / 6.0);
+    p = fma(p, c, 33554432.0);
+    p = fma(p, c, 2147483648.0);
+    return (unsigned long long)__double_as_longlong(fma(p, c, 4503599627370496.0 + 68719476736.0)) & 0xfffffffffffffull;
 }
 
 // exp(-b / 32) and its inverse for b = 32 q + r, as products of exp(-q) and exp(-r / 32): correctly rounded values, so that
@@ -102,7 +101,7 @@ struct RowBins {                      // the scaled logit of a row's tokens
     double qmax;                      // floor(x) of the largest
     __device__ __forceinline__ double x(uint32_t key) const { return (double)key_logit(key) * per_t; }
     __device__ __forceinline__ double bin(double xv) const { return qmax - floor(xv); }
-    __device__ __forceinline__ unsigned long long units(double xv) const { return exp_units((xv - floor(xv)) * (1.0 / 32.0)); }
+    __device__ __forceinline__ unsigned long long units(double xv) const { return exp_units(xv - floor(xv)); }
 };
 
 struct RowArgs {
@@ -169,9 +168,20 @@ __device__ __forceinline__ uint32_t load_tokens(const RowArgs& r, int first, int
     return block_max<SB_THREADS / 64>(top, buf);               // and a barrier: the keys are written
 }
 
-__device__ __forceinline__ void count_key(uint32_t k, const RowBins& rb, unsigned long long* hist) {
-    const double x = rb.x(k), b = rb.bin(x);
-    if (k && b < (double)SB_BINS) atomicAdd(&hist[(int)b], rb.units(x) << 14 | 1ull);
+// Counts N tokens: their bins and units first, side by side, then the additions.  (Key 0 reads as NaN, which no bin takes.)
+template <int N>
+__device__ __forceinline__ void count_keys(const uint32_t* k, const RowBins& rb, unsigned long long* hist) {
+    unsigned long long v[N];
+    int b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const double x = rb.x(k[i]), f = rb.bin(x);
+        b[i] = f < (double)SB_BINS ? (int)f : -1;
+        v[i] = rb.units(x) << 14 | 1ull;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (b[i] >= 0) atomicAdd(&hist[b[i]], v[i]);
 }
 
 // hist[] of the slice's n tokens, counted from rb.qmax.
@@ -179,8 +189,13 @@ __device__ __forceinline__ void count_slice(const uint32_t* keys, int n, const R
 #pragma unroll 1
     for (int i = threadIdx.x; i < SB_BINS; i += SB_THREADS) hist[i] = 0ull;
     __syncthreads();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += SB_THREADS) count_key(keys[i], rb, hist);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += 4 * SB_THREADS) {
+        uint32_t k[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = i + j * SB_THREADS < n ? keys[i + j * SB_THREADS] : 0u;
+        count_keys<4>(k, rb, hist);
+    }
     __syncthreads();
 }
 
@@ -893,7 +908,7 @@ __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs 
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) count_key(k[h][j], rb, sh.hist);
+            for (int j = 0; j < 8; j += 4) count_keys<4>(&k[h][j], rb, sh.hist);
         __syncthreads();
         if (tid == 0) sh.found = 0;
         __syncthreads();

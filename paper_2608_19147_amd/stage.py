@@ -309,8 +309,8 @@ class Stage:
                 raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {dev}")
         S, n = shape
         sp, empty = _on(self, stream, dev)
-        count, path = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.int32, device=dev)
-        nxt, keep = empty(S, dtype=torch.int32, device=dev), empty(shape, dtype=torch.uint8, device=dev)
+        count, path = empty(S, dtype=torch.int32, device=dev), empty((S, n), dtype=torch.int32, device=dev)
+        nxt, keep = empty(S, dtype=torch.int32, device=dev), empty((S, n), dtype=torch.uint8, device=dev)
         check(self.lib.stage_tree_accept(self.handle, parents.data_ptr(), tokens.data_ptr(), sampled.data_ptr(), S, n,
                                          count.data_ptr(), path.data_ptr(), nxt.data_ptr(), keep.data_ptr(), sp))
         return count, path, nxt, keep

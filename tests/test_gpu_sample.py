@@ -1,6 +1,6 @@
 """Sampling against its 64-bit form: the token has to be the same wherever no cut
 and no draw of the 64-bit form comes within 1e-9 of the kept weight of another
-outcome (the kernel's sums are exact to 2^-43 a token and 2^-50 a bin, and leave
+outcome (the kernel's sums are exact to 2^-36 a token and 2^-50 a bin, and leave
 out at most 1.4e-8 of the weight at its far end, which no u or top_p reaches);
 p within fp32's rounding and those 1.4e-8."""
 import numpy as np
