@@ -409,7 +409,7 @@ __device__ __forceinline__ v16f mx4_mfma(v8i a, v8i b, v16f c, int step, uint32_
 // its odd ones (as pairs they would have to be moved to neighbouring registers first).
 // Results go through LDS of the wave's own, two tiles at a time, so that short loops
 // store their rows, 16 or 32 bytes a lane: stores straight from the registers were
-// 20 KB of instructions for MT = 8, and fetching them took most of 12 us a workgroup.
+// 20 KB of instructions for 8 tiles, and fetching them took most of 12 us a workgroup.
 constexpr int STORE_LD = 72;                                       // rows 4 apart lie in other banks
 constexpr int store_lds(int mt) { return 4 * (mt < 2 ? 1 : 2) * 32 * STORE_LD * 4; }
 // LDS accesses of a wave's lanes on either side keep their order (the unit takes a wave's in order).
@@ -496,16 +496,15 @@ __device__ __forceinline__ void store_tiles(const Mx4Gemm& p, int mt0, int g, co
     }
 }
 
-// Scale words of MT row tiles and a group of W, four steps at once.
+// Scale words of MT row tiles (1, 2 or 4, from a multiple of MT on) and a group of W,
+// four steps at once.
 template <int NT, int MT>
 struct ScaleLoad {
-    const uint32_t* a[(MT + 3) / 4];
+    const uint32_t* a;
     const u32x2* w;
     __device__ __forceinline__ ScaleLoad(const Mx4Gemm& p, int mt0, int g, int lane) {
-        const int quads = p.w.steps / 4, groups = (p.a.tiles + 3) / 4;
-#pragma unroll
-        for (int q = 0; q < (MT + 3) / 4; ++q)
-            a[q] = (const uint32_t*)p.a.s + ((size_t)min(mt0 / 4 + q, groups - 1) * quads * NT * 64 + lane) * 4 + (MT < 4 ? mt0 % 4 : 0);
+        const int quads = p.w.steps / 4;
+        a = (const uint32_t*)p.a.s + ((size_t)(mt0 / 4) * quads * NT * 64 + lane) * 4 + mt0 % 4;
         w = (const u32x2*)p.w.s + (size_t)g * quads * 64 + lane;
     }
     __device__ __forceinline__ void load(int quad, uint32_t (&as)[MT][NT], uint32_t (&ws)[2]) const {
@@ -513,21 +512,19 @@ struct ScaleLoad {
         ws[0] = v[0];
         ws[1] = v[1];
 #pragma unroll
-        for (int q = 0; q < (MT + 3) / 4; ++q)
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t* s = a + ((size_t)quad * NT + n) * 256;
+            if constexpr (MT == 1) as[0][n] = s[0];
+            else if constexpr (MT == 2) {
+                const u32x2 t = *(const u32x2*)s;
+                as[0][n] = t[0];
+                as[1][n] = t[1];
+            } else {
+                const u32x4 t = *(const u32x4*)s;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint32_t* s = a[q] + ((size_t)quad * NT + n) * 256;
-                if constexpr (MT == 1) as[0][n] = s[0];
-                else if constexpr (MT == 2) {
-                    const u32x2 t = *(const u32x2*)s;
-                    as[0][n] = t[0];
-                    as[1][n] = t[1];
-                } else {
-                    const u32x4 t = *(const u32x4*)s;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) as[4 * q + i][n] = t[i];
-                }
+                for (int i = 0; i < 4; ++i) as[i][n] = t[i];
             }
+        }
     }
 };
 
@@ -647,9 +644,9 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
 }
 
 // The same product for many rows, where the matrix cores are to be the bound.
-// A step of 64 k is 2 MT NT products of 32 or 64 cycles a wave, one wave a SIMD,
-// which issues in order: whatever the wave waits for or cannot issue leaves the
-// matrix core idle.  So
+// A step of 64 k is 2 MT NT products of 32 or 64 cycles a wave, and with 16-bit rows
+// one wave a SIMD, which issues in order: whatever the wave waits for or cannot issue
+// leaves the matrix core idle.  So
 //  - loads run D steps ahead in registers, W's fragments to their use, the
 //    activations' (a wave loads a quarter of a step's) into one of two LDS
 //    buffers;
@@ -658,16 +655,19 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
 //  - fragments are read AHEAD of their products, across the step's end: the
 //    barrier that frees one buffer and opens the other stands where the first
 //    fragment of the next step is read, under the products in between.
-// Everything is unrolled over D steps (a divisor of the step count), so that the
-// rings are registers.
-template <int T, int MT, int D>
-__global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
+// Everything is unrolled over D = 4 steps (steps_per is a multiple), so that the rings
+// are registers.  With 4-bit rows they leave room for two workgroups a CU, one of which
+// works while the other one starts or stores (tiles of 8 x 32 rows, one a CU, and of
+// 4 x 32, two a CU: 2048 x 28672 x 8192 253 and 261 us, 2048 x 14336 x 4096 78 and 75,
+// 2048 x 4096 x 14336 96 and 77).
+template <int T, int MT>
+__global__ __launch_bounds__(256, T ? 1 : 2) void mx4_pipe_kernel(Mx4Gemm p) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
     constexpr int PIECES = MT * NT * U, PW = PIECES / 4;           // kilobytes of a step's fragments; loaded by a wave
     constexpr int FRAGS = MT * NT;                                 // of a step
     constexpr int AHEAD = 3, RING = AHEAD + 1;                     // fragments read before their products
-    constexpr int QUADS = D / 4, OPEN = FRAGS - AHEAD;             // OPEN: the fragment before whose products the barrier stands
-    static_assert(PIECES % 4 == 0 && D % 4 == 0 && FRAGS % RING == 0 && PW <= OPEN && PW + 2 <= FRAGS, "rings");
+    constexpr int D = 4, OPEN = FRAGS - AHEAD;                     // OPEN: the fragment before whose products the barrier stands
+    static_assert(PIECES % 4 == 0 && FRAGS % RING == 0 && PW <= OPEN && PW + 2 <= FRAGS, "rings");
     constexpr int BUF = PIECES * 1024;
     __shared__ __attribute__((aligned(16))) uint8_t smem[2 * BUF > store_lds(MT) ? 2 * BUF : store_lds(MT)];
     u32x4* const lds[2] = {(u32x4*)smem, (u32x4*)(smem + BUF)};
@@ -688,7 +688,7 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
     }
     v16f acc[MT][2] = {};
     u32x4 ar[D][PW], wr[D][2], fr[RING][U];
-    uint32_t ws[QUADS][2], as[QUADS][MT][NT], wsn[2], asn[MT][NT];
+    uint32_t ws[2], as[MT][NT], wsn[2], asn[MT][NT];             // scales of these four steps and of the next
     auto load_a = [&](int slot, int q, int s) { ar[slot][q] = ap[q][(size_t)min(s, last) * (NT * U * 64)]; };
     auto load_w = [&](int slot, int j, int s) { wr[slot][j] = wp[(size_t)min(s, last) * 128 + j * 64]; };
     auto write_a = [&](int slot, int q, int buf) { lds[buf][(wave * PW + q) * 64 + lane] = ar[slot][q]; };
@@ -697,8 +697,7 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
         for (int u = 0; u < U; ++u) fr[ring][u] = lds[buf][(f * U + u) * 64 + lane];
     };
     // steps s0 .. s0 + D - 1 of both operands; step s0 to LDS, and its first fragments to registers
-#pragma unroll
-    for (int q = 0; q < QUADS; ++q) sl.load(min(s0 + 4 * q, last) / 4, as[q], ws[q]);
+    sl.load(s0 / 4, as, ws);
 #pragma unroll
     for (int d = 0; d < D; ++d) {
 #pragma unroll
@@ -728,10 +727,8 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
                     load_a((d + 1) % D, f, s + d + 1 + D);
                 } else if (f < PW + 2) {
                     load_w((d + D - 1) % D, f - PW, s + d - 1 + D);     // the step before is done with its own
-                } else if (f == PW + 2 && d % 4 == 0) {
-                    // the four steps before are done with their scales; where there is one set, the next one waits
-                    if constexpr (QUADS > 1) sl.load(min(s + d - 4 + D, last) / 4, as[(d / 4 + QUADS - 1) % QUADS], ws[(d / 4 + QUADS - 1) % QUADS]);
-                    else sl.load(min(s + 4, last) / 4, asn, wsn);
+                } else if (f == PW + 2 && d == 0) {
+                    sl.load(min(s + 4, last) / 4, asn, wsn);
                 }
                 const u32x4 lo = fr[f % RING][0], hi = U == 2 ? fr[f % RING][U - 1] : u32x4{0u, 0u, 0u, 0u};
                 const v8i a = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
@@ -739,19 +736,17 @@ __global__ __launch_bounds__(256) void mx4_pipe_kernel(Mx4Gemm p) {
                 for (int j = 0; j < 2; ++j) {
                     const u32x4 w = wr[d][j];
                     const v8i b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
-                    acc[f / NT][j] = mx4_mfma<FMT>(a, b, acc[f / NT][j], d & 3, as[d / 4][f / NT][f % NT], ws[d / 4][j]);
+                    acc[f / NT][j] = mx4_mfma<FMT>(a, b, acc[f / NT][j], d, as[f / NT][f % NT], ws[j]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if constexpr (QUADS == 1) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) ws[0][j] = wsn[j];
+        for (int j = 0; j < 2; ++j) ws[j] = wsn[j];
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) as[0][t][n] = asn[t][n];
-        }
+            for (int n = 0; n < NT; ++n) as[t][n] = asn[t][n];
     }
     __syncthreads();                                               // the buffers are read
     if (off) return;
@@ -947,11 +942,11 @@ hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
     return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
 }
 
-template <int T, int MT, int D>
+template <int T, int MT>
 hipError_t run_pipe(Mx4Gemm p, hipStream_t st) {
     p.mtiles = (p.a.tiles + MT - 1) / MT;
     const int ntiles = (p.w.groups + 3) / 4;
-    mx4_pipe_kernel<T, MT, D><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), 0, st>>>(p);
+    mx4_pipe_kernel<T, MT><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
 }
@@ -962,32 +957,34 @@ hipError_t run_pipe(Mx4Gemm p, hipStream_t st) {
 // costs STEP (us), and a CU's workgroups take turns: larger tiles read less per
 // product, so they win once every CU has work (2048 x 4096 x 4096: 75, 65 and 60 us
 // with MT 1, 2 and 4).  START is what a tile's code and stores add, which is why small
-// products take small tiles (300 x 300 x 300 with 4-bit rows: 13, 15, 21 and 32 us with
-// MT 1, 2, 4 and 8); from MT 4 on a CU holds one workgroup and each round pays it.
-// Splits cost a launch and their sums' way to memory and back (33 x 256 x 14336: 64 us
-// unsplit, 20 in 16 splits; 700 x 2048 x 700: 15 and 21 in two).
+// products take small tiles (300 x 300 x 300 with 4-bit rows: 13, 15 and 21 us with MT
+// 1, 2 and 4); where MT 4 has one workgroup a CU, each round pays it.  Splits cost a
+// launch and their sums' way to memory and back (33 x 256 x 14336: 64 us unsplit, 20 in
+// 16 splits; 700 x 2048 x 700: 15 and 21 in two).
 float mx4_plan(Mx4Gemm& p, int n_cus) {
-    constexpr int MTS[4] = {1, 2, 4, 8};
-    constexpr float START[4] = {0.0f, 1.8f, 6.5f, 15.0f};
-    constexpr float STEP[3][4] = {{0.15f, 0.185f, 0.25f, 0.36f}, {0.25f, 0.40f, 0.52f, 0.0f}, {0.35f, 0.55f, 0.75f, 0.0f}};   // terms 0, 2, 3
+    constexpr int MTS[3] = {1, 2, 4};
+    constexpr float START[3] = {0.0f, 1.8f, 6.5f};
+    constexpr float STEP[3][3] = {{0.15f, 0.185f, 0.25f}, {0.25f, 0.40f, 0.52f}, {0.35f, 0.55f, 0.75f}};   // terms 0, 2, 3
     constexpr float BASE = 11.0f, JOIN = 4.0f, RATE = 7e6f;        // launches; the sums' launch; bytes a us
     constexpr int MAX_SPLIT = 24;
-    const int unit = p.w.steps % 8 == 0 ? 8 : 4, units = p.w.steps / unit;
+    const int units = p.w.steps / 4;
     const float* step = STEP[p.a.terms ? p.a.terms - 1 : 0];
     const float sums = (float)p.a.tiles * 32.0f * (float)p.w.groups * 64.0f * 8.0f / RATE;
     float least = 3.4e38f;
-    for (int i = 0; i < (p.a.terms || unit == 4 ? 3 : 4); ++i) {   // MT 8 has the long form only
+    for (int i = 0; i < 3; ++i) {
         const float wgs = (float)((p.a.tiles + MTS[i] - 1) / MTS[i]) * (float)((p.w.groups + 3) / 4);
         for (int s = 1; s <= MAX_SPLIT && s <= units; ++s) {
             const int per = (units + s - 1) / s, split = (units + per - 1) / per;
             if (split != s) continue;
-            const float rounds = fmaxf(1.0f, ceilf(wgs * (float)s / (float)n_cus));
-            const float us = BASE + rounds * (float)(per * unit) * step[i] + (MTS[i] >= 4 ? rounds : 1.0f) * START[i] + (s > 1 ? JOIN + (float)s * sums : 0.0f);
+            float rounds = fmaxf(1.0f, wgs * (float)s / (float)n_cus);
+            if (MTS[i] < 4 || p.a.terms) rounds = ceilf(rounds);       // else two workgroups a CU fill each other's gaps
+            const float us = BASE + rounds * (float)(per * 4) * step[i] + (MTS[i] == 4 && p.a.terms ? rounds : 1.0f) * START[i] +
+                             (s > 1 ? JOIN + (float)s * sums : 0.0f);
             if (us < least) {
                 least = us;
                 p.mt = MTS[i];
                 p.split = s;
-                p.steps_per = per * unit;
+                p.steps_per = per * 4;
             }
         }
     }
@@ -1012,21 +1009,16 @@ bool mx4_rows_direct(const Mx4Gemm& rows, int n_cus) {
 }
 
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
-    if (p.steps_per % 8 == 0 && p.w.steps % 8 == 0) switch (p.a.terms * 10 + p.mt) {
-        case 8: return run_pipe<0, 8, 8>(p, st);
-        case 24: return run_pipe<2, 4, 4>(p, st);
-        case 34: return run_pipe<3, 4, 4>(p, st);
-    }
     switch (p.a.terms * 10 + p.mt) {
         case 1: return run_gemm<0, 1, 4>(p, st);
         case 2: return run_gemm<0, 2, 4>(p, st);
-        case 4: return run_gemm<0, 4, 4>(p, st);
+        case 4: return run_pipe<0, 4>(p, st);
         case 21: return run_gemm<2, 1, 4>(p, st);
         case 22: return run_gemm<2, 2, 2>(p, st);
-        case 24: return run_gemm<2, 4, 2>(p, st);
+        case 24: return run_pipe<2, 4>(p, st);
         case 31: return run_gemm<3, 1, 4>(p, st);
         case 32: return run_gemm<3, 2, 2>(p, st);
-        case 34: return run_gemm<3, 4, 2>(p, st);
+        case 34: return run_pipe<3, 4>(p, st);
         default: return hipErrorInvalidValue;
     }
 }

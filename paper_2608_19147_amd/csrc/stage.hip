@@ -586,7 +586,6 @@ int mx4_load(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int 
     w.k = k;
     w.groups = (n + 63) / 64;
     w.steps = (k + 255) / 256 * 4;
-    if (k >= 2048) w.steps = (k + 511) / 512 * 8;          // the many-row product takes 8 steps at a time
     const size_t cb = (size_t)n * ((k + 1) / 2), sb = (size_t)n * ((k + 31) / 32);
     void *tc = nullptr, *ts = nullptr;
     auto undo = [&](int rc) {
