@@ -104,6 +104,19 @@ def test_dequantize_every_code(stage, dtype):
     assert torch.equal(out[ok], ref[ok])
 
 
+@pytest.mark.parametrize("dtype,m,k", [("bf16", 1030, 16389), ("f16", 1030, 16389), ("f32", 1030, 8197)])
+def test_round_trip_large(stage, dtype, m, k):
+    """More values than the caches hold, odd rows: those of single rows on their own."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    x = torch.randn((m, k), device="cuda", generator=g).to(DT[dtype])
+    codes, scales = stage.mx4_quantize(x)
+    out = stage.mx4_dequantize(codes, scales, k, DT[dtype])
+    for r in (0, 1, m // 2, m - 1):
+        c, s, _, _ = _check_quantize(stage, x[r:r + 1].cpu())
+        assert torch.equal(codes[r:r + 1].cpu(), c.cpu()) and torch.equal(scales[r:r + 1].cpu(), s.cpu())
+        assert torch.equal(out[r:r + 1].cpu(), stage.mx4_dequantize(c.cuda(), s.cuda(), k, DT[dtype]).cpu())
+
+
 @pytest.mark.parametrize("m,k", [(1, 1), (3, 40), (2, 4096), (33, 129)])
 def test_round_trip(stage, m, k):
     x = _rows(m, k, 3, "bf16")
