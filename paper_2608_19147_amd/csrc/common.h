@@ -390,7 +390,7 @@ struct SampleRow {
 constexpr int SAMPLE_SLICE = 8192;                 // tokens one workgroup counts
 constexpr int SAMPLE_SMALL = 3 * SAMPLE_SLICE;     // tokens of a row that one workgroup holds in LDS
 constexpr int SAMPLE_MAX_SLICES = 128;             // 2^20 tokens
-constexpr size_t SAMPLE_ROW_BYTES = 46080;         // workspace of a row (RowSpace)
+constexpr size_t SAMPLE_ROW_BYTES = 78848;         // workspace of a row (RowSpace)
 struct SampleArgs {
     const void* logits; int dt; size_t ld; int V;
     int slices;                                    // of a row, 0 for one; with more, the rows' and slices' workspace:

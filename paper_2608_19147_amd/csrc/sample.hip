@@ -23,7 +23,9 @@
 namespace stg {
 
 constexpr int SB_BINS = 1024;        // bins of 1/32 of a unit of logit / T
-constexpr int SB_CAP = 4096;         // tokens of the bins that matter that are gathered
+constexpr int SB_CAP = 8192;         // tokens of the bins that matter that are gathered: 128256 spread over 2 units of
+                                     // logit / T are up to 1600 a bin, and two or three bins matter
+constexpr int SB_CAP_SMALL = 4096;   // and of a row held in LDS
 constexpr int SB_RANK = 256;         // tokens that are ranked by counting larger ones
 constexpr int SB_RANGES = 4;         // runs of bins that are gathered
 constexpr int SB_THREADS = 512;      // of a workgroup
@@ -407,13 +409,13 @@ __device__ __forceinline__ Place place_in_ranked(int at, int n, int c0, unsigned
 // fewest whose units together reach `t`, all of them if none do (BY_MASS), or
 // those of at least `t` units each (BY_VALUE, which names no token).  listed > 0:
 // the part's tokens stand among the list's first `listed`.  Otherwise, above
-// SB_CAP of them, passes over the row narrow the part to a bucket of its keys' range (or
+// cap of them, passes over the row narrow the part to a bucket of its keys' range (or
 // find a token of equal ones by index), then gather it.  The part's tokens are
 // narrowed the same way, in LDS (sel), until SB_RANK are left, which are ranked.
 // Whole workgroup; every thread gets the result.  (One loop over the row serves
 // every kind of pass, and the caller calls this in one place: a row is one
 // workgroup's work once, so instructions come from memory, not from the cache.)
-__device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb, Part part, unsigned long long* list, int listed, Want want,
+__device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb, Part part, unsigned long long* list, int cap, int listed, Want want,
                                             unsigned long long t, unsigned long long* sel, SampleShared& sh) {
     enum Pass : int { RANGE, PIECES, COUNT, PICK, VALUE, GATHER };
     const int tid = threadIdx.x;
@@ -423,7 +425,7 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
         const int run = ((r.V + SB_THREADS - 1) / SB_THREADS + 7) / 8 * 8;   // COUNT, PICK: neighbours of one thread
         int shift = 0, kth = 0;
         unsigned upto = 0, mine = 0;
-        Pass pass = part.n <= SB_CAP ? GATHER : want == BY_VALUE ? VALUE : RANGE;
+        Pass pass = part.n <= cap ? GATHER : want == BY_VALUE ? VALUE : RANGE;
         for (;;) {
             __syncthreads();
             if (tid == 0) { sh.klo = 0xffffffffu; sh.khi = 0u; sh.fill = 0u; sh.place = Place{0, 0ull, 0u, -1}; }
@@ -459,7 +461,7 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
                         if (pass == PICK && ahead + n == (unsigned)kth) sh.place.index = i + j;
                     } else {
                         const unsigned f = atomicAdd(&sh.fill, 1u);
-                        if (f < (unsigned)SB_CAP) store_coherent(&list[f], ((unsigned long long)k[j] << 32) | (uint32_t)~(i + j));
+                        if (f < (unsigned)cap) store_coherent(&list[f], ((unsigned long long)k[j] << 32) | (uint32_t)~(i + j));
                     }
                 }
             }
@@ -496,7 +498,7 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
                 part.n = (int)sh.pieces[s];
                 c0 = (int)sh.c0;
                 u0 = sh.u0;
-                pass = part.n > SB_CAP ? RANGE : GATHER;
+                pass = part.n > cap ? RANGE : GATHER;
             } else if (pass == VALUE) {
                 unsigned tc;
                 unsigned long long tu;
@@ -710,7 +712,7 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
 // The slice's tokens (n of them) of the plan's runs go into the list; a wave asks
 // once for their places.
 template <class Put>
-__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* keys, int slice, int n, unsigned* fill, Put put) {
+__device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* keys, int slice, int n, int cap, unsigned* fill, Put put) {
     const int tid = threadIdx.x;
     unsigned m = 0;
 #pragma unroll 2
@@ -728,7 +730,7 @@ __device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* k
     at = (unsigned)__builtin_amdgcn_readlane((int)at, 63) + upto - mine;
     while (m) {
         const int i = (__ffs(m) - 1) * SB_THREADS + tid;
-        if (at < (unsigned)SB_CAP) put(at, ((unsigned long long)keys[i] << 32) | (uint32_t)~(slice * SL_LEN + i));
+        if (at < (unsigned)cap) put(at, ((unsigned long long)keys[i] << 32) | (uint32_t)~(slice * SL_LEN + i));
         ++at;
         m &= m - 1u;
     }
@@ -736,9 +738,9 @@ __device__ __forceinline__ void take_tokens(const RowPlan& pl, const uint32_t* k
 
 // The cuts and the draw of a row, by one workgroup: its running sums in sh.cum
 // and sh.cumc, the tokens of the plan's runs in the list (unless they are more
-// than SB_CAP: then the row is read again, place by place).
+// than cap: then the row is read again, place by place).
 __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const RowArgs& r, const RowPlan& plan, float u,
-                                         unsigned long long* list, unsigned long long* sel, SampleShared& sh) {
+                                         unsigned long long* list, int cap, unsigned long long* sel, SampleShared& sh) {
     const int tid = threadIdx.x;
     const SampleRow p = a.rows[row];
     const RowBins rb{p.per_t, plan.qmax};
@@ -747,7 +749,7 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
     const bool by_k = p.top_k > 0 && (unsigned)p.top_k < nall, by_p = p.top_p < 1.0f;
     auto before = [&](int b) { return b ? sh.cum[b - 1] : 0.0; };
     auto cbefore = [&](int b) { return b ? sh.cumc[b - 1] : 0u; };
-    bool listed = plan.n <= (unsigned)SB_CAP, ranked = plan.n <= (unsigned)SB_RANK;
+    bool listed = plan.n <= (unsigned)cap, ranked = plan.n <= (unsigned)SB_RANK;
     if (ranked) {                               // few: ranked together, bin behind bin
         if (tid < (int)plan.n) sh.ranked[tid] = list[tid];
         __syncthreads();
@@ -810,7 +812,7 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
         const int at = start(b), cnt = (int)(sh.cumc[b] - cbefore(b));
         if (ranked && at >= 0) pl = place_in_ranked(at, cnt, 0, 0ull, want, t, rb, sh);
         else {
-            pl = find_place(r, rb, Part{b, 0u, 0xffffffffu, cnt}, list, listed && at >= 0 ? (int)plan.n : 0, want, t, sel, sh);
+            pl = find_place(r, rb, Part{b, 0u, 0xffffffffu, cnt}, list, cap, listed && at >= 0 ? (int)plan.n : 0, want, t, sel, sh);
             listed = listed && at >= 0;         // find_place took the list's memory
             ranked = false;                     // and that of the ranked ones
         }
@@ -844,7 +846,7 @@ __device__ __forceinline__ float row_u(const SampleArgs& a, int row) { return a.
 // kernels below; 24000 tokens: 22 and 28, 24 and 31).
 struct SmallShared {
     SampleShared sh;
-    alignas(16) unsigned long long list[SB_CAP];
+    alignas(16) unsigned long long list[SB_CAP_SMALL];
     alignas(16) uint32_t keys[SL_LEN];             // and those of the row's other slices behind them
 };
 static_assert(sizeof(SmallShared) + (SAMPLE_SMALL - SL_LEN) * 4 <= 160 * 1024 && SAMPLE_SMALL % SL_LEN == 0, "LDS");
@@ -875,12 +877,12 @@ __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) 
         __syncthreads();
     }
     const RowPlan plan = make_plan(a.rows[row], u, rb, top, bc, bu, sh);
-    if (plan.n <= (unsigned)SB_CAP)
+    if (plan.n <= (unsigned)SB_CAP_SMALL)
 #pragma unroll 1
         for (int s = 0; s < slices; ++s)
-            take_tokens(plan, keys + s * SL_LEN, s, min(SL_LEN, a.V - s * SL_LEN), &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
+            take_tokens(plan, keys + s * SL_LEN, s, min(SL_LEN, a.V - s * SL_LEN), SB_CAP_SMALL, &sh.fill, [&](unsigned at, unsigned long long v) { list[at] = v; });
     __syncthreads();
-    draw_row(a, row, r, plan, u, list, (unsigned long long*)keys, sh);
+    draw_row(a, row, r, plan, u, list, SB_CAP_SMALL, (unsigned long long*)keys, sh);
 }
 
 // Counts one slice of a row; the row's last workgroup to end joins the counts and makes the plan.
@@ -1014,7 +1016,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a)
     const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
     const int n = min(SL_LEN, a.V - slice * SL_LEN);
     load_tokens(r, slice * SL_LEN, n, keys, buf);
-    take_tokens(plan, keys, slice, n, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
+    take_tokens(plan, keys, slice, n, SB_CAP, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
 }
 
 // The cuts and the draw, one workgroup a row.
@@ -1032,7 +1034,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
         sh.cumc[j * SB_THREADS + tid] = ws->cumc[j * SB_THREADS + tid];
     }
     __syncthreads();
-    draw_row(a, row, r, plan, row_u(a, row), ws->list, sel, sh);
+    draw_row(a, row, r, plan, row_u(a, row), ws->list, SB_CAP, sel, sh);
 }
 
 hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st) {
