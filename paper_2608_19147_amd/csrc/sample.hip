@@ -50,7 +50,8 @@ __device__ __forceinline__ unsigned long long exp_units(double f) {
     p = fma(p, c, 2097152.0 / 6.0);
     p = fma(p, c, 33554432.0);
     p = fma(p, c, 2147483648.0);
-    return (unsigned long long)__double_as_longlong(fma(p, c, 4503599627370496.0 + 68719476736.0)) & 0xfffffffffffffull;
+    p = fma(p, c, 4503599627370496.0 + 68719476736.0);
+    return (unsigned long long)__double_as_longlong(p) & 0xfffffffffffffull;
 }
 
 // exp(-b / 32) and its inverse for b = 32 q + r, as products of exp(-q) and exp(-r / 32): correctly rounded values, so that
@@ -101,7 +102,8 @@ __device__ __forceinline__ double bin_inverse(int b) { return INV_Q[b >> 5] * IN
 struct RowBins {                      // the scaled logit of a row's tokens
     double per_t;                     // 32 / T
     double qmax;                      // floor(x) of the largest
-    __device__ __forceinline__ double x(uint32_t key) const { return (double)key_logit(key) * per_t; }
+    __device__ __forceinline__ double x(float logit) const { return (double)logit * per_t; }
+    __device__ __forceinline__ double x(uint32_t key) const { return x(key_logit(key)); }
     __device__ __forceinline__ double bin(double xv) const { return qmax - floor(xv); }
     __device__ __forceinline__ unsigned long long units(double xv) const { return exp_units(xv - floor(xv)); }
 };
@@ -110,9 +112,8 @@ struct RowArgs {
     const void* logits; int dt; size_t base; int V;
 };
 
-// Keys of tokens i .. i + 7 (i a multiple of 8); 0 past the row's end.
-__device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)[8]) {
-    float v[8];
+// Logits of tokens i .. i + 7 (i a multiple of 8) as they are; -inf past the row's end.
+__device__ __forceinline__ void load_logits(const RowArgs& r, int i, float (&v)[8]) {
     if (i + 8 <= r.V) {
         if (r.dt == DT_F32) {
             const u32x4_any* p = (const u32x4_any*)((const float*)r.logits + r.base + i);
@@ -132,9 +133,16 @@ __device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = i + j < r.V ? v[j] : -INFINITY;
     }
+}
+// Their keys.
+__device__ __forceinline__ void load_keys(const RowArgs& r, int i, uint32_t (&k)[8]) {
+    float v[8];
+    load_logits(r, i, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) k[j] = rank_key(v[j]);
 }
+// A logit as its key orders it: -inf if it is not ranked.
+__device__ __forceinline__ float ranked_logit(float l) { return fminf(l >= -3.402823466e38f ? l : -INFINITY, 3.402823466e38f); }
 
 // One slice of a row: its largest token; its bins, counted from that one's
 // (sum << 14 | count), stand apart.
@@ -170,9 +178,10 @@ __device__ __forceinline__ uint32_t load_tokens(const RowArgs& r, int first, int
     return block_max<SB_THREADS / 64>(top, buf);               // and a barrier: the keys are written
 }
 
-// Counts N tokens: their bins and units first, side by side, then the additions.  (Key 0 reads as NaN, which no bin takes.)
-template <int N>
-__device__ __forceinline__ void count_keys(const uint32_t* k, const RowBins& rb, unsigned long long* hist) {
+// Counts N tokens (keys, or ranked logits): their bins and units first, side by side, then the additions.  (Key 0 reads as
+// NaN, which as -inf no bin takes.)
+template <int N, class K>
+__device__ __forceinline__ void count_keys(const K* k, const RowBins& rb, unsigned long long* hist) {
     unsigned long long v[N];
     int b[N];
 #pragma unroll
@@ -895,22 +904,25 @@ __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs 
     RowBins rb{a.rows[row].per_t, 0.0};
     {
         const RowArgs r{a.logits, a.dt, (size_t)row * a.ld, a.V};
-        // keys in registers: without them in LDS four workgroups share a CU
-        uint32_t k[2][8], top = 0;
+        // in registers: without them in LDS four workgroups share a CU; as keys they took 12 more instructions a token
+        float l[2][8], most = -INFINITY;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            load_keys(r, slice * SL_LEN + h * (SL_LEN / 2) + tid * 8, k[h]);
+            load_logits(r, slice * SL_LEN + h * (SL_LEN / 2) + tid * 8, l[h]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = max(top, k[h][j]);
+            for (int j = 0; j < 8; ++j) {
+                l[h][j] = ranked_logit(l[h][j]);
+                most = fmaxf(most, l[h][j]);
+            }
         }
 #pragma unroll 1
         for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
-        top = block_max<SB_THREADS / 64>(top, sh.wave_c);
+        const uint32_t top = block_max<SB_THREADS / 64>(rank_key(most), sh.wave_c);
         rb.qmax = floor(rb.x(top));
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 8; j += 4) count_keys<4>(&k[h][j], rb, sh.hist);
+            for (int j = 0; j < 8; j += 4) count_keys<4>(&l[h][j], rb, sh.hist);
         __syncthreads();
         if (tid == 0) sh.found = 0;
         __syncthreads();
