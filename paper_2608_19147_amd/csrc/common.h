@@ -393,7 +393,7 @@ constexpr int SAMPLE_MAX_SLICES = 128;             // 2^20 tokens
 constexpr size_t SAMPLE_ROW_BYTES = 78848;         // workspace of a row (RowSpace)
 struct SampleArgs {
     const void* logits; int dt; size_t ld; int V;
-    int slices;                                    // of a row, 0 for one; with more, the rows' and slices' workspace:
+    int slices;                                    // of a row, 0 if it is held in LDS; else the rows' and slices' workspace:
     uint8_t* rows_ws;                              // [MAX_ROWS] x SAMPLE_ROW_BYTES
     void* heads; unsigned long long* bins;         // [m][slices], [m][slices][bins]
     const float* u;                                // [m], or null: 0, the first of the ranking

@@ -71,7 +71,9 @@ __device__ __forceinline__ uint32_t absbits(float v) { return __float_as_uint(v)
 
 // Eight values of a row a thread, four neighbouring threads a block: their
 // largest magnitude is shared by lane exchanges, each writes 4 bytes of codes.
-// Bound by memory: 2 bytes a value read (16 bits), 17/32 written.
+// Bound by memory: 2 bytes a value read (16 bits), 17/32 written (2048 x 14336:
+// 13.8 us, 5.4 TB/s where a large copy reaches 5.1; one row of 4096: 2.0 us, the
+// least a launch takes).
 template <int DT>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, size_t ld, int m, int k, int chunks,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -129,7 +131,7 @@ hipError_t launch_mx4_quantize(const void* x, int dt, int64_t ld, int m, int k, 
 }
 
 // Eight values a thread.  Bound by memory: 17/32 bytes a value read, 2 written (16
-// bits).  PAST_L2: the values are stored past the L2s, which they would fill (2048 x
+// bits; 2048 x 14336: 20 us, 3.7 TB/s, mostly writes).  PAST_L2: the values are stored past the L2s, which they would fill (2048 x
 // 14336 rounded and back: 36.6 us through them, 32.6 past them).
 template <int DT, bool PAST_L2>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
@@ -201,6 +203,7 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, in
 // ------------------------------------------------------------------ weights
 
 // One thread per 16-byte piece (32 codes: one row and block) of the packed form.
+// Runs once a matrix, so it reads the codes byte by byte.
 __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                        Mx4Mat w) {
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;     // [group][step][j][lane]
@@ -301,7 +304,9 @@ __device__ __forceinline__ uint32_t top16(const float (&v)[16]) {
 // 16 values of one row (half a block) a thread; the two threads of a block are
 // neighbours and share its largest magnitude.  A workgroup takes 32 rows by two
 // steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
-// m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).
+// m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).  Bound
+// by memory (517 x 14336 in two terms: 14.8 MB read, 33 written, 7.7 us), for few
+// rows by its launch (20 x 4096 in three: 4.4 us).
 template <int T, int DT>
 __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, size_t ld, int m, int k, int steps,
                                                        uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
@@ -548,7 +553,9 @@ __device__ __forceinline__ int xcd_run(int bid, int nwg) {
 // over steps_per = a multiple of 4 steps of K (blockIdx.z: the split).  The
 // activations' fragments are shared by the four waves through LDS, double
 // buffered; W's go from memory to the registers that the product reads, each
-// used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.
+// used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.  With few
+// rows bound by reading the weights (20 x 128256 x 4096: 53 us, 5.2 TB/s), with some
+// hundred by loads that the few waves of a CU do not cover (256 x 4096 x 4096: 15 us).
 //
 // split > 1: fp32 sums to part [split][tiles of 32 rows][n], joined by mx4_reduce_kernel.
 template <int T, int MT, int KS>
@@ -651,7 +658,10 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
     store_tiles<MT>(p, mt0, g, acc, smem);
 }
 
-// The same product for many rows, where the matrix cores are to be the bound.
+// The same product for many rows, where the matrix cores are to be the bound: 2048 x
+// 28672 x 8192 with 4-bit rows runs at 3.7 to 4.0 PFLOP/s.  Random codes draw so much
+// power there that the clock falls to 1.5 GHz from 2.1 with equal ones (same cycles),
+// where the instruction alone could do 5; the rest is starts and stores.
 // A step of 64 k is 2 MT NT products of 32 or 64 cycles a wave, and with 16-bit rows
 // one wave a SIMD, which issues in order: whatever the wave waits for or cannot issue
 // leaves the matrix core idle.  So
@@ -769,7 +779,8 @@ __global__ __launch_bounds__(256, T ? 1 : 2) void mx4_pipe_kernel(Mx4Gemm p) {
 // Bound by the latency of one read after a launch and by fetching the code, so
 // there is one copy of the conversion; where many outputs or long rows make the
 // terms that every workgroup makes for itself the larger part, the rows are
-// prepared once instead (mx4_rows_direct below).
+// prepared once instead (mx4_rows_direct below).  One row of 4096 x 4096: 4.9 us, of
+// which the weights' 8.9 MB could be read in 1.8.
 constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
 __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, size_t ldx, int seg) {
@@ -903,6 +914,7 @@ hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx,
 
 // out = the sum of the splits, in their order: four outputs a thread, and eight
 // splits' on their way at a time (other XCDs wrote them: a read takes over a us).
+// Bound by memory (517 x 4096 in three splits: 27 MB read, 6.3 us).
 __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
     const int quads = (p.w.n + 3) / 4;
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
@@ -1031,7 +1043,8 @@ hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
     }
 }
 
-// out[m][H] = fp16(RMSNorm(row) * gamma): the input of an MXFP4 head.
+// out[m][H] = fp16(RMSNorm(row) * gamma): the input of an MXFP4 head.  A sum of
+// squares in fp32, one rounding to the 11 bits that three E4M3 terms hold.
 __global__ __launch_bounds__(256) void rms_rows_kernel(const void* __restrict__ x, int dt, const uint16_t* __restrict__ gamma, int H,
                                                        float eps, uint16_t* __restrict__ out) {
     __shared__ float buf[256];

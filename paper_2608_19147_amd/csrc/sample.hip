@@ -18,6 +18,12 @@
 // than 2^20 e^-31.9 = 1.5e-8 of the kept weight) are left out: neither u nor
 // top_p, 24-bit numbers below 1, comes nearer to 1 than 6e-8, so no draw and no
 // cut falls there.
+//
+// What bounds it is not the reading (64 bf16 rows of 128256: 16 MB, 3.3 us) but the
+// chain of small steps: count, plan, gather, draw, each a launch or a workgroup's
+// code run once, from memory.  Rows whose logits are nearly equal have more tokens in
+// the bins that matter than are gathered, and are read again, place by place, by one
+// workgroup: a row of 128256 equal ones takes 0.2 to 0.6 ms.
 #include "device.h"
 
 namespace stg {
@@ -851,8 +857,8 @@ __device__ __forceinline__ void draw_nothing(const SampleArgs& a, int row) {
 __device__ __forceinline__ float row_u(const SampleArgs& a, int row) { return a.u ? fminf(fmaxf(a.u[row], 0.0f), 0.99999994f) : 0.0f; }
 
 // A row of up to SAMPLE_SMALL tokens by one workgroup, in LDS: one launch, and no
-// workspace (16384 tokens, a row and 16 rows: 17 and 24 us, 23 and 31 through the three
-// kernels below; 24000 tokens: 22 and 28, 24 and 31).
+// workspace (1000 tokens 12 us; 16384 tokens, a row and 16 rows: 16 and 23 us, 23 and 31
+// through the three kernels below; 24000 tokens: 21 and 27, 24 and 31).
 struct SmallShared {
     SampleShared sh;
     alignas(16) unsigned long long list[SB_CAP_SMALL];
@@ -895,6 +901,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) 
 }
 
 // Counts one slice of a row; the row's last workgroup to end joins the counts and makes the plan.
+// 20 rows of 128256: 17 us, of which a slice takes 5, the joining 3 and the plan 4; 64 rows: 27.
 __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
     const int slice = blockIdx.x, row = blockIdx.y, ns = gridDim.x, tid = threadIdx.x;
@@ -1017,7 +1024,7 @@ __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs 
     }
 }
 
-// Gathers one slice's tokens of the plan's runs.
+// Gathers one slice's tokens of the plan's runs.  20 rows: 5 us; 64 rows, most of whose slices have some: 9.
 __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t keys[SL_LEN];
     __shared__ uint32_t buf[SB_THREADS / 64];
@@ -1031,7 +1038,8 @@ __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a)
     take_tokens(plan, keys, slice, n, SB_CAP, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
 }
 
-// The cuts and the draw, one workgroup a row.
+// The cuts and the draw, one workgroup a row.  20 rows: 12 us, about 1 a step; 64 rows with up to some thousand
+// gathered tokens each, narrowed in LDS: 26.
 __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
     __shared__ unsigned long long sel[SB_CAP];
@@ -1084,7 +1092,8 @@ hipError_t launch_sample_clear(uint8_t* rows, hipStream_t st) {
 // One wave a slot, one lane a node.  A node is reached if its parent is and it
 // is the parent's first child whose token is the one sampled there; node 0 is.
 // Each step takes the lowest such child, so it goes to a later node and the walk
-// ends after at most n steps.
+// ends after at most n steps.  One slot of 15 nodes 1.7 us, 256 of 64 nodes 2.9: the
+// launch.
 __global__ __launch_bounds__(64) void tree_accept_kernel(const int32_t* __restrict__ parents, const int32_t* __restrict__ tokens,
                                                          const int32_t* __restrict__ sampled, int n, int32_t* __restrict__ count,
                                                          int32_t* __restrict__ path, int32_t* __restrict__ next,
