@@ -438,6 +438,7 @@ typedef struct StageSampling {
  * [M]; u: device fp32 [M] in [0, 1) (values outside are taken as the nearest
  * inside).  A row without a ranked token gives token -1 and p 0.
  * 1 <= M <= STAGE_MAX_ROWS.  The result does not depend on the other rows.
+ * Params are read by the call: a captured one replays with those it was made with.
  * Allocates a workspace on first use above 24576 tokens (kept, grown when a larger
  * vocabulary comes).
  * Errors: INVALID (NULL, dtype, params), SHAPE (vocab, ld), CAPACITY (M, vocab),

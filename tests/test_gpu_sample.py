@@ -258,3 +258,30 @@ def test_other_device_refused(stage, monkeypatch):
         with pytest.raises(ValueError, match="the stage is on"):
             call()
     mat.free()
+
+
+def test_capture(stage):
+    """A row that one workgroup holds is sampled in a graph, with the logits and u of each replay; longer rows, which use
+    the stage's workspace, refuse."""
+    M, V = 5, 20000
+    params = [Sampling(*q) for q in MIX[:M]]
+    z, u = torch.zeros((M, V), device="cuda"), torch.zeros(M, device="cuda")
+    wide = torch.from_numpy(_logits(2, 30000, 80)).float().cuda()
+    stage.sample(z, params, u)
+    stage.sample(wide, Sampling(), u[:2].clone())
+    u2 = torch.zeros(2, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        tok, p = stage.sample(z, params, u)
+        with pytest.raises(StageError) as ei:
+            stage.sample(wide, Sampling(), u2)
+        assert ei.value.code == -7
+    for i in range(3):
+        z.copy_(torch.from_numpy(_logits(M, V, 81 + i)).float())
+        u.copy_(torch.from_numpy(np.random.default_rng(90 + i).random(M).astype(np.float32)))
+        stage.sample(wide, Sampling(), u2)
+        g.replay()
+        eager = stage.sample(z, params, u)
+        torch.cuda.synchronize()
+        assert torch.equal(tok, eager[0]) and torch.equal(p, eager[1])
