@@ -943,32 +943,31 @@ __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
     else store_run<DT_BF16, 4>(p.out, p.ld, p.w.n, row, col, v);
 }
 
-static hipError_t run_reduce(const Mx4Gemm& p, hipStream_t st) {
+static hipError_t run_reduce(const Mx4Gemm& p, hipStream_t st, hipEvent_t done) {
     const size_t n = (size_t)p.m * ((p.w.n + 3) / 4);
-    mx4_reduce_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st>>>(p);
-    return hipGetLastError();
+    return launch_done(mx4_reduce_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, done, p);
 }
 
 template <int T, int MT, int KS>
-hipError_t run_gemm(Mx4Gemm p, hipStream_t st) {
+hipError_t run_gemm(Mx4Gemm p, hipStream_t st, hipEvent_t done) {
     p.mtiles = (p.a.tiles + MT - 1) / MT;
     const int ntiles = (p.w.groups + 3) / 4;
     constexpr int BUFS = 2 * MT * KS * (T ? 2 * T : 1) * 1024, LDS = BUFS > store_lds(MT) ? BUFS : store_lds(MT);
     hipError_t e = hipSuccess;
     if (LDS > 65536) e = hipFuncSetAttribute((const void*)mx4_gemm_kernel<T, MT, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return e;
-    mx4_gemm_kernel<T, MT, KS><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), LDS, st>>>(p);
-    e = hipGetLastError();
-    return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
+    e = launch_done(mx4_gemm_kernel<T, MT, KS>, dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), LDS, st,
+                    p.split > 1 ? nullptr : done, p);
+    return e == hipSuccess && p.split > 1 ? run_reduce(p, st, done) : e;
 }
 
 template <int T, int MT>
-hipError_t run_pipe(Mx4Gemm p, hipStream_t st) {
+hipError_t run_pipe(Mx4Gemm p, hipStream_t st, hipEvent_t done) {
     p.mtiles = (p.a.tiles + MT - 1) / MT;
     const int ntiles = (p.w.groups + 3) / 4;
-    mx4_pipe_kernel<T, MT><<<dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), 0, st>>>(p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess && p.split > 1 ? run_reduce(p, st) : e;
+    const hipError_t e = launch_done(mx4_pipe_kernel<T, MT>, dim3((unsigned)(p.mtiles * ntiles), 1, (unsigned)p.split), dim3(256), 0,
+                                     st, p.split > 1 ? nullptr : done, p);
+    return e == hipSuccess && p.split > 1 ? run_reduce(p, st, done) : e;
 }
 
 // Row tiles of 32 a workgroup (MT) and splits of K: the pair of least time by what
@@ -1028,17 +1027,17 @@ bool mx4_rows_direct(const Mx4Gemm& rows, int n_cus) {
     return us < mx4_plan(p, n_cus);
 }
 
-hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st) {
+hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st, hipEvent_t done) {
     switch (p.a.terms * 10 + p.mt) {
-        case 1: return run_gemm<0, 1, 4>(p, st);
-        case 2: return run_gemm<0, 2, 4>(p, st);
-        case 4: return run_pipe<0, 4>(p, st);
-        case 21: return run_gemm<2, 1, 4>(p, st);
-        case 22: return run_gemm<2, 2, 2>(p, st);
-        case 24: return run_pipe<2, 4>(p, st);
-        case 31: return run_gemm<3, 1, 4>(p, st);
-        case 32: return run_gemm<3, 2, 2>(p, st);
-        case 34: return run_pipe<3, 4>(p, st);
+        case 1: return run_gemm<0, 1, 4>(p, st, done);
+        case 2: return run_gemm<0, 2, 4>(p, st, done);
+        case 4: return run_pipe<0, 4>(p, st, done);
+        case 21: return run_gemm<2, 1, 4>(p, st, done);
+        case 22: return run_gemm<2, 2, 2>(p, st, done);
+        case 24: return run_pipe<2, 4>(p, st, done);
+        case 31: return run_gemm<3, 1, 4>(p, st, done);
+        case 32: return run_gemm<3, 2, 2>(p, st, done);
+        case 34: return run_pipe<3, 4>(p, st, done);
         default: return hipErrorInvalidValue;
     }
 }

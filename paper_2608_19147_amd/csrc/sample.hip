@@ -1057,20 +1057,19 @@ __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
     draw_row(a, row, r, plan, row_u(a, row), ws->list, SB_CAP, sel, sh);
 }
 
-hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st) {
+hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st, hipEvent_t done) {
     if (!a.slices) {
         // on every launch: the attribute belongs to the device that is current
         const int lds = (int)sizeof(SmallShared) + (a.V - 1) / SL_LEN * SL_LEN * 4;
         const hipError_t e = hipFuncSetAttribute((const void*)sample_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
-        sample_small_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), lds, st>>>(a);
-        return hipGetLastError();
+        return launch_done(sample_small_kernel, dim3((unsigned)m), dim3(SB_THREADS), lds, st, done, a);
     }
     const dim3 g((unsigned)a.slices, (unsigned)m);
     sample_count_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
     sample_gather_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
-    sample_draw_kernel<<<dim3((unsigned)m), dim3(SB_THREADS), 0, st>>>(a);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_done(sample_draw_kernel, dim3((unsigned)m), dim3(SB_THREADS), 0, st, done, a) : e;
 }
 
 size_t sample_slice_bytes(int slices) { return (size_t)MAX_ROWS * slices * (sizeof(SliceHead) + 8 * SB_BINS); }

@@ -428,6 +428,12 @@ hipError_t mark_done(Stage* st, hipStream_t s) {
     return e;
 }
 
+// The same for a call whose last launch signals done_ev itself.
+void mark_launched(Stage* st, hipStream_t s) {
+    st->done_used = true;
+    st->last_stream = s;
+}
+
 constexpr size_t PROF_MAX_LAUNCHES = 65536;
 
 // Records the start (begin = true) or stop event of a profiled launch.
@@ -620,9 +626,9 @@ constexpr int MX4_PASS = 2048;                             // rows of one produc
 
 int mx4_terms(int dt, int act, int odt) { return act == 4 ? 0 : dt == DT_BF16 && odt != DT_F32 ? 2 : 3; }
 
-// out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).
+// out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).  done: signalled by the last launch, or null.
 int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
-            hipStream_t s) {
+            hipStream_t s, hipEvent_t done) {
     const size_t xb = dt == DT_F32 ? 4 : 2, ob = odt == DT_F32 ? 4 : 2;
     for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
         const int mm = std::min(MX4_PASS, m - m0);
@@ -650,7 +656,7 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
             if ((rc = grow(&st->mx_p, &st->mx_p_cap, (size_t)p.split * a.tiles * 32 * p.part_ld * 4))) return rc;
             p.part = (float*)st->mx_p;
         }
-        HIP_TRY(launch_mx4_gemm(p, s));
+        HIP_TRY(launch_mx4_gemm(p, s, m0 + mm < m ? nullptr : done));
     }
     return STAGE_OK;
 }
@@ -669,9 +675,9 @@ int check_sampling(const StageSampling* params, int M) {
     return STAGE_OK;
 }
 
-// params null: the whole softmax, and the first of the ranking (u null).
+// params null: the whole softmax, and the first of the ranking (u null).  done: as in mx4_run.
 int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, const StageSampling* params, const float* u,
-               int32_t* token, float* p, float* top, hipStream_t s) {
+               int32_t* token, float* p, float* top, hipStream_t s, hipEvent_t done) {
     SampleArgs a{};
     a.logits = logits;
     a.dt = dt;
@@ -702,7 +708,7 @@ int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, 
         if (q.temperature == 0.0f) a.rows[i].top_k = 1;
         else a.rows[i] = SampleRow{32.0 / (double)q.temperature, q.top_k, q.top_p, q.min_p};
     }
-    HIP_TRY(launch_sample(a, M, s));
+    HIP_TRY(launch_sample(a, M, s, done));
     return STAGE_OK;
 }
 
@@ -730,9 +736,9 @@ int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params,
     float* lg = logits_out ? logits_out : st->logits;
     HIP_TRY(order_on(st, s));
     HIP_TRY(launch_rms_rows(hidden, dt_code(c.act_dtype), st->final_norm, M, c.hidden, c.rms_eps, st->head_rows, s));
-    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F16, c.hidden, M, 16, lg, DT_F32, st->vocab, s))) return rc;
-    if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s))) return rc;
-    HIP_TRY(mark_done(st, s));
+    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F16, c.hidden, M, 16, lg, DT_F32, st->vocab, s, nullptr))) return rc;
+    if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s, st->done_ev))) return rc;
+    mark_launched(st, s);
     return STAGE_OK;
 }
 
@@ -1691,9 +1697,9 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
             return STAGE_OK;
         }
         HIP_TRY(order_on(st, s));
-        int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s);
+        int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s, st->done_ev);
         if (rc) return rc;
-        HIP_TRY(mark_done(st, s));
+        mark_launched(st, s);
         return STAGE_OK;
     });
 }
@@ -1745,12 +1751,12 @@ int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, in
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
         if (vocab <= SAMPLE_SMALL)                         // no workspace, nothing to order
-            return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);
+            return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s, nullptr);
         if ((rc = not_captured(s))) return rc;
         HIP_TRY(order_on(st, s));
-        rc = sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s);
+        rc = sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s, st->done_ev);
         if (rc) return rc;
-        HIP_TRY(mark_done(st, s));
+        mark_launched(st, s);
         return STAGE_OK;
     });
 }
@@ -1771,8 +1777,8 @@ int stage_head_sample(Stage* st, const void* hidden, int M, const StageSampling*
         if ((rc = not_captured(s)) || (rc = ensure_logits(st))) return rc;
         float* lg = logits_out ? logits_out : st->logits;
         if ((rc = stage_head_top1(st, hidden, M, st->head_tok, st->head_p, nullptr, lg, stream))) return rc;
-        if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token_out, p_out, nullptr, s))) return rc;
-        HIP_TRY(mark_done(st, s));
+        if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token_out, p_out, nullptr, s, st->done_ev))) return rc;
+        mark_launched(st, s);
         return STAGE_OK;
     });
 }

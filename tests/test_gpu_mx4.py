@@ -324,6 +324,34 @@ def test_product_streams(stage):
     mat.free()
 
 
+def test_product_order(stage):
+    """Long products, split and not, on the default stream and two others in turn: each waits for the whole of the one before
+    it, also where that took several passes or a sampling call came between."""
+    mats = []
+    for n, k in ((4096, 4096), (520, 8200), (8192, 700)):
+        codes, scales = _weights(n, k, 27)
+        mats.append(stage.mx4_matrix(torch.from_numpy(mx4_pack(codes)), torch.from_numpy(scales), k))
+    calls = [(mats[i % 3], _rows(m, mats[i % 3].k, 28 + i, "bf16").cuda()) for i, m in enumerate((1500, 300, 2500, 65, 2000, 700, 2100, 1000))]
+    z = torch.from_numpy(np.random.default_rng(29).standard_normal((20, 60000))).float().cuda()
+    u = torch.full((20,), 0.4, device="cuda")
+    want = [mat.product(x) for mat, x in calls]
+    tok, p = stage.sample(z, Sampling(), u)
+    torch.cuda.synchronize()
+    streams = [None, torch.cuda.Stream(), torch.cuda.Stream()]
+    for r in range(4):
+        got = []
+        for i, (mat, x) in enumerate(calls):
+            got.append(mat.product(x, stream=streams[(i + r) % 3]))
+            if i % 3 == 1:
+                t2, p2 = stage.sample(z, Sampling(), u, stream=streams[(i + r + 1) % 3])
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        assert torch.equal(t2, tok) and torch.equal(p2, p)
+    for mat in mats:
+        mat.free()
+
+
 def test_capture(stage):
     """Rounding and products of few rows use no memory of the stage and can be captured; a larger product refuses and
     leaves the capture whole."""
