@@ -378,7 +378,9 @@ float mx4_plan(Mx4Gemm& p, int n_cus);
 template <class... A>
 hipError_t launch_done(void (*kernel)(A...), dim3 grid, dim3 block, unsigned lds, hipStream_t st, hipEvent_t done, A... args) {
     void* p[] = {(void*)&args...};
-    return hipExtLaunchKernel((const void*)kernel, grid, block, p, lds, st, nullptr, done, 0);
+    const hipError_t e = hipExtLaunchKernel((const void*)kernel, grid, block, p, lds, st, nullptr, done, 0);
+    if (e != hipSuccess) (void)hipGetLastError();      // the caller reports it, not the next launch
+    return e;
 }
 hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st, hipEvent_t done);
 // A product of up to MX4_ROWS_MAX rows that prepares them itself and needs no workspace (p.a: only terms), and whether
