@@ -555,7 +555,8 @@ __device__ __forceinline__ int xcd_run(int bid, int nwg) {
 // buffered; W's go from memory to the registers that the product reads, each
 // used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.  With few
 // rows bound by reading the weights (20 x 128256 x 4096: 53 us, 5.2 TB/s), with some
-// hundred by loads that the few waves of a CU do not cover (256 x 4096 x 4096: 15 us).
+// hundred by what a CU reads, 12 KB a step of one tile at some 50 GB/s (256 x 4096 x
+// 4096: 15 us; a second set of waves on the other half of K gained 3%).
 //
 // split > 1: fp32 sums to part [split][tiles of 32 rows][n], joined by mx4_reduce_kernel.
 template <int T, int MT, int KS>
