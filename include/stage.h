@@ -394,9 +394,9 @@ int stage_mx4_create(Stage* stage, const uint8_t* codes, const uint8_t* scales, 
 int stage_mx4_free(Mx4Matrix* matrix);
 
 /* out [m][n] = x [m][k] W^T, sums in fp32, rounded once to out_dtype.
- *   act_bits 16: x (F16 or BF16) enters as a sum of block-scaled E4M3 terms, 3 of
- *                them within 2^-18 of the largest magnitude of the element's block
- *                of 32, or 2 within 2^-14 for BF16 rows with a 16-bit out_dtype;
+ *   act_bits 16: x (F16 or BF16) enters as a sum of 3 block-scaled E4M3 terms,
+ *                within 2^-18 of the largest magnitude of the element's block of 32
+ *                (its larger elements exactly);
  *   act_bits  4: x (any dtype) is rounded to MXFP4 first (stage_mx4_quantize).
  * A row of x with a NaN or an infinity gives NaN, as does a NaN scale of W in
  * its column.  1 <= m <= STAGE_MAX_PREFILL.  out must not overlap x.  Allocates a

@@ -17,11 +17,13 @@
 // multiple of 2^-10 and below 12, and nothing is cut.  (Scaled to E4M3's full
 // range instead, results of 32 bits were 1e-5 off.)  What a term leaves of x is
 // at most 2^-4 of x and of a block at most 2^-4 of its largest magnitude (half
-// the last of 4 bits), or 2^-10 where E4M3's smallest step decides: two terms
-// come within 2^-14 of a block's largest magnitude, three within 2^-18, and the
-// larger elements of bf16 (8 significant bits) and f16 (11) are exact in two and
-// three terms.  Two terms are taken for bf16 rows with 16-bit results, three
-// otherwise.  Activations of 4 bits are one E2M1 term.
+// the last of 4 bits), or 2^-10 where E4M3's smallest step decides: three terms
+// come within 2^-18 of a block's largest magnitude, and the larger elements are
+// exact.  (Two terms, 2^-14, kept some 6 of the 8 bits of a bf16 element 2^-8
+// below its block's largest: 16-bit results were 3e-4 apart from those of products
+// in fp32, single ones by a step; three terms take 87 us at 517 x 4096 x 14336 and
+// one row of 4096 x 4096 6.9, two took 66 and 6.7.)
+// Activations of 4 bits are one E2M1 term.
 #include "device.h"
 
 namespace stg {
@@ -361,7 +363,6 @@ hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, i
         case DT_F32: MX4_PREP(0, DT_F32); break;
         case DT_F16: MX4_PREP(0, DT_F16); break;
         case DT_BF16: MX4_PREP(0, DT_BF16); break;
-        case 8 + DT_BF16: MX4_PREP(2, DT_BF16); break;
         case 12 + DT_F16: MX4_PREP(3, DT_F16); break;
         case 12 + DT_BF16: MX4_PREP(3, DT_BF16); break;
         default: return hipErrorInvalidValue;
@@ -904,7 +905,6 @@ hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx,
         case DT_F32: MX4_ROWS(0, DT_F32); break;
         case DT_F16: MX4_ROWS(0, DT_F16); break;
         case DT_BF16: MX4_ROWS(0, DT_BF16); break;
-        case 8 + DT_BF16: MX4_ROWS(2, DT_BF16); break;
         case 12 + DT_F16: MX4_ROWS(3, DT_F16); break;
         case 12 + DT_BF16: MX4_ROWS(3, DT_BF16); break;
         default: return hipErrorInvalidValue;
@@ -984,11 +984,11 @@ hipError_t run_pipe(Mx4Gemm p, hipStream_t st, hipEvent_t done) {
 float mx4_plan(Mx4Gemm& p, int n_cus) {
     constexpr int MTS[3] = {1, 2, 4};
     constexpr float START[3] = {0.0f, 1.8f, 6.5f};
-    constexpr float STEP[3][3] = {{0.15f, 0.185f, 0.25f}, {0.25f, 0.40f, 0.52f}, {0.35f, 0.55f, 0.75f}};   // terms 0, 2, 3
+    constexpr float STEP[2][3] = {{0.15f, 0.185f, 0.25f}, {0.35f, 0.55f, 0.75f}};      // one E2M1 term, three E4M3 terms
     constexpr float BASE = 11.0f, JOIN = 4.0f, RATE = 7e6f;        // launches; the sums' launch; bytes a us
     constexpr int MAX_SPLIT = 24;
     const int units = p.w.steps / 4;
-    const float* step = STEP[p.a.terms ? p.a.terms - 1 : 0];
+    const float* step = STEP[p.a.terms ? 1 : 0];
     const float sums = (float)p.a.tiles * 32.0f * (float)p.w.groups * 64.0f * 8.0f / RATE;
     float least = 3.4e38f;
     for (int i = 0; i < 3; ++i) {
@@ -1017,10 +1017,10 @@ float mx4_plan(Mx4Gemm& p, int n_cus) {
 // launches; 16 x 14336 x 4096: 40 and 19; one row of 14336 x 14336: 26 and 30.
 bool mx4_rows_direct(const Mx4Gemm& rows, int n_cus) {
     constexpr float BASE = 6.0f, SHARE = 0.65f, RATE = 16e6f;
-    constexpr float START[3] = {0.8f, 1.0f, 2.0f}, TERMS[3] = {0.06f, 0.15f, 0.21f};
+    constexpr float START[2] = {0.8f, 2.0f}, TERMS[2] = {0.06f, 0.21f};
     Mx4Gemm p = rows;
     if (p.m > MX4_ROWS_MAX) return false;
-    const int t = p.a.terms ? p.a.terms - 1 : 0;
+    const int t = p.a.terms ? 1 : 0;
     const float wgs = 4.0f * (float)p.w.groups * (float)((p.m + 15) / 16);
     const float own = START[t] + TERMS[t] * (float)(p.m < 16 ? p.m : 16) * (float)p.w.k * 1e-3f;
     const float us = BASE + fmaxf(1.0f, SHARE * wgs / (float)n_cus) * own + (float)p.w.n * (float)p.w.k * 0.53f / RATE;
@@ -1033,9 +1033,6 @@ hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st, hipEvent_t done) {
         case 1: return run_gemm<0, 1, 4>(p, st, done);
         case 2: return run_gemm<0, 2, 4>(p, st, done);
         case 4: return run_pipe<0, 4>(p, st, done);
-        case 21: return run_gemm<2, 1, 4>(p, st, done);
-        case 22: return run_gemm<2, 2, 2>(p, st, done);
-        case 24: return run_pipe<2, 4>(p, st, done);
         case 31: return run_gemm<3, 1, 4>(p, st, done);
         case 32: return run_gemm<3, 2, 2>(p, st, done);
         case 34: return run_pipe<3, 4>(p, st, done);

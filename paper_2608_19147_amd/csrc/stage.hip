@@ -624,7 +624,7 @@ int mx4_load(Stage* st, const uint8_t* codes, const uint8_t* scales, int n, int 
 
 constexpr int MX4_PASS = 2048;                             // rows of one product pass
 
-int mx4_terms(int dt, int act, int odt) { return act == 4 ? 0 : dt == DT_BF16 && odt != DT_F32 ? 2 : 3; }
+int mx4_terms(int act) { return act == 4 ? 0 : 3; }
 
 // out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).  done: signalled by the last launch, or null.
 int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
@@ -633,7 +633,7 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
     for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
         const int mm = std::min(MX4_PASS, m - m0);
         Mx4Act a{};
-        a.terms = mx4_terms(dt, act, odt);
+        a.terms = mx4_terms(act);
         a.tiles = (mm + 31) / 32;
         a.steps = w.steps;
         const size_t nt = a.terms ? a.terms : 1;
@@ -1681,7 +1681,7 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
         hipStream_t s = (hipStream_t)stream;
         Mx4Gemm p{};
         p.w = w->m;
-        p.a.terms = mx4_terms(any_dt(x_dtype), act_bits, any_dt(out_dtype));
+        p.a.terms = mx4_terms(act_bits);
         p.m = m;
         p.out = out;
         p.dt = any_dt(out_dtype);
