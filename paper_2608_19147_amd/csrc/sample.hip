@@ -562,7 +562,9 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
     int n = part.n;
 #pragma unroll 1
     while (n > SB_RANK) {
-        // buckets of the keys' range, highest first; of the index where all keys are equal
+        // buckets of the keys' range, highest first; where all keys are equal, of the range of their indices, which differ.
+        // Either range is that of the tokens left, so its two ends fall into different buckets and every pass ends with
+        // fewer tokens.
         __syncthreads();
         uint32_t lo = 0xffffffffu, hi = 0u;
 #pragma unroll 1
@@ -575,9 +577,20 @@ __device__ __forceinline__ Place find_place(const RowArgs& r, const RowBins& rb,
         for (int i = tid; i < SB_BINS; i += SB_THREADS) sh.hist[i] = 0ull;
         hi = block_max<SB_THREADS / 64>(hi, sh.wave_c);
         lo = ~block_max<SB_THREADS / 64>(~lo, sh.wave_c);
-        const uint32_t range = lo == hi ? (uint32_t)r.V - 1u : hi - lo;
-        const int shift = max(0, 22 - (int)__clz(range | 1u));       // range >> shift < 1024
-        auto bucket = [&](unsigned long long v) { return (lo == hi ? ~(uint32_t)v : hi - (uint32_t)(v >> 32)) >> shift; };
+        const bool equal = lo == hi;
+        if (equal) {
+            lo = 0xffffffffu, hi = 0u;                               // of the list's lower words, ~index
+#pragma unroll 1
+            for (int i = tid; i < n; i += SB_THREADS) {
+                const uint32_t k = (uint32_t)sel[i];
+                lo = min(lo, k);
+                hi = max(hi, k);
+            }
+            hi = block_max<SB_THREADS / 64>(hi, sh.wave_c);
+            lo = ~block_max<SB_THREADS / 64>(~lo, sh.wave_c);
+        }
+        const int shift = max(0, 22 - (int)__clz((hi - lo) | 1u));   // (hi - lo) >> shift < 1024
+        auto bucket = [&](unsigned long long v) { return (hi - (equal ? (uint32_t)v : (uint32_t)(v >> 32))) >> shift; };
 #pragma unroll 1
         for (int i = tid; i < n; i += SB_THREADS) {
             const unsigned long long v = sel[i];

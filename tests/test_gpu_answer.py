@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import synth
-from answer_ref import BLOCK, mx4_pack
+from answer_ref import BLOCK, mx4_pack, sample
 from gpu_cases import Pair
+from paper_2608_19147_amd import Sampling
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +40,33 @@ def test_small_elements_keep_their_bits(stage, m, n, k, out):
     tol = 2.0 ** -18 * top
     tol += (np.abs(ref) + tol) * torch.finfo(out).eps / 2
     assert (np.abs(got - ref) <= tol).all()
+
+
+def _drawn(stage, z, rows, near_ok=0):
+    """Rows (params, u) drawn from the one logits row z, each against the 64-bit form, unless that comes within 1e-9 of
+    another outcome."""
+    d = z.cuda()[None].repeat(len(rows), 1)
+    tok, p = stage.sample(d, [Sampling(*q) for q, _ in rows], torch.tensor([u for _, u in rows], device="cuda"))
+    near = 0
+    for (q, u), t, pr in zip(rows, tok.tolist(), p.tolist()):
+        rt, rp, gap = sample(z.double().numpy(), *q, u)
+        if gap < 1e-9:
+            near += 1
+            continue
+        assert t == rt, (q, u, t, rt)
+        assert abs(pr - rp) <= rp * (2.0 ** -24 + 3e-8)
+    assert near <= near_ok
+
+
+@pytest.mark.parametrize("V", [30000, 262144, 262145, 1 << 20])
+@pytest.mark.parametrize("n", [257, 300, 1024, 8192])
+@pytest.mark.parametrize("rest", [-np.inf, -12.0])
+def test_runs_of_equal_logits(stage, V, n, rest):
+    """More equal neighbours than are ranked at once, at the row's start, across a power of two and at its end, beside
+    nothing and beside many lower tokens."""
+    rows = [((1.0, 0, 1.0, 0.0), 0.0), ((1.0, 0, 1.0, 0.0), 0.4375), ((1.0, 0, 1.0, 0.0), 0.9990234375), ((1.0, n // 2 + 1, 1.0, 0.0), 0.8125),
+            ((1.0, 0, 0.5, 0.0), 0.9375), ((0.7, n + 5, 0.2531, 0.5), 0.5625)]
+    for at in (0, 16384 - n // 3, V - n):
+        z = torch.full((V,), rest)
+        z[at:at + n] = 1.5
+        _drawn(stage, z, rows, near_ok=1)
