@@ -408,8 +408,9 @@ int stage_mx4_product(Mx4Matrix* matrix, const void* x, int x_dtype, int64_t ldx
 
 /* stage_head_attach with the LM head [vocab][hidden] in MXFP4 (any group size of
  * the stage's own weights).  stage_head_top1 and stage_head_sample then use it:
- * RMSNorm rows rounded to fp16, times the head with act_bits 16.  Synchronizes
- * the stream.  One head per stage.
+ * RMSNorm rows in fp32, which enter the product as 3 block-scaled E4M3 terms
+ * (within 2^-12 of each element, or 2^-18 of the largest of its block of 32).
+ * Synchronizes the stream.  One head per stage.
  * Errors: INVALID (NULL), SHAPE (vocab < 1), CAPACITY (vocab), UNSUPPORTED
  * (already attached, capturing stream), OOM, HIP. */
 int stage_head_attach_mx4(Stage* stage, const uint16_t* final_norm, const uint8_t* codes, const uint8_t* scales, int vocab,

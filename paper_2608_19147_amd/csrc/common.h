@@ -388,8 +388,8 @@ hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st, hipEvent_t done);
 constexpr int MX4_ROWS_MAX = 64;
 bool mx4_rows_direct(const Mx4Gemm& p, int n_cus);
 hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx, hipStream_t st);
-// out [m][H] fp16 = RMSNorm(row) * gamma.
-hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st);
+// out [m][H] fp32 = RMSNorm(row) * gamma.
+hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, float* out, hipStream_t st);
 
 // ---- sampling and drafted trees (sample.hip)
 struct SampleRow {

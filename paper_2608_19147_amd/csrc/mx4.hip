@@ -363,6 +363,7 @@ hipError_t launch_mx4_prep(const Mx4Act& a, const void* x, int dt, int64_t ld, i
         case DT_F32: MX4_PREP(0, DT_F32); break;
         case DT_F16: MX4_PREP(0, DT_F16); break;
         case DT_BF16: MX4_PREP(0, DT_BF16); break;
+        case 12 + DT_F32: MX4_PREP(3, DT_F32); break;
         case 12 + DT_F16: MX4_PREP(3, DT_F16); break;
         case 12 + DT_BF16: MX4_PREP(3, DT_BF16); break;
         default: return hipErrorInvalidValue;
@@ -1040,10 +1041,11 @@ hipError_t launch_mx4_gemm(const Mx4Gemm& p, hipStream_t st, hipEvent_t done) {
     }
 }
 
-// out[m][H] = fp16(RMSNorm(row) * gamma): the input of an MXFP4 head.  A sum of
-// squares in fp32, one rounding to the 11 bits that three E4M3 terms hold.
+// out[m][H] = RMSNorm(row) * gamma in fp32: the input of an MXFP4 head, whose E4M3
+// terms then take it at whatever power of two gamma gives it (fp16 rows ended at
+// 65504) and leave 2^-12 of a block's larger elements.
 __global__ __launch_bounds__(256) void rms_rows_kernel(const void* __restrict__ x, int dt, const uint16_t* __restrict__ gamma, int H,
-                                                       float eps, uint16_t* __restrict__ out) {
+                                                       float eps, float* __restrict__ out) {
     __shared__ float buf[256];
     const size_t row = (size_t)blockIdx.x * H;
     float s = 0.0f;
@@ -1052,10 +1054,10 @@ __global__ __launch_bounds__(256) void rms_rows_kernel(const void* __restrict__ 
         s += v * v;
     }
     const float rs = rsqrtf(block_sum256(s, buf) / (float)H + eps);
-    for (int i = threadIdx.x; i < H; i += 256) out[row + i] = f32_to_f16(load_val(x, dt, row + i) * rs * load_val(gamma, dt, i));
+    for (int i = threadIdx.x; i < H; i += 256) out[row + i] = load_val(x, dt, row + i) * rs * load_val(gamma, dt, i);
 }
 
-hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, uint16_t* out, hipStream_t st) {
+hipError_t launch_rms_rows(const void* x, int dt, const uint16_t* gamma, int m, int H, float eps, float* out, hipStream_t st) {
     rms_rows_kernel<<<dim3((unsigned)m), dim3(256), 0, st>>>(x, dt, gamma, H, eps, out);
     return hipGetLastError();
 }

@@ -163,7 +163,7 @@ struct Stage {
     uint16_t* final_norm = nullptr;
     float4* top1_part = nullptr;                       // [MAX_ROWS][head tiles]
     Mx4Matrix* head4 = nullptr;                        // or an MXFP4 head (stage_head_attach_mx4), freed with the stage
-    uint16_t* head_rows = nullptr;                     // its normalized input rows, fp16 [MAX_ROWS][H]
+    float* head_rows = nullptr;                        // its normalized input rows [MAX_ROWS][H]
     float *logits = nullptr, *head_p = nullptr;        // logits rows [MAX_ROWS][vocab] and [MAX_ROWS], on first need
     int32_t* head_tok = nullptr;
     // workspace of the MXFP4 products: activation fragments and their scales, grown on need
@@ -626,7 +626,7 @@ constexpr int MX4_PASS = 2048;                             // rows of one produc
 
 int mx4_terms(int act) { return act == 4 ? 0 : 3; }
 
-// out = x W^T on stream s; act 4 or 16 (16-bit rows as they are).  done: signalled by the last launch, or null.
+// out = x W^T on stream s; act 4 or 16 (E4M3 terms).  done: signalled by the last launch, or null.
 int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
             hipStream_t s, hipEvent_t done) {
     const size_t xb = dt == DT_F32 ? 4 : 2, ob = odt == DT_F32 ? 4 : 2;
@@ -736,7 +736,7 @@ int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params,
     float* lg = logits_out ? logits_out : st->logits;
     HIP_TRY(order_on(st, s));
     HIP_TRY(launch_rms_rows(hidden, dt_code(c.act_dtype), st->final_norm, M, c.hidden, c.rms_eps, st->head_rows, s));
-    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F16, c.hidden, M, 16, lg, DT_F32, st->vocab, s, nullptr))) return rc;
+    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F32, c.hidden, M, 16, lg, DT_F32, st->vocab, s, nullptr))) return rc;
     if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s, st->done_ev))) return rc;
     mark_launched(st, s);
     return STAGE_OK;
@@ -1718,7 +1718,8 @@ int stage_head_attach_mx4(Stage* st, const uint16_t* final_norm, const uint8_t* 
         int rc = not_captured(s);
         if (rc) return rc;
         HIP_TRY(order_on(st, s));
-        uint16_t *fn = nullptr, *rows = nullptr;
+        uint16_t* fn = nullptr;
+        float* rows = nullptr;
         if ((rc = st->alloc(&fn, (size_t)H)) || (rc = st->alloc(&rows, (size_t)MAX_ROWS * H))) return rc;
         HIP_TRY(hipMemcpyAsync(fn, final_norm, (size_t)H * 2, weights_on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice, s));
         std::unique_ptr<Mx4Matrix> m(new Mx4Matrix());

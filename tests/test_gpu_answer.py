@@ -70,3 +70,24 @@ def test_runs_of_equal_logits(stage, V, n, rest):
         z = torch.full((V,), rest)
         z[at:at + n] = 1.5
         _drawn(stage, z, rows, near_ok=1)
+
+
+@pytest.mark.parametrize("power", [15, -13])
+def test_head_norm_weight_range(power):
+    """A final norm weight times a power of two gives the logits times that power, bit for bit: the normalized rows have no
+    largest or smallest value that it could meet."""
+    shape = synth.TINY
+    fn, _ = synth.make_head(shape, 64, 352)
+    x = synth.make_hidden(shape, 20, 353).cuda()
+    w = torch.from_numpy(np.random.default_rng(354).standard_normal((1003, shape.hidden)) * 0.02).float().cuda()
+    logits = []
+    for s in (0, power):
+        scaled = fn * 2.0 ** s
+        assert torch.equal(scaled.double(), fn.double() * 2.0 ** s)
+        p = Pair(shape, 355, with_oracle=False)
+        p.gpu.attach_head_mx4(scaled.cuda(), *p.gpu.mx4_quantize(w))
+        tok, pr, _, lg = p.gpu.head_top1(x, with_logits=True)
+        assert torch.equal(tok.long(), lg.argmax(1)) and bool((pr > 0).all())
+        logits.append(lg.double() * 2.0 ** -s)
+        p.close()
+    assert torch.equal(*logits)
