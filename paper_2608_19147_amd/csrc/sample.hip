@@ -835,6 +835,10 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int row, const Row
             const float share = step == 1 ? p.top_p : u;
             const double goal = (double)share * W;
             b = C <= (int)sh.cumc[0] ? 0 : min(end, wave_search(SB_BINS, [&](int i) { return step == 3 ? sh.cum[i] > goal : sh.cum[i] >= goal; }));
+            // running weights are sums in different orders: an empty bin's may be a rounding step above that of the bins ahead,
+            // with the goal in between, and the place is then where the next tokens start
+            const unsigned c = cbefore(b);
+            if (sh.cumc[b] == c) b = min(end, wave_search(SB_BINS, [&](int i) { return sh.cumc[i] > c; }));
             t = target(share, b, step == 1) + (step == 3 ? 1ull : 0ull);
         }
         const int at = start(b), cnt = (int)(sh.cumc[b] - cbefore(b));

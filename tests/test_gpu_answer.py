@@ -91,3 +91,40 @@ def test_head_norm_weight_range(power):
         logits.append(lg.double() * 2.0 ** -s)
         p.close()
     assert torch.equal(*logits)
+
+
+U_NEAR = 1 - 2.0 ** -12
+
+
+def _border_row(seed, at, V=1000):
+    """A logits row whose first 100 tokens in rank, in bins 0 to 21 of 1/32, hold U_NEAR of its weight to within some units
+    in the last place of a double (`at`, 0 to 63, moves it by them), with empty bins behind them.  Every logit is exact:
+    a multiple of 2^-17."""
+    r = np.random.default_rng([356, seed])
+    weight = lambda b, f: np.rint(2.0 ** 36 * np.exp((f - 0.5) / 32)) * np.exp(-b / 32)  # noqa: E731
+    bins, part = np.sort(r.integers(0, 22, 100)), r.integers(0, 4096, 100) / 4096
+    bins[0] = 0
+    ahead = weight(bins, part).sum()
+    left, f, tail = ahead * (1 - U_NEAR) / U_NEAR + (at - 32) * 0.5 * np.spacing(ahead), 4095 / 4096, []
+    for b in range(300, 1024):
+        n = int(left / weight(b, f))
+        left -= n * weight(b, f)
+        tail += [b] * n
+    x = np.concatenate([-np.sort(bins - part), f - np.array(tail)])
+    z = np.full(V, -np.inf)
+    z[:len(x)] = x / 32
+    return z
+
+
+@pytest.mark.parametrize("V", [1000, 30000])
+def test_draw_between_bins(stage, V):
+    """A draw at the border between two bins that have empty ones in between, one unit in the last place after the other: the
+    last token ahead of it or the first behind, never none."""
+    for seed in range(24):
+        z = np.stack([_border_row(seed, at, V) for at in range(64)])
+        assert np.array_equal(z, z.astype(np.float32))
+        tok, p = stage.sample(torch.from_numpy(z).float().cuda(), Sampling(), torch.full((64,), U_NEAR, device="cuda"))
+        for row, t, q in zip(z, tok.tolist(), p.tolist()):
+            assert t in (99, 100)
+            w = np.exp(row - row[0])
+            assert abs(q - w[t] / w.sum()) <= q * (2.0 ** -24 + 3e-8)
