@@ -428,11 +428,24 @@ hipError_t mark_done(Stage* st, hipStream_t s) {
     return e;
 }
 
-// The same for a call whose last launch signals done_ev itself.
-void mark_launched(Stage* st, hipStream_t s) {
-    st->done_used = true;
-    st->last_stream = s;
-}
+// A call's work on stream s, from order_on to launched(), after its last launch, which signals done_ev itself.  A call that
+// ends before that, with an error, is marked behind whatever it has queued, which may still use the workspace.
+struct WorkOn {
+    Stage* st;
+    hipStream_t s;
+    bool open = true;
+    WorkOn(Stage* st_, hipStream_t s_) : st(st_), s(s_) {}
+    WorkOn(const WorkOn&) = delete;
+    WorkOn& operator=(const WorkOn&) = delete;
+    ~WorkOn() {
+        if (open && mark_done(st, s) != hipSuccess) (void)hipGetLastError();   // the call reports its own error
+    }
+    void launched() {
+        st->done_used = true;
+        st->last_stream = s;
+        open = false;
+    }
+};
 
 constexpr size_t PROF_MAX_LAUNCHES = 65536;
 
@@ -735,10 +748,11 @@ int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params,
     if (rc) return rc;
     float* lg = logits_out ? logits_out : st->logits;
     HIP_TRY(order_on(st, s));
+    WorkOn work(st, s);
     HIP_TRY(launch_rms_rows(hidden, dt_code(c.act_dtype), st->final_norm, M, c.hidden, c.rms_eps, st->head_rows, s));
     if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F32, c.hidden, M, 16, lg, DT_F32, st->vocab, s, nullptr))) return rc;
     if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s, st->done_ev))) return rc;
-    mark_launched(st, s);
+    work.launched();
     return STAGE_OK;
 }
 
@@ -1579,6 +1593,7 @@ int stage_head_top1(Stage* st, const void* hidden, int M, int32_t* token_out, fl
     HIP_TRY(hipSetDevice(st->device));
     hipStream_t s = (hipStream_t)stream;
     HIP_TRY(order_on(st, s));
+    WorkOn work(st, s);
     HIP_TRY(launch_bprep(hidden, act_dt, H, st->final_norm, act_dt, H, c.rms_eps, M, st->bp[0], st->bc[0], st->kp,
                          st->rsb, s));
     GemvArgs a{};
@@ -1600,6 +1615,7 @@ int stage_head_top1(Stage* st, const void* hidden, int M, int32_t* token_out, fl
     a.top1_part = st->top1_part;
     HIP_TRY(launch_gemm_bp(a, s));
     HIP_TRY(launch_top1_merge(st->top1_part, M, st->head.pm.ntiles, token_out, p_out, logit_out, s));
+    work.open = false;
     HIP_TRY(mark_done(st, s));
     return STAGE_OK;
 }
@@ -1697,9 +1713,10 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
             return STAGE_OK;
         }
         HIP_TRY(order_on(st, s));
+        WorkOn work(st, s);
         int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s, st->done_ev);
         if (rc) return rc;
-        mark_launched(st, s);
+        work.launched();
         return STAGE_OK;
     });
 }
@@ -1755,9 +1772,10 @@ int stage_sample(Stage* st, const void* logits, int dtype, int64_t ld, int M, in
             return sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s, nullptr);
         if ((rc = not_captured(s))) return rc;
         HIP_TRY(order_on(st, s));
+        WorkOn work(st, s);
         rc = sample_run(st, logits, any_dt(dtype), ld, M, vocab, params, u, token_out, p_out, nullptr, s, st->done_ev);
         if (rc) return rc;
-        mark_launched(st, s);
+        work.launched();
         return STAGE_OK;
     });
 }
@@ -1778,8 +1796,9 @@ int stage_head_sample(Stage* st, const void* hidden, int M, const StageSampling*
         if ((rc = not_captured(s)) || (rc = ensure_logits(st))) return rc;
         float* lg = logits_out ? logits_out : st->logits;
         if ((rc = stage_head_top1(st, hidden, M, st->head_tok, st->head_p, nullptr, lg, stream))) return rc;
+        WorkOn work(st, s);
         if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token_out, p_out, nullptr, s, st->done_ev))) return rc;
-        mark_launched(st, s);
+        work.launched();
         return STAGE_OK;
     });
 }

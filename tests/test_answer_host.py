@@ -1,0 +1,41 @@
+"""The host code of the last stage's operators around calls that fail, with a
+stand-in for the HIP runtime (hip_host.cpp) and no GPU."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2608_19147_amd import _lib
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    """ask(question, *arguments): what host_stage.py answers."""
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2608_19147_amd import build
+
+        build.build()
+    so = str(tmp_path_factory.mktemp("host") / "hip_host.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", os.path.join(HERE, "hip_host.cpp"), "-o", so], check=True)
+
+    def run(*args):
+        env = {**os.environ, "LD_PRELOAD": so, "STAGE_PERSISTENT": "0", "OPENBLAS_NUM_THREADS": "1"}
+        r = subprocess.run([sys.executable, os.path.join(HERE, "host_stage.py"), *args], env=env, capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stderr
+        return json.loads(r.stdout)
+
+    return run
+
+
+@pytest.mark.parametrize("name", ["product", "product_passes", "product_one_pass", "sample", "top1_mx4", "sample_mx4", "sample_int4"])
+def test_order_behind_a_failed_call(ask, name):
+    """A call whose second or later launch fails has queued work that uses the stage's workspace: the next call, on another
+    stream, waits for it."""
+    seen = ask("order", name)
+    assert seen
+    for q in seen:
+        assert q["rc"] == -5 and q["rc2"] == 0 and q["ordered"], q
