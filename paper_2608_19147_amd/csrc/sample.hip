@@ -1084,8 +1084,10 @@ hipError_t launch_sample(const SampleArgs& a, int m, hipStream_t st, hipEvent_t 
     }
     const dim3 g((unsigned)a.slices, (unsigned)m);
     sample_count_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;                             // nothing behind it: the plan would be an earlier call's
     sample_gather_kernel<<<g, dim3(SB_THREADS), 0, st>>>(a);
-    const hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     return e == hipSuccess ? launch_done(sample_draw_kernel, dim3((unsigned)m), dim3(SB_THREADS), 0, st, done, a) : e;
 }
 

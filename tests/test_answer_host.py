@@ -31,7 +31,19 @@ def ask(tmp_path_factory):
     return run
 
 
-@pytest.mark.parametrize("name", ["product", "product_passes", "product_one_pass", "sample", "top1_mx4", "sample_mx4", "sample_int4"])
+CALLS = ["product", "product_passes", "product_one_pass", "sample", "top1_mx4", "sample_mx4", "sample_int4"]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_nothing_behind_a_failed_launch(ask, name):
+    """The launch that fails is a call's last one: what would come next reads what it did not write."""
+    seen = ask("order", name)
+    assert seen
+    for q in seen:
+        assert q["queued"] == q["at"] - 1, q
+
+
+@pytest.mark.parametrize("name", CALLS)
 def test_order_behind_a_failed_call(ask, name):
     """A call whose second or later launch fails has queued work that uses the stage's workspace: the next call, on another
     stream, waits for it."""
