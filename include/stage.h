@@ -341,7 +341,12 @@ int stage_head_attach(Stage* stage, const uint16_t* final_norm, const QuantMatri
  *                  write; test support).
  * All outputs are device pointers; 1 <= M <= STAGE_MAX_ROWS.  Stream-ordered
  * with the stage's other calls (it uses the stage's workspace).
- * Errors: INVALID (NULL, no head), CAPACITY (M), HIP. */
+ * With a head of stage_head_attach_mx4 a row without a logit above -inf (every
+ * row with a NaN is one) gives token -1, p 0 and logit -inf; +inf ranks as the
+ * largest finite number; a capturing stream is refused; and a call without
+ * logits_out allocates [STAGE_MAX_ROWS][vocab] on first use.
+ * Errors: INVALID (NULL, no head), CAPACITY (M), OOM, HIP; with that head
+ * UNSUPPORTED (capturing stream). */
 int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out, float* p_out, float* logit_out,
                     float* logits_out, void* stream);
 

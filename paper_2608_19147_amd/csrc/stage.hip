@@ -1584,40 +1584,42 @@ int stage_embed(Stage* st, const int32_t* ids, int n, void* hidden_out, void* st
 
 int stage_head_top1(Stage* st, const void* hidden, int M, int32_t* token_out, float* p_out, float* logit_out,
                     float* logits_out, void* stream) {
-    if (!st || !hidden || !token_out || !p_out) return fail(STAGE_E_INVALID, "NULL argument");
-    if (st->head4) return head4_run(st, hidden, M, nullptr, nullptr, token_out, p_out, logit_out, logits_out, stream);
-    if (!st->head_ok) return fail(STAGE_E_INVALID, "no head attached (stage_head_attach)");
-    if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
-    const StageConfig& c = st->cfg;
-    const int H = c.hidden, act_dt = dt_code(c.act_dtype);
-    HIP_TRY(hipSetDevice(st->device));
-    hipStream_t s = (hipStream_t)stream;
-    HIP_TRY(order_on(st, s));
-    WorkOn work(st, s);
-    HIP_TRY(launch_bprep(hidden, act_dt, H, st->final_norm, act_dt, H, c.rms_eps, M, st->bp[0], st->bc[0], st->kp,
-                         st->rsb, s));
-    GemvArgs a{};
-    a.W = st->head.pm;
-    a.M = M;
-    a.kp = st->kp;
-    a.kg = st->head.bp_kg;
-    a.ksplit = 1;
-    a.partial = st->gpart;
-    a.counters = st->gcnt;
-    a.bp_in = st->bp[0];
-    a.bc_in = st->bc[0];
-    a.cb_in = st->cbf[0];
-    a.norm = 2;
-    a.epi = EPI_TOP1;
-    bp_form(a, st->head, M, st->n_cus);
-    a.out = logits_out;
-    a.out_ld = st->vocab;
-    a.top1_part = st->top1_part;
-    HIP_TRY(launch_gemm_bp(a, s));
-    HIP_TRY(launch_top1_merge(st->top1_part, M, st->head.pm.ntiles, token_out, p_out, logit_out, s));
-    work.open = false;
-    HIP_TRY(mark_done(st, s));
-    return STAGE_OK;
+    return guarded([&]() -> int {
+        if (!st || !hidden || !token_out || !p_out) return fail(STAGE_E_INVALID, "NULL argument");
+        if (st->head4) return head4_run(st, hidden, M, nullptr, nullptr, token_out, p_out, logit_out, logits_out, stream);
+        if (!st->head_ok) return fail(STAGE_E_INVALID, "no head attached (stage_head_attach)");
+        if (M < 1 || M > MAX_ROWS) return fail(STAGE_E_CAPACITY, "M must be in [1, STAGE_MAX_ROWS]");
+        const StageConfig& c = st->cfg;
+        const int H = c.hidden, act_dt = dt_code(c.act_dtype);
+        HIP_TRY(hipSetDevice(st->device));
+        hipStream_t s = (hipStream_t)stream;
+        HIP_TRY(order_on(st, s));
+        WorkOn work(st, s);
+        HIP_TRY(launch_bprep(hidden, act_dt, H, st->final_norm, act_dt, H, c.rms_eps, M, st->bp[0], st->bc[0], st->kp,
+                             st->rsb, s));
+        GemvArgs a{};
+        a.W = st->head.pm;
+        a.M = M;
+        a.kp = st->kp;
+        a.kg = st->head.bp_kg;
+        a.ksplit = 1;
+        a.partial = st->gpart;
+        a.counters = st->gcnt;
+        a.bp_in = st->bp[0];
+        a.bc_in = st->bc[0];
+        a.cb_in = st->cbf[0];
+        a.norm = 2;
+        a.epi = EPI_TOP1;
+        bp_form(a, st->head, M, st->n_cus);
+        a.out = logits_out;
+        a.out_ld = st->vocab;
+        a.top1_part = st->top1_part;
+        HIP_TRY(launch_gemm_bp(a, s));
+        HIP_TRY(launch_top1_merge(st->top1_part, M, st->head.pm.ntiles, token_out, p_out, logit_out, s));
+        work.open = false;
+        HIP_TRY(mark_done(st, s));
+        return STAGE_OK;
+    });
 }
 
 int stage_mx4_quantize(Stage* st, const void* x, int dtype, int64_t ld, int m, int k, uint8_t* codes, uint8_t* scales, void* stream) {

@@ -98,7 +98,9 @@ const char* hipGetErrorString(int) { return "error of the stand-in"; }
 
 // Notes start anew: launch `at` (from 1 on) fails, 0 none; and so does the `alloc`-th operator new.
 void host_start(int at, long alloc, int capture) {
+    alloc_fail_at = 0;
     notes.clear();
+    notes.reserve(1 << 20);                    // taking notes allocates nothing
     launches = 0;
     fail_at = at;
     allocs = 0;

@@ -103,5 +103,21 @@ def order(name):
     return out
 
 
+def allocations(name, capture):
+    """Statuses of the call while its first, second, ... host allocation fails, up to the one that needs no more."""
+    out = []
+    for n in range(1, 40):
+        st = make_stage()
+        f = call(st, name)
+        host.host_start(0, n, int(capture))
+        rc = f(1)
+        host.host_start(0, 0, 0)
+        out.append(rc)
+        lib.stage_destroy(st)
+        if rc != -4:
+            break
+    return out
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*sys.argv[2:])))

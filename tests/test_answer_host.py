@@ -51,3 +51,13 @@ def test_order_behind_a_failed_call(ask, name):
     assert seen
     for q in seen:
         assert q["rc"] == -5 and q["rc2"] == 0 and q["ordered"], q
+
+
+@pytest.mark.parametrize("name", CALLS + ["top1_int4"])
+@pytest.mark.parametrize("capture", [0, 1])
+def test_no_host_memory(ask, name, capture):
+    """A host allocation that fails is STAGE_E_OOM, and no exception leaves the call; the last status is that of the call
+    with memory."""
+    got = ask("allocations", name, str(capture))
+    assert got[:-1] == [-4] * (len(got) - 1)
+    assert got[-1] == (-7 if capture and name != "top1_int4" else 0)

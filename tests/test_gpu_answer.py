@@ -128,3 +128,23 @@ def test_draw_between_bins(stage, V):
             assert t in (99, 100)
             w = np.exp(row - row[0])
             assert abs(q - w[t] / w.sum()) <= q * (2.0 ** -24 + 3e-8)
+
+
+def test_head_row_without_a_token():
+    """A hidden row with a NaN or an infinity has no token through an MXFP4 head: -1, probability 0, from both calls; the
+    rows beside it have theirs."""
+    shape = synth.TINY
+    p = Pair(shape, 357, with_oracle=False)
+    fn, _ = synth.make_head(shape, 64, 357)
+    w = torch.from_numpy(np.random.default_rng(358).standard_normal((1003, shape.hidden)) * 0.02).float().cuda()
+    p.gpu.attach_head_mx4(fn.cuda(), *p.gpu.mx4_quantize(w))
+    x = synth.make_hidden(shape, 4, 359)
+    want = [t.tolist() for t in p.gpu.head_top1(x.cuda())[:3]]
+    x[1, 7], x[2, 0] = float("nan"), float("inf")
+    tok, pr, top, lg = p.gpu.head_top1(x.cuda(), with_logits=True)
+    assert bool(torch.isnan(lg[1:3]).all())
+    assert tok.tolist() == [want[0][0], -1, -1, want[0][3]] and pr.tolist() == [want[1][0], 0.0, 0.0, want[1][3]]
+    assert top.tolist() == [want[2][0], -np.inf, -np.inf, want[2][3]]
+    tok, pr, _ = p.gpu.head_sample(x.cuda(), Sampling(), torch.full((4,), 0.5, device="cuda"))
+    assert tok[1:3].tolist() == [-1, -1] and pr[1:3].tolist() == [0.0, 0.0] and min(tok[0].item(), tok[3].item()) >= 0
+    p.close()
