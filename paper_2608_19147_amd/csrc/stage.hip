@@ -725,15 +725,12 @@ int sample_run(Stage* st, const void* logits, int dt, int64_t ld, int M, int V, 
     return STAGE_OK;
 }
 
-int ensure_logits(Stage* st) {
-    if (st->logits) return STAGE_OK;
-    float* l = nullptr;
-    int rc = st->head_p ? STAGE_OK : st->alloc(&st->head_p, MAX_ROWS);
-    if (!rc && !st->head_tok) rc = st->alloc(&st->head_tok, MAX_ROWS);
-    if (!rc) rc = st->alloc(&l, (size_t)MAX_ROWS * st->vocab);
-    if (!rc) st->logits = l;
-    return rc;
+// A buffer of the head's calls, allocated on first need.
+template <class T>
+int ensure(Stage* st, T** p, size_t n) {
+    return *p ? STAGE_OK : st->alloc(p, n);
 }
+int ensure_logits(Stage* st) { return ensure(st, &st->logits, (size_t)MAX_ROWS * st->vocab); }
 
 // RMSNorm, the MXFP4 head and, per row, a token: params and u as in sample_run.
 int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params, const float* u, int32_t* token, float* p,
@@ -1795,7 +1792,9 @@ int stage_head_sample(Stage* st, const void* hidden, int M, const StageSampling*
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
-        if ((rc = not_captured(s)) || (rc = ensure_logits(st))) return rc;
+        if ((rc = not_captured(s)) || (!logits_out && (rc = ensure_logits(st))) || (rc = ensure(st, &st->head_tok, MAX_ROWS)) ||
+            (rc = ensure(st, &st->head_p, MAX_ROWS)))
+            return rc;
         float* lg = logits_out ? logits_out : st->logits;
         if ((rc = stage_head_top1(st, hidden, M, st->head_tok, st->head_p, nullptr, lg, stream))) return rc;
         WorkOn work(st, s);

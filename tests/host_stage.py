@@ -119,5 +119,14 @@ def allocations(name, capture):
     return out
 
 
+def largest_allocation(name):
+    """Bytes of the largest device allocation that the stage's first such call makes, beside a [64][VOCAB] array of logits."""
+    st = make_stage()
+    f = call(st, name)
+    host.host_start(0, 0, 0)
+    assert f(1) == 0
+    return host.host_largest_malloc(), 64 * VOCAB * 4
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*sys.argv[2:])))

@@ -61,3 +61,12 @@ def test_no_host_memory(ask, name, capture):
     got = ask("allocations", name, str(capture))
     assert got[:-1] == [-4] * (len(got) - 1)
     assert got[-1] == (-7 if capture and name != "top1_int4" else 0)
+
+
+@pytest.mark.parametrize("name", ["top1_mx4", "sample_mx4", "sample_int4"])
+def test_logits_workspace(ask, name):
+    """Logits rows are allocated for calls that give none, and only for those."""
+    most, logits = ask("largest_allocation", name)
+    assert most == logits
+    most, logits = ask("largest_allocation", name + "_logits")
+    assert most < logits
