@@ -18,8 +18,8 @@ import torch
 from . import _lib
 from ._lib import check
 
-# the current stream's handle of a device (what torch.cuda.current_stream(i).cuda_stream holds, without its objects)
-from torch._C import _cuda_getCurrentRawStream as _raw_stream
+# The current stream's handle of a device: by a name that torch keeps to itself, which makes no objects, where it is there.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 MATRIX_NAMES = ("wq", "wk", "wv", "wo", "wg", "wu", "wd")
 _DT = {"f16": _lib.DTYPE_F16, "bf16": _lib.DTYPE_BF16}

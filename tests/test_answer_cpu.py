@@ -3,6 +3,8 @@ work, the drafted tree's bookkeeping, and the binding's argument forms."""
 import ctypes
 import os
 import struct
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -158,3 +160,10 @@ def test_chain_is_step_inputs():
     assert (pos == tpos).all()
     tri = np.tril(np.ones((3, 3), np.uint8))
     assert (rows == mask[:, None] * np.concatenate([np.ones((3, 4), np.uint8), tri], 1)[None]).all()
+
+
+def test_import_without_cuda_names():
+    """The package, its driver and its binding import with a torch that has no streams, as CPU builds of it have none."""
+    code = ("import torch\ndel torch._C._cuda_getCurrentRawStream\n"
+            "import paper_2608_19147_amd.stage as s, paper_2608_19147_amd.driver\nassert callable(s._raw_stream)")
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
