@@ -92,6 +92,11 @@ def _on(stage, stream, device):
     return int(stream.cuda_stream), empty
 
 
+def _weights_on(stage, stream, t: torch.Tensor) -> int:
+    """The stream handle of a call that packs weights from ``t``, on the stage's device or on the host."""
+    return _on(stage, stream, t.device if t.is_cuda else torch.device("cuda", stage.device_index))[0]
+
+
 class Stage:
     """One pipeline stage on the current GPU.
 
@@ -253,14 +258,13 @@ class Stage:
         [vocab, ceil(H/2)], scales uint8 [vocab, ceil(H/32)], all on the host or
         all on the device."""
         on_dev = _check_mx4(codes, scales, self.shape.hidden)
-        if on_dev:
-            _on(self, None, codes.device)
+        sp = _weights_on(self, stream, codes)
         if tuple(final_norm.shape) != (self.shape.hidden,) or final_norm.dtype != self.act_dtype or not final_norm.is_contiguous():
             raise ValueError("final_norm must be a contiguous [hidden] tensor in the activation dtype")
         if final_norm.device != codes.device:
             raise ValueError("final_norm, codes and scales must be on one device")
         check(self.lib.stage_head_attach_mx4(self.handle, final_norm.data_ptr(), codes.data_ptr(), scales.data_ptr(),
-                                             codes.shape[0], on_dev, _stream_ptr(stream)))
+                                             codes.shape[0], on_dev, sp))
         self.vocab = int(codes.shape[0])
 
     def head_sample(self, hidden: torch.Tensor, params, u: torch.Tensor, with_logits: bool = False, stream=None):
@@ -469,13 +473,12 @@ class Mx4Matrix:
 
     def __init__(self, stage: Stage, codes: torch.Tensor, scales: torch.Tensor, k: int, stream=None):
         on_dev = _check_mx4(codes, scales, k)
-        if on_dev:
-            _on(stage, None, codes.device)
+        sp = _weights_on(stage, stream, codes)
         self.stage, self.lib = stage, stage.lib
         self.n, self.k = int(codes.shape[0]), int(k)
         h = ctypes.c_void_p()
         check(self.lib.stage_mx4_create(stage.handle, codes.data_ptr(), scales.data_ptr(), self.n, self.k, on_dev,
-                                        _stream_ptr(stream), ctypes.byref(h)))
+                                        sp, ctypes.byref(h)))
         self.handle = h
         _LIVE_MATRICES.add(self)
 

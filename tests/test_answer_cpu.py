@@ -5,6 +5,7 @@ import os
 import struct
 import subprocess
 import sys
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -167,3 +168,33 @@ def test_import_without_cuda_names():
     code = ("import torch\ndel torch._C._cuda_getCurrentRawStream\n"
             "import paper_2608_19147_amd.stage as s, paper_2608_19147_amd.driver\nassert callable(s._raw_stream)")
     subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
+class _Lib:
+    """Takes every call of the binding and notes its arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+def test_weights_go_by_the_stage_device(monkeypatch):
+    """MXFP4 weights are packed on the current stream of the stage's device, whatever device is current, or on a stream of
+    that device; a stream of another one is refused."""
+    from paper_2608_19147_amd import Mx4Matrix, Stage, stage as binding
+
+    monkeypatch.setattr(binding, "_raw_stream", lambda index: 1000 + index)
+    st = Stage.__new__(Stage)
+    st.lib, st.handle, st.device_index = _Lib(), None, 3
+    st.shape, st.act_dtype = SimpleNamespace(hidden=64), torch.float16
+    codes, scales, norm = torch.zeros((5, 32), dtype=torch.uint8), torch.zeros((5, 2), dtype=torch.uint8), torch.ones(64, dtype=torch.float16)
+    makers = (lambda **kw: Mx4Matrix(st, codes, scales, 64, **kw), lambda **kw: st.attach_head_mx4(norm, codes, scales, **kw))
+    for make in makers:
+        make()
+        assert st.lib.calls[-1][1][6] == 1003
+        make(stream=SimpleNamespace(device=torch.device("cuda", 3), cuda_stream=77))
+        assert st.lib.calls[-1][1][6] == 77
+        with pytest.raises(ValueError, match="stream"):
+            make(stream=SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=77))
