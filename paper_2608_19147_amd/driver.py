@@ -63,10 +63,14 @@ class VerifyDriver:
         verifies a drafted tree per slot: parents [S, n], every node's parent before
         it, node 0 (the last accepted token) the root.  A node sees the slot's valid
         rows, its ancestors and itself; its position is the number of valid rows plus
-        its depth.  Applies the reorder to the valid masks first (it persists)."""
+        its depth.  Applies the reorder to the valid masks first (it persists, unless the
+        call is refused)."""
+        valid = self.valid
         if beam_idx is not None:
             beam_idx = np.asarray(beam_idx, np.int32)
-            self.valid = self.valid[beam_idx]
+            if beam_idx.shape != (self.n_slots,) or not ((beam_idx >= 0) & (beam_idx < self.n_slots)).all():
+                raise ValueError("beam_idx must name a slot for each slot")
+            valid = valid[beam_idx]
         parents = np.asarray(parents)
         s, n = parents.shape
         if s != self.n_slots or n < 1 or (n > 1 and not ((parents[:, 1:] >= 0) & (parents[:, 1:] < np.arange(1, n))).all()):
@@ -79,8 +83,9 @@ class VerifyDriver:
             see[:, i] = see[slot, parents[:, i]]
             see[:, i, i] = 1
             depth[:, i] = depth[slot, parents[:, i]] + 1
-        past = np.broadcast_to(self.valid[:, None, :], (s, n, self.physical_len))
-        positions = self.valid.sum(axis=1).astype(np.int32)[:, None] + depth
+        self.valid = valid
+        past = np.broadcast_to(valid[:, None, :], (s, n, self.physical_len))
+        positions = valid.sum(axis=1).astype(np.int32)[:, None] + depth
         return positions, np.concatenate([past, see], axis=2), beam_idx
 
     def accept_tree(self, keep: np.ndarray) -> np.ndarray:

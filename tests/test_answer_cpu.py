@@ -198,3 +198,16 @@ def test_weights_go_by_the_stage_device(monkeypatch):
         assert st.lib.calls[-1][1][6] == 77
         with pytest.raises(ValueError, match="stream"):
             make(stream=SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=77))
+
+
+@pytest.mark.parametrize("parents,beam", [([[-1, 1], [-1, 0]], [1, 0]), ([[-1, 0]], [1, 0]), ([[-1, 0], [-1, 0]], [0]), ([[-1, 0], [-1, 0]], [0, 2])])
+def test_refused_tree_leaves_the_slots(parents, beam):
+    """A tree or an order of the slots that is refused has not reordered them: the call can be made again."""
+    d = VerifyDriver(2, 3)
+    d.valid[0, 2] = 0
+    was = d.valid.copy()
+    with pytest.raises((ValueError, IndexError)):
+        d.tree_inputs(np.array(parents), np.array(beam))
+    assert np.array_equal(d.valid, was) and d.n_slots == 2
+    pos, _, _ = d.tree_inputs(np.array([[-1, 0]] * 2), np.array([1, 0]))
+    assert pos.tolist() == [[3, 4], [2, 3]]
