@@ -31,6 +31,7 @@ class VerifyDriver:
     def __init__(self, n_slots: int, past: int):
         self.n_slots = n_slots
         self.valid = np.ones((n_slots, past), np.uint8)
+        self._nodes: Optional[int] = None                     # of the last tree_inputs, until its nodes are recorded
 
     @property
     def physical_len(self) -> int:
@@ -83,7 +84,7 @@ class VerifyDriver:
             see[:, i] = see[slot, parents[:, i]]
             see[:, i, i] = 1
             depth[:, i] = depth[slot, parents[:, i]] + 1
-        self.valid = valid
+        self.valid, self._nodes = valid, n
         past = np.broadcast_to(valid[:, None, :], (s, n, self.physical_len))
         positions = valid.sum(axis=1).astype(np.int32)[:, None] + depth
         return positions, np.concatenate([past, see], axis=2), beam_idx
@@ -94,5 +95,7 @@ class VerifyDriver:
         keep = (np.asarray(keep) != 0).astype(np.uint8)
         if keep.ndim != 2 or keep.shape[0] != self.n_slots:
             raise ValueError("keep must be [slots, nodes]")
-        self.valid = np.concatenate([self.valid, keep], axis=1)
+        if self._nodes not in (None, keep.shape[1]):
+            raise ValueError(f"keep has {keep.shape[1]} nodes, the tree {self._nodes}")
+        self.valid, self._nodes = np.concatenate([self.valid, keep], axis=1), None
         return keep.sum(axis=1).astype(np.int32)

@@ -211,3 +211,15 @@ def test_refused_tree_leaves_the_slots(parents, beam):
     assert np.array_equal(d.valid, was) and d.n_slots == 2
     pos, _, _ = d.tree_inputs(np.array([[-1, 0]] * 2), np.array([1, 0]))
     assert pos.tolist() == [[3, 4], [2, 3]]
+
+
+def test_kept_nodes_are_those_of_the_tree():
+    """The nodes recorded are those of the last forward's tree: another number of them would shift every later mask."""
+    d = VerifyDriver(2, 3)
+    d.tree_inputs(np.array([[-1, 0, 1]] * 2))
+    for n in (2, 4):
+        with pytest.raises(ValueError):
+            d.accept_tree(np.ones((2, n), np.uint8))
+    assert d.physical_len == 3
+    assert d.accept_tree(np.array([[1, 1, 0], [1, 0, 0]], np.uint8)).tolist() == [2, 1]
+    assert d.physical_len == 6
