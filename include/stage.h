@@ -404,7 +404,8 @@ int stage_mx4_free(Mx4Matrix* matrix);
  *                (its larger elements exactly);
  *   act_bits  4: x (any dtype) is rounded to MXFP4 first (stage_mx4_quantize).
  * A row of x with a NaN or an infinity gives NaN, as does a NaN scale of W in
- * its column.  1 <= m <= STAGE_MAX_PREFILL.  out must not overlap x.  Allocates a
+ * its column.  The order in which a row's sums are added, and with it the last bits,
+ * depends on m.  1 <= m <= STAGE_MAX_PREFILL.  out must not overlap x.  Allocates a
  * workspace on first use (kept, grown when a larger product comes).
  * Errors: INVALID (NULL, dtype, act_bits), SHAPE (strides), CAPACITY (m),
  * UNSUPPORTED (F32 rows with act_bits 16; a capturing stream with m above 64), OOM, HIP. */
@@ -415,7 +416,8 @@ int stage_mx4_product(Mx4Matrix* matrix, const void* x, int x_dtype, int64_t ldx
  * the stage's own weights).  stage_head_top1 and stage_head_sample then use it:
  * RMSNorm rows in fp32, which enter the product as 3 block-scaled E4M3 terms
  * (within 2^-12 of each element, or 2^-18 of the largest of its block of 32).
- * Synchronizes the stream.  One head per stage.
+ * A row's logits are the same bits whatever rows come with it.  Synchronizes the
+ * stream.  One head per stage.
  * Errors: INVALID (NULL), SHAPE (vocab < 1), CAPACITY (vocab), UNSUPPORTED
  * (already attached, capturing stream), OOM, HIP. */
 int stage_head_attach_mx4(Stage* stage, const uint16_t* final_norm, const uint8_t* codes, const uint8_t* scales, int vocab,

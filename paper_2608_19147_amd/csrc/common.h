@@ -372,8 +372,8 @@ struct Mx4Gemm {
     float* part; int part_ld;                      // split > 1: their sums [split][32 a.tiles][part_ld]
     int mtiles;                                    // set by the launcher
 };
-// Sets mt, split and steps_per for p.w and p.a; the time that they should take, in us.
-float mx4_plan(Mx4Gemm& p, int n_cus);
+// Sets mt, split (only_split if that is not 0) and steps_per for p.w and p.a; the time that they should take, in us.
+float mx4_plan(Mx4Gemm& p, int n_cus, int only_split = 0);
 // A launch that signals `done` (or nothing) at its end: 2.5 us of host time where an event recorded behind it takes 5.8.
 template <class... A>
 hipError_t launch_done(void (*kernel)(A...), dim3 grid, dim3 block, unsigned lds, hipStream_t st, hipEvent_t done, A... args) {

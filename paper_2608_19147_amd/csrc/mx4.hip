@@ -981,8 +981,9 @@ hipError_t run_pipe(Mx4Gemm p, hipStream_t st, hipEvent_t done) {
 // products take small tiles (300 x 300 x 300 with 4-bit rows: 13, 15 and 21 us with MT
 // 1, 2 and 4); where MT 4 has one workgroup a CU, each round pays it.  Splits cost a
 // launch and their sums' way to memory and back (33 x 256 x 14336: 64 us unsplit, 20 in
-// 16 splits; 700 x 2048 x 700: 15 and 21 in two).
-float mx4_plan(Mx4Gemm& p, int n_cus) {
+// 16 splits; 700 x 2048 x 700: 15 and 21 in two).  The split alone says in which order
+// a row's sums are added.
+float mx4_plan(Mx4Gemm& p, int n_cus, int only_split) {
     constexpr int MTS[3] = {1, 2, 4};
     constexpr float START[3] = {0.0f, 1.8f, 6.5f};
     constexpr float STEP[2][3] = {{0.15f, 0.185f, 0.25f}, {0.35f, 0.55f, 0.75f}};      // one E2M1 term, three E4M3 terms
@@ -996,7 +997,7 @@ float mx4_plan(Mx4Gemm& p, int n_cus) {
         const float wgs = (float)((p.a.tiles + MTS[i] - 1) / MTS[i]) * (float)((p.w.groups + 3) / 4);
         for (int s = 1; s <= MAX_SPLIT && s <= units; ++s) {
             const int per = (units + s - 1) / s, split = (units + per - 1) / per;
-            if (split != s) continue;
+            if (split != s || (only_split && s != only_split)) continue;
             float rounds = fmaxf(1.0f, wgs * (float)s / (float)n_cus);
             if (MTS[i] < 4 || p.a.terms) rounds = ceilf(rounds);       // else two workgroups a CU fill each other's gaps
             const float us = BASE + rounds * (float)(per * 4) * step[i] + (MTS[i] == 4 && p.a.terms ? rounds : 1.0f) * START[i] +

@@ -639,9 +639,10 @@ constexpr int MX4_PASS = 2048;                             // rows of one produc
 
 int mx4_terms(int act) { return act == 4 ? 0 : 3; }
 
-// out = x W^T on stream s; act 4 or 16 (E4M3 terms).  done: signalled by the last launch, or null.
+// out = x W^T on stream s; act 4 or 16 (E4M3 terms).  done: signalled by the last launch, or null.  alike: K is split as for
+// one tile of rows, so that a row's sums are the same bits whatever m is (64 rows of 32000 x 4096 in two splits then).
 int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int m, int act, void* out, int odt, int64_t ldo,
-            hipStream_t s, hipEvent_t done) {
+            bool alike, hipStream_t s, hipEvent_t done) {
     const size_t xb = dt == DT_F32 ? 4 : 2, ob = odt == DT_F32 ? 4 : 2;
     for (int m0 = 0; m0 < m; m0 += MX4_PASS) {
         const int mm = std::min(MX4_PASS, m - m0);
@@ -663,7 +664,14 @@ int mx4_run(Stage* st, const Mx4Mat& w, const void* x, int dt, int64_t ldx, int 
         p.out = (uint8_t*)out + (size_t)m0 * ldo * ob;
         p.dt = odt;
         p.ld = (size_t)ldo;
-        mx4_plan(p, st->n_cus);
+        if (alike) {
+            Mx4Gemm one = p;
+            one.a.tiles = 1;
+            mx4_plan(one, st->n_cus);
+            mx4_plan(p, st->n_cus, one.split);
+        } else {
+            mx4_plan(p, st->n_cus);
+        }
         p.part_ld = 64 * w.groups;
         if (p.split > 1) {
             if ((rc = grow(&st->mx_p, &st->mx_p_cap, (size_t)p.split * a.tiles * 32 * p.part_ld * 4))) return rc;
@@ -747,7 +755,7 @@ int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params,
     HIP_TRY(order_on(st, s));
     WorkOn work(st, s);
     HIP_TRY(launch_rms_rows(hidden, dt_code(c.act_dtype), st->final_norm, M, c.hidden, c.rms_eps, st->head_rows, s));
-    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F32, c.hidden, M, 16, lg, DT_F32, st->vocab, s, nullptr))) return rc;
+    if ((rc = mx4_run(st, st->head4->m, st->head_rows, DT_F32, c.hidden, M, 16, lg, DT_F32, st->vocab, true, s, nullptr))) return rc;
     if ((rc = sample_run(st, lg, DT_F32, st->vocab, M, st->vocab, params, u, token, p, top, s, st->done_ev))) return rc;
     work.launched();
     return STAGE_OK;
@@ -1713,7 +1721,7 @@ int stage_mx4_product(Mx4Matrix* w, const void* x, int x_dtype, int64_t ldx, int
         }
         HIP_TRY(order_on(st, s));
         WorkOn work(st, s);
-        int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, s, st->done_ev);
+        int rc = mx4_run(st, w->m, x, any_dt(x_dtype), ldx, m, act_bits, out, any_dt(out_dtype), ldo, false, s, st->done_ev);
         if (rc) return rc;
         work.launched();
         return STAGE_OK;

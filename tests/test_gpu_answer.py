@@ -148,3 +148,20 @@ def test_head_row_without_a_token():
     tok, pr, _ = p.gpu.head_sample(x.cuda(), Sampling(), torch.full((4,), 0.5, device="cuda"))
     assert tok[1:3].tolist() == [-1, -1] and pr[1:3].tolist() == [0.0, 0.0] and min(tok[0].item(), tok[3].item()) >= 0
     p.close()
+
+
+def test_head_rows_alike():
+    """A row's logits through an MXFP4 head, bit for bit, whether it comes alone, in a verify or among 64 rows (K is long
+    enough here for the rows' number to matter to how a product splits it)."""
+    shape = synth.StageShape("alike", 16, n_layers=1, hidden=1024, n_q_heads=2, n_kv_heads=1, head_dim=128, ffn=512)
+    p = Pair(shape, 360, with_oracle=False)
+    fn, _ = synth.make_head(shape, 64, 360)
+    w = torch.from_numpy(np.random.default_rng(361).standard_normal((1000, shape.hidden)) * 0.02).float().cuda()
+    p.gpu.attach_head_mx4(fn.cuda(), *p.gpu.mx4_quantize(w))
+    x = synth.make_hidden(shape, 64, 362).cuda()
+    u = torch.from_numpy(np.random.default_rng(363).random(64).astype(np.float32)).cuda()
+    tok, pr, lg = p.gpu.head_sample(x, Sampling(0.9, 0, 0.95), u, with_logits=True)
+    for a, b in ((0, 1), (7, 27), (20, 53), (63, 64)):
+        t, q, z = p.gpu.head_sample(x[a:b].clone(), Sampling(0.9, 0, 0.95), u[a:b].clone(), with_logits=True)
+        assert torch.equal(z, lg[a:b]) and torch.equal(t, tok[a:b]) and torch.equal(q, pr[a:b])
+    p.close()
