@@ -165,3 +165,15 @@ def test_head_rows_alike():
         t, q, z = p.gpu.head_sample(x[a:b].clone(), Sampling(0.9, 0, 0.95), u[a:b].clone(), with_logits=True)
         assert torch.equal(z, lg[a:b]) and torch.equal(t, tok[a:b]) and torch.equal(q, pr[a:b])
     p.close()
+
+
+@pytest.mark.parametrize("value", [0.0, float(np.finfo(np.float32).min), float(np.finfo(np.float32).max), -1e-45])
+def test_equal_extremes_by_index(stage, value):
+    """300 equal logits at the ends of the range, some -inf ones between them: u of them by count, exactly."""
+    z = torch.full((400,), -np.inf)
+    at = np.sort(np.random.default_rng(364).permutation(400)[:300])
+    z[torch.from_numpy(at)] = value
+    us = np.array([0.0, 1 / 300, 0.1, 1 / 3, 0.5, 0.7, 0.99, 1 - 2.0 ** -24], np.float32)
+    tok, p = stage.sample(z.cuda()[None].repeat(len(us), 1), Sampling(), torch.from_numpy(us).cuda())
+    assert tok.tolist() == [at[int(float(u) * 300)] for u in us]
+    assert (p.double() - 1 / 300).abs().max().item() <= 2.0 ** -24 / 300
