@@ -368,7 +368,7 @@ int stage_head_top1(Stage* stage, const void* hidden, int M, int32_t* token_out,
  * and refuse a capturing stream (STAGE_E_UNSUPPORTED), but for stage_mx4_product of
  * up to 64 rows: it has a form without a workspace, taken where that is faster and on
  * every capturing stream (where K or n is long that costs time there: 16 rows of 4096
- * by 14336 outputs 40 us instead of 19; and sums are added in another order).  The
+ * by 14336 outputs 49 us instead of 20; and sums are added in another order).  The
  * calling thread's current device is left as it was.
  * ------------------------------------------------------------------------ */
 

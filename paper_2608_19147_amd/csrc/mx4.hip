@@ -784,10 +784,13 @@ __global__ __launch_bounds__(256, T ? 1 : 2) void mx4_pipe_kernel(Mx4Gemm p) {
 // terms that every workgroup makes for itself the larger part, the rows are
 // prepared once instead (mx4_rows_direct below).  One row of 4096 x 4096: 4.9 us, of
 // which the weights' 8.9 MB could be read in 1.8.
-constexpr int ROW_WAVES = 8, ROW_BATCH = 4, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
+constexpr int ROW_WAVES = 8, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
 __global__ __launch_bounds__(64 * ROW_WAVES) void mx4_rows_kernel(Mx4Gemm p, const void* __restrict__ x, size_t ldx, int seg) {
     constexpr int NT = T ? T : 1, U = T ? 2 : 1, FMT = T ? 0 : 4;
+    // chunks whose weights are on their way at once: with three terms 4 took 165 registers, one workgroup a CU where 2 take
+    // 107, two (one row of 28672 x 8192: 42 and 30 us)
+    constexpr int ROW_BATCH = T ? 2 : 4;
     typedef float v4f __attribute__((ext_vector_type(4)));
     // fragments [chunk][term][half][block or quarter kb][row]; scales [chunk][term][row] words of 4 blocks; sums
     __shared__ __attribute__((aligned(16))) uint8_t frags[ROW_LDS];
@@ -1015,11 +1018,13 @@ float mx4_plan(Mx4Gemm& p, int n_cus, int only_split) {
 
 // Whether up to 64 rows go through mx4_rows_kernel: its workgroups share CUs, each
 // makes the terms of 16 rows for itself (TERMS, us for 1000 values) after START, and
-// reads weights.  16 x 4096 x 4096 in two terms: 14.5 us so, 17 through the plan's three
-// launches; 16 x 14336 x 4096: 40 and 19; one row of 14336 x 14336: 26 and 30.
+// reads weights.  8 x 4096 x 4096 in three terms: 9.9 us so, 18.9 through the plan's three
+// launches; 16 x 14336 x 4096: 49 and 20; one row of 14336 x 14336: 29 and 34, two: 35
+// and 34.  The picks of 196 sizes from 64 x 256 to 28672 x 14336 and 1 to 64 rows are the
+// faster way or within 10% of it but for three (13 to 19% where K is long).
 bool mx4_rows_direct(const Mx4Gemm& rows, int n_cus) {
     constexpr float BASE = 6.0f, SHARE = 0.65f, RATE = 16e6f;
-    constexpr float START[2] = {0.8f, 2.0f}, TERMS[2] = {0.06f, 0.21f};
+    constexpr float START[2] = {0.8f, 1.0f}, TERMS[2] = {0.06f, 0.21f};
     Mx4Gemm p = rows;
     if (p.m > MX4_ROWS_MAX) return false;
     const int t = p.a.terms ? 1 : 0;
