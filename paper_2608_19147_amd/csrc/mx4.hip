@@ -21,8 +21,8 @@
 // come within 2^-18 of a block's largest magnitude, and the larger elements are
 // exact.  (Two terms, 2^-14, kept some 6 of the 8 bits of a bf16 element 2^-8
 // below its block's largest: 16-bit results were 3e-4 apart from those of products
-// in fp32, single ones by a step; three terms take 87 us at 517 x 4096 x 14336 and
-// one row of 4096 x 4096 6.9, two took 66 and 6.7.)
+// in fp32, single ones by a step; three terms take 85 us at 517 x 4096 x 14336 and
+// 7.0 for one row of 4096 x 4096, two took 66 and 6.7.)
 // Activations of 4 bits are one E2M1 term.
 #include "device.h"
 
@@ -132,9 +132,11 @@ hipError_t launch_mx4_quantize(const void* x, int dt, int64_t ld, int m, int k, 
     return hipGetLastError();
 }
 
-// Eight values a thread.  Bound by memory: 17/32 bytes a value read, 2 written (16
-// bits; 2048 x 14336: 20 us, 3.7 TB/s, mostly writes).  PAST_L2: the values are stored past the L2s, which they would fill (2048 x
-// 14336 rounded and back: 36.6 us through them, 32.6 past them).
+// Eight values a thread.  Reads 17/32 bytes a value and writes 2 (16 bits; 2048 x 14336:
+// 20 us, 3.7 TB/s).  Bound by the issue of vector instructions, 29 a value: 12,800 a SIMD
+// in 42,800 busy cycles; a fill writes as much in 10 us.  PAST_L2: the values are stored
+// past the L2s, which they would fill (2048 x 14336 rounded and back: 36.6 us through
+// them, 32.6 past them).
 template <int DT, bool PAST_L2>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                              int m, int k, int chunks, void* __restrict__ out, size_t ld) {
@@ -307,8 +309,8 @@ __device__ __forceinline__ uint32_t top16(const float (&v)[16]) {
 // neighbours and share its largest magnitude.  A workgroup takes 32 rows by two
 // steps: it reads 256 bytes of a 16-bit row and writes whole fragments.  Rows from
 // m and columns from k on are zero.  T terms of E4M3 (T = 0: one E2M1 term).  Bound
-// by memory (517 x 14336 in two terms: 14.8 MB read, 33 written, 7.7 us), for few
-// rows by its launch (20 x 4096 in three: 4.4 us).
+// by memory (517 x 14336 in three terms: 14.8 MB read, 24 written, 9.0 us), for few
+// rows by its launch (20 x 4096 in three: 5.1 us).
 template <int T, int DT>
 __global__ __launch_bounds__(256) void mx4_prep_kernel(const void* __restrict__ x, size_t ld, int m, int k, int steps,
                                                        uint8_t* __restrict__ a, uint8_t* __restrict__ as) {
@@ -557,8 +559,8 @@ __device__ __forceinline__ int xcd_run(int bid, int nwg) {
 // buffered; W's go from memory to the registers that the product reads, each
 // used for MT tiles.  T terms of E4M3 (0: one of E2M1), KS steps a buffer.  With few
 // rows bound by reading the weights (20 x 128256 x 4096: 53 us, 5.2 TB/s), with some
-// hundred by what a CU reads, 12 KB a step of one tile at some 50 GB/s (256 x 4096 x
-// 4096: 15 us; a second set of waves on the other half of K gained 3%).
+// hundred by what a CU reads, 14 KB a step of one tile with three terms, 0.35 us (256 x
+// 4096 x 4096: 19 us; a second set of waves on the other half of K gained 3%).
 //
 // split > 1: fp32 sums to part [split][tiles of 32 rows][n], joined by mx4_reduce_kernel.
 template <int T, int MT, int KS>
@@ -663,8 +665,10 @@ __global__ __launch_bounds__(256) void mx4_gemm_kernel(Mx4Gemm p) {
 
 // The same product for many rows, where the matrix cores are to be the bound: 2048 x
 // 28672 x 8192 with 4-bit rows runs at 3.7 to 4.0 PFLOP/s.  Random codes draw so much
-// power there that the clock falls to 1.5 GHz from 2.1 with equal ones (same cycles),
-// where the instruction alone could do 5; the rest is starts and stores.
+// power that the clock falls to 1.5 GHz from 2.1 with equal ones (same cycles); the
+// instruction alone, out of registers, does 6.5 on them.  A product is at work in 57% of
+// a CU's cycles: the others are starts, stores and the end of 3.5 rounds of workgroups.
+// With three terms (517 x 4096 x 14336: 76 us) it is at work in 87%.
 // A step of 64 k is 2 MT NT products of 32 or 64 cycles a wave, and with 16-bit rows
 // one wave a SIMD, which issues in order: whatever the wave waits for or cannot issue
 // leaves the matrix core idle.  So
@@ -782,7 +786,7 @@ __global__ __launch_bounds__(256, T ? 1 : 2) void mx4_pipe_kernel(Mx4Gemm p) {
 // Bound by the latency of one read after a launch and by fetching the code, so
 // there is one copy of the conversion; where many outputs or long rows make the
 // terms that every workgroup makes for itself the larger part, the rows are
-// prepared once instead (mx4_rows_direct below).  One row of 4096 x 4096: 4.9 us, of
+// prepared once instead (mx4_rows_direct below).  One row of 4096 x 4096: 5.4 us, of
 // which the weights' 8.9 MB could be read in 1.8.
 constexpr int ROW_WAVES = 8, ROW_LDS = 48 * 1024, ROW_SEG = 128 * ROW_WAVES;
 template <int T, int DT>
@@ -919,7 +923,7 @@ hipError_t launch_mx4_rows(const Mx4Gemm& p, const void* x, int dt, int64_t ldx,
 
 // out = the sum of the splits, in their order: four outputs a thread, and eight
 // splits' on their way at a time (other XCDs wrote them: a read takes over a us).
-// Bound by memory (517 x 4096 in three splits: 27 MB read, 6.3 us).
+// Bound by memory (517 x 4096 in three splits: 27 MB read, 7.5 us).
 __global__ __launch_bounds__(256) void mx4_reduce_kernel(Mx4Gemm p) {
     const int quads = (p.w.n + 3) / 4;
     const size_t idx = blockIdx.x * (size_t)256 + threadIdx.x;
@@ -979,12 +983,12 @@ hipError_t run_pipe(Mx4Gemm p, hipStream_t st, hipEvent_t done) {
 // the parts cost, measured from 16 x 4096 x 4096 to 2048 x 28672 x 8192 (the picks are
 // within 1% of the best pair on average, 7% at worst).  A workgroup's step of 64 k
 // costs STEP (us), and a CU's workgroups take turns: larger tiles read less per
-// product, so they win once every CU has work (2048 x 4096 x 4096: 75, 65 and 60 us
+// product, so they win once every CU has work (2048 x 4096 x 4096: 102, 84 and 77 us
 // with MT 1, 2 and 4).  START is what a tile's code and stores add, which is why small
-// products take small tiles (300 x 300 x 300 with 4-bit rows: 13, 15 and 21 us with MT
+// products take small tiles (300 x 300 x 300 with 4-bit rows: 12, 15 and 20 us with MT
 // 1, 2 and 4); where MT 4 has one workgroup a CU, each round pays it.  Splits cost a
-// launch and their sums' way to memory and back (33 x 256 x 14336: 64 us unsplit, 20 in
-// 16 splits; 700 x 2048 x 700: 15 and 21 in two).  The split alone says in which order
+// launch and their sums' way to memory and back (33 x 256 x 14336: 84 us unsplit, 21 in
+// 12 splits; 700 x 2048 x 700: 15 and 22 in two).  The split alone says in which order
 // a row's sums are added.
 float mx4_plan(Mx4Gemm& p, int n_cus, int only_split) {
     constexpr int MTS[3] = {1, 2, 4};

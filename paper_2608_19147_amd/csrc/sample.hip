@@ -19,11 +19,14 @@
 // top_p, 24-bit numbers below 1, comes nearer to 1 than 6e-8, so no draw and no
 // cut falls there.
 //
-// What bounds it is not the reading (64 bf16 rows of 128256: 16 MB, 3.3 us) but the
-// chain of small steps: count, plan, gather, draw, each a launch or a workgroup's
-// code run once, from memory.  Rows whose logits are nearly equal have more tokens in
-// the bins that matter than are gathered, and are read again, place by place, by one
-// workgroup: a row of 128256 equal ones takes 0.2 to 0.6 ms.
+// What bounds it is not the reading (64 bf16 rows of 128256: 16 MB, 3.3 us).  For one
+// row to some it is the chain of small steps: count, plan, gather, draw, each a launch
+// or a workgroup's code run once, from memory.  With 64 rows the counting itself is
+// bound by the issue of vector instructions, most of them on 64-bit numbers: 47 a token,
+// 5,900 a SIMD, which at 4 cycles each are 23,600 of a CU's 28,300 busy cycles.  Rows
+// whose logits are nearly equal have more tokens in the bins that matter than are
+// gathered, and are read again, place by place, by one workgroup: a row of 128256 equal
+// ones takes 0.2 to 0.6 ms.
 #include "device.h"
 
 namespace stg {
@@ -918,7 +921,7 @@ __global__ __launch_bounds__(SB_THREADS) void sample_small_kernel(SampleArgs a) 
 }
 
 // Counts one slice of a row; the row's last workgroup to end joins the counts and makes the plan.
-// 20 rows of 128256: 17 us, of which a slice takes 5, the joining 3 and the plan 4; 64 rows: 27.
+// 20 rows of 128256: 17 us, of which a slice takes 5, the joining 3 and the plan 4; 64 rows: 26.
 __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
     const int slice = blockIdx.x, row = blockIdx.y, ns = gridDim.x, tid = threadIdx.x;
@@ -1041,7 +1044,7 @@ __global__ __launch_bounds__(SB_THREADS, 6) void sample_count_kernel(SampleArgs 
     }
 }
 
-// Gathers one slice's tokens of the plan's runs.  20 rows: 5 us; 64 rows, most of whose slices have some: 9.
+// Gathers one slice's tokens of the plan's runs.  20 rows: 6 us; 64 rows, most of whose slices have some: 10.
 __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t keys[SL_LEN];
     __shared__ uint32_t buf[SB_THREADS / 64];
@@ -1055,8 +1058,8 @@ __global__ __launch_bounds__(SB_THREADS) void sample_gather_kernel(SampleArgs a)
     take_tokens(plan, keys, slice, n, SB_CAP, &ws->fill, [&](unsigned at, unsigned long long v) { ws->list[at] = v; });
 }
 
-// The cuts and the draw, one workgroup a row.  20 rows: 12 us, about 1 a step; 64 rows with up to some thousand
-// gathered tokens each, narrowed in LDS: 26.
+// The cuts and the draw, one workgroup a row.  20 rows: 14 us, about 1 a step; 64 rows with up to some thousand
+// gathered tokens each, narrowed in LDS: 27.
 __global__ __launch_bounds__(SB_THREADS) void sample_draw_kernel(SampleArgs a) {
     __shared__ SampleShared sh;
     __shared__ unsigned long long sel[SB_CAP];
