@@ -1744,13 +1744,23 @@ int stage_head_attach_mx4(Stage* st, const uint16_t* final_norm, const uint8_t* 
         HIP_TRY(order_on(st, s));
         uint16_t* fn = nullptr;
         float* rows = nullptr;
-        if ((rc = st->alloc(&fn, (size_t)H)) || (rc = st->alloc(&rows, (size_t)MAX_ROWS * H))) return rc;
-        HIP_TRY(hipMemcpyAsync(fn, final_norm, (size_t)H * 2, weights_on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice, s));
         std::unique_ptr<Mx4Matrix> m(new Mx4Matrix());
         m->stage = st;
-        if ((rc = mx4_load(st, codes, scales, vocab, H, weights_on_device, s, &m->m))) return rc;
-        st->allocs.push_back(m->m.w);
-        st->allocs.push_back(m->m.s);
+        const size_t had = st->allocs.size();
+        auto load = [&]() -> int {
+            int e = mx4_load(st, codes, scales, vocab, H, weights_on_device, s, &m->m);
+            if (e) return e;
+            st->allocs.push_back(m->m.w);
+            st->allocs.push_back(m->m.s);
+            if ((e = st->alloc(&fn, (size_t)H)) || (e = st->alloc(&rows, (size_t)MAX_ROWS * H))) return e;
+            HIP_TRY(hipMemcpyAsync(fn, final_norm, (size_t)H * 2, weights_on_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice, s));
+            HIP_TRY(hipStreamSynchronize(s));
+            return STAGE_OK;
+        };
+        if ((rc = load())) {                               // nothing of it stays
+            for (; st->allocs.size() > had; st->allocs.pop_back()) (void)hipFree(st->allocs.back());
+            return rc;
+        }
         st->weight_bytes += (int64_t)m->m.groups * m->m.steps * (2048 + 128) + 2 * (int64_t)H;
         st->final_norm = fn;
         st->head_rows = rows;

@@ -17,7 +17,7 @@ struct dim3 { uint32_t x, y, z; };
 namespace {
 std::string notes;
 int last = 0, fail_at = 0, launches = 0, capturing = 0;
-long alloc_fail_at = 0, allocs = 0;
+long alloc_fail_at = 0, allocs = 0, malloc_fail_at = 0, mallocs = 0, live = 0;
 intptr_t handles = 100;
 long long max_malloc = 0;
 dim3 cfg_grid, cfg_block;
@@ -61,11 +61,13 @@ int hipExtLaunchKernel(const void*, dim3, dim3, ptr*, size_t, ptr st, ptr, ptr d
 int hipLaunchCooperativeKernel(const void*, dim3, dim3, ptr*, unsigned, ptr st) { return launch(st, 0); }
 
 int hipMalloc(ptr* p, size_t n) {
+    if (malloc_fail_at && ++mallocs == malloc_fail_at) return last = 2;   // hipErrorOutOfMemory
     if ((long long)n > max_malloc) max_malloc = (long long)n;
     *p = calloc(n ? n : 1, 1);
+    ++live;
     return *p ? 0 : (last = 2);
 }
-int hipFree(ptr p) { free(p); return 0; }
+int hipFree(ptr p) { live -= p ? 1 : 0; free(p); return 0; }
 int hipHostMalloc(ptr* p, size_t n, unsigned) { *p = calloc(n ? n : 1, 1); return *p ? 0 : 2; }
 int hipHostFree(ptr p) { free(p); return 0; }
 int hipMemcpy(void* d, const void* s, size_t n, int) { memcpy(d, s, n); return 0; }
@@ -112,6 +114,9 @@ void host_start(int at, long alloc, int capture) {
 // Lines "L stream 0" (launched), "R stream event" (event recorded behind it), "W stream event" (stream waits).
 const char* host_notes() { alloc_fail_at = 0; return notes.c_str(); }
 int host_last_error() { return last; }
+// From now on the `at`-th hipMalloc fails, 0 none.
+void host_fail_malloc(long at) { malloc_fail_at = at; mallocs = 0; }
+long host_live() { return live; }
 long long host_largest_malloc() { return max_malloc; }
 
 }  // extern "C"

@@ -22,6 +22,8 @@ host = ctypes.CDLL(os.environ["LD_PRELOAD"])
 host.host_start.argtypes = [ctypes.c_int, ctypes.c_long, ctypes.c_int]
 host.host_notes.restype = ctypes.c_char_p
 host.host_largest_malloc.restype = ctypes.c_longlong
+host.host_fail_malloc.argtypes = [ctypes.c_long]
+host.host_live.restype = ctypes.c_long
 KEEP = []
 
 
@@ -126,6 +128,28 @@ def largest_allocation(name):
     host.host_start(0, 0, 0)
     assert f(1) == 0
     return host.host_largest_malloc(), 64 * VOCAB * 4
+
+
+def weights_without_memory(name):
+    """Per device allocation that fails while weights are packed: the status, and what the failed call leaves allocated; at
+    last those of the call with memory."""
+    out = []
+    norm, (codes, scales) = array(np.zeros(H, np.uint16)), mx4(VOCAB, H)
+    h = ctypes.c_void_p()
+    st = make_stage()
+    for n in range(1, 20):
+        host.host_start(0, 0, 0)
+        had = host.host_live()
+        host.host_fail_malloc(n)
+        if name == "head":
+            rc = lib.stage_head_attach_mx4(st, norm, codes, scales, VOCAB, 0, None)
+        else:
+            rc = lib.stage_mx4_create(st, codes, scales, VOCAB, H, 0, None, ctypes.byref(h))
+        host.host_fail_malloc(0)
+        out.append((rc, host.host_live() - had, host.host_last_error()))
+        if rc == 0:
+            break
+    return out
 
 
 if __name__ == "__main__":

@@ -70,3 +70,11 @@ def test_logits_workspace(ask, name):
     assert most == logits
     most, logits = ask("largest_allocation", name + "_logits")
     assert most < logits
+
+
+@pytest.mark.parametrize("name", ["head", "matrix"])
+def test_weights_without_memory(ask, name):
+    """MXFP4 weights that do not fit leave nothing allocated and no error behind, and the call can be made again."""
+    got = ask("weights_without_memory", name)
+    assert len(got) >= 5 and got[-1][0] == 0
+    assert [tuple(g) for g in got[:-1]] == [(-4, 0, 0)] * (len(got) - 1)
