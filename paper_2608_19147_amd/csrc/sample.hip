@@ -692,7 +692,9 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
         lo[3] = min(end, bin_reaching((double)u * wlo));
         hi[3] = min(end, wave_search(SB_BINS, [&](int i) { return sh.cum[i] > thi; }));
     }
-    // in order and apart: a run that starts in or right behind an earlier one is joined to it
+    // In order and apart: a run that starts in or right behind an earlier one is joined to it.  A run may lie within the
+    // one ahead of it (top_p's from the first bin to top_k's cut, the draw's at its start, top_k's at its end), so each
+    // takes the furthest end so far before they are joined.
 #pragma unroll
     for (int i = 0; i < SB_RANGES; ++i)
 #pragma unroll
@@ -703,9 +705,12 @@ __device__ __forceinline__ RowPlan make_plan(const SampleRow& p, float u, const 
                 lo[j + 1] = l; hi[j + 1] = h;
             }
 #pragma unroll
+    for (int i = 1; i < SB_RANGES; ++i)
+        if (lo[i] < SB_BINS) hi[i] = max(hi[i], hi[i - 1]);
+#pragma unroll
     for (int i = SB_RANGES - 1; i > 0; --i)
         if (lo[i] < SB_BINS && lo[i] <= hi[i - 1] + 1) {
-            hi[i - 1] = max(hi[i - 1], hi[i]);
+            hi[i - 1] = hi[i];
             lo[i] = SB_BINS;
         }
     // The least key whose bin is b or less, for the ends of the runs: x rises with the key, so a logit next to q / per_t

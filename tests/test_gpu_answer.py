@@ -177,3 +177,15 @@ def test_equal_extremes_by_index(stage, value):
     tok, p = stage.sample(z.cuda()[None].repeat(len(us), 1), Sampling(), torch.from_numpy(us).cuda())
     assert tok.tolist() == [at[int(float(u) * 300)] for u in us]
     assert (p.double() - 1 / 300).abs().max().item() <= 2.0 ** -24 / 300
+
+
+@pytest.mark.parametrize("V", [4, 11, 36, 700, 9000, 30000, 128256])
+def test_few_kept(stage, V):
+    """Few tokens kept by top_k, cut by top_p (and min_p) over bins that lie apart: the bins in which the cuts and the draw
+    can fall lie within each other."""
+    r = np.random.default_rng([365, V])
+    for _ in range(6):
+        z = torch.from_numpy(r.standard_normal(V) * np.exp(r.uniform(-2, 2))).float()
+        rows = [((float(r.choice([0.3, 0.7, 1.0, 1.5])), int(r.choice([2, 2, 3, 5, 8])), float(r.choice([0.5, 0.9, 0.95, 0.999])),
+                  float(r.choice([0, 0, 0.01, 0.05]))), float(np.float32(r.random()))) for _ in range(64)]
+        _drawn(stage, z, rows, near_ok=1)
