@@ -111,7 +111,12 @@ __device__ __forceinline__ double bin_inverse(int b) { return INV_Q[b >> 5] * IN
 struct RowBins {                      // the scaled logit of a row's tokens
     double per_t;                     // 32 / T
     double qmax;                      // floor(x) of the largest
-    __device__ __forceinline__ double x(float logit) const { return (double)logit * per_t; }
+    // Rounded by itself, wherever it is used: joined to the subtraction of its floor in one instruction, the product's
+    // rounding would be in the fraction (more than 1 from x = 2^54 on), in one place and not in another.
+    __device__ __forceinline__ double x(float logit) const {
+#pragma clang fp contract(off)
+        return (double)logit * per_t;
+    }
     __device__ __forceinline__ double x(uint32_t key) const { return x(key_logit(key)); }
     __device__ __forceinline__ double bin(double xv) const { return qmax - floor(xv); }
     __device__ __forceinline__ unsigned long long units(double xv) const { return exp_units(xv - floor(xv)); }

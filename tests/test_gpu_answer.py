@@ -189,3 +189,47 @@ def test_few_kept(stage, V):
         rows = [((float(r.choice([0.3, 0.7, 1.0, 1.5])), int(r.choice([2, 2, 3, 5, 8])), float(r.choice([0.5, 0.9, 0.95, 0.999])),
                   float(r.choice([0, 0, 0.01, 0.05]))), float(np.float32(r.random()))) for _ in range(64)]
         _drawn(stage, z, rows, near_ok=1)
+
+
+@pytest.mark.parametrize("V", [20, 9000, 30000])
+@pytest.mark.parametrize("scale", [1e3, 1e12, 1e30, 3e38])
+def test_large_logits(stage, V, scale):
+    """Logits far beyond the numbers that have fractions, some of them equal: the first ones share the weight by count, at
+    every temperature."""
+    r = np.random.default_rng([366, V])
+    z = r.standard_normal(V).clip(-1, 0.8)
+    z[r.permutation(V)[: V // 4]] = 0.9
+    z = torch.from_numpy((z * scale).astype(np.float32))
+    first = np.flatnonzero(z.numpy() == z.numpy().max())
+    rows = [(t, p, m, float(np.float32(u))) for t in (1e-3, 0.3, 0.7, 1.0, 30.0) for p, m in ((1.0, 0.0), (0.5, 0.0), (1.0, 1.0)) for u in (0.0, 0.3, 0.99)]
+    if scale < 1e4:
+        rows = [q for q in rows if q[0] < 0.5]                # so that the other tokens weigh nothing
+    tok, p = stage.sample(z.cuda()[None].repeat(len(rows), 1), [Sampling(t, 0, q, m) for t, q, m, _ in rows], torch.tensor([u for *_, u in rows], device="cuda"))
+    for (t, q, m, u), got, pr in zip(rows, tok.tolist(), p.tolist()):
+        kept = int(np.ceil(q * len(first)))
+        assert got == first[int(u * kept)] and abs(pr - 1 / kept) <= 2.0 ** -24 / kept, (t, q, m, u, got, pr)
+
+
+def test_infinite_logits(stage):
+    """+inf ranks as the largest finite number, however that is scaled."""
+    for dtype in (torch.float16, torch.bfloat16, torch.float32):
+        z = torch.zeros((15, 300), dtype=dtype)
+        z[:, 7::10] = np.inf
+        ts = [1e-3, 0.3, 0.7, 1.5, 30.0]
+        us = [0.0, 0.41, 0.97]
+        tok, p = stage.sample(z.cuda(), [Sampling(t) for t in ts for _ in us], torch.tensor(us * 5, device="cuda"))
+        assert tok.tolist() == [7 + 10 * int(float(np.float32(u)) * 30) for u in us] * 5
+        assert (p.double() - 1 / 30).abs().max().item() <= 2.0 ** -24 / 30
+
+
+@pytest.mark.parametrize("spread", [0.5, 50.0, 5000.0])
+def test_min_p_one(stage, spread):
+    """min_p 1 keeps the first token (and its equals) at every temperature."""
+    r = np.random.default_rng([367, int(spread)])
+    for V in (30, 9000, 40000):
+        z = torch.from_numpy(r.standard_normal((40, V)) * spread).half()
+        ts = [(1e-3, 0.3, 0.7, 1.1, 30.0)[i % 5] for i in range(40)]
+        tok, p = stage.sample(z.cuda(), [Sampling(t, 0, 1.0, 1.0) for t in ts], torch.full((40,), 0.5, device="cuda"))
+        for row, t, q in zip(z.double().numpy(), tok.tolist(), p.tolist()):
+            first = np.flatnonzero(row == row.max())
+            assert t == first[len(first) // 2] and abs(q - 1 / len(first)) <= 2.0 ** -24
