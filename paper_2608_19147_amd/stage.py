@@ -497,8 +497,8 @@ class Mx4Matrix:
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """x W^T [m, n] of device rows x [m, k]: 16-bit rows to within 2^-18 of the
         largest magnitude of each block of 32 (``act_bits`` 16), or rounded to MXFP4
-        first (4, also float32 rows), in ``out_dtype`` (x's by default) or into ``out`` [m, n], whose rows may be part of wider ones
-        and must not overlap x."""
+        first (4, also float32 rows), in ``out_dtype`` (x's by default) or into
+        ``out`` [m, n], whose rows may be part of wider ones and must not overlap x."""
         ldx = _rows(x, "x")
         m, k = x.shape
         if k != self.k:
