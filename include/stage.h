@@ -479,6 +479,147 @@ int stage_tree_accept(Stage* stage, const int32_t* parents, const int32_t* token
                       int32_t* count_out, int32_t* path_out, int32_t* next_out, uint8_t* keep_out, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The paged cache: sequences that share the pages of what they have in common.
+ *
+ * A pool holds pages of page_rows cache rows for every layer of its stage; a
+ * sequence is a list of pages and a length.  Sequences forked from one another
+ * share whole pages, which nothing writes while they are shared; a step is a batch
+ * of sequences with new rows each: it writes the rows (rotary included) and attends,
+ * reading a run of pages that several sequences share once for all of them.
+ * stage_forward_paged takes a batch through the stage's layers that way.
+ *
+ * Device work of these calls is ordered with the stage's other calls like a forward.
+ * A capturing stream is refused (STAGE_E_UNSUPPORTED), but for kv_step_write and
+ * kv_step_attend: they use the step's metadata and the caller's memory alone, so a
+ * graph can hold them; its replays are ordered by the caller, behind the step's plan
+ * (synchronize before the capture), and a step that was captured takes no other plan.
+ * The pages of a sequence that is freed, truncated or compacted may be taken by the
+ * next call that needs pages, behind the work issued before it; steps that were
+ * planned with it, and graphs that hold them, then read other rows.
+ * The calling thread's current device is left as it was.
+ * ------------------------------------------------------------------------ */
+
+typedef struct KVPages KVPages;
+typedef struct KVSeq KVSeq;
+typedef struct KVStep KVStep;
+
+/* Most new rows of one step (of all its sequences), and most axes of positions. */
+#define STAGE_MAX_STEP_ROWS 8192
+#define STAGE_MAX_AXES 4
+
+/* A pool of n_pages pages of page_rows (16, 32, 64, 128 or 256) rows.  k, v: the
+ * caller's device memory, [n_layers][n_pages][Hkv][page_rows][D] each in kv_dtype,
+ * aligned to 16 bytes, kept until the pool is freed.  pair_axis: host uint8 [D/2] or
+ * NULL: which of n_axes positions turns rotary pair i, as for images and video (time,
+ * height, width); NULL: the first (n_axes 1).  Free pages are handed out lowest first.
+ * Bound to the stage, and freed before it, after its sequences and steps.
+ * Errors: INVALID (NULL, alignment, an axis out of range), CAPACITY (n_pages < 1, more
+ * than 2^31 - 1 rows; n_axes), UNSUPPORTED (page_rows), OOM, HIP. */
+int kv_pages_create(Stage* stage, int n_pages, int page_rows, void* k, void* v, const uint8_t* pair_axis, int n_axes, KVPages** out);
+int kv_pages_free(KVPages* pool);
+int kv_pages_available(const KVPages* pool, int* free_pages);
+
+/* An empty sequence; it takes pages as rows come. */
+int kv_seq_create(KVPages* pool, KVSeq** out);
+/* Gives back what it does not share. */
+int kv_seq_free(KVSeq* seq);
+int kv_seq_length(const KVSeq* seq, int* length_out);
+/* The page of each page_rows rows, in order: pages_out host int32 [capacity] (or NULL), count_out their number. */
+int kv_seq_pages(const KVSeq* seq, int32_t* pages_out, int capacity, int* count_out);
+
+/* n new sequences, the i-th from seqs[i] (which may stand there more than once; all of
+ * one pool): its first lengths[i] rows (lengths NULL: all), or with keep[i] (host uint8
+ * [its length]; keep or keep[i] NULL: none dropped) those of them with keep[i][j] != 0,
+ * closed up.  Whole pages ahead of the first row that is left out are shared; the rows
+ * behind them are copied to new pages.  The sequences themselves are unchanged.
+ * Errors: INVALID (NULL, n < 1, a length out of range), STATE_MISMATCH (pools),
+ * CAPACITY (free pages; more than 2^24 / (2 n_layers Hkv) blocks of 64 rows copied),
+ * UNSUPPORTED (capturing stream), OOM, HIP; nothing is created on error. */
+int kv_seq_fork(KVSeq* const* seqs, const int32_t* lengths, const uint8_t* const* keep, int n, KVSeq** out, void* stream);
+
+/* Drop the rows with keep[j] == 0 (host uint8 [length]) and close the others up, in
+ * place; shared pages that change are replaced by new ones.
+ * Errors: INVALID (NULL), CAPACITY (free pages), UNSUPPORTED (capturing stream), OOM, HIP. */
+int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream);
+
+/* Drop the rows from new_len on, and the pages that held only those.  No device work. */
+int kv_seq_truncate(KVSeq* seq, int new_len);
+
+/* Append n rows: k, v device [n_layers][Hkv][n][D] in kv_dtype, aligned to 16 bytes
+ * (K after rotary), or rows [start, start + n) of a slot of a KV state of the same
+ * stage, as the slot sees them.  A shared last page is replaced by a copy first.
+ * Errors: INVALID (NULL, alignment, n < 1, range), STATE_MISMATCH (stages), CAPACITY
+ * (free pages, 2^31 - 1 rows), UNSUPPORTED (capturing stream), OOM, HIP. */
+int kv_seq_append(KVSeq* seq, const void* k, const void* v, int n, void* stream);
+int kv_seq_load(KVSeq* seq, KVState* state, int slot, int start, int n, void* stream);
+
+/* Rows [start, start + count) of one layer to k_out, v_out: device [Hkv][count][D].
+ * Errors: INVALID (NULL, range), UNSUPPORTED (capturing stream), OOM, HIP. */
+int kv_seq_read(KVSeq* seq, int layer, int start, int count, void* k_out, void* v_out, void* stream);
+
+/* One sequence of a step, with P rows, and its n_tokens new ones:
+ *   positions : host int32 [n_axes][n_tokens], or NULL: the step's rows are not turned
+ *               (for every sequence of a step, or for none)
+ *   attention_mask      : host uint8 [P + n_tokens] or NULL; 0 hides that row from
+ *                         every new one
+ *   attention_mask_rows : host uint8 [n_tokens][P + n_tokens] or NULL: one mask per
+ *                         new row
+ * New row i sees row j iff j <= P + i and both masks keep j. */
+typedef struct KVStepRequest {
+    KVSeq*         seq;
+    int32_t        n_tokens;
+    const int32_t* positions;
+    const uint8_t* attention_mask;
+    const uint8_t* attention_mask_rows;
+} KVStepRequest;
+
+/* A step holds the metadata of one batch on the device, and can be planned again. */
+int kv_step_create(KVPages* pool, KVStep** out);
+int kv_step_free(KVStep* step);
+
+/* Make room for the new rows in each sequence (whose length is then P + n_tokens; a
+ * shared last page is replaced by a copy), and lay out the step: M = sum of n_tokens
+ * rows, request-major.
+ * Errors: INVALID (NULL, n_tokens < 1, positions for some only), STATE_MISMATCH (another
+ * pool's sequence, one twice), CAPACITY (M, a position, free pages, rows, masks above
+ * 2^31 words), UNSUPPORTED (capturing stream, a captured step), OOM, HIP; nothing has
+ * changed on error. */
+int kv_step_plan(KVStep* step, const KVStepRequest* reqs, int n_req, void* stream);
+
+/* One layer's new rows: q [M][Hq D], k, v [M][Hkv D] (F32, F16 or BF16, one dtype; row
+ * strides ld count elements; no alignment beyond the element's).  Pair (i, i + D/2) of
+ * every q and k head turns by its axis' position (none without positions); k and v go to
+ * their rows of the pages, q to q_out [M][Hq D] (F32, F16 or BF16), which may be q itself
+ * (same dtype and stride).
+ * Errors: INVALID (NULL, dtype, layer, a step without plan), SHAPE (strides), HIP. */
+int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype,
+                  void* q_out, int64_t ldqo, int q_out_dtype, void* stream);
+
+/* Bytes of workspace that kv_step_attend of this plan needs (0: none). */
+int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
+
+/* out [M][Hq D] = attention of the rotated queries q [M][Hq D] over one layer's pages:
+ * softmax of scale q.k (scale 0: 1/sqrt(D)) over the rows that each new row sees; a row
+ * that sees none gives zeros.  q: kv_dtype, or F32 (as two terms of kv_dtype: within
+ * 2^-17 of each element in bf16, 2^-22 in fp16); out: F32, F16 or BF16, not overlapping q.
+ * Scores and sums in fp32; probabilities enter as one or two terms of kv_dtype (two where
+ * a kv head has at most 64 query vectors of the run, and with F32 queries).  What rows
+ * that are not seen hold, infinities and NaN too, reaches no result.
+ * workspace: device memory of kv_step_workspace bytes, aligned to 16, not used by another
+ * call at the same time (two graphs need two).
+ * Errors: INVALID (NULL, dtype, layer, scale, workspace, a step without plan), SHAPE
+ * (strides), HIP. */
+int kv_step_attend(KVStep* step, int layer, const void* q, int q_dtype, int64_t ldq, void* out, int out_dtype, int64_t ldo, float scale,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/* stage_forward over sequences of one pool: plans them as kv_step_plan does (positions
+ * are required), then takes hidden_in [M][H] through every layer.  A new row must see at
+ * least one row.  Masked-out rows stay and are hidden as in stage_forward, or leave by
+ * kv_seq_truncate and kv_seq_compact.
+ * Errors: as kv_step_plan and stage_forward (M at most STAGE_MAX_ROWS). */
+int stage_forward_paged(Stage* stage, const KVStepRequest* reqs, int n_req, const void* hidden_in, void* hidden_out, void* stream);
+
+/* ------------------------------------------------------------------------
  * First-stage role ("Per-Stage Export Pipeline": the first shard also holds
  * the token embedding; in the "Overview" figure the stage-0 shard runs the
  * embeddings before its layers).  The lookup is a plain row gather.

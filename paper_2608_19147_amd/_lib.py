@@ -19,6 +19,8 @@ MAX_ROWS = 64
 STATIC_SCRATCH_BYTES = 64 << 20   # STAGE_STATIC_SCRATCH_BYTES
 MAX_PREFILL = 8192                # STAGE_MAX_PREFILL
 MAX_VOCAB = 1 << 20               # STAGE_MAX_VOCAB
+MAX_STEP_ROWS = 8192              # STAGE_MAX_STEP_ROWS
+MAX_AXES = 4                      # STAGE_MAX_AXES
 
 # Every function that include/stage.h declares.
 EXPORTS = (
@@ -31,6 +33,9 @@ EXPORTS = (
     "stage_head_attach", "stage_head_top1", "stage_prefill", "stage_embed_attach", "stage_embed",
     "stage_mx4_quantize", "stage_mx4_dequantize", "stage_mx4_create", "stage_mx4_free", "stage_mx4_product",
     "stage_head_attach_mx4", "stage_sample", "stage_head_sample", "stage_tree_accept",
+    "kv_pages_create", "kv_pages_free", "kv_pages_available", "kv_seq_create", "kv_seq_free", "kv_seq_length", "kv_seq_pages",
+    "kv_seq_fork", "kv_seq_compact", "kv_seq_truncate", "kv_seq_append", "kv_seq_load", "kv_seq_read",
+    "kv_step_create", "kv_step_free", "kv_step_plan", "kv_step_write", "kv_step_workspace", "kv_step_attend", "stage_forward_paged",
 )
 KERNEL_CLASSES = {"qkv": 0, "attn": 1, "oproj": 2, "gateup": 3, "down": 4, "persistent": 5}
 
@@ -60,6 +65,13 @@ class StageRequest(ctypes.Structure):
         ("state", ctypes.c_void_p), ("n_tokens", ctypes.c_int32), ("positions", ctypes.c_void_p),
         ("beam_idx", ctypes.c_void_p), ("attention_mask", ctypes.c_void_p), ("mask_len", ctypes.c_int32),
         ("attention_mask_rows", ctypes.c_void_p),
+    ]
+
+
+class KVStepRequest(ctypes.Structure):
+    _fields_ = [
+        ("seq", ctypes.c_void_p), ("n_tokens", ctypes.c_int32), ("positions", ctypes.c_void_p),
+        ("attention_mask", ctypes.c_void_p), ("attention_mask_rows", ctypes.c_void_p),
     ]
 
 
@@ -116,6 +128,26 @@ def load() -> ctypes.CDLL:
         "stage_sample": (I, [V, V, I, L, I, I, V, V, V, V, V]),
         "stage_head_sample": (I, [V, V, I, V, V, V, V, V, V]),
         "stage_tree_accept": (I, [V, V, V, V, I, I, V, V, V, V, V]),
+        "kv_pages_create": (I, [V, I, I, V, V, V, I, P(V)]),
+        "kv_pages_free": (I, [V]),
+        "kv_pages_available": (I, [V, P(I)]),
+        "kv_seq_create": (I, [V, P(V)]),
+        "kv_seq_free": (I, [V]),
+        "kv_seq_length": (I, [V, P(I)]),
+        "kv_seq_pages": (I, [V, V, I, P(I)]),
+        "kv_seq_fork": (I, [V, V, V, I, V, V]),
+        "kv_seq_compact": (I, [V, V, V]),
+        "kv_seq_truncate": (I, [V, I]),
+        "kv_seq_append": (I, [V, V, V, I, V]),
+        "kv_seq_load": (I, [V, V, I, I, I, V]),
+        "kv_seq_read": (I, [V, I, I, I, V, V, V]),
+        "kv_step_create": (I, [V, P(V)]),
+        "kv_step_free": (I, [V]),
+        "kv_step_plan": (I, [V, P(KVStepRequest), I, V]),
+        "kv_step_write": (I, [V, I, V, L, V, L, V, L, I, V, L, I, V]),
+        "kv_step_workspace": (I, [V, P(L)]),
+        "kv_step_attend": (I, [V, I, V, I, L, V, I, L, ctypes.c_float, V, L, V]),
+        "stage_forward_paged": (I, [V, P(KVStepRequest), I, V, V, V]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libstage.so")
-SOURCES = ["stage.hip", "kernels.hip", "persistent.hip", "mx4.hip", "sample.hip"]
+SOURCES = ["stage.hip", "kernels.hip", "persistent.hip", "mx4.hip", "sample.hip", "kv_pages.hip", "paged.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

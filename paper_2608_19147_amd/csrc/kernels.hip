@@ -19,6 +19,7 @@
 //                decide visibility inside an online softmax (exp2 domain);
 //                attn_merge_kernel then combines the split partials.
 #include "device.h"
+#include "paged.h"
 
 #include <climits>
 
@@ -530,6 +531,12 @@ __global__ __launch_bounds__(256) void bprep_kernel(const void* in, int in_dt, i
         if (k0 + 256 * i < K) bp_put(bp, bc, kp, m, k, xs[i] * rs * gs[i], k < K);   // whole 32-lane groups
     }
     if (blockIdx.y == 0 && tid == 0) rs_out[m] = rs;
+}
+
+// Rows as they are (an attention's output) as the prepared input of the o product.
+__global__ __launch_bounds__(256) void bprep_plain_kernel(const float* in, int K, uint16_t* bp, float* bc, int kp) {
+    const int m = blockIdx.x, k = 256 * blockIdx.y + threadIdx.x;
+    bp_put(bp, bc, kp, m, k, k < K ? in[(size_t)m * K + k] : 0.f, k < K);
 }
 
 // Inputs of the row factors: the first 32 of this thread's quarter of row m's
@@ -1395,6 +1402,12 @@ hipError_t launch_gemm_pf(const PfArgs& a, hipStream_t st) {
     const unsigned grid = 8u * (unsigned)((total + 7) / 8);
     if (a.W.k % 128) gemm_pf_kernel<true><<<dim3(grid), dim3(256), 0, st>>>(a);
     else gemm_pf_kernel<false><<<dim3(grid), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_bprep_plain(const float* in, int K, int M, uint16_t* bp, float* bc, int kp, hipStream_t st) {
+    if (M < 1 || M > MAX_ROWS || K < 1 || K % 32 || kp < K) return hipErrorInvalidValue;
+    bprep_plain_kernel<<<dim3(M, (K + 255) / 256), dim3(256), 0, st>>>(in, K, bp, bc, kp);
     return hipGetLastError();
 }
 

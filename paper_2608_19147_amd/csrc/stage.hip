@@ -1,21 +1,7 @@
 // Host runtime of libstage: validation, weight repack, workspace, KV states,
 // metadata staging and the per-layer launch sequence of stage_forward.
-#include "stage.h"
-#include "common.h"
+#include "runtime.h"
 
-#include <algorithm>
-#include <array>
-#include <climits>
-#include <cmath>
-#include <cstdlib>
-#include <cstring>
-#include <memory>
-#include <mutex>
-#include <new>
-#include <string>
-#include <vector>
-
-using namespace stg;
 
 // Fixed device staging of kv_capture_noalloc: one copy per GPU the library
 // runs on, held until the process ends.  Host code never passes this name to
@@ -29,21 +15,6 @@ constexpr int SCRATCH_MAX_DEVICES = 64;
 std::mutex g_scratch_mu;
 std::array<uint8_t*, SCRATCH_MAX_DEVICES> g_scratch_ptr{};   // address of `scratch` on each device
 
-
-thread_local std::string g_err;
-
-int fail(int code, const std::string& msg) {
-    g_err = msg;
-    return code;
-}
-
-#define HIP_TRY(expr)                                                                          \
-    do {                                                                                       \
-        hipError_t e_ = (expr);                                                                \
-        if (e_ != hipSuccess) return fail(STAGE_E_HIP, std::string(#expr) + ": " + hipGetErrorString(e_)); \
-    } while (0)
-
-constexpr int META_RING = 4;
 constexpr int PF_ROWS = 2048;            // prompt rows per prefill pass (all layers)
 static_assert(PF_ROWS * 2 <= MAX_ROWS * ATTN_MAX_SPLITS, "attention partials of a prefill pass");
 
@@ -64,12 +35,6 @@ uint8_t* scratch_ptr(int dev) {
     std::lock_guard<std::mutex> lk(g_scratch_mu);
     return g_scratch_ptr[dev];
 }
-
-struct DevMat {
-    PackedMat pm;
-    int ksplit = 1, cps = 1;
-    int bp_split = 1, bp_kg = 1;   // prepared-operand product: splits of K, groups of 128 k per wave
-};
 
 // K split of a prepared-operand product (a function of the matrix only): about
 // one workgroup of 4 waves per CU (more splits of K lengthen the last-arrival
@@ -120,151 +85,7 @@ void bp_form(GemvArgs& a, const DevMat& m, int M, int n_cus) {
     a.pt = a.pair_rot && M > 16 ? 2 : 1;
 }
 
-struct LayerDev {
-    DevMat qkv, o, gu, d;
-    uint16_t* attn_norm = nullptr;
-    uint16_t* ffn_norm = nullptr;
-};
-
-int dt_code(int stage_dt) { return stage_dt == STAGE_DTYPE_BF16 ? DT_BF16 : DT_F16; }
-
-size_t align16(size_t x) { return (x + 15) & ~(size_t)15; }
-
 }  // namespace
-
-struct Stage {
-    StageConfig cfg{};
-    int device = 0;
-    std::vector<LayerDev> layers;
-    std::vector<void*> allocs;
-    float2* rope = nullptr;
-    float *x = nullptr, *qkv = nullptr, *attn = nullptr, *act = nullptr, *gpart = nullptr, *apart = nullptr, *ssq = nullptr;
-    unsigned *gcnt = nullptr, *acnt = nullptr;
-    int ntiles_h = 0;
-    // prepared inputs of the matrix-core products (2..64 rows), double-buffered
-    bool bp_ok = false;
-    int kp = 0;                                        // row stride: max K rounded up to 128
-    uint16_t* bp[2] = {nullptr, nullptr};              // [MAX_ROWS][kp] codes
-    float* bc[2] = {nullptr, nullptr};                 // [MAX_ROWS][kp / 32] corrections
-    float* cbf[2] = {nullptr, nullptr};                // [MAX_ROWS] scale each row was prepared with
-    float* rsb = nullptr;                              // [MAX_ROWS] rs of the last normalization
-    uint8_t* meta_dev = nullptr;
-    size_t meta_cap = 0;
-    uint8_t* meta_host[META_RING] = {};
-    hipEvent_t meta_ev[META_RING] = {};
-    bool meta_ev_used[META_RING] = {};
-    int ring_i = 0;
-    int64_t weight_bytes = 0;
-    uint64_t fingerprint = 0;                          // of the config, rotary table and norm weights (KV blobs)
-    // final-stage epilogue: final RMSNorm weight and INT4 LM head (stage_head_attach)
-    bool head_ok = false;
-    int vocab = 0;
-    DevMat head;
-    uint16_t* final_norm = nullptr;
-    float4* top1_part = nullptr;                       // [MAX_ROWS][head tiles]
-    Mx4Matrix* head4 = nullptr;                        // or an MXFP4 head (stage_head_attach_mx4), freed with the stage
-    float* head_rows = nullptr;                        // its normalized input rows [MAX_ROWS][H]
-    float *logits = nullptr, *head_p = nullptr;        // logits rows [MAX_ROWS][vocab] and [MAX_ROWS], on first need
-    int32_t* head_tok = nullptr;
-    // workspace of the MXFP4 products: activation fragments and their scales, grown on need
-    // and the sums of split products
-    uint8_t *mx_a = nullptr, *mx_s = nullptr, *mx_p = nullptr;
-    size_t mx_a_cap = 0, mx_s_cap = 0, mx_p_cap = 0;
-    // workspace of the sampling calls: the slices' counts, grown on need
-    uint8_t *smp = nullptr, *smp_rows = nullptr;
-    size_t smp_cap = 0;
-    // first-stage role: token embedding table [embed_vocab][H] in act dtype (stage_embed_attach)
-    uint16_t* embed = nullptr;
-    int embed_vocab = 0;
-    unsigned* embed_err = nullptr;                     // set by a gather that met an id outside the table
-    // prefill workspace for pf_rows prompt rows: residual fp32 [rows][H], q|k|v fp32
-    // [rows][NQKV], prepared inputs (64-row blocks; [1]: the down product's)
-    float *pf_x = nullptr, *pf_qkv = nullptr, *pf_bc[2] = {nullptr, nullptr};
-    uint16_t* pf_bp[2] = {nullptr, nullptr};
-    float* pf_part = nullptr;                          // sums of the split residual products [splits][rows][H]
-    size_t pf_rows = 0;
-    // persistent-kernel weights (row layout) and barrier state
-    bool ps_ok = false;
-    int cpl_h = 0, cpl_q = 0, cpl_f = 0, kc_h = 0, kc_q = 0, kc_f = 0, ng_h = 0, ng_q = 0, ng_f = 0;
-    std::vector<PsLayer> ps_host;
-    PsLayer* ps_layers = nullptr;
-    uint8_t* ps_wb[4] = {nullptr, nullptr, nullptr, nullptr};   // code slabs per matrix kind (all layers)
-    size_t ps_wl[4] = {0, 0, 0, 0};                            // bytes per layer in each slab
-    unsigned* err = nullptr;
-    unsigned spin_limit = 1u << 20;                     // exchange wait passes (STAGE_PS_SPIN_LIMIT)
-    int dbg_layer = -1, dbg_keys = 0, dbg_rows = 0;     // armed attention record (test support)
-    float* dbg_q = nullptr;                             // [MAX_ROWS][Hq][D]
-    float* dbg_logits = nullptr;                        // [MAX_ROWS][Hq][dbg_keys]
-    int ps_nwg = 0;
-    int n_cus = 0;                                      // compute units of the device
-    int ps_rpw_qkv = 0, ps_rpw_h = 0, ps_rpw_gu = 0;    // rows per workgroup of the single-launch forward
-    unsigned long long *ll_qkv = nullptr, *ll_o = nullptr, *ll_part = nullptr, *ll_act = nullptr;   // its flag-word
-    unsigned* ll_x = nullptr;                                                                       // exchange buffers
-    unsigned ll_epoch = 0;                              // flag numbers used so far
-    bool ps_coop = false;                               // cooperative launch (STAGE_COOP=1), else a plain launch
-    int attn_vector = 0;                                // attention on the vector units (STAGE_ATTN_VECTOR=1)
-    bool attn_dma = true;                               // cache rows by direct loads where allowed (STAGE_ATTN_DMA=0: off)
-    int gemm_min_rows = 1;                              // rows from which products use the matrix cores (STAGE_GEMM_MIN_ROWS)
-    unsigned long long* trace = nullptr;   // phase stamps of the last persistent forward (STAGE_PS_TRACE=1)
-    int prof_class = -1;
-    std::vector<hipEvent_t> prof_ev;   // start/stop pairs
-    size_t prof_used = 0;              // events recorded
-    // Device work of every call on this stage (and on its KV states) runs in call
-    // order: done_ev marks the end of the last call's work on last_stream, and a
-    // call on another stream waits for it first (see order_on / mark_done).
-    hipEvent_t done_ev = nullptr;
-    hipStream_t last_stream = nullptr;
-    bool done_used = false;
-
-    std::array<void*, 7> pf_buffers() const { return {pf_x, pf_qkv, pf_bp[0], pf_bp[1], pf_bc[0], pf_bc[1], pf_part}; }
-
-    ~Stage() {
-        for (hipEvent_t e : prof_ev) (void)hipEventDestroy(e);
-        if (pf_x) {
-            (void)hipSetDevice(device);
-            (void)hipDeviceSynchronize();
-            for (void* p : pf_buffers()) (void)hipFree(p);
-        }
-        if (done_ev) (void)hipEventDestroy(done_ev);
-        (void)hipSetDevice(device);
-        (void)hipDeviceSynchronize();
-        for (void* p : allocs) (void)hipFree(p);
-        for (void* p : {(void*)mx_a, (void*)mx_s, (void*)mx_p, (void*)smp})
-            if (p) (void)hipFree(p);
-        if (meta_dev) (void)hipFree(meta_dev);
-        for (int i = 0; i < META_RING; ++i) {
-            if (meta_host[i]) (void)hipHostFree(meta_host[i]);
-            if (meta_ev[i]) (void)hipEventDestroy(meta_ev[i]);
-        }
-    }
-
-    template <class T>
-    int alloc(T** p, size_t n_elems) {
-        void* q = nullptr;
-        if (n_elems == 0) n_elems = 1;
-        if (hipMalloc(&q, n_elems * sizeof(T)) != hipSuccess) {
-            (void)hipGetLastError();
-            return fail(STAGE_E_OOM, "device allocation of " + std::to_string(n_elems * sizeof(T)) + " bytes failed");
-        }
-        allocs.push_back(q);
-        *p = (T*)q;
-        return STAGE_OK;
-    }
-};
-
-struct Mx4Matrix {
-    Stage* stage = nullptr;
-    Mx4Mat m{};
-};
-
-struct KVState {
-    Stage* stage = nullptr;
-    int S = 0, cap = 0, P = 0;
-    uint16_t* kc = nullptr;
-    uint16_t* vc = nullptr;
-    int16_t* table[2] = {nullptr, nullptr};
-    int cur = 0;
-};
 
 namespace {
 
@@ -383,70 +204,6 @@ int check_config(const StageConfig* c) {
     return STAGE_OK;
 }
 
-int ensure_meta(Stage* st, size_t bytes) {
-    if (bytes <= st->meta_cap) return STAGE_OK;
-    size_t cap = std::max<size_t>(bytes, 2 * st->meta_cap);
-    cap = std::max<size_t>(cap, 1 << 16);
-    HIP_TRY(hipDeviceSynchronize());   // old buffers may still be read by queued work
-    if (st->meta_dev) HIP_TRY(hipFree(st->meta_dev));
-    st->meta_dev = nullptr;
-    for (int i = 0; i < META_RING; ++i) {
-        if (st->meta_host[i]) HIP_TRY(hipHostFree(st->meta_host[i]));
-        st->meta_host[i] = nullptr;
-        st->meta_ev_used[i] = false;
-    }
-    if (hipMalloc(&st->meta_dev, cap) != hipSuccess) {
-        (void)hipGetLastError();
-        st->meta_cap = 0;
-        return fail(STAGE_E_OOM, "metadata allocation failed");
-    }
-    for (int i = 0; i < META_RING; ++i) {
-        if (hipHostMalloc(&st->meta_host[i], cap, hipHostMallocDefault) != hipSuccess) {
-            (void)hipGetLastError();
-            st->meta_cap = 0;
-            return fail(STAGE_E_OOM, "pinned metadata allocation failed");
-        }
-    }
-    st->meta_cap = cap;
-    return STAGE_OK;
-}
-
-// Calls on one stage run on the device in the order they were made, whatever
-// streams they are issued on: the workspace, the metadata buffer and the flag
-// numbers of the single-launch forward are per stage.  A call on a stream other
-// than the previous call's first makes its stream wait for that call's work.
-hipError_t order_on(Stage* st, hipStream_t s) {
-    if (st->done_used && s != st->last_stream) return hipStreamWaitEvent(s, st->done_ev, 0);
-    return hipSuccess;
-}
-hipError_t mark_done(Stage* st, hipStream_t s) {
-    const hipError_t e = hipEventRecord(st->done_ev, s);
-    if (e == hipSuccess) {
-        st->done_used = true;
-        st->last_stream = s;
-    }
-    return e;
-}
-
-// A call's work on stream s, from order_on to launched(), after its last launch, which signals done_ev itself.  A call that
-// ends before that, with an error, is marked behind whatever it has queued, which may still use the workspace.
-struct WorkOn {
-    Stage* st;
-    hipStream_t s;
-    bool open = true;
-    WorkOn(Stage* st_, hipStream_t s_) : st(st_), s(s_) {}
-    WorkOn(const WorkOn&) = delete;
-    WorkOn& operator=(const WorkOn&) = delete;
-    ~WorkOn() {
-        if (open && mark_done(st, s) != hipSuccess) (void)hipGetLastError();   // the call reports its own error
-    }
-    void launched() {
-        st->done_used = true;
-        st->last_stream = s;
-        open = false;
-    }
-};
-
 constexpr size_t PROF_MAX_LAUNCHES = 65536;
 
 // Records the start (begin = true) or stop event of a profiled launch.
@@ -468,22 +225,6 @@ uint64_t fnv1a(uint64_t h, const void* p, size_t n) {
     const uint8_t* b = (const uint8_t*)p;
     for (size_t i = 0; i < n; ++i) h = (h ^ b[i]) * 0x100000001b3ULL;
     return h;
-}
-
-// Copies `bytes` of host data into the next pinned metadata ring slot and from
-// there to the device metadata buffer (stream-ordered); *dev is its device copy.
-int meta_upload(Stage* st, const void* host, size_t bytes, hipStream_t s, const uint8_t** dev) {
-    int rc = ensure_meta(st, std::max<size_t>(bytes, 16));
-    if (rc) return rc;
-    const int slot_i = st->ring_i;
-    st->ring_i = (st->ring_i + 1) % META_RING;
-    if (st->meta_ev_used[slot_i]) HIP_TRY(hipEventSynchronize(st->meta_ev[slot_i]));
-    if (bytes) std::memcpy(st->meta_host[slot_i], host, bytes);
-    HIP_TRY(hipMemcpyAsync(st->meta_dev, st->meta_host[slot_i], std::max<size_t>(bytes, 16), hipMemcpyHostToDevice, s));
-    HIP_TRY(hipEventRecord(st->meta_ev[slot_i], s));
-    st->meta_ev_used[slot_i] = true;
-    *dev = st->meta_dev;
-    return STAGE_OK;
 }
 
 // Kept rows of every slot: src[b * Pn + i] = the i-th kept row of slot b
@@ -530,48 +271,6 @@ std::vector<uint8_t> blob_header(const Stage* st, int S, int Pn, const std::vect
 
 // ---------------------------------------------------------------- the last stage's answer
 
-// The current device of the calling thread, back when the call ends.
-struct DeviceGuard {
-    int prev = -1;
-    hipError_t err;
-    explicit DeviceGuard(int dev) {
-        err = hipGetDevice(&prev);
-        if (err == hipSuccess && prev != dev) err = hipSetDevice(dev);
-        else prev = -1;
-    }
-    ~DeviceGuard() {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
-
-// No C++ exception leaves a C entry.
-template <class F>
-int guarded(F f) noexcept {
-    try {
-        return f();
-    } catch (const std::bad_alloc&) {
-        try { return fail(STAGE_E_OOM, "host allocation failed"); } catch (...) { return STAGE_E_OOM; }
-    } catch (...) {
-        try { return fail(STAGE_E_INVALID, "unexpected failure"); } catch (...) { return STAGE_E_INVALID; }
-    }
-}
-
-// A call that uses the stage's workspace cannot be captured: a replay would not be ordered with the stage's other calls.
-int captured(hipStream_t s, bool& yes) {
-    hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
-    HIP_TRY(hipStreamIsCapturing(s, &c));
-    yes = c != hipStreamCaptureStatusNone;
-    return STAGE_OK;
-}
-int not_captured(hipStream_t s) {
-    bool yes = false;
-    const int rc = captured(s, yes);
-    return rc ? rc : yes ? fail(STAGE_E_UNSUPPORTED, "this call cannot be captured into a graph") : STAGE_OK;
-}
-
-bool dtype_ok(int dt) { return dt == STAGE_DTYPE_F32 || dt == STAGE_DTYPE_F16 || dt == STAGE_DTYPE_BF16; }
-int any_dt(int dt) { return dt == STAGE_DTYPE_F32 ? (int)DT_F32 : dt_code(dt); }
-
 constexpr int TREE_MAX_SLOTS = 1 << 24;
 constexpr int64_t MX4_MAX_DIM = 1 << 24;
 constexpr int64_t MX4_MAX_VALUES = (int64_t)1 << 34;      // a launch has fewer than 2^32 threads, of 8 values
@@ -580,21 +279,6 @@ constexpr int64_t MX4_MAX_VALUES = (int64_t)1 << 34;      // a launch has fewer 
 int mx4_dims(int64_t rows, int64_t k) {
     if (rows < 1 || k < 1) return fail(STAGE_E_INVALID, "rows and k must be positive");
     if (rows > MX4_MAX_DIM || k > MX4_MAX_DIM || rows * k > MX4_MAX_VALUES) return fail(STAGE_E_CAPACITY, "matrix too large");
-    return STAGE_OK;
-}
-
-int grow(uint8_t** p, size_t* cap, size_t bytes) {
-    if (*cap >= bytes) return STAGE_OK;
-    HIP_TRY(hipDeviceSynchronize());                       // queued work may still read the old one
-    if (*p) HIP_TRY(hipFree(*p));
-    *p = nullptr;
-    *cap = 0;
-    if (hipMalloc(p, bytes) != hipSuccess) {
-        (void)hipGetLastError();
-        *p = nullptr;
-        return fail(STAGE_E_OOM, "workspace allocation failed");
-    }
-    *cap = bytes;
     return STAGE_OK;
 }
 
@@ -764,6 +448,202 @@ int head4_run(Stage* st, const void* hidden, int M, const StageSampling* params,
 }  // namespace
 
 // ====================================================================== C ABI
+
+int stg::run_layers(Stage* st, int M, const void* hidden_in, void* hidden_out, hipStream_t s, LayerAttention& attention) {
+    const StageConfig& c = st->cfg;
+    const int H = c.hidden, D = c.head_dim, Hq = c.n_q_heads, F = c.ffn;
+    const int act_dt = dt_code(c.act_dtype), nqkv = Hq * D + 2 * c.n_kv_heads * D;
+    auto run_gemv = [&](const DevMat& m, GemvArgs a, size_t in_row_elems, size_t out_row_elems, size_t resid_row_elems,
+                        int in_elem_bytes, int resid_elem_bytes) -> hipError_t {
+        a.W = m.pm;
+        a.ksplit = m.ksplit;
+        a.cps = m.cps;
+        a.partial = st->gpart;
+        a.counters = st->gcnt;
+        for (int m0 = 0; m0 < M; m0 += GEMV_MAX_M) {
+            GemvArgs b = a;
+            b.M = std::min(GEMV_MAX_M, M - m0);
+            b.in = (const uint8_t*)a.in + (size_t)m0 * in_row_elems * in_elem_bytes;
+            b.out = a.out + (size_t)m0 * out_row_elems;
+            if (a.resid) b.resid = (const uint8_t*)a.resid + (size_t)m0 * resid_row_elems * resid_elem_bytes;
+            if (a.ssq_in) b.ssq_in = a.ssq_in + (size_t)m0 * a.ssq_tiles;
+            if (a.ssq_out) b.ssq_out = a.ssq_out + (size_t)m0 * m.pm.ntiles;
+            if (a.out_act) b.out_act = (uint8_t*)a.out_act + (size_t)m0 * a.out_act_ld * 2;
+            hipError_t e = launch_gemv(b, s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
+
+    // 2..64 rows: each product reads its input prepared by the kernel before it
+    const bool use_bp = st->bp_ok && M >= st->gemm_min_rows && M <= MAX_ROWS;
+    int bcur = 0;                                           // buffer holding the next product's input
+    auto bp_in = [&](GemvArgs& a, int norm) {
+        a.bp_in = st->bp[bcur];
+        a.bc_in = st->bc[bcur];
+        a.cb_in = st->cbf[bcur];
+        a.norm = norm;
+    };
+    auto bp_out = [&](GemvArgs& a) {
+        a.bp_out = st->bp[1 - bcur];
+        a.bc_out = st->bc[1 - bcur];
+        a.cb_out = st->cbf[1 - bcur];
+    };
+    auto run_bp = [&](const DevMat& m, GemvArgs a) -> hipError_t {
+        a.W = m.pm;
+        a.M = M;
+        a.kp = st->kp;
+        a.partial = st->gpart;
+        a.counters = st->gcnt;
+        a.ksplit = m.bp_split;
+        a.kg = m.bp_kg;
+        bp_form(a, m, M, st->n_cus);
+        return launch_gemm_bp(a, s);
+    };
+
+    for (int l = 0; l < c.n_layers; ++l) {
+        const LayerDev& Ld = st->layers[l];
+        const bool first = (l == 0), last = (l == c.n_layers - 1);
+        // q|k|v = RMSNorm(x) W_qkv^T
+        if (use_bp) {
+            GemvArgs a{};
+            a.eps = c.rms_eps;
+            a.ssq_in = st->ssq;
+            a.ssq_tiles = st->ntiles_h;
+            a.epi = EPI_STORE;
+            a.out = st->qkv;
+            a.out_ld = nqkv;
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, true, s));
+            if (first) {
+                HIP_TRY(launch_bprep(hidden_in, act_dt, H, Ld.attn_norm, act_dt, H, c.rms_eps, M, st->bp[bcur], st->bc[bcur],
+                                     st->kp, st->rsb, s));
+                bp_in(a, 2);
+            } else {
+                bp_in(a, 1);
+                a.rs_out = st->rsb;
+            }
+            HIP_TRY(run_bp(Ld.qkv, a));
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, false, s));
+        } else {
+            GemvArgs a{};
+            a.in = first ? hidden_in : (const void*)st->x;
+            a.in_dt = first ? act_dt : DT_F32;
+            a.in_ld = H;
+            a.gamma = Ld.attn_norm;
+            a.gamma_dt = act_dt;
+            a.rms = first ? RMS_FULLROW : RMS_PARTIALS;
+            a.eps = c.rms_eps;
+            a.ssq_in = first ? nullptr : st->ssq;
+            a.ssq_tiles = st->ntiles_h;
+            a.epi = EPI_STORE;
+            a.out = st->qkv;
+            a.out_ld = nqkv;
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, true, s));
+            HIP_TRY(run_gemv(Ld.qkv, a, H, nqkv, 0, first ? 2 : 4, 0));
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, false, s));
+        }
+        // attention (rotary, append, mask, online softmax, split merge)
+        {
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_ATTN, true, s));
+            HIP_TRY(attention.run(l, use_bp ? st->bp[1 - bcur] : nullptr, use_bp ? st->bc[1 - bcur] : nullptr));
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_ATTN, false, s));
+            if (use_bp) bcur = 1 - bcur;
+        }
+        // x = residual + o W_o^T
+        {
+            GemvArgs a{};
+            a.in = st->attn;
+            a.in_dt = DT_F32;
+            a.in_ld = Hq * D;
+            a.rms = RMS_NONE;
+            a.epi = EPI_RESID;
+            a.out = st->x;
+            a.out_ld = H;
+            a.resid = first ? hidden_in : (const void*)st->x;
+            a.resid_dt = first ? act_dt : DT_F32;
+            a.resid_ld = H;
+            a.ssq_out = st->ssq;
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_OPROJ, true, s));
+            if (use_bp) {                                   // also prepares RMSNorm_ffn's input (c = rs_attn)
+                bp_in(a, 0);
+                bp_out(a);
+                a.gamma_next = Ld.ffn_norm;
+                a.gamma_next_dt = act_dt;
+                a.rs_in = st->rsb;
+                HIP_TRY(run_bp(Ld.o, a));
+                bcur = 1 - bcur;
+            } else {
+                HIP_TRY(run_gemv(Ld.o, a, Hq * D, H, H, 4, first ? 2 : 4));
+            }
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_OPROJ, false, s));
+        }
+        // act = silu(h2 W_g^T) * (h2 W_u^T), h2 = RMSNorm(x)
+        {
+            GemvArgs a{};
+            a.in = st->x;
+            a.in_dt = DT_F32;
+            a.in_ld = H;
+            a.gamma = Ld.ffn_norm;
+            a.gamma_dt = act_dt;
+            a.rms = RMS_PARTIALS;
+            a.eps = c.rms_eps;
+            a.ssq_in = st->ssq;
+            a.ssq_tiles = st->ntiles_h;
+            a.epi = EPI_SWIGLU;
+            a.out = st->act;
+            a.out_ld = F;
+            a.n_valid = F;
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_GATEUP, true, s));
+            if (use_bp) {                                   // also prepares the down product's input
+                bp_in(a, 1);
+                bp_out(a);
+                a.rs_out = st->rsb;
+                HIP_TRY(run_bp(Ld.gu, a));
+                bcur = 1 - bcur;
+            } else {
+                HIP_TRY(run_gemv(Ld.gu, a, H, F, 0, 4, 0));
+            }
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_GATEUP, false, s));
+        }
+        // x = x + act W_d^T  (last layer also writes hidden_out)
+        {
+            GemvArgs a{};
+            a.in = st->act;
+            a.in_dt = DT_F32;
+            a.in_ld = F;
+            a.rms = RMS_NONE;
+            a.epi = EPI_RESID;
+            a.out = st->x;
+            a.out_ld = H;
+            a.resid = st->x;
+            a.resid_dt = DT_F32;
+            a.resid_ld = H;
+            a.ssq_out = st->ssq;
+            if (last) {
+                a.out_act = hidden_out;
+                a.out_act_dt = act_dt;
+                a.out_act_ld = H;
+            }
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_DOWN, true, s));
+            if (use_bp) {                                   // also prepares the next layer's q|k|v input (c = rs_ffn)
+                bp_in(a, 0);
+                if (!last) {
+                    bp_out(a);
+                    a.gamma_next = st->layers[l + 1].attn_norm;
+                    a.gamma_next_dt = act_dt;
+                    a.rs_in = st->rsb;
+                }
+                HIP_TRY(run_bp(Ld.d, a));
+                if (!last) bcur = 1 - bcur;
+            } else {
+                HIP_TRY(run_gemv(Ld.d, a, F, H, H, 4, 4));
+            }
+            HIP_TRY(prof_mark(st, STAGE_KERNEL_DOWN, false, s));
+        }
+    }
+
+    return STAGE_OK;
+}
 
 extern "C" {
 
@@ -2461,227 +2341,56 @@ int stage_forward(Stage* st, const StageRequest* reqs, int n_req, const void* hi
         }
         return STAGE_OK;
     }
-    auto run_gemv = [&](const DevMat& m, GemvArgs a, size_t in_row_elems, size_t out_row_elems, size_t resid_row_elems,
-                        int in_elem_bytes, int resid_elem_bytes) -> hipError_t {
-        a.W = m.pm;
-        a.ksplit = m.ksplit;
-        a.cps = m.cps;
-        a.partial = st->gpart;
-        a.counters = st->gcnt;
-        for (int m0 = 0; m0 < M; m0 += GEMV_MAX_M) {
-            GemvArgs b = a;
-            b.M = std::min(GEMV_MAX_M, M - m0);
-            b.in = (const uint8_t*)a.in + (size_t)m0 * in_row_elems * in_elem_bytes;
-            b.out = a.out + (size_t)m0 * out_row_elems;
-            if (a.resid) b.resid = (const uint8_t*)a.resid + (size_t)m0 * resid_row_elems * resid_elem_bytes;
-            if (a.ssq_in) b.ssq_in = a.ssq_in + (size_t)m0 * a.ssq_tiles;
-            if (a.ssq_out) b.ssq_out = a.ssq_out + (size_t)m0 * m.pm.ntiles;
-            if (a.out_act) b.out_act = (uint8_t*)a.out_act + (size_t)m0 * a.out_act_ld * 2;
-            hipError_t e = launch_gemv(b, s);
-            if (e != hipSuccess) return e;
-        }
-        return hipSuccess;
-    };
-
-    // 2..64 rows: each product reads its input prepared by the kernel before it
-    const bool use_bp = st->bp_ok && M >= st->gemm_min_rows && M <= MAX_ROWS;
-    int bcur = 0;                                           // buffer holding the next product's input
-    auto bp_in = [&](GemvArgs& a, int norm) {
-        a.bp_in = st->bp[bcur];
-        a.bc_in = st->bc[bcur];
-        a.cb_in = st->cbf[bcur];
-        a.norm = norm;
-    };
-    auto bp_out = [&](GemvArgs& a) {
-        a.bp_out = st->bp[1 - bcur];
-        a.bc_out = st->bc[1 - bcur];
-        a.cb_out = st->cbf[1 - bcur];
-    };
-    auto run_bp = [&](const DevMat& m, GemvArgs a) -> hipError_t {
-        a.W = m.pm;
-        a.M = M;
-        a.kp = st->kp;
-        a.partial = st->gpart;
-        a.counters = st->gcnt;
-        a.ksplit = m.bp_split;
-        a.kg = m.bp_kg;
-        bp_form(a, m, M, st->n_cus);
-        return launch_gemm_bp(a, s);
-    };
-
-    for (int l = 0; l < c.n_layers; ++l) {
-        const LayerDev& Ld = st->layers[l];
-        const bool first = (l == 0), last = (l == c.n_layers - 1);
-        // q|k|v = RMSNorm(x) W_qkv^T
-        if (use_bp) {
-            GemvArgs a{};
-            a.eps = c.rms_eps;
-            a.ssq_in = st->ssq;
-            a.ssq_tiles = st->ntiles_h;
-            a.epi = EPI_STORE;
-            a.out = st->qkv;
-            a.out_ld = nqkv;
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, true, s));
-            if (first) {
-                HIP_TRY(launch_bprep(hidden_in, act_dt, H, Ld.attn_norm, act_dt, H, c.rms_eps, M, st->bp[bcur], st->bc[bcur],
-                                     st->kp, st->rsb, s));
-                bp_in(a, 2);
-            } else {
-                bp_in(a, 1);
-                a.rs_out = st->rsb;
-            }
-            HIP_TRY(run_bp(Ld.qkv, a));
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, false, s));
-        } else {
-            GemvArgs a{};
-            a.in = first ? hidden_in : (const void*)st->x;
-            a.in_dt = first ? act_dt : DT_F32;
-            a.in_ld = H;
-            a.gamma = Ld.attn_norm;
-            a.gamma_dt = act_dt;
-            a.rms = first ? RMS_FULLROW : RMS_PARTIALS;
-            a.eps = c.rms_eps;
-            a.ssq_in = first ? nullptr : st->ssq;
-            a.ssq_tiles = st->ntiles_h;
-            a.epi = EPI_STORE;
-            a.out = st->qkv;
-            a.out_ld = nqkv;
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, true, s));
-            HIP_TRY(run_gemv(Ld.qkv, a, H, nqkv, 0, first ? 2 : 4, 0));
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_QKV, false, s));
-        }
-        // attention (rotary, append, mask, online softmax, split merge)
-        {
-            AttnArgs a{};
-            a.qkv = st->qkv;
-            a.qkv_ld = nqkv;
-            a.out = st->attn;
-            a.out_ld = Hq * D;
-            a.meta = meta;
-            a.rope = st->rope;
+    // attention (rotary, append, mask, online softmax, split merge)
+    struct StateAttention : LayerAttention {
+        Stage* st;
+        AttnArgs a{};
+        int M, head_dim, queries_per_item_max;
+        hipStream_t s;
+        hipError_t run(int l, uint16_t* bp, float* bc) override {
             a.layer = l;
-            a.Hq = Hq;
-            a.Hkv = Hkv;
-            a.kv_dt = dt_code(c.kv_dtype);
-            a.qscale = (float)(1.4426950408889634 / std::sqrt((double)D));
-            a.part = st->apart;
-            a.counters = st->acnt;
-            // splits per (slot, kv head) follow the request's own length and slot count
-            // only (its split_len), so
-            // batch-mates never change a request's result; nsplit_max bounds the grid
-            // and is the stride of the partials
-            a.nsplit_max = max_splits;
-            a.vector_path = st->attn_vector;
-            a.dma = attn_dma_ok ? 1 : 0;
+            a.bp_out = bp;
+            a.bc_out = bc;
+            a.kp = bp ? st->kp : 0;
+            a.dbg_q = a.dbg_logits = nullptr;
+            a.dbg_keys = 0;
             if (l == st->dbg_layer && !st->attn_vector) {    // test support: record this layer's queries and scores
-                HIP_TRY(launch_fill_u32((uint32_t*)st->dbg_logits, (size_t)M * Hq * st->dbg_keys, 0xFFFFFFFFu, s));   // NaN
+                const hipError_t e = launch_fill_u32((uint32_t*)st->dbg_logits, (size_t)M * a.Hq * st->dbg_keys, 0xFFFFFFFFu, s);   // NaN
+                if (e != hipSuccess) return e;
                 a.dbg_q = st->dbg_q;
                 a.dbg_logits = st->dbg_logits;
                 a.dbg_keys = st->dbg_keys;
                 st->dbg_rows = M;
             }
-            if (use_bp) {
-                a.bp_out = st->bp[1 - bcur];
-                a.bc_out = st->bc[1 - bcur];
-                a.kp = st->kp;
-            }
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_ATTN, true, s));
-            HIP_TRY(launch_attention(a, D, max_queries_item, s));
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_ATTN, false, s));
-            if (use_bp) bcur = 1 - bcur;
+            return launch_attention(a, head_dim, queries_per_item_max, s);
         }
-        // x = residual + o W_o^T
-        {
-            GemvArgs a{};
-            a.in = st->attn;
-            a.in_dt = DT_F32;
-            a.in_ld = Hq * D;
-            a.rms = RMS_NONE;
-            a.epi = EPI_RESID;
-            a.out = st->x;
-            a.out_ld = H;
-            a.resid = first ? hidden_in : (const void*)st->x;
-            a.resid_dt = first ? act_dt : DT_F32;
-            a.resid_ld = H;
-            a.ssq_out = st->ssq;
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_OPROJ, true, s));
-            if (use_bp) {                                   // also prepares RMSNorm_ffn's input (c = rs_attn)
-                bp_in(a, 0);
-                bp_out(a);
-                a.gamma_next = Ld.ffn_norm;
-                a.gamma_next_dt = act_dt;
-                a.rs_in = st->rsb;
-                HIP_TRY(run_bp(Ld.o, a));
-                bcur = 1 - bcur;
-            } else {
-                HIP_TRY(run_gemv(Ld.o, a, Hq * D, H, H, 4, first ? 2 : 4));
-            }
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_OPROJ, false, s));
-        }
-        // act = silu(h2 W_g^T) * (h2 W_u^T), h2 = RMSNorm(x)
-        {
-            GemvArgs a{};
-            a.in = st->x;
-            a.in_dt = DT_F32;
-            a.in_ld = H;
-            a.gamma = Ld.ffn_norm;
-            a.gamma_dt = act_dt;
-            a.rms = RMS_PARTIALS;
-            a.eps = c.rms_eps;
-            a.ssq_in = st->ssq;
-            a.ssq_tiles = st->ntiles_h;
-            a.epi = EPI_SWIGLU;
-            a.out = st->act;
-            a.out_ld = F;
-            a.n_valid = F;
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_GATEUP, true, s));
-            if (use_bp) {                                   // also prepares the down product's input
-                bp_in(a, 1);
-                bp_out(a);
-                a.rs_out = st->rsb;
-                HIP_TRY(run_bp(Ld.gu, a));
-                bcur = 1 - bcur;
-            } else {
-                HIP_TRY(run_gemv(Ld.gu, a, H, F, 0, 4, 0));
-            }
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_GATEUP, false, s));
-        }
-        // x = x + act W_d^T  (last layer also writes hidden_out)
-        {
-            GemvArgs a{};
-            a.in = st->act;
-            a.in_dt = DT_F32;
-            a.in_ld = F;
-            a.rms = RMS_NONE;
-            a.epi = EPI_RESID;
-            a.out = st->x;
-            a.out_ld = H;
-            a.resid = st->x;
-            a.resid_dt = DT_F32;
-            a.resid_ld = H;
-            a.ssq_out = st->ssq;
-            if (last) {
-                a.out_act = hidden_out;
-                a.out_act_dt = act_dt;
-                a.out_act_ld = H;
-            }
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_DOWN, true, s));
-            if (use_bp) {                                   // also prepares the next layer's q|k|v input (c = rs_ffn)
-                bp_in(a, 0);
-                if (!last) {
-                    bp_out(a);
-                    a.gamma_next = st->layers[l + 1].attn_norm;
-                    a.gamma_next_dt = act_dt;
-                    a.rs_in = st->rsb;
-                }
-                HIP_TRY(run_bp(Ld.d, a));
-                if (!last) bcur = 1 - bcur;
-            } else {
-                HIP_TRY(run_gemv(Ld.d, a, F, H, H, 4, 4));
-            }
-            HIP_TRY(prof_mark(st, STAGE_KERNEL_DOWN, false, s));
-        }
-    }
+    } attention;
+    attention.st = st;
+    attention.M = M;
+    attention.head_dim = D;
+    attention.queries_per_item_max = max_queries_item;
+    attention.s = s;
+    AttnArgs& a = attention.a;
+    a.qkv = st->qkv;
+    a.qkv_ld = nqkv;
+    a.out = st->attn;
+    a.out_ld = Hq * D;
+    a.meta = meta;
+    a.rope = st->rope;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.kv_dt = dt_code(c.kv_dtype);
+    a.qscale = (float)(1.4426950408889634 / std::sqrt((double)D));
+    a.part = st->apart;
+    a.counters = st->acnt;
+    // splits per (slot, kv head) follow the request's own length and slot count
+    // only (its split_len), so
+    // batch-mates never change a request's result; nsplit_max bounds the grid
+    // and is the stride of the partials
+    a.nsplit_max = max_splits;
+    a.vector_path = st->attn_vector;
+    a.dma = attn_dma_ok ? 1 : 0;
+    if (int rc2 = run_layers(st, M, hidden_in, hidden_out, s, attention)) return rc2;
 
     // ---------------- commit host-side state
     HIP_TRY(mark_done(st, s));

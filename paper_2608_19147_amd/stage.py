@@ -30,11 +30,12 @@ _DT_OF = {torch.float32: _lib.DTYPE_F32, torch.float16: _lib.DTYPE_F16, torch.bf
 
 _LIVE_STATES: "weakref.WeakSet[KVState]" = weakref.WeakSet()
 _LIVE_MATRICES: "weakref.WeakSet[Mx4Matrix]" = weakref.WeakSet()
+_LIVE_POOLS: "weakref.WeakSet[PagePool]" = weakref.WeakSet()
 _LIVE_STAGES: "weakref.WeakSet[Stage]" = weakref.WeakSet()
 
 
 def close_all() -> None:
-    """Free every live KV state and MXFP4 matrix, then every live stage.  Registered with
+    """Free every live KV state, MXFP4 matrix and page pool, then every live stage.  Registered with
     atexit, so the library's device synchronizations and frees run while the
     interpreter and the HIP runtime are both still whole, rather than from
     ``__del__`` during interpreter shutdown."""
@@ -42,6 +43,8 @@ def close_all() -> None:
         kv.free()
     for m in list(_LIVE_MATRICES):
         m.free()
+    for pool in list(_LIVE_POOLS):
+        pool.free()
     for st in list(_LIVE_STAGES):
         st.close()
 
@@ -148,7 +151,7 @@ class Stage:
 
     # ------------------------------------------------------------------
     def close(self) -> None:
-        """Free the stage's device memory (its KV states first)."""
+        """Free the stage's device memory (its KV states, matrices and page pools first)."""
         if getattr(self, "handle", None):
             for kv in list(_LIVE_STATES):
                 if kv.stage is self:
@@ -156,6 +159,9 @@ class Stage:
             for m in list(_LIVE_MATRICES):
                 if m.stage is self:
                     m.free()
+            for pool in list(_LIVE_POOLS):
+                if pool.stage is self:
+                    pool.free()
             check(self.lib.stage_destroy(self.handle))
             self.handle = None
 
@@ -387,6 +393,32 @@ class Stage:
 
     def new_state(self, n_slots: int, capacity: int) -> "KVState":
         return KVState(self, n_slots, capacity)
+
+    def new_pages(self, n_pages: int, page_rows: int = 64, pair_axis=None) -> "PagePool":
+        """A pool of ``n_pages`` pages of ``page_rows`` (16, 32, 64, 128 or 256) cache
+        rows for sequences that share pages.  ``pair_axis`` [head_dim / 2] names the
+        axis of positions that turns each rotary pair (None: one axis)."""
+        return PagePool(self, n_pages, page_rows, pair_axis)
+
+    def forward_paged(self, requests: Sequence["PagedRequest"], hidden_in: torch.Tensor, hidden_out: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+        """``forward`` over sequences of one pool: hidden_in [M, H] (device, act dtype),
+        rows request-major.  Positions are required; every new row must see a row."""
+        for t, name in ((hidden_in, "hidden_in"), (hidden_out, "hidden_out")):
+            if t is not None and (t.dim() != 2 or t.shape[1] != self.shape.hidden or t.dtype != self.act_dtype or not t.is_cuda
+                                  or not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous device [M, hidden] tensor in the activation dtype")
+        M = sum(int(r.n_tokens) for r in requests)
+        if hidden_in.shape[0] != M or hidden_out is not None and hidden_out.shape[0] != M:
+            raise ValueError(f"the requests have {M} rows")
+        if hidden_out is not None and hidden_out.device != hidden_in.device:
+            raise ValueError("hidden_in and hidden_out must be on one device")
+        sp, empty = _on(self, stream, hidden_in.device)
+        arr, keep = _step_requests(requests)
+        if hidden_out is None:
+            hidden_out = empty(hidden_in.shape, dtype=self.act_dtype, device=hidden_in.device)
+        check(self.lib.stage_forward_paged(self.handle, arr, len(requests), hidden_in.data_ptr(), hidden_out.data_ptr(), sp))
+        return hidden_out
 
     def debug_dequant(self, layer: int, which: str, row_layout: bool = False) -> np.ndarray:
         """The matrix as the kernels decode it (tiled layout, or the row layout
@@ -645,3 +677,316 @@ class KVState:
         check(self.lib.kv_read(self.handle, layer, slot, start, count, ctypes.c_void_p(k.data_ptr()),
                                ctypes.c_void_p(v.data_ptr()), 1, ctypes.c_void_p(_stream_ptr(stream))))
         return k, v
+
+
+class PagePool:
+    """Pages of cache rows for every layer of a stage, and the sequences that hold
+    them (``Stage.new_pages``).  ``k`` and ``v`` are the pages [n_layers, n_pages,
+    n_kv_heads, page_rows, head_dim]; they start as zeros, and free ones are handed
+    out lowest first."""
+
+    def __init__(self, stage: Stage, n_pages: int, page_rows: int, pair_axis=None):
+        sh = stage.shape
+        axis = None
+        if pair_axis is not None:
+            axis = np.asarray(pair_axis)
+            if axis.shape != (sh.head_dim // 2,) or ((axis < 0) | (axis >= _lib.MAX_AXES)).any() or (axis != axis.astype(np.uint8)).any():
+                raise ValueError(f"pair_axis must name an axis below {_lib.MAX_AXES} for each of {sh.head_dim // 2} pairs")
+            axis = np.ascontiguousarray(axis, dtype=np.uint8)
+        if n_pages < 1 or page_rows not in (16, 32, 64, 128, 256):
+            raise ValueError("n_pages must be positive and page_rows 16, 32, 64, 128 or 256")
+        self.stage, self.lib = stage, stage.lib
+        self.n_pages, self.page_rows = int(n_pages), int(page_rows)
+        self.n_axes = 1 if axis is None else int(axis.max()) + 1
+        dev = torch.device("cuda", stage.device_index)
+        shape = (sh.n_layers, self.n_pages, sh.n_kv_heads, self.page_rows, sh.head_dim)
+        self.k = torch.zeros(shape, dtype=stage.kv_dtype, device=dev)
+        self.v = torch.zeros(shape, dtype=stage.kv_dtype, device=dev)
+        # the zeros are there before any stream's first call on the pool
+        torch.cuda.current_stream(dev).synchronize()
+        self._members: "weakref.WeakSet" = weakref.WeakSet()
+        h = ctypes.c_void_p()
+        check(self.lib.kv_pages_create(stage.handle, self.n_pages, self.page_rows, self.k.data_ptr(), self.v.data_ptr(),
+                                       None if axis is None else axis.ctypes.data, self.n_axes, ctypes.byref(h)))
+        self.handle = h
+        _LIVE_POOLS.add(self)
+
+    def free(self) -> None:
+        """Free the pool's sequences and steps, then the pool."""
+        if getattr(self, "handle", None):
+            for m in list(self._members):
+                m.free()
+            check(self.lib.kv_pages_free(self.handle))
+            self.handle = None
+            self.k = self.v = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    @property
+    def free_pages(self) -> int:
+        n = ctypes.c_int()
+        check(self.lib.kv_pages_available(self.handle, ctypes.byref(n)))
+        return n.value
+
+    def new_sequence(self) -> "PagedSequence":
+        h = ctypes.c_void_p()
+        check(self.lib.kv_seq_create(self.handle, ctypes.byref(h)))
+        return PagedSequence(self, h)
+
+    def new_step(self) -> "PagedStep":
+        return PagedStep(self)
+
+    def fork(self, seqs: Sequence["PagedSequence"], lengths=None, keep=None, stream=None) -> List["PagedSequence"]:
+        """One new sequence per entry of ``seqs`` (which may repeat): its first
+        ``lengths[i]`` rows (all by default), of them those that ``keep[i]`` (uint8,
+        nonzero = kept; None: all) keeps.  Whole pages ahead of the first row left out
+        are shared, the other rows copied."""
+        n = len(seqs)
+        if lengths is not None and len(lengths) != n or keep is not None and len(keep) != n:
+            raise ValueError(f"lengths and keep must have {n} entries")
+        for q in seqs:
+            q._check(self)
+        lens = None if lengths is None else np.ascontiguousarray(lengths, dtype=np.int32)
+        masks, kp = None, None
+        if keep is not None:
+            masks = [None if k is None else np.ascontiguousarray(k, dtype=np.uint8) for k in keep]
+            for i, m in enumerate(masks):
+                if m is not None and m.shape != (int(lens[i]) if lens is not None else seqs[i].length,):
+                    raise ValueError(f"keep[{i}] must have one entry per row")
+            kp = (ctypes.c_void_p * n)(*[None if m is None else m.ctypes.data for m in masks])
+        out = (ctypes.c_void_p * n)()
+        check(self.lib.kv_seq_fork((ctypes.c_void_p * n)(*[q.handle for q in seqs]), None if lens is None else lens.ctypes.data, kp, n,
+                                   out, _pool_stream(self.stage, stream)))
+        return [PagedSequence(self, ctypes.c_void_p(h)) for h in out]
+
+
+def _pool_stream(stage: Stage, stream) -> int:
+    return _on(stage, stream, torch.device("cuda", stage.device_index))[0]
+
+
+class PagedSequence:
+    """A sequence of cache rows in a pool's pages (``PagePool.new_sequence``, ``PagePool.fork``)."""
+
+    def __init__(self, pool: PagePool, handle):
+        self.pool, self.lib, self.handle = pool, pool.lib, handle
+        pool._members.add(self)
+
+    def _check(self, pool: PagePool) -> None:
+        if self.handle is None:
+            raise ValueError("the sequence has been freed")
+        if self.pool is not pool:
+            raise ValueError("the sequence belongs to another pool")
+
+    def free(self) -> None:
+        """Give back the pages that no other sequence holds."""
+        if getattr(self, "handle", None):
+            check(self.lib.kv_seq_free(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    @property
+    def length(self) -> int:
+        n = ctypes.c_int()
+        check(self.lib.kv_seq_length(self.handle, ctypes.byref(n)))
+        return n.value
+
+    @property
+    def pages(self) -> List[int]:
+        """The page of each ``page_rows`` rows."""
+        n = ctypes.c_int()
+        check(self.lib.kv_seq_pages(self.handle, None, 0, ctypes.byref(n)))
+        out = np.empty(n.value, np.int32)
+        check(self.lib.kv_seq_pages(self.handle, out.ctypes.data, n.value, ctypes.byref(n)))
+        return out.tolist()
+
+    def truncate(self, new_len: int) -> None:
+        check(self.lib.kv_seq_truncate(self.handle, int(new_len)))
+
+    def compact(self, keep, stream=None) -> int:
+        """Drop the rows that ``keep`` (uint8 [length], nonzero = kept) does not keep
+        and close the others up.  Returns the new length."""
+        keep = np.ascontiguousarray(keep, dtype=np.uint8)
+        if keep.shape != (self.length,):
+            raise ValueError(f"keep must have {self.length} entries")
+        check(self.lib.kv_seq_compact(self.handle, keep.ctypes.data, _pool_stream(self.pool.stage, stream)))
+        return self.length
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+        """Append rows k, v [L][Hkv][n][D] (device, KV dtype; K after rotary)."""
+        st = self.pool.stage
+        sh = st.shape
+        for t, name in ((k, "k"), (v, "v")):
+            if t.dim() != 4 or t.dtype != st.kv_dtype or not t.is_cuda or t.shape[2] < 1 \
+                    or (t.shape[0], t.shape[1], t.shape[3]) != (sh.n_layers, sh.n_kv_heads, sh.head_dim):
+                raise ValueError(f"{name} must be a device [layers, kv heads, rows, head_dim] tensor in the KV dtype")
+        if k.shape != v.shape or k.device != v.device:
+            raise ValueError("k and v must be alike")
+        sp, _ = _on(st, stream, k.device)
+        k, v = (t if t.is_contiguous() and t.data_ptr() % 16 == 0 else _copy_on(t, stream) for t in (k, v))
+        check(self.lib.kv_seq_append(self.handle, k.data_ptr(), v.data_ptr(), int(k.shape[2]), sp))
+
+    def load(self, state: "KVState", slot: int = 0, start: int = 0, count: Optional[int] = None, stream=None) -> None:
+        """Append rows [start, start + count) of a slot of a KV state, as the slot sees them."""
+        if count is None:
+            count = state.length - start
+        check(self.lib.kv_seq_load(self.handle, state.handle, int(slot), int(start), int(count), _pool_stream(self.pool.stage, stream)))
+
+    def read(self, layer: int, start: int = 0, count: Optional[int] = None, stream=None):
+        """Rows [start, start + count) of one layer: K, V [Hkv, count, D]."""
+        st = self.pool.stage
+        if count is None:
+            count = self.length - start
+        if count < 0:
+            raise ValueError("count must not be negative")
+        dev = torch.device("cuda", st.device_index)
+        sp, empty = _on(st, stream, dev)
+        k, v = (empty((st.shape.n_kv_heads, count, st.shape.head_dim), dtype=st.kv_dtype, device=dev) for _ in range(2))
+        check(self.lib.kv_seq_read(self.handle, int(layer), int(start), int(count), k.data_ptr() or 16, v.data_ptr() or 16, sp))
+        return k, v
+
+
+def _copy_on(t: torch.Tensor, stream) -> torch.Tensor:
+    """A contiguous copy made on ``stream`` (None: the current one), where the call that takes it runs."""
+    if stream is None:
+        return t.clone(memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return t.clone(memory_format=torch.contiguous_format)
+
+
+@dataclass
+class PagedRequest:
+    """One sequence of a step and its ``n_tokens`` new rows: positions int32
+    [n_tokens] or [n_axes, n_tokens] (None: rows are not turned), mask [P + n_tokens]
+    uint8 (nonzero = visible) or None, mask_rows [n_tokens, P + n_tokens] uint8 (one
+    mask per new row) or None.  New row i sees row j iff j <= P + i and both masks
+    keep j."""
+
+    seq: PagedSequence
+    n_tokens: int
+    positions: Optional[np.ndarray] = None
+    mask: Optional[np.ndarray] = None
+    mask_rows: Optional[np.ndarray] = None
+
+
+def _step_requests(requests: Sequence[PagedRequest]):
+    """The C array of a step's requests, and what has to live as long as its call."""
+    arr = (_lib.KVStepRequest * len(requests))()
+    keep = []
+
+    def put(a, dtype, shape, name):
+        if a is None:
+            return None
+        a = np.ascontiguousarray(a, dtype=dtype)
+        if a.shape != shape and a.size == int(np.prod(shape)) and len(shape) == 2 and shape[0] == 1:
+            a = a.reshape(shape)
+        if a.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, is {list(a.shape)}")
+        keep.append(a)
+        return a.ctypes.data
+
+    for c, r in zip(arr, requests):
+        r.seq._check(r.seq.pool)
+        n, T = int(r.n_tokens), r.seq.length + int(r.n_tokens)
+        c.seq, c.n_tokens = r.seq.handle, n
+        c.positions = put(r.positions, np.int32, (r.seq.pool.n_axes, n), "positions")
+        c.attention_mask = put(r.mask, np.uint8, (T,), "mask")
+        c.attention_mask_rows = put(r.mask_rows, np.uint8, (n, T), "mask_rows")
+    return arr, keep
+
+
+class PagedStep:
+    """A batch of sequences with new rows each (``PagePool.new_step``): ``plan`` makes
+    room for them, then every layer's rows are written (``write``) and attend
+    (``attend``).  Rows are request-major."""
+
+    def __init__(self, pool: PagePool):
+        self.pool, self.lib = pool, pool.lib
+        sh = pool.stage.shape
+        self._nq, self._nk = sh.n_q_heads * sh.head_dim, sh.n_kv_heads * sh.head_dim
+        h = ctypes.c_void_p()
+        check(self.lib.kv_step_create(pool.handle, ctypes.byref(h)))
+        self.handle = h
+        self.rows = self._ws = 0
+        pool._members.add(self)
+
+    def free(self) -> None:
+        if getattr(self, "handle", None):
+            check(self.lib.kv_step_free(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    def plan(self, requests: Sequence[PagedRequest], stream=None) -> None:
+        """Make room for the new rows of each request's sequence, whose length grows by
+        them, and lay out the step."""
+        for r in requests:
+            r.seq._check(self.pool)
+        arr, keep = _step_requests(requests)
+        check(self.lib.kv_step_plan(self.handle, arr, len(requests), _pool_stream(self.pool.stage, stream)))
+        ws = ctypes.c_int64()
+        check(self.lib.kv_step_workspace(self.handle, ctypes.byref(ws)))
+        self.rows, self._ws = sum(int(r.n_tokens) for r in requests), ws.value
+
+    def _in(self, t: torch.Tensor, width: int, name: str, device=None) -> int:
+        ld = _rows(t, name)
+        if t.shape[0] != self.rows or t.shape[1] != width or device is not None and t.device != device:
+            raise ValueError(f"{name} must be [{self.rows}, {width}]" + ("" if device is None else f" on {device}"))
+        return ld
+
+    def write(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+        """Turn q [M, Hq D] and k [M, Hkv D] by the rows' positions, store k and v [M,
+        Hkv D] in their rows of the pages, and return q (in the KV dtype, or in
+        ``q_out``).  Rows may be parts of wider ones; all of one dtype."""
+        st, dev = self.pool.stage, q.device
+        ldq, ldk, ldv = self._in(q, self._nq, "q"), self._in(k, self._nk, "k", dev), self._in(v, self._nk, "v", dev)
+        if q.dtype != k.dtype or q.dtype != v.dtype:
+            raise ValueError("q, k and v must have one dtype")
+        sp, empty = _on(st, stream, dev)
+        if q_out is None:
+            q_out, ldo = empty((self.rows, self._nq), dtype=st.kv_dtype, device=dev), self._nq
+        else:
+            ldo = self._in(q_out, self._nq, "q_out", dev)
+        check(self.lib.kv_step_write(self.handle, layer, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _DT_OF[q.dtype],
+                                     q_out.data_ptr(), ldo, _DT_OF[q_out.dtype], sp))
+        return q_out
+
+    def attend(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, out_dtype: Optional[torch.dtype] = None,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention [M, Hq D] of the turned queries q [M, Hq D] (KV dtype or float32)
+        over the rows that they see (``scale`` 1/sqrt(head_dim) by default), in
+        ``out_dtype`` (q's by default) or into ``out``; a row that sees none gives
+        zeros."""
+        st, dev = self.pool.stage, q.device
+        ldq = self._in(q, self._nq, "q")
+        if q.dtype != torch.float32 and q.dtype != st.kv_dtype:
+            raise ValueError("q must be float32 or in the KV dtype")
+        if scale is not None and not scale > 0:
+            raise ValueError("scale must be positive")
+        sp, empty = _on(st, stream, dev)
+        if out is None:
+            out_dtype = out_dtype or q.dtype
+            if out_dtype not in _DT_OF:
+                raise ValueError("out_dtype must be float32, float16 or bfloat16")
+            out, ldo = empty((self.rows, self._nq), dtype=out_dtype, device=dev), self._nq
+        else:
+            if out_dtype not in (None, out.dtype):
+                raise ValueError("out has another dtype")
+            ldo = self._in(out, self._nq, "out", dev)
+        room = empty(self._ws, dtype=torch.uint8, device=dev) if self._ws else None
+        check(self.lib.kv_step_attend(self.handle, layer, q.data_ptr(), _DT_OF[q.dtype], ldq, out.data_ptr(), _DT_OF[out.dtype], ldo,
+                                      scale or 0.0, room.data_ptr() if room is not None else None, self._ws, sp))
+        return out
