@@ -514,3 +514,299 @@ def test_load_from_a_state(stages):
             assert all(torch.equal(a, b) for a, b in zip(s.read(l), want))
     pool.free()
     state.free()
+
+
+# ------------------------------------------------------------------ the forward over sequences
+
+@pytest.fixture(scope="module")
+def pair():
+    import synth
+    from gpu_cases import Pair
+    p = Pair(synth.TINY, 77)
+    yield p
+    p.close()
+
+
+def _twin(pair, rows_k, rows_v, cap=400):
+    """A KV state and the oracle's with the given rows [L, Hkv, n, D]."""
+    import oracle
+    g = pair.gpu.new_state(1, cap)
+    o = oracle.OracleState(pair.shape, 1, cap)
+    if rows_k.shape[2]:
+        g.append(rows_k[:, None].contiguous(), rows_v[:, None].contiguous())
+        o.append(rows_k[:, None].double().cpu().numpy(), rows_v[:, None].double().cpu().numpy())
+    return g, o
+
+
+@pytest.mark.parametrize("n", [[1, 1, 1], [3, 1, 5], [20, 17, 9]])
+@pytest.mark.parametrize("page", [16, 64])
+def test_forward_over_shared_pages(pair, n, page):
+    """Requests that share a prefix, through the stage: as stage_forward of states that hold the prefix each (to rounding), and as
+    the oracle; twice in turn, so that the second forward reads what the first wrote.  One request hides rows, one is a tree."""
+    import oracle
+    from gpu_cases import TOL_STAGE, Request, host, rel_err
+    import synth
+    st = pair.gpu
+    pool = st.new_pages(60, page)
+    base = pool.new_sequence()
+    k, v = ref.rows(st, 200, 5, 0.7), ref.rows(st, 200, 6)
+    base.append(k, v)
+    seqs = pool.fork([base] * 3)
+    mine = [(ref.rows(st, m, 10 + m, 0.7), ref.rows(st, m, 20 + m)) for m in (1, 40, 13)]
+    states, oracles = [], []
+    for s, (a, b) in zip(seqs, mine):
+        s.append(a, b)
+        g, o = _twin(pair, torch.cat([k, a], 2), torch.cat([v, b], 2))
+        states.append(g)
+        oracles.append(o)
+    for turn in range(2):
+        P = [s.length for s in seqs]
+        pos = [np.arange(p, p + m, dtype=np.int32) for p, m in zip(P, n)]
+        masks = [np.ones(P[0] + n[0], np.uint8), _holes(P[1] + n[1], n[1], 3), None]
+        rows = [None, None, _tree(n[2], P[2] + n[2], 4)]
+        x = synth.make_hidden(pair.shape, sum(n), 0, 3 + turn).cuda()
+        got = st.forward_paged([PagedRequest(s, m, positions=p, mask=mk, mask_rows=w) for s, m, p, mk, w in zip(seqs, n, pos, masks, rows)], x)
+        same = st.forward([Request(g, p[None], None if mk is None else mk[None], None, None if w is None else w[None])
+                           for g, p, mk, w in zip(states, pos, masks, rows)], x)
+        row = 0
+        for i in range(3):
+            a, b = got[row:row + n[i]], same[row:row + n[i]]
+            see = ref.sees(P[i], n[i], masks[i], rows[i]).astype(np.uint8)
+            want = oracle.forward(pair.orc, oracles[i], host(x[row:row + n[i]]), pos[i][None], None, None, see[None])
+            assert rel_err(host(a), want) <= TOL_STAGE
+            assert rel_err(host(a), want) <= 1.5 * rel_err(host(b), want) + 1e-3
+            row += n[i]
+    for i in range(3):
+        assert seqs[i].length == states[i].length
+        for l in range(pair.shape.n_layers):
+            a, b = seqs[i].read(l), states[i].read(l, 0, 0, states[i].length)
+            assert all(rel_err(host(x), host(y)) <= TOL_STAGE for x, y in zip(a, b))
+    pool.free()
+    for g in states:
+        g.free()
+
+
+def test_forward_generates_from_forks(pair):
+    """One prompt prefilled into a state, loaded into pages, forked, decoded by several requests at once, one of them with its
+    rejected rows cut or compacted away: each goes on as a state of its own would."""
+    from gpu_cases import TOL_STAGE, Request, host, rel_err
+    import synth
+    st = pair.gpu
+    prompt = synth.make_hidden(pair.shape, 90, 0, 8).cuda()
+    states = [st.new_state(1, 200) for _ in range(3)]
+    for g in states:
+        st.prefill(g, np.arange(90), prompt)
+    pool = st.new_pages(40, 16)
+    base = pool.new_sequence()
+    base.load(states[0])
+    seqs = pool.fork([base] * 3)
+    base.free()
+    for turn in range(4):
+        x = synth.make_hidden(pair.shape, 3 * 4, 0, 20 + turn).cuda()
+        P = [s.length for s in seqs]
+        got = st.forward_paged([PagedRequest(s, 4, positions=np.arange(p, p + 4)) for s, p in zip(seqs, P)], x)
+        for i, g in enumerate(states):
+            want = st.forward([Request(g, np.arange(P[i], P[i] + 4, dtype=np.int32)[None], np.ones((1, P[i] + 4), np.uint8))], x[4 * i:4 * i + 4])
+            assert rel_err(host(got[4 * i:4 * i + 4]), host(want)) <= TOL_STAGE
+        keep = np.ones(P[1] + 4, np.uint8)
+        keep[P[1] + 1:P[1] + 3] = 0                              # the second and third new rows were rejected
+        seqs[1].compact(keep)
+        states[1].compact(keep[None])
+        seqs[2].truncate(P[2] + 1)
+        states[2].truncate(P[2] + 1)
+        assert [s.length for s in seqs] == [g.length for g in states]
+    pool.free()
+    for g in states:
+        g.free()
+
+
+def test_forward_refused(pair):
+    st = pair.gpu
+    pool, other = st.new_pages(4, 16), st.new_pages(4, 16)
+    a, b, c = pool.new_sequence(), pool.new_sequence(), other.new_sequence()
+    x = torch.zeros((2, pair.shape.hidden), dtype=st.act_dtype, device="cuda")
+    pos = np.zeros(1, np.int32)
+    for reqs, code in (([PagedRequest(a, 1), PagedRequest(b, 1)], -1),                                    # no positions
+                       ([PagedRequest(a, 1, pos), PagedRequest(a, 1, pos)], -6),                          # twice
+                       ([PagedRequest(a, 1, pos), PagedRequest(c, 1, pos)], -6),                          # another pool
+                       ([PagedRequest(a, 1, pos), PagedRequest(b, 1, pos + 10 ** 6)], -3),                # position
+                       ([PagedRequest(a, 1, pos), PagedRequest(b, 1, pos, mask=np.zeros(1, np.uint8))], -1)):
+        with pytest.raises(StageError) as e:
+            st.forward_paged(reqs, x)
+        assert e.value.code == code and a.length == b.length == c.length == 0 and pool.free_pages == 4
+    with pytest.raises(StageError) as e:
+        st.forward_paged([PagedRequest(a, 65, np.arange(65))], torch.zeros((65, pair.shape.hidden), dtype=st.act_dtype, device="cuda"))
+    assert e.value.code == -3
+    with pytest.raises(ValueError):
+        st.forward_paged([PagedRequest(a, 1, pos)], x)
+    with pytest.raises(StageError) as e:                         # hidden rows overlap
+        st.forward_paged([PagedRequest(a, 1, pos), PagedRequest(b, 1, pos)], x, hidden_out=x)
+    assert e.value.code == -1
+    small = st.new_pages(1, 16)
+    d, f = small.new_sequence(), small.new_sequence()
+    with pytest.raises(StageError) as e:
+        st.forward_paged([PagedRequest(d, 1, pos), PagedRequest(f, 1, pos)], x)
+    assert e.value.code == -3 and small.free_pages == 1 and d.length == 0
+    for p in (pool, other, small):
+        p.free()
+
+
+# ------------------------------------------------------------------ streams, graphs
+
+def test_graphs_of_a_step(stages):
+    """Two graphs of a step's write and attention on two streams at once, and eager calls in between: every replay gives the eager
+    result for the queries that stand there then."""
+    st = stages(Hq=8, Hkv=2, D=128, kv="bf16")
+    prefixes, own, n = BATCHES["same prefix"]
+    pool, seqs, P = _batch(st, 16, prefixes, own, n)
+    step = pool.new_step()
+    step.plan([PagedRequest(q, m, positions=np.arange(p, p + m)) for q, m, p in zip(seqs, n, P)])
+    M = sum(n)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    xs = [torch.randn((M, 8 * 128), device="cuda", generator=g).to(torch.bfloat16) for _ in range(8)]
+    kv = torch.randn((M, 2 * 128), device="cuda", generator=g).to(torch.bfloat16)
+    eager = [step.attend(0, step.write(0, x, kv, kv)) for x in xs]
+    held = []
+    for j in range(2):
+        s = torch.cuda.Stream()
+        x = xs[0].clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out = step.attend(0, step.write(0, x, kv, kv))
+        held.append((s, x, graph, out))
+    for i in range(0, 8, 2):
+        for j, (s, x, graph, out) in enumerate(held):
+            with torch.cuda.stream(s):
+                x.copy_(xs[i + j])
+                graph.replay()
+        again = step.attend(0, step.write(0, xs[i], kv, kv))
+        torch.cuda.synchronize()
+        assert torch.equal(again, eager[i])
+        for j, (s, x, graph, out) in enumerate(held):
+            assert torch.equal(out, eager[i + j])
+    with pytest.raises(StageError) as e:                         # the graphs hold this plan
+        step.plan([PagedRequest(seqs[0], 1)])
+    assert e.value.code == -7
+    del held
+    pool.free()
+
+
+def test_capture_refused(stages):
+    st = stages(Hq=4, Hkv=2, D=64, kv="bf16")
+    pool = st.new_pages(8, 16)
+    a = pool.new_sequence()
+    r = ref.rows(st, 20, 1)
+    a.append(r, r)
+    step = pool.new_step()
+    calls = [lambda: pool.fork([a]), lambda: a.append(r, r), lambda: a.compact(np.zeros(20, np.uint8)), lambda: a.read(0),
+             lambda: step.plan([PagedRequest(a, 1)])]
+    for call in calls:
+        graph, codes = torch.cuda.CUDAGraph(), []
+        with torch.cuda.graph(graph):
+            torch.zeros(1, device="cuda")
+            try:
+                call()
+            except StageError as e:
+                codes.append(e.code)
+        assert codes == [-7]
+    assert a.length == 20 and pool.free_pages == 6
+    pool.free()
+
+
+def test_calls_on_other_streams(stages):
+    """A sequence appended on one stream, forked on a second, stepped on a third and read on a fourth: in the order of the calls."""
+    st = stages(L=2, Hq=4, Hkv=2, D=128, kv="f16")
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    k, v = ref.rows(st, 3000, 1), ref.rows(st, 3000, 2)
+    new = [_q(st, 4, 20 + i)[:, :2 * 128] for i in range(2)]
+    q = _q(st, 4, 30)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        pool = st.new_pages(2 * 190, 16)
+        a = pool.new_sequence()
+        a.append(k, v, stream=streams[0])
+        b = pool.fork([a], keep=[np.arange(3000) % 3 != 0], stream=streams[1])[0]
+        step = pool.new_step()
+        step.plan([PagedRequest(a, 3), PagedRequest(b, 1)], stream=streams[2])
+        step.write(1, q, *new, stream=streams[3])
+        out = step.attend(1, q, stream=streams[0])
+        got = b.read(1, stream=streams[1])
+        for s in streams:
+            s.synchronize()
+        want = torch.arange(3000, device="cuda") % 3 != 0
+        assert torch.equal(got[0], torch.cat([k[1][:, want], new[0][3:].view(1, 2, 128).transpose(0, 1)], 1))
+        assert torch.equal(out, step.attend(1, q))
+        pool.free()
+
+
+def test_binding_refusals(stages):
+    st = stages(Hq=4, Hkv=2, D=64, kv="bf16")
+    pool, other = st.new_pages(8, 16), st.new_pages(2, 16)
+    a = pool.new_sequence()
+    step = pool.new_step()
+    q, k = _q(st, 2, 1), _q(st, 2, 2)[:, :128]
+    with pytest.raises(ValueError):
+        step.write(0, q, k, k)                                   # no plan: no rows
+    with pytest.raises(ValueError):
+        step.plan([PagedRequest(other.new_sequence(), 1)])
+    with pytest.raises(ValueError):
+        step.plan([PagedRequest(a, 2, mask=np.ones(3, np.uint8))])
+    with pytest.raises(ValueError):
+        step.plan([PagedRequest(a, 2, mask_rows=np.ones((1, 2), np.uint8))])
+    with pytest.raises(ValueError):
+        step.plan([PagedRequest(a, 2, positions=np.zeros((3, 2), np.int32))])
+    with pytest.raises(StageError) as e:
+        step.plan([PagedRequest(a, 8 * 16 + 1)])
+    assert e.value.code == -3 and a.length == 0 and pool.free_pages == 8
+    with pytest.raises(StageError) as e:
+        step.plan([PagedRequest(a, 0)])
+    assert e.value.code == -1
+    with pytest.raises(StageError) as e:
+        step.plan([])
+    assert e.value.code == -1
+    step.plan([PagedRequest(a, 2)])
+    for bad in (q[:1], q.half(), q.double(), q.t(), q.cpu(), _q(st, 2, 1).repeat(1, 2)):
+        with pytest.raises(ValueError):
+            step.attend(0, bad)
+    for layer in (-1, 1):
+        with pytest.raises(StageError):
+            step.attend(layer, q)
+        with pytest.raises(StageError):
+            step.write(layer, q, k, k)
+    with pytest.raises(ValueError):
+        step.attend(0, q, scale=0.0)
+    with pytest.raises(StageError):
+        step.attend(0, q, scale=math.inf)
+    with pytest.raises(ValueError):
+        step.write(0, q, k.float(), k)
+    with pytest.raises(ValueError):
+        step.write(0, q, k, _q(st, 2, 2)[:, :64])
+    with pytest.raises(ValueError):
+        pool.fork([a], lengths=[1, 2])
+    with pytest.raises(StageError):
+        pool.fork([a], lengths=[3])
+    with pytest.raises(ValueError):
+        pool.fork([a], keep=[np.ones(1, np.uint8)])
+    with pytest.raises(ValueError):
+        a.append(ref.rows(st, 1, 1), ref.rows(st, 2, 1))
+    with pytest.raises(ValueError):
+        a.append(ref.rows(st, 1, 1).float(), ref.rows(st, 1, 1).float())
+    for args in ((0, 0, 3), (0, -1, 1), (1, 0, 1), (0, 2, 1)):
+        with pytest.raises(StageError):
+            a.read(*args)
+    with pytest.raises(StageError):
+        a.truncate(3)
+    with pytest.raises(ValueError):
+        a.compact(np.ones(3, np.uint8))
+    a.free()
+    with pytest.raises(ValueError):
+        pool.fork([a])
+    with pytest.raises(ValueError):
+        st.new_pages(4, 48)
+    with pytest.raises(ValueError):
+        st.new_pages(4, 16, pair_axis=np.full(32, 4))
+    with pytest.raises(ValueError):
+        st.new_pages(4, 16, pair_axis=np.zeros(31))
+    pool.free()
+    other.free()
