@@ -52,9 +52,9 @@ struct KVStep {
     int ring = 0;
     // the plan
     bool planned = false, captured = false, turned = false, merge = false;
-    int M = 0, n_items = 0;
+    int M = 0, n_few = 0, n_many = 0;
     size_t parts = 0;
-    size_t o_items = 0, o_rows = 0, o_rowlist = 0, o_tables = 0, o_slots = 0, o_pos = 0, o_masks = 0;
+    size_t o_items = 0, o_rows = 0, o_list = 0, o_tables = 0, o_slots = 0, o_pos = 0, o_masks = 0;
 
     size_t part_bytes() const {
         const StageConfig& c = pool->stage->cfg;
@@ -133,20 +133,21 @@ void pack_bits(const uint8_t* m, int n, uint32_t* out) {
 // parent of) theirs.
 struct Run {
     int k0, k1, rows, n_rows, seq, parent;
+    bool shared;
     int chunk = 0, splits = 1, slot = 0;
 };
 
 struct Layout {
     std::vector<PagedItem> items;
-    std::vector<PagedRow> rows;
+    std::vector<PagedRow> rows, list;
     std::vector<int> rowlist, tables, slots, pos;
     std::vector<uint32_t> masks;
+    int n_few = 0;
     size_t parts = 0;
     bool merge = false;
 };
 
 constexpr int SHARE_KEYS = 128;                    // fewest keys worth a run of their own
-constexpr int SHARE_QUERIES = 64;                  // a sequence with more query vectors a kv head fills tiles alone
 constexpr int SPLIT_STEPS = 8;                     // fewest steps of 32 keys of a split
 
 // The runs of a batch: sequences sorted by their whole pages, so that those that share pages are neighbours; a common
@@ -161,8 +162,8 @@ struct RunBuilder {
     std::vector<int>& rowlist;
 
     int whole(int s) const { return P[s] / pool->page_rows; }
-    int add(const int* order, int cnt, int k0, int k1, int parent) {
-        Run r{k0, k1, (int)rowlist.size(), 0, order[0], parent};
+    int add(const int* order, int cnt, int k0, int k1, int parent, bool shared) {
+        Run r{k0, k1, (int)rowlist.size(), 0, order[0], parent, shared};
         for (int i = 0; i < cnt; ++i)
             for (int t = 0; t < n[order[i]]; ++t) rowlist.push_back(row0[order[i]] + t);
         r.n_rows = (int)rowlist.size() - r.rows;
@@ -173,7 +174,7 @@ struct RunBuilder {
         const int pr = pool->page_rows;
         for (;;) {
             if (cnt == 1) {
-                add(order, 1, from * pr, P[order[0]] + n[order[0]], parent);
+                add(order, 1, from * pr, P[order[0]] + n[order[0]], parent, false);
                 return;
             }
             const std::vector<int>&a = *pages[order[0]], &b = *pages[order[cnt - 1]];
@@ -181,7 +182,7 @@ struct RunBuilder {
             int lcp = from;
             while (lcp < lim && a[lcp] == b[lcp]) ++lcp;
             if ((lcp - from) * pr >= SHARE_KEYS) {
-                parent = add(order, cnt, from * pr, lcp * pr, parent);
+                parent = add(order, cnt, from * pr, lcp * pr, parent, true);
                 from = lcp;
             }
             // sets with the same page at lcp; a sequence that ends there is alone.  The last set goes on in this loop.
@@ -199,36 +200,50 @@ struct RunBuilder {
     }
 };
 
-int tiles_of(int q) { return q > 64 ? 4 : q > 32 ? 2 : 1; }
-
+// Splits of the runs, their tiles as workgroups and each row's partial results.  A tile is up to 64 query vectors (128 in
+// runs with more, which are prompts'), a split a whole number of steps of 32 keys.  Splits are as long as leaves every
+// place on the card a workgroup (four a CU; two of the larger tiles) and no more: what a split adds is a partial result of
+// each of its query vectors, written and read.
 void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table_off, std::vector<Run>& runs, Layout& L) {
     const StageConfig& c = pool->stage->cfg;
     const int gs = c.n_q_heads / c.n_kv_heads;
-    // time of a run's tile, in steps of a workgroup: one tile's keys are shared by its four waves
     auto steps = [](int k0, int k1) { return (k1 + 31) / 32 - k0 / 32; };
-    double total = 0;
-    for (const Run& r : runs)
-        for (int q = 0; q < r.n_rows * gs; q += 128) {
-            const int nq = std::min(128, r.n_rows * gs - q);
-            const int last = L.rowlist[r.rows + (q + nq - 1) / gs];
-            total += (double)steps(r.k0, std::min(r.k1, std::max(r.k0 + 1, L.rows[last].limit))) * tiles_of(nq) / 4;
+    auto many = [&](const Run& r) { return !r.shared && (long)r.n_rows * gs > PAGED_FEW; };
+    auto tiles = [&](const Run& r) { const int t = many(r) ? PAGED_MANY : PAGED_FEW; return (r.n_rows * gs + t - 1) / t; };
+    for (int kind = 0; kind < 2; ++kind) {
+        const long places = (long)(kind ? 2 : 4) * n_cus;
+        int longest = 0;
+        long all = 0;
+        for (const Run& r : runs)
+            if (many(r) == (kind == 1)) {
+                longest = std::max(longest, steps(r.k0, r.k1));
+                all += tiles(r);
+            }
+        if (!all) continue;
+        // the shortest split with which the workgroups fit in the places
+        int lo = std::min(SPLIT_STEPS, longest), hi = longest;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            long wgs = 0;
+            for (const Run& r : runs)
+                if (many(r) == (kind == 1)) wgs += (long)tiles(r) * ((steps(r.k0, r.k1) + mid - 1) / mid);
+            if (wgs * c.n_kv_heads <= places) hi = mid;
+            else lo = mid + 1;
         }
-    total *= c.n_kv_heads;
-    const double share = total / (2.0 * n_cus);    // two workgroups a CU at once
-    for (Run& r : runs) {
-        const int nqt = tiles_of(std::min(128, r.n_rows * gs)), all = steps(r.k0, r.k1);
-        int st = std::max(SPLIT_STEPS, (int)std::ceil(share * 4 / nqt));
-        const int S = (all + st - 1) / st;
-        st = (all + S - 1) / S;
-        r.chunk = 32 * st;
-        r.splits = (all + st - 1) / st;
-        if (r.parent >= 0) r.slot = runs[r.parent].slot + runs[r.parent].splits;
+        for (Run& r : runs)
+            if (many(r) == (kind == 1)) {
+                const int n = steps(r.k0, r.k1), S = (n + lo - 1) / lo, st = (n + S - 1) / S;
+                r.chunk = 32 * st;
+                r.splits = (n + st - 1) / st;
+            }
     }
     std::vector<float> cost;
-    for (const Run& r : runs) {
-        const int a0 = r.k0 / 32 * 32;             // splits end at whole steps
-        for (int q = 0; q < r.n_rows * gs; q += 128) {
-            const int nq = std::min(128, r.n_rows * gs - q), nqt = tiles_of(nq);
+    std::vector<char> kind;
+    for (Run& r : runs) {
+        if (r.parent >= 0) r.slot = runs[r.parent].slot + runs[r.parent].splits;
+        const int a0 = r.k0 / 32 * 32, T = many(r) ? PAGED_MANY : PAGED_FEW;   // splits end at whole steps
+        for (int q = 0; q < r.n_rows * gs; q += T) {
+            const int nq = std::min(T, r.n_rows * gs - q);
             int lo = INT_MAX, hi = 0;
             bool masked = false;
             for (int i = q / gs; i <= (q + nq - 1) / gs; ++i) {
@@ -240,25 +255,23 @@ void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table
             for (int j = 0; j < r.splits; ++j) {
                 const int kb = std::max(r.k0, a0 + j * r.chunk), ke = std::min({r.k1, a0 + (j + 1) * r.chunk, hi});
                 if (ke <= kb) break;
-                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, nqt | (!masked && lo >= ke ? 8 : 0)});
-                cost.push_back((float)steps(kb, ke) * nqt);
+                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, !masked && lo >= ke});
+                cost.push_back((float)steps(kb, ke));
+                kind.push_back(many(r));
             }
         }
     }
-    // the longest first
+    // small tiles first; of each kind the longest
     std::vector<int> at(L.items.size());
     std::iota(at.begin(), at.end(), 0);
-    std::stable_sort(at.begin(), at.end(), [&](int x, int y) { return cost[x] > cost[y]; });
+    std::stable_sort(at.begin(), at.end(), [&](int x, int y) { return kind[x] != kind[y] ? kind[x] < kind[y] : cost[x] > cost[y]; });
     std::vector<PagedItem> sorted(L.items.size());
     for (size_t i = 0; i < at.size(); ++i) sorted[i] = L.items[at[i]];
     L.items.swap(sorted);
+    L.n_few = (int)std::count(kind.begin(), kind.end(), 0);
     // a row's partial results: its ancestors' splits, and those of its own run that begin before its limit
-    std::vector<char> parent(runs.size(), 0);
-    for (const Run& r : runs)
-        if (r.parent >= 0) parent[r.parent] = 1;
-    for (size_t k = 0; k < runs.size(); ++k) {
-        const Run& r = runs[k];
-        if (parent[k]) continue;                   // (a shared run is never a row's last)
+    for (const Run& r : runs) {
+        if (r.shared) continue;                    // never a row's last
         const int a0 = r.k0 / 32 * 32;
         for (int i = 0; i < r.n_rows; ++i) {
             PagedRow& w = L.rows[L.rowlist[r.rows + i]];
@@ -270,6 +283,8 @@ void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table
             }
         }
     }
+    L.list.reserve(L.rowlist.size());
+    for (int row : L.rowlist) L.list.push_back(L.rows[row]);
 }
 
 struct Planned {                                   // of one request
@@ -434,7 +449,7 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
         table_off.push_back((int)L.tables.size());
         L.tables.insert(L.tables.end(), p.pages.begin(), p.pages.end());
         for (int i = 0; i < p.n; ++i) {
-            L.rows[row + i] = PagedRow{p.P + i + 1, -1, 0, 1};
+            L.rows[row + i] = PagedRow{row + i, p.P + i + 1, -1, 0, 1, {}};
             L.slots.push_back(pool->slot(p.pages, p.P + i));
         }
         lay_out_masks(reqs[r], p.P, row, L);
@@ -449,7 +464,7 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     RunBuilder rb{pool, pages, P, n, row0, runs, L.rowlist};
     const int gs = c.n_q_heads / c.n_kv_heads;
     std::iota(order.begin(), order.end(), 0);
-    auto alone = std::stable_partition(order.begin(), order.end(), [&](int x) { return (long)n[x] * gs <= SHARE_QUERIES; });
+    auto alone = std::stable_partition(order.begin(), order.end(), [&](int x) { return (long)n[x] * gs <= PAGED_FEW; });
     std::sort(order.begin(), alone, [&](int x, int y) {
         return std::lexicographical_compare(pages[x]->begin(), pages[x]->begin() + rb.whole(x), pages[y]->begin(), pages[y]->begin() + rb.whole(y));
     });
@@ -460,7 +475,7 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
         return fail(STAGE_E_CAPACITY, "too many rows in one step");
 
     size_t bytes = 0;
-    const size_t o_items = place(bytes, L.items), o_rows = place(bytes, L.rows), o_rowlist = place(bytes, L.rowlist),
+    const size_t o_items = place(bytes, L.items), o_rows = place(bytes, L.rows), o_list = place(bytes, L.list),
                  o_tables = place(bytes, L.tables), o_slots = place(bytes, L.slots), o_pos = place(bytes, L.pos),
                  o_masks = place(bytes, L.masks), o_moves = place(bytes, moves);
     if (int rc = step_room(step, bytes)) return rc;
@@ -470,7 +485,7 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     };
     put(o_items, L.items.data(), L.items.size() * sizeof(PagedItem));
     put(o_rows, L.rows.data(), L.rows.size() * sizeof(PagedRow));
-    put(o_rowlist, L.rowlist.data(), L.rowlist.size() * 4);
+    put(o_list, L.list.data(), L.list.size() * sizeof(PagedRow));
     put(o_tables, L.tables.data(), L.tables.size() * 4);
     put(o_slots, L.slots.data(), L.slots.size() * 4);
     put(o_pos, L.pos.data(), L.pos.size() * 4);
@@ -494,11 +509,12 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     step->turned = turned;
     step->merge = L.merge;
     step->M = M;
-    step->n_items = (int)L.items.size();
+    step->n_few = L.n_few;
+    step->n_many = (int)L.items.size() - L.n_few;
     step->parts = L.parts;
     step->o_items = o_items;
     step->o_rows = o_rows;
-    step->o_rowlist = o_rowlist;
+    step->o_list = o_list;
     step->o_tables = o_tables;
     step->o_slots = o_slots;
     step->o_pos = o_pos;
@@ -533,10 +549,11 @@ PagedAttend attend_args(const KVStep* step, int layer, float scale, void* ws) {
     a.Hkv = c.n_kv_heads;
     a.gs = c.n_q_heads / c.n_kv_heads;
     a.items = (const PagedItem*)(step->dev + step->o_items);
-    a.n_items = step->n_items;
+    a.n_few = step->n_few;
+    a.n_many = step->n_many;
     a.rows = (const PagedRow*)(step->dev + step->o_rows);
     a.M = step->M;
-    a.rowlist = (const int*)(step->dev + step->o_rowlist);
+    a.list = (const PagedRow*)(step->dev + step->o_list);
     a.tables = (const int*)(step->dev + step->o_tables);
     a.masks = (const uint32_t*)(step->dev + step->o_masks);
     a.scale2 = (float)(1.4426950408889634 * (scale == 0.f ? 1.0 / std::sqrt((double)c.head_dim) : (double)scale));

@@ -13,28 +13,32 @@ struct PagedPool {
 };
 
 // A run of keys that some rows see, met by a tile of their query vectors: one workgroup per kv head.  Query vector c of
-// the run's rows is head c % gs (of the kv head's) of row rowlist[rows + c / gs]; the tile takes q0 <= c < q0 + nq.
+// the run's rows is head c % gs (of the kv head's) of row list[rows + c / gs]; the tile takes q0 <= c < q0 + nq.
 struct PagedItem {
     int rows, q0, nq;
     int kb, ke;                                    // keys, by their place in the sequence
     int table;                                     // of a sequence that holds the run: tables[table + key / page_rows] is its page
     int slot;                                      // which of a row's partial results this is
-    int form;                                      // query tiles of 32 (1, 2 or 4), + 8: no row's limit or mask cuts the run
+    int open;                                      // no row's limit or mask cuts the run
 };
 struct PagedRow {
+    int row;
     int limit;                                     // keys below it are seen
     int mask;                                      // word offset of its bits in masks, or -1
     int part, nparts;                              // its partial results: [part, part + nparts); one: it goes straight to out
+    int spare[3];
 };
+constexpr int PAGED_FEW = 64;                      // most query vectors of a tile of the first kernel
+constexpr int PAGED_MANY = 128;                    // and of the second
 
 struct PagedAttend {
     const void* q; int q_dt; size_t ldq;           // [M][Hq D], rotated
     void* out; int out_dt; size_t ldo;
     const uint16_t *k, *v;                         // the layer's
     int shift, Hkv, gs;
-    const PagedItem* items; int n_items;
-    const PagedRow* rows; int M;
-    const int* rowlist; const int* tables; const uint32_t* masks;
+    const PagedItem* items; int n_few, n_many;     // tiles of up to 64 query vectors, then those of up to 128
+    const PagedRow* list; const PagedRow* rows; int M;   // of the runs; [M]
+    const int* tables; const uint32_t* masks;
     float scale2;                                  // log2(e) times the softmax's scale
     float* part_o; float2* part_ml;                // [parts][Hq][D], [parts][Hq] (max, sum)
     bool merge;                                    // some row has more than one partial result
