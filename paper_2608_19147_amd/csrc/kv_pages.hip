@@ -52,7 +52,8 @@ struct KVStep {
     int ring = 0;
     // the plan
     bool planned = false, captured = false, turned = false, merge = false;
-    int M = 0, n_few = 0, n_many = 0;
+    bool many = false;
+    int M = 0, n_items = 0;
     size_t parts = 0;
     size_t o_items = 0, o_rows = 0, o_list = 0, o_tables = 0, o_slots = 0, o_pos = 0, o_masks = 0;
 
@@ -142,12 +143,13 @@ struct Layout {
     std::vector<PagedRow> rows, list;
     std::vector<int> rowlist, tables, slots, pos;
     std::vector<uint32_t> masks;
-    int n_few = 0;
     size_t parts = 0;
-    bool merge = false;
+    bool merge = false, many = false;
 };
 
 constexpr int SHARE_KEYS = 128;                    // fewest keys worth a run of their own
+constexpr int SHARE_QUERIES = 64;                  // a sequence with more query vectors a kv head fills tiles alone
+constexpr double START_STEPS = 6, PART_STEPS = 1.0 / 16;   // a workgroup's start and end, and a partial result, in steps
 constexpr int SPLIT_STEPS = 8;                     // fewest steps of 32 keys of a split
 
 // The runs of a batch: sequences sorted by their whole pages, so that those that share pages are neighbours; a common
@@ -200,75 +202,76 @@ struct RunBuilder {
     }
 };
 
-// Splits of the runs, their tiles as workgroups and each row's partial results.  A tile is up to 64 query vectors (128 in
-// runs with more, which are prompts'), a split a whole number of steps of 32 keys.  Splits are as long as leaves every
-// place on the card a workgroup (four a CU; two of the larger tiles) and no more: what a split adds is a partial result of
-// each of its query vectors, written and read.
+// Splits of the runs, their tiles as workgroups and each row's partial results.  A tile is up to 16 query vectors where no
+// run has more (decoding rows), else up to 128; a split is a whole number of steps of 32 keys.  Splits are as long as leaves
+// every place on the card a workgroup (four a CU; two of the larger tiles) and no more: what a split adds is a partial
+// result of each of its query vectors, written and read.
 void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table_off, std::vector<Run>& runs, Layout& L) {
     const StageConfig& c = pool->stage->cfg;
     const int gs = c.n_q_heads / c.n_kv_heads;
     auto steps = [](int k0, int k1) { return (k1 + 31) / 32 - k0 / 32; };
-    auto many = [&](const Run& r) { return !r.shared && (long)r.n_rows * gs > PAGED_FEW; };
-    auto tiles = [&](const Run& r) { const int t = many(r) ? PAGED_MANY : PAGED_FEW; return (r.n_rows * gs + t - 1) / t; };
-    for (int kind = 0; kind < 2; ++kind) {
-        const long places = (long)(kind ? 2 : 4) * n_cus;
-        int longest = 0;
-        long all = 0;
-        for (const Run& r : runs)
-            if (many(r) == (kind == 1)) {
-                longest = std::max(longest, steps(r.k0, r.k1));
-                all += tiles(r);
-            }
-        if (!all) continue;
-        // the shortest split with which the workgroups fit in the places
-        int lo = std::min(SPLIT_STEPS, longest), hi = longest;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            long wgs = 0;
-            for (const Run& r : runs)
-                if (many(r) == (kind == 1)) wgs += (long)tiles(r) * ((steps(r.k0, r.k1) + mid - 1) / mid);
-            if (wgs * c.n_kv_heads <= places) hi = mid;
-            else lo = mid + 1;
+    for (const Run& r : runs) L.many = L.many || (long)r.n_rows * gs > PAGED_FEW;
+    const int T = L.many ? PAGED_MANY : PAGED_FEW;
+    const long places = (long)(L.many ? 2 : 4) * n_cus;
+    auto tiles = [&](const Run& r) { return (r.n_rows * gs + T - 1) / T; };
+    // the split after which the card should be done first: the places' share of all workgroups' steps, starts and partial
+    // results, and the longest of them
+    int longest = 0;
+    for (const Run& r : runs) longest = std::max(longest, steps(r.k0, r.k1));
+    int lo = longest;
+    double best = 1e30;
+    for (int C = std::min(SPLIT_STEPS, longest);; C = std::min(longest, C + std::max(1, C / 16))) {
+        double all = 0;
+        long wgs = 0;
+        int most = 0;
+        for (const Run& r : runs) {
+            const int n = steps(r.k0, r.k1), S = (n + C - 1) / C, t = tiles(r), q = r.n_rows * gs;
+            all += (double)t * (n + S * START_STEPS) + (S > 1 || r.parent >= 0 || r.shared ? S * q * PART_STEPS : 0.0);
+            most = std::max(most, (n + S - 1) / S);
+            wgs += (long)t * S;
         }
-        for (Run& r : runs)
-            if (many(r) == (kind == 1)) {
-                const int n = steps(r.k0, r.k1), S = (n + lo - 1) / lo, st = (n + S - 1) / S;
-                r.chunk = 32 * st;
-                r.splits = (n + st - 1) / st;
-            }
+        // (in more than one round the last ones leave places empty)
+        const double time = std::max(all * c.n_kv_heads / places, (double)most + START_STEPS) + (wgs * c.n_kv_heads > places ? most * 0.5 : 0.0);
+        if (time < best) {
+            best = time;
+            lo = C;
+        }
+        if (C == longest) break;
     }
-    std::vector<float> cost;
-    std::vector<char> kind;
     for (Run& r : runs) {
+        const int n = steps(r.k0, r.k1), S = (n + lo - 1) / lo, st = (n + S - 1) / S;
+        r.chunk = 32 * st;
+        r.splits = (n + st - 1) / st;
         if (r.parent >= 0) r.slot = runs[r.parent].slot + runs[r.parent].splits;
-        const int a0 = r.k0 / 32 * 32, T = many(r) ? PAGED_MANY : PAGED_FEW;   // splits end at whole steps
+    }
+    std::vector<int> cost;
+    for (const Run& r : runs) {
+        const int a0 = r.k0 / 32 * 32;             // splits end at whole steps
         for (int q = 0; q < r.n_rows * gs; q += T) {
             const int nq = std::min(T, r.n_rows * gs - q);
-            int lo = INT_MAX, hi = 0;
+            int low = INT_MAX, high = 0;
             bool masked = false;
             for (int i = q / gs; i <= (q + nq - 1) / gs; ++i) {
                 const PagedRow& w = L.rows[L.rowlist[r.rows + i]];
-                lo = std::min(lo, w.limit);
-                hi = std::max(hi, w.limit);
+                low = std::min(low, w.limit);
+                high = std::max(high, w.limit);
                 masked = masked || w.mask >= 0;
             }
             for (int j = 0; j < r.splits; ++j) {
-                const int kb = std::max(r.k0, a0 + j * r.chunk), ke = std::min({r.k1, a0 + (j + 1) * r.chunk, hi});
+                const int kb = std::max(r.k0, a0 + j * r.chunk), ke = std::min({r.k1, a0 + (j + 1) * r.chunk, high});
                 if (ke <= kb) break;
-                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, !masked && lo >= ke});
-                cost.push_back((float)steps(kb, ke));
-                kind.push_back(many(r));
+                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, masked ? 2 : low >= ke});
+                cost.push_back(steps(kb, ke));
             }
         }
     }
-    // small tiles first; of each kind the longest
+    // the longest first
     std::vector<int> at(L.items.size());
     std::iota(at.begin(), at.end(), 0);
-    std::stable_sort(at.begin(), at.end(), [&](int x, int y) { return kind[x] != kind[y] ? kind[x] < kind[y] : cost[x] > cost[y]; });
+    std::stable_sort(at.begin(), at.end(), [&](int x, int y) { return cost[x] > cost[y]; });
     std::vector<PagedItem> sorted(L.items.size());
     for (size_t i = 0; i < at.size(); ++i) sorted[i] = L.items[at[i]];
     L.items.swap(sorted);
-    L.n_few = (int)std::count(kind.begin(), kind.end(), 0);
     // a row's partial results: its ancestors' splits, and those of its own run that begin before its limit
     for (const Run& r : runs) {
         if (r.shared) continue;                    // never a row's last
@@ -464,7 +467,7 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     RunBuilder rb{pool, pages, P, n, row0, runs, L.rowlist};
     const int gs = c.n_q_heads / c.n_kv_heads;
     std::iota(order.begin(), order.end(), 0);
-    auto alone = std::stable_partition(order.begin(), order.end(), [&](int x) { return (long)n[x] * gs <= PAGED_FEW; });
+    auto alone = std::stable_partition(order.begin(), order.end(), [&](int x) { return (long)n[x] * gs <= SHARE_QUERIES; });
     std::sort(order.begin(), alone, [&](int x, int y) {
         return std::lexicographical_compare(pages[x]->begin(), pages[x]->begin() + rb.whole(x), pages[y]->begin(), pages[y]->begin() + rb.whole(y));
     });
@@ -509,8 +512,8 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     step->turned = turned;
     step->merge = L.merge;
     step->M = M;
-    step->n_few = L.n_few;
-    step->n_many = (int)L.items.size() - L.n_few;
+    step->many = L.many;
+    step->n_items = (int)L.items.size();
     step->parts = L.parts;
     step->o_items = o_items;
     step->o_rows = o_rows;
@@ -549,8 +552,8 @@ PagedAttend attend_args(const KVStep* step, int layer, float scale, void* ws) {
     a.Hkv = c.n_kv_heads;
     a.gs = c.n_q_heads / c.n_kv_heads;
     a.items = (const PagedItem*)(step->dev + step->o_items);
-    a.n_few = step->n_few;
-    a.n_many = step->n_many;
+    a.n_items = step->n_items;
+    a.many = step->many;
     a.rows = (const PagedRow*)(step->dev + step->o_rows);
     a.M = step->M;
     a.list = (const PagedRow*)(step->dev + step->o_list);

@@ -19,7 +19,7 @@ struct PagedItem {
     int kb, ke;                                    // keys, by their place in the sequence
     int table;                                     // of a sequence that holds the run: tables[table + key / page_rows] is its page
     int slot;                                      // which of a row's partial results this is
-    int open;                                      // no row's limit or mask cuts the run
+    int open;                                      // 1: no row's limit or mask cuts the run, 2: some row has a mask
 };
 struct PagedRow {
     int row;
@@ -28,15 +28,14 @@ struct PagedRow {
     int part, nparts;                              // its partial results: [part, part + nparts); one: it goes straight to out
     int spare[3];
 };
-constexpr int PAGED_FEW = 64;                      // most query vectors of a tile of the first kernel
-constexpr int PAGED_MANY = 128;                    // and of the second
+constexpr int PAGED_FEW = 16, PAGED_MANY = 128;    // most query vectors of a tile, of the two kernels
 
 struct PagedAttend {
     const void* q; int q_dt; size_t ldq;           // [M][Hq D], rotated
     void* out; int out_dt; size_t ldo;
     const uint16_t *k, *v;                         // the layer's
     int shift, Hkv, gs;
-    const PagedItem* items; int n_few, n_many;     // tiles of up to 64 query vectors, then those of up to 128
+    const PagedItem* items; int n_items; bool many;   // many: some tile has more than PAGED_FEW query vectors
     const PagedRow* list; const PagedRow* rows; int M;   // of the runs; [M]
     const int* tables; const uint32_t* masks;
     float scale2;                                  // log2(e) times the softmax's scale

@@ -95,6 +95,11 @@ __device__ __forceinline__ float lanes_sum4(float v) {
 // Queries of the cache's type enter as they are, fp32 ones as two terms of it (QT = 2).
 
 
+// A maximum that rises by less than this (in powers of two) does not move the base that is subtracted: probabilities up to
+// 2^LAG cost no bits, in 16-bit floats either, and the outputs are seldom rescaled (a wave does when one of its query
+// vectors has to, which for 32 of them was nearly every step: 4 x 1024 rows behind 2048 224 -> 211 us).
+constexpr float LAG = 8.f;
+
 template <int D>
 __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 template <int D>
@@ -104,6 +109,14 @@ __device__ __forceinline__ int swz_v(int row) { return D == 128 ? 2 * (row & 7) 
 __device__ __forceinline__ uint32_t here(uint32_t v) {
     asm volatile("" : "+v"(v));
     return v;
+}
+
+// Values that were loaded are there from here on: first used inside a loop, they would be waited for in every turn of it,
+// and the rows under way with them (64 rows behind 4096 shared ones 38 -> 32.5 us).
+template <int N>
+__device__ __forceinline__ void settle(u32x4 (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
 // This lane's part of the direct loads of 16 rows of a page, a kilobyte (1024 / (2 D) rows) an instruction: byte offsets
@@ -128,6 +141,9 @@ __device__ __forceinline__ void load_rows16(const uint8_t* src, uint32_t lane_of
         PAGED_LOAD(3);
     }
 #undef PAGED_LOAD
+}
+__device__ __forceinline__ void load_word(const uint32_t* src, uint32_t* lds) {   // one a lane
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 
@@ -158,25 +174,75 @@ __device__ __forceinline__ void read_v16(uint32_t v, u32x2* f) {   // 64 dims
         : "v"(v), "v"(v ^ 32u), "v"(v ^ 64u), "v"(v ^ 96u)
         : "memory");
 }
-__device__ __forceinline__ void read_k32(uint32_t k, u32x4* f, bool upper) {
-    const uint32_t x = upper ? k ^ 128u : k;
-    asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-                 : "v"(x), "v"(x ^ 32u), "v"(x ^ 64u), "v"(x ^ 96u)
-                 : "memory");
+__device__ __forceinline__ uint32_t read_word(uint32_t at) {
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(v) : "v"(at) : "memory");
+    return v;
 }
-// Two 32-dim fragments (at v and v ^ 64) of 32 keys: four reads each, 8 keys apart (RB bytes a row).
-template <int RB>
-__device__ __forceinline__ void read_v32(uint32_t v, u32x2* f) {
-    asm volatile(
-        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\tds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
-        "ds_read_b64_tr_b16 %3, %8 offset:%12\n\tds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %6, %9 offset:%11\n\tds_read_b64_tr_b16 %7, %9 offset:%12\n\ts_waitcnt lgkmcnt(0)"
-        : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
-        : "v"(v), "v"(v ^ 64u), "n"(8 * RB), "n"(16 * RB), "n"(24 * RB)
-        : "memory");
+// All of a step of 32 keys: K's fragments and V's, 32 dims of V at v ^ (64 t), its reads 8 keys apart (RB bytes a row).
+template <int D>
+__device__ __forceinline__ void read_step32(uint32_t k, uint32_t v, u32x4* f, u32x2* w) {
+    constexpr int RB = 2 * D;
+    if constexpr (D == 128)
+        asm volatile(
+            "ds_read_b128 %0, %24\n\t"
+            "ds_read_b128 %1, %25\n\t"
+            "ds_read_b128 %2, %26\n\t"
+            "ds_read_b128 %3, %27\n\t"
+            "ds_read_b128 %4, %28\n\t"
+            "ds_read_b128 %5, %29\n\t"
+            "ds_read_b128 %6, %30\n\t"
+            "ds_read_b128 %7, %31\n\t"
+            "ds_read_b64_tr_b16 %8, %32\n\t"
+            "ds_read_b64_tr_b16 %9, %32 offset:%36\n\t"
+            "ds_read_b64_tr_b16 %10, %32 offset:%37\n\t"
+            "ds_read_b64_tr_b16 %11, %32 offset:%38\n\t"
+            "ds_read_b64_tr_b16 %12, %33\n\t"
+            "ds_read_b64_tr_b16 %13, %33 offset:%36\n\t"
+            "ds_read_b64_tr_b16 %14, %33 offset:%37\n\t"
+            "ds_read_b64_tr_b16 %15, %33 offset:%38\n\t"
+            "ds_read_b64_tr_b16 %16, %34\n\t"
+            "ds_read_b64_tr_b16 %17, %34 offset:%36\n\t"
+            "ds_read_b64_tr_b16 %18, %34 offset:%37\n\t"
+            "ds_read_b64_tr_b16 %19, %34 offset:%38\n\t"
+            "ds_read_b64_tr_b16 %20, %35\n\t"
+            "ds_read_b64_tr_b16 %21, %35 offset:%36\n\t"
+            "ds_read_b64_tr_b16 %22, %35 offset:%37\n\t"
+            "ds_read_b64_tr_b16 %23, %35 offset:%38\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7]), "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7]), "=&v"(w[8]), "=&v"(w[9]), "=&v"(w[10]), "=&v"(w[11]), "=&v"(w[12]), "=&v"(w[13]), "=&v"(w[14]), "=&v"(w[15])
+            : "v"(k), "v"(k ^ 32u), "v"(k ^ 64u), "v"(k ^ 96u), "v"(k ^ 128u), "v"(k ^ 160u), "v"(k ^ 192u), "v"(k ^ 224u), "v"(v), "v"(v ^ 64u), "v"(v ^ 128u), "v"(v ^ 192u), "n"(8 * RB), "n"(16 * RB), "n"(24 * RB)
+            : "memory");
+    else
+        asm volatile(
+            "ds_read_b128 %0, %12\n\t"
+            "ds_read_b128 %1, %13\n\t"
+            "ds_read_b128 %2, %14\n\t"
+            "ds_read_b128 %3, %15\n\t"
+            "ds_read_b64_tr_b16 %4, %16\n\t"
+            "ds_read_b64_tr_b16 %5, %16 offset:%18\n\t"
+            "ds_read_b64_tr_b16 %6, %16 offset:%19\n\t"
+            "ds_read_b64_tr_b16 %7, %16 offset:%20\n\t"
+            "ds_read_b64_tr_b16 %8, %17\n\t"
+            "ds_read_b64_tr_b16 %9, %17 offset:%18\n\t"
+            "ds_read_b64_tr_b16 %10, %17 offset:%19\n\t"
+            "ds_read_b64_tr_b16 %11, %17 offset:%20\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7])
+            : "v"(k), "v"(k ^ 32u), "v"(k ^ 64u), "v"(k ^ 96u), "v"(v), "v"(v ^ 64u), "n"(8 * RB), "n"(16 * RB), "n"(24 * RB)
+            : "memory");
 }
 
+// The larger magnitudes of two pairs of 16-bit floats, as integers; whether one of a pair is no number.
+__device__ __forceinline__ uint32_t larger(uint32_t m, uint32_t x) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+}
+template <int KVDT>
+__device__ __forceinline__ bool no_number(uint32_t m) {
+    constexpr uint32_t INF = KVDT == DT_BF16 ? 0x7f80u : 0x7c00u;
+    return (m & 0xffffu) >= INF || (m >> 16) >= INF;
+}
 // Bits 15 and 31: the halves of x whose exponent is all ones (no number).
 template <int KVDT>
 __device__ __forceinline__ uint32_t not_numbers(uint32_t x) {
@@ -238,6 +304,12 @@ __device__ __forceinline__ void put_result(const PagedAttend& a, const PagedRow&
     }
 }
 
+// s where bit b of the bits is set, else -infinity.
+__device__ __forceinline__ float seen(float s, uint32_t bits, int b) {
+    const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)bits, b, 1);
+    return __uint_as_float((__float_as_uint(s) & m) | (~m & 0xff800000u));
+}
+
 // The bits of a step of AK keys from key k0 on that lie in the item's run, and of those the ones below `limit`.
 template <int AK>
 __device__ __forceinline__ uint32_t run_bits(int kb, int ke, int k0) {
@@ -246,60 +318,58 @@ __device__ __forceinline__ uint32_t run_bits(int kb, int ke, int k0) {
 }
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : ~0u >> (32 - n); }
 
-// ---- tiles of up to 64 query vectors
+// ---- tiles of up to 16 query vectors
 //
-// Decoding rows, verifies, and what they share.  The four waves are NQT tiles of 16 query vectors by KG = 4 / NQT key
-// groups, which take alternate steps and are merged through LDS.  A step is 16 keys (one page's), or 32 where the four
-// waves share it: what a step costs beside its products is then half.  Bound by memory: what counts is bytes in flight, so
-// a wave holds at most 128 registers and a workgroup 33 KB of LDS, and four workgroups share a CU (16 x 8 KB under way).
-// A wave with a buffer of one step (NQT = 1, D = 128) reads all of it into registers before it asks for the next;
-// otherwise each key group has a ring of NB steps.  A probability enters as its rounded part and the residual (2^-17 in
-// bf16), in one product: the second operand's 32 k slots hold 16 keys twice, those of V^T repeat them.
-template <int D, int KVDT, int QT, int NQT>
-__device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml) {
-    constexpr int H = NQT == 4 ? 2 : 1, AK = 16 * H;   // 16-key parts of a step
-    constexpr int RB = 2 * D, SB = AK * RB, KT = D / 32, MB = D / 16;
-    constexpr int KG = 4 / NQT, NB = 128 * 256 / (KG * 2 * SB);   // key groups; steps that a group's ring holds
-    constexpr int NL = (NQT == 1 ? 2 : 1) * 16 * RB / 1024;   // loads of a wave and step
+// Decoding rows.  The four waves take alternate steps of 16 keys (one page's) and are merged through LDS.  Bound by memory:
+// what counts is bytes in flight.  A wave holds NB steps in LDS of its own; it reads all of a step into registers, then
+// asks for the step NB further on in its place, so that no barrier stands between.  A probability enters as its rounded
+// part and the residual (2^-17 in bf16), in one product: the second operand's 32 k slots hold 16 keys twice, those of V^T
+// repeat them.
+template <int D, int KVDT, int QT, int NB>
+__device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml, uint32_t* words) {
+    constexpr int AK = 16, RB = 2 * D, SB = AK * RB, KT = D / 32, MB = D / 16, KG = 4;
+    constexpr int NL = 2 * SB / 1024;              // loads of a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qt = wave % NQT, kg = wave / NQT, ql = lane & 15, lg = lane >> 4;
+    const int ql = lane & 15, lg = lane >> 4;
     const int Hq = a.Hkv * a.gs, pmask = (1 << a.shift) - 1;
     const int s0 = it.kb / AK, s1 = (it.ke + AK - 1) / AK, turns = (s1 - s0 + KG - 1) / KG;
-    uint8_t* ring = lds + kg * NB * 2 * SB;
+    uint8_t* ring = lds + wave * NB * 2 * SB;
+    words += wave * NB * 64;
+    const bool open = it.open & 1, masked = it.open & 2;
 
-    const int c0 = it.q0 + 16 * qt + ql;
     int limit, mask;                               // of the lane's row
     {
-        const PagedRow* r = a.list + it.rows + min(c0, it.q0 + it.nq - 1) / a.gs;
+        const PagedRow* r = a.list + it.rows + min(it.q0 + ql, it.q0 + it.nq - 1) / a.gs;
         limit = r->limit;
         mask = r->mask;
     }
-
-    // Step i of the group: with one tile the wave loads K and V; of two waves one K, one V; of four, of 16 rows each.  Every
-    // row of a page may be read.
     const size_t head_at = ((size_t)g << a.shift) * RB, page_bytes = ((size_t)a.Hkv << a.shift) * RB;
     const uint32_t lk = lane_k<D>(), lv = lane_v<D>();
-    const bool loads_v = NQT == 1 || (NQT == 2 ? qt == 1 : qt >= 2), loads_k = NQT == 1 || !loads_v;
-    const int part16 = NQT == 4 ? qt & 1 : 0;
-    auto issue = [&](int i) {
-        const int key = AK * (s0 + kg + KG * i) + 16 * part16;
-        const int page = uniform_load(a.tables, (size_t)it.table + (min(key, it.ke - 1) >> a.shift));
+    auto page_of = [&](int i) { return uniform_load(a.tables, (size_t)it.table + (min(AK * (s0 + wave + KG * i), it.ke - 1) >> a.shift)); };
+    int page = page_of(0);                         // of the step asked for next, known a step ahead
+    auto issue = [&](int i) {                      // this wave's step i; every row of a page may be read
+        const int key = AK * (s0 + wave + KG * i);
         const size_t at = (size_t)page * page_bytes + head_at + (size_t)(key & pmask) * RB;
-        uint8_t* buf = ring + (NB > 1 ? i % NB : 0) * 2 * SB + part16 * 16 * RB;
-        if (loads_k) load_rows16<D, false>((const uint8_t*)a.k + at, lk, buf);
-        if (loads_v) load_rows16<D, true>((const uint8_t*)a.v + at, lv, buf + SB);
+        uint8_t* buf = ring + i % NB * 2 * SB;
+        load_rows16<D, false>((const uint8_t*)a.k + at, lk, buf);
+        load_rows16<D, true>((const uint8_t*)a.v + at, lv, buf + SB);
+        if (masked) load_word(a.masks + (size_t)max(mask, 0) + min(key, it.ke - 1) / 32, words + i % NB * 64);   // (to registers it would hold up the rows)
+        page = page_of(i + 1);
     };
 #pragma unroll
-    for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
+    for (int i = 0; i < NB; ++i)
         if (i < turns) issue(i);
 
     u32x4 qf[QT][KT];
     float sc = a.scale2;
     {
-        const int cq = min(c0, it.q0 + it.nq - 1);
+        const int cq = min(it.q0 + ql, it.q0 + it.nq - 1);
         sc *= load_query<KVDT, QT, KT, 4>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * lg, 32, qf);
     }
-
+    limit = (int)here((uint32_t)limit);
+    mask = (int)here((uint32_t)mask);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) settle(qf[t]);
     const uint32_t ka = lds_addr(ring) + ql * RB + 16 * (lg ^ swz_k<D>(ql));
     const int vkey = 4 * lg + (ql >> 2);
     const uint32_t va = lds_addr(ring) + SB + vkey * RB + 16 * (swz_v<D>(vkey) + ((ql & 3) >> 1)) + 8 * (ql & 1);
@@ -310,59 +380,45 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
     for (int mb = 0; mb < MB; ++mb) o[mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     for (int i = 0; i < turns; ++i) {
-        const int k0 = AK * (s0 + kg + KG * i);
-        if constexpr (NB > 1) {
-            if (i + NB - 2 < turns) wait_loads<(NB - 2) * NL>();   // this wave's loads of step i are there
-            else wait_loads<0>();
-            if constexpr (NQT > 1) bare_barrier();                 // every wave's are, and the buffer of step i - 1 has been read
-            if (i + NB - 1 < turns) issue(i + NB - 1);
-        } else {
-            wait_loads<0>();
-        }
-        const bool whole = it.open && k0 >= it.kb && k0 + AK <= it.ke;
-        uint32_t in = ~0u, see = ~0u;              // keys of the step in the run; those that this lane's query vector sees
+        const int k0 = AK * (s0 + wave + KG * i);
+        if (NB == 1 || i + NB - 1 >= turns) wait_loads<0>();   // step i is there
+        else if (masked) wait_loads<(NB - 1) * (NL + 1)>();
+        else wait_loads<(NB - 1) * NL>();
+        const bool whole = open && k0 >= it.kb && k0 + AK <= it.ke;
+        uint32_t in = 0xFFFFu, see = 0xFFFFu;      // keys of the step in the run; those that this lane's query vector sees
         bool work = true;
         if (!whole) {
             in = run_bits<AK>(it.kb, it.ke, k0);
             see = in & bits_below(limit - k0);
-            if (mask >= 0 && see) see &= a.masks[(size_t)mask + k0 / 32] >> (H == 1 ? k0 & 16 : 0);
+            if (masked) {
+                const uint32_t w = read_word(lds_addr(words) + i % NB * 256 + 4 * lane);
+                see &= mask >= 0 ? w >> (k0 & 16) : ~0u;
+            }
             work = __any(see != 0u);
         }
-        f32x4_t s[H];
+        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
         u32x2 vf[MB];
-        const uint32_t off = NB > 1 ? i % NB * (2 * SB) : 0;
-        auto read_v = [&](int h) {
-            const uint32_t v = here(va + off + h * 16 * RB);
+        const uint32_t off = i % NB * (2 * SB);
+        if (work) {
+            u32x4 kf[KT];
+            read_k16<D>(here(ka + off), kf);
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                s = mma16<KVDT>(kf[t], qf[0][t], s);
+                if constexpr (QT == 2) s = mma16<KVDT>(kf[t], qf[1][t], s);
+            }
+            const uint32_t v = here(va + off);
             read_v16(v, vf);
             if constexpr (MB == 8) read_v16(v ^ 128u, vf + 4);
-        };
-        if (work) {
-#pragma unroll
-            for (int h = 0; h < H; ++h) {
-                u32x4 kf[KT];
-                read_k16<D>(here(ka + off + h * 16 * RB), kf);
-                s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    s[h] = mma16<KVDT>(kf[t], qf[0][t], s[h]);
-                    if constexpr (QT == 2) s[h] = mma16<KVDT>(kf[t], qf[1][t], s[h]);
-                }
-            }
-            if constexpr (H == 1) read_v(0);
         }
-        if constexpr (NB == 1) {
-            if (i + 1 < turns) issue(i + 1);       // the buffer is read
-        }
+        if (i + NB < turns) issue(i + NB);         // the step's place is free
         if (!work) continue;
         if (!whole) {
 #pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[h][j] = (see >> (16 * h + 4 * lg + j)) & 1u ? s[h][j] : -INFINITY;
+            for (int j = 0; j < 4; ++j) s[j] = seen(s[j], see >> (4 * lg), j);
         }
-        float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
-        if constexpr (H == 2) mx = fmaxf(mx, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        if (__any(mx > base)) {
+        const float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        if (__any((mx - base) * sc > LAG)) {
             const float top = fmaxf(base, lanes_max<4>(mx));
             const float corr = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((base - top) * sc);
             base = top;
@@ -373,50 +429,49 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
                 for (int j = 0; j < 4; ++j) o[mb][j] *= corr;
         }
         const float nb = base == -INFINITY ? 0.f : -base * sc;
-        uint32_t bad = 0u;
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[h][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][j], sc, nb));   // the probabilities
-            lsum += (s[h][0] + s[h][1]) + (s[h][2] + s[h][3]);
-            if constexpr (H == 2) read_v(h);
-            if (!whole) {
-                // Rows outside the run enter as zeros: what they hold is nobody's.  Of the others, a value that is no number
-                // must reach the query vectors that see it and no other (0 times it is no number either): it is taken out
-                // of the products and added where it is seen.
-                uint32_t m[2];
+        for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], sc, nb));   // the probabilities
+        lsum += (s[0] + s[1]) + (s[2] + s[3]);
+        bool bad = false;
+        if (!whole) {
+            // Rows outside the run enter as zeros: what they hold is nobody's.  Of the others, a value that is no number must
+            // reach the query vectors that see it and no other (0 times it is no number either): it is taken out of the
+            // products and added where it is seen.
+            if (in != 0xFFFFu) {
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const uint32_t bits = in >> (16 * h + 4 * lg + 2 * w);
-                    m[w] = (bits & 1u ? 0xFFFFu : 0u) | (bits & 2u ? 0xFFFF0000u : 0u);
+                    const uint32_t bits = in >> (4 * lg + 2 * w), m = (bits & 1u ? 0xFFFFu : 0u) | (bits & 2u ? 0xFFFF0000u : 0u);
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) vf[mb][w] &= m;
                 }
+            }
+            uint32_t top = 0u;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) top = larger(larger(top, vf[mb][0]), vf[mb][1]);
+            bad = __any(no_number<KVDT>(top));
+            if (bad) {
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const uint32_t x = vf[mb][w] & m[w], no = not_numbers<KVDT>(x);
-                        vf[mb][w] = x & ~((no >> 15) * 0xFFFFu);
-                        bad |= no;
-                    }
+                    for (int w = 0; w < 2; ++w) vf[mb][w] &= ~((not_numbers<KVDT>(vf[mb][w]) >> 15) * 0xFFFFu);
             }
-            u32x4 pb;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const float p0 = s[h][2 * w], p1 = s[h][2 * w + 1];
-                pb[w] = pack2<KVDT>(p0, p1);
-                pb[2 + w] = pack2<KVDT>(p0 - kv_float<KVDT>((uint16_t)pb[w]), p1 - kv_float<KVDT>((uint16_t)(pb[w] >> 16)));
-            }
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) o[mb] = mma16<KVDT>(u32x4{vf[mb][0], vf[mb][1], vf[mb][0], vf[mb][1]}, pb, o[mb]);
         }
-        if (!whole && __any(bad != 0u)) {
+        u32x4 pb;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            pb[w] = pack2<KVDT>(s[2 * w], s[2 * w + 1]);
+            pb[2 + w] = pack2<KVDT>(s[2 * w] - kv_float<KVDT>((uint16_t)pb[w]), s[2 * w + 1] - kv_float<KVDT>((uint16_t)(pb[w] >> 16)));
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) o[mb] = mma16<KVDT>(u32x4{vf[mb][0], vf[mb][1], vf[mb][0], vf[mb][1]}, pb, o[mb]);
+        if (bad) {
 #pragma unroll 1
             for (int key = 0; key < AK; ++key) {
                 if (!((in >> key) & 1u)) continue;
                 float p = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4 * H; ++j) p = (key & 3) + key / 16 * 4 == j ? s[j / 4][j % 4] : p;
-                p = __shfl(p, 16 * ((key >> 2) & 3) + ql);
+                for (int j = 0; j < 4; ++j) p = (key & 3) == j ? s[j] : p;
+                p = __shfl(p, 16 * (key >> 2) + ql);
                 const int page = uniform_load(a.tables, (size_t)it.table + ((k0 + key) >> a.shift));
                 const uint16_t* vr = a.v + ((((size_t)page * a.Hkv + g) << a.shift) + ((k0 + key) & pmask)) * D + here(4 * lg);
                 if ((see >> key) & 1u) {
@@ -435,77 +490,71 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
     // ---- results: dims 16 mb + 4 lg .. + 3 of the lane's query vector
     lsum = lanes_sum4(lsum);
     base = base == -INFINITY ? base : base * sc;
-    int cq = min(c0, it.q0 + it.nq - 1);
+    __syncthreads();                               // every wave has read its last step
+    f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][64]
+    if (lg == 0) sml[wave * 16 + ql] = float2{base, lsum};
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) so[(wave * MB + mb) * 64 + lane] = o[mb];
+    __syncthreads();
+    int cq = it.q0 + ql;
     asm volatile("" : "+v"(cq));                   // its row is read again: it need not stay in registers through the loop
+    if (cq >= it.q0 + it.nq) return;
     const PagedRow ri = a.list[it.rows + cq / a.gs];
+    if (it.slot >= ri.nparts) return;              // (a row that ends before this run has no part of it)
     const int head = g * a.gs + cq % a.gs;
-    const bool mine = c0 < it.q0 + it.nq && it.slot < ri.nparts;   // (a row that ends before this run has no part of it)
     const size_t part = ((size_t)(ri.part + it.slot) * Hq + head);
-    if constexpr (KG == 1) {
-        if (!mine) return;
-        if (ri.nparts > 1 && lg == 0) a.part_ml[part] = float2{base, lsum};
-        const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+    float top = -INFINITY, sum = 0.f, f[KG];
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) put_result<D>(a, ri, part, head, 16 * mb + 4 * lg, o[mb], inv);
-    } else {
-        __syncthreads();                           // every wave has read its last step
-        f32x4_t* so = (f32x4_t*)lds;               // [wave][MB][64]
-        if (lg == 0) sml[wave * 16 + ql] = float2{base, lsum};
+    for (int k = 0; k < KG; ++k) top = fmaxf(top, sml[k * 16 + ql].x);
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) so[(wave * MB + mb) * 64 + lane] = o[mb];
-        __syncthreads();
-        if (!mine) return;
-        float top = -INFINITY, sum = 0.f, f[KG];
+    for (int k = 0; k < KG; ++k) {
+        const float2 ml = sml[k * 16 + ql];
+        f[k] = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        sum += ml.y * f[k];
+    }
+    if (ri.nparts > 1 && lg == 0 && wave == 0) a.part_ml[part] = float2{top, sum};
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-        for (int k = 0; k < KG; ++k) top = fmaxf(top, sml[(k * NQT + qt) * 16 + ql].x);
+    for (int u = 0; u < MB / KG; ++u) {            // the waves share the dims
+        const int mb = wave + KG * u;
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KG; ++k) {
-            const float2 ml = sml[(k * NQT + qt) * 16 + ql];
-            f[k] = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-            sum += ml.y * f[k];
-        }
-        if (ri.nparts > 1 && lg == 0 && kg == 0) a.part_ml[part] = float2{top, sum};
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-#pragma unroll
-        for (int u = 0; u < MB / KG; ++u) {        // the tile's waves share its dims
-            const int mb = kg + KG * u;
-            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < KG; ++k) v += so[((k * NQT + qt) * MB + mb) * 64 + lane] * f[k];
-            put_result<D>(a, ri, part, head, 16 * mb + 4 * lg, v, inv);
-        }
+        for (int k = 0; k < KG; ++k) v += so[(k * MB + mb) * 64 + lane] * f[k];
+        put_result<D>(a, ri, part, head, 16 * mb + 4 * lg, v, inv);
     }
 }
 
+// Batches of nothing else: at most 128 registers a wave and 33 KB of LDS, so that four workgroups share a CU (16 x 8 KB
+// under way; 4 x 131072 rows of 8 x 128: two workgroups of 16 KB a wave 359 us, four of 8 KB 315).
 template <int D, int KVDT, int QT>
 __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[128 * 256];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[32768];
     __shared__ float2 sml[64];
+    __shared__ uint32_t words[4 * 128 / D * 64];
     const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
-    const PagedItem it = uniform_load(a.items, b);
-    if (it.nq <= 16) few_item<D, KVDT, QT, 1>(a, it, g, lds, sml);
-    else if (it.nq <= 32) few_item<D, KVDT, QT, 2>(a, it, g, lds, sml);
-    else few_item<D, KVDT, QT, 4>(a, it, g, lds, sml);
+    few_item<D, KVDT, QT, 128 / D>(a, uniform_load(a.items, b), g, lds, sml, words);
 }
 
 // ---- tiles of up to 128 query vectors
 //
-// Prompts.  A wave takes 32 query vectors and every key of the run, on 32 x 32 x 16 products; the four waves share steps of
-// 32 keys in a ring of four.  Bound by the matrix cores and, as much, by LDS (a wave reads a step for 32 query vectors) and
-// the exponentials.  P: terms of a probability (1: rounded to the cache's type, while the sum keeps it whole).
-template <int D, int KVDT, int QT, int PT>
-__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
-    constexpr int AK = 32, RB = 2 * D, SB = AK * RB, KT = D / 16, MB = D / 32, NB = 4;
-    constexpr int NL = 2 * SB / 1024 / 4;          // kilobytes of a step that a wave loads
-    __shared__ __attribute__((aligned(1024))) uint8_t ring[NB * 2 * SB];
-    const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
-    const PagedItem it = uniform_load(a.items, a.n_few + b);
+// Verifies, what many rows share, prompts.  On 32 x 32 x 16 products: NQT tiles of 32 query vectors by KG = 4 / NQT key
+// groups, which take alternate steps of 32 keys.  A group's waves share a ring of NQT steps; alone (NQT = 1) a wave reads
+// its step into registers before it asks for the next.  Bound by the matrix cores and, as much, by LDS (a wave reads a step
+// for 32 query vectors) and the exponentials.  P: terms of a probability (1: rounded to the cache's type, while the sum
+// keeps it whole).
+template <int D, int KVDT, int QT, int PT, int NQT>
+__device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml, uint32_t* words) {
+    constexpr int AK = 32, RB = 2 * D, SB = AK * RB, KT = D / 16, MB = D / 32, KG = 4 / NQT, NB = NQT;
+    constexpr int NL = 2 * SB / 1024 / NQT;        // a wave's loads of a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ql = lane & 31, h = lane >> 5;
+    const int qt = wave % NQT, kg = wave / NQT, ql = lane & 31, h = lane >> 5;
     const int Hq = a.Hkv * a.gs, pmask = (1 << a.shift) - 1;
-    const int s0 = it.kb / AK, turns = (it.ke + AK - 1) / AK - s0;
+    const int s0 = it.kb / AK, s1 = (it.ke + AK - 1) / AK, turns = (s1 - s0 + KG - 1) / KG;
+    uint8_t* ring = lds + kg * NB * 2 * SB;
+    words += wave * NB * 64;
+    const bool open = it.open & 1, masked = it.open & 2;
 
-    const int c0 = it.q0 + 32 * wave + ql;
+    const int c0 = it.q0 + 32 * qt + ql;
     int limit, mask;
     {
         const PagedRow* r = a.list + it.rows + min(c0, it.q0 + it.nq - 1) / a.gs;
@@ -514,17 +563,30 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
     }
 
     const size_t head_at = ((size_t)g << a.shift) * RB, page_bytes = ((size_t)a.Hkv << a.shift) * RB;
-    const uint32_t lane_at = wave < 2 ? lane_k<D>() : lane_v<D>();
-    auto issue = [&](int i) {                      // waves 0, 1: 16 rows of K each; 2, 3: of V
-        const int key = AK * (s0 + i) + (wave & 1) * 16;
-        const int page = uniform_load(a.tables, (size_t)it.table + (min(key, it.ke - 1) >> a.shift));
-        const size_t at = (size_t)page * page_bytes + head_at + (size_t)(key & pmask) * RB;
-        uint8_t* buf = ring + i % NB * 2 * SB + (wave & 1) * 16 * RB;
-        if (wave < 2) load_rows16<D, false>((const uint8_t*)a.k + at, lane_at, buf);
-        else load_rows16<D, true>((const uint8_t*)a.v + at, lane_at, buf + SB);
+    const uint32_t lk = lane_k<D>(), lv = lane_v<D>();
+    // a wave's 16-row parts of a step's K and V: all four, two of one, or one; their pages are known a step ahead
+    constexpr int NP = 4 / NQT, PG = NQT == 4 ? 1 : 2;
+    int page[PG];
+    auto pages_of = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < PG; ++u)
+            page[u] = uniform_load(a.tables, (size_t)it.table + (min(AK * (s0 + kg + KG * i) + 16 * (NQT == 4 ? qt & 1 : u), it.ke - 1) >> a.shift));
+    };
+    pages_of(0);
+    auto issue = [&](int i) {
+        uint8_t* buf = ring + (NB > 1 ? i % NB : 0) * 2 * SB;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+            const int p = qt * NP + u, half = p & 1, key = AK * (s0 + kg + KG * i) + 16 * half;
+            const size_t at = (size_t)page[PG == 2 ? u & 1 : 0] * page_bytes + head_at + (size_t)(key & pmask) * RB;
+            if (p < 2) load_rows16<D, false>((const uint8_t*)a.k + at, lk, buf + half * 16 * RB);
+            else load_rows16<D, true>((const uint8_t*)a.v + at, lv, buf + SB + half * 16 * RB);
+        }
+        if (masked) load_word(a.masks + (size_t)max(mask, 0) + min(AK * (s0 + kg + KG * i), it.ke - 1) / 32, words + (NB > 1 ? i % NB : 0) * 64);
+        pages_of(i + 1);
     };
 #pragma unroll
-    for (int i = 0; i < NB - 1; ++i)
+    for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
         if (i < turns) issue(i);
 
     u32x4 qf[QT][KT];
@@ -534,6 +596,10 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
         sc *= load_query<KVDT, QT, KT, 2>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * h, 16, qf);
     }
 
+    limit = (int)here((uint32_t)limit);
+    mask = (int)here((uint32_t)mask);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) settle(qf[t]);
     const uint32_t ka = lds_addr(ring) + ql * RB + 16 * (h ^ swz_k<D>(ql));
     const int j16 = lane & 15, vkey = 4 * h + (j16 >> 2);   // keys 8 apart have the same place
     const uint32_t va = lds_addr(ring) + SB + vkey * RB + 16 * ((2 * ((lane >> 4) & 1)) ^ swz_v<D>(vkey)) + 16 * ((j16 & 3) >> 1) + 8 * (j16 & 1);
@@ -546,52 +612,56 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
         for (int r = 0; r < 16; ++r) o[mb][r] = 0.f;
 
     for (int i = 0; i < turns; ++i) {
-        const int k0 = AK * (s0 + i);
-        if (i + NB - 2 < turns) wait_loads<(NB - 2) * NL>();
-        else wait_loads<0>();
-        bare_barrier();
-        if (i + NB - 1 < turns) issue(i + NB - 1);
-        uint32_t in = ~0u, see = ~0u;
-        bool whole = it.open && k0 >= it.kb && k0 + AK <= it.ke, work = true;
+        const int k0 = AK * (s0 + kg + KG * i);
+        if (NB == 1 || i + NB - 2 >= turns) wait_loads<0>();   // this wave's loads of step i are there
+        else if (masked) wait_loads<(NB > 1 ? NB - 2 : 0) * (NL + 1)>();
+        else wait_loads<(NB > 1 ? NB - 2 : 0) * NL>();
+        if constexpr (NB > 1) {
+            bare_barrier();                        // every wave's are, and the buffer of step i - 1 has been read
+            if (i + NB - 1 < turns) issue(i + NB - 1);
+        }
+        uint32_t in = ~0u, see = ~0u;              // keys of the step in the run; those that this lane's query vector sees
+        bool whole = open && k0 >= it.kb && k0 + AK <= it.ke, work = true;
         if (!whole) {
             in = run_bits<AK>(it.kb, it.ke, k0);
             see = in & bits_below(limit - k0);
-            if (mask >= 0 && see) see &= a.masks[(size_t)mask + k0 / 32];
+            if (masked) {
+                const uint32_t w = read_word(lds_addr(words) + (NB > 1 ? i % NB * 256 : 0) + 4 * lane);
+                see &= mask >= 0 ? w : ~0u;
+            }
             work = __any(see != 0u);
             whole = !__any(see != ~0u);            // a prompt's rows see whole steps well before their own keys
         }
-        if (!work) continue;
-        const uint32_t off = i % NB * (2 * SB);
-        u32x4 kf[KT];
+        const uint32_t off = NB > 1 ? i % NB * (2 * SB) : 0;
         f32x16_t s;
+        u32x4 vf[MB][2];
+        if (work) {
+            u32x4 kf[KT];
+            u32x2 p[4 * MB];
+            read_step32<D>(here(ka + off), here(va + off), kf, p);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+            for (int e = 0; e < 2 * MB; ++e) vf[e / 2][e % 2] = u32x4{p[2 * e][0], p[2 * e][1], p[2 * e + 1][0], p[2 * e + 1][1]};
 #pragma unroll
-        for (int t = 0; t < KT; t += 4) {
-            read_k32(here(ka + off), kf + t, t != 0);
+            for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-            for (int u = t; u < t + 4; ++u) {
+            for (int u = 0; u < KT; ++u) {
                 s = mma32<KVDT>(kf[u], qf[0][u], s);
                 if constexpr (QT == 2) s = mma32<KVDT>(kf[u], qf[1][u], s);
             }
         }
-        u32x4 vf[MB][2];
-#pragma unroll
-        for (int mb = 0; mb < MB; mb += 2) {
-            u32x2 p[8];
-            read_v32<RB>(here((va + off) ^ (64u * mb)), p);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vf[mb + e / 2][e % 2] = u32x4{p[2 * e][0], p[2 * e][1], p[2 * e + 1][0], p[2 * e + 1][1]};
+        if constexpr (NB == 1) {
+            if (i + 1 < turns) issue(i + 1);       // the buffer is read
         }
+        if (!work) continue;
         if (!whole) {
             const uint32_t x = see >> (4 * h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = (x >> (8 * (r / 4) + r % 4)) & 1u ? s[r] : -INFINITY;
+            for (int r = 0; r < 16; ++r) s[r] = seen(s[r], x, 8 * (r / 4) + r % 4);
         }
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        if (__any(mx > base)) {
+        if (__any((mx - base) * sc > LAG)) {
             const float top = fmaxf(base, lanes_max<2>(mx));
             const float corr = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((base - top) * sc);
             base = top;
@@ -607,21 +677,31 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
         for (int r = 0; r < 16; ++r) pv[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, nb));
         lsum += (((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]))) +
                 (((pv[8] + pv[9]) + (pv[10] + pv[11])) + ((pv[12] + pv[13]) + (pv[14] + pv[15])));
-        uint32_t bad = 0u;
+        bool bad = false;
         if (!whole) {                              // as in few_item
+            if (in != ~0u) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t bits = in >> (16 * t + 8 * (w >> 1) + 4 * h + 2 * (w & 1));
-                    const uint32_t m = (bits & 1u ? 0xFFFFu : 0u) | (bits & 2u ? 0xFFFF0000u : 0u);
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t bits = in >> (16 * t + 8 * (w >> 1) + 4 * h + 2 * (w & 1));
+                        const uint32_t m = (bits & 1u ? 0xFFFFu : 0u) | (bits & 2u ? 0xFFFF0000u : 0u);
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) {
-                        const uint32_t x = vf[mb][t][w] & m, no = not_numbers<KVDT>(x);
-                        vf[mb][t][w] = x & ~((no >> 15) * 0xFFFFu);
-                        bad |= no;
+                        for (int mb = 0; mb < MB; ++mb) vf[mb][t][w] &= m;
                     }
-                }
+            }
+            uint32_t top = 0u;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int w = 0; w < 8; ++w) top = larger(top, vf[mb][w / 4][w % 4]);
+            bad = __any(no_number<KVDT>(top));
+            if (bad) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) vf[mb][w / 4][w % 4] &= ~((not_numbers<KVDT>(vf[mb][w / 4][w % 4]) >> 15) * 0xFFFFu);
+            }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -639,7 +719,7 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
                 if constexpr (PT == 2) o[mb] = mma32<KVDT>(vf[mb][t], pr, o[mb]);
             }
         }
-        if (!whole && __any(bad != 0u)) {
+        if (bad) {
 #pragma unroll 1
             for (int key = 0; key < AK; ++key) {
                 if (!((in >> key) & 1u)) continue;
@@ -647,8 +727,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) p = 4 * (key / 8) + key % 4 == r ? pv[r] : p;
                 p = __shfl(p, 32 * ((key >> 2) & 1) + ql);
-                const int page = uniform_load(a.tables, (size_t)it.table + ((k0 + key) >> a.shift));
-                const uint16_t* vr = a.v + ((((size_t)page * a.Hkv + g) << a.shift) + ((k0 + key) & pmask)) * D + here(4 * h);
+                const int pg = uniform_load(a.tables, (size_t)it.table + ((k0 + key) >> a.shift));
+                const uint16_t* vr = a.v + ((((size_t)pg * a.Hkv + g) << a.shift) + ((k0 + key) & pmask)) * D + here(4 * h);
                 if ((see >> key) & 1u) {
 #pragma unroll
                     for (int mb = 0; mb < MB; ++mb)
@@ -671,19 +751,59 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
         lsum = lo + hi;
     }
     base = base == -INFINITY ? base : base * sc;
-    int cq = min(c0, it.q0 + it.nq - 1);
+    auto quad = [&](int q) { return f32x4_t{o[q / 4][q % 4 * 4], o[q / 4][q % 4 * 4 + 1], o[q / 4][q % 4 * 4 + 2], o[q / 4][q % 4 * 4 + 3]}; };
+    f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][4][64]
+    if constexpr (KG > 1) {
+        __syncthreads();                           // every wave has read its last step
+        if (h == 0) sml[wave * 32 + ql] = float2{base, lsum};
+#pragma unroll
+        for (int q = 0; q < 4 * MB; ++q) so[(wave * MB * 4 + q) * 64 + lane] = quad(q);
+        __syncthreads();
+    }
+    int cq = c0;
     asm volatile("" : "+v"(cq));
+    if (cq >= it.q0 + it.nq) return;
     const PagedRow ri = a.list[it.rows + cq / a.gs];
+    if (it.slot >= ri.nparts) return;
     const int head = g * a.gs + cq % a.gs;
-    if (c0 >= it.q0 + it.nq || it.slot >= ri.nparts) return;
     const size_t part = ((size_t)(ri.part + it.slot) * Hq + head);
-    if (ri.nparts > 1 && h == 0) a.part_ml[part] = float2{base, lsum};
-    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+    if constexpr (KG == 1) {
+        if (ri.nparts > 1 && h == 0) a.part_ml[part] = float2{base, lsum};
+        const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
+        for (int q = 0; q < 4 * MB; ++q) put_result<D>(a, ri, part, head, 8 * q + 4 * h, quad(q), inv);
+    } else {
+        float top = -INFINITY, sum = 0.f, f[KG];
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4)
-            put_result<D>(a, ri, part, head, 32 * mb + 8 * r4 + 4 * h, f32x4_t{o[mb][4 * r4], o[mb][4 * r4 + 1], o[mb][4 * r4 + 2], o[mb][4 * r4 + 3]}, inv);
+        for (int k = 0; k < KG; ++k) top = fmaxf(top, sml[(k * NQT + qt) * 32 + ql].x);
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+            const float2 ml = sml[(k * NQT + qt) * 32 + ql];
+            f[k] = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+            sum += ml.y * f[k];
+        }
+        if (ri.nparts > 1 && h == 0 && kg == 0) a.part_ml[part] = float2{top, sum};
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        for (int q = kg; q < MB * 4; q += KG) {    // the tile's waves share its dims
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KG; ++k) v += so[((k * NQT + qt) * MB * 4 + q) * 64 + lane] * f[k];
+            put_result<D>(a, ri, part, head, 8 * q + 4 * h, v, inv);
+        }
+    }
+}
+
+template <int D, int KVDT, int QT, int PT>
+__global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * 2 * 32 * 2 * D];
+    __shared__ float2 sml[128];
+    __shared__ uint32_t words[4 * 4 * 64];
+    const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+    const PagedItem it = uniform_load(a.items, b);
+    if (it.nq <= 16) few_item<D, KVDT, QT, 2>(a, it, g, lds, sml, words);
+    else if (it.nq <= 32) many_item<D, KVDT, QT, PT, 1>(a, it, g, lds, sml, words);
+    else if (it.nq <= 64) many_item<D, KVDT, QT, PT, 2>(a, it, g, lds, sml, words);
+    else many_item<D, KVDT, QT, PT, 4>(a, it, g, lds, sml, words);
 }
 
 // Rows with several partial results: m = max m_r, o = sum o_r 2^(m_r - m) / sum l_r 2^(m_r - m), added in the order of the
@@ -898,34 +1018,21 @@ bool move_grid(int n, int pieces, int& chunks, dim3& grid) {
 }  // namespace
 
 hipError_t launch_paged_attend(const PagedAttend& a, int D, int kv_dt, hipStream_t st, hipEvent_t done) {
-    const size_t few = (size_t)a.n_few * a.Hkv, many = (size_t)a.n_many * a.Hkv, waves = (size_t)a.M * a.Hkv * a.gs;
-    if (a.n_few < 0 || a.n_many < 0 || few + many < 1 || few + many >= (1u << 24) || waves >= (1u << 24)) return hipErrorInvalidValue;
+    const size_t items = (size_t)a.n_items * a.Hkv, waves = (size_t)a.M * a.Hkv * a.gs;
+    if (a.n_items < 1 || items >= (1u << 24) || waves >= (1u << 24)) return hipErrorInvalidValue;
     const bool f32 = a.q_dt == DT_F32, bf = kv_dt == DT_BF16;
     if ((!f32 && a.q_dt != kv_dt) || (D != 64 && D != 128)) return hipErrorInvalidValue;
-    const dim3 block(256);
-    hipError_t e = hipSuccess;
-#define PAGED_PICK(D_, KERNEL, F32_, H16_, GRID, DONE)                                                            \
-    (f32 ? bf ? launch_done(KERNEL<D_, DT_BF16, F32_>, GRID, block, 0, st, DONE, a)                               \
-              : launch_done(KERNEL<D_, DT_F16, F32_>, GRID, block, 0, st, DONE, a)                                \
-         : bf ? launch_done(KERNEL<D_, DT_BF16, H16_>, GRID, block, 0, st, DONE, a)                               \
-              : launch_done(KERNEL<D_, DT_F16, H16_>, GRID, block, 0, st, DONE, a))
-    if (few) {
-        const dim3 grid((unsigned)few);
-        const hipEvent_t d = a.merge || many ? nullptr : done;
-        e = D == 128 ? PAGED_PICK(128, paged_few_kernel, 2, 1, grid, d) : PAGED_PICK(64, paged_few_kernel, 2, 1, grid, d);
-        if (e != hipSuccess) return e;
-    }
-#define PAGED_TWO 2, 2
-#define PAGED_ONE 1, 1
-    if (many) {
-        const dim3 grid((unsigned)many);
-        const hipEvent_t d = a.merge ? nullptr : done;
-        e = D == 128 ? PAGED_PICK(128, paged_many_kernel, PAGED_TWO, PAGED_ONE, grid, d)
-                     : PAGED_PICK(64, paged_many_kernel, PAGED_TWO, PAGED_ONE, grid, d);
-        if (e != hipSuccess) return e;
-    }
-    if (!a.merge) return e;
-    const dim3 mg((unsigned)((waves + 3) / 4));
+    const dim3 block(256), grid((unsigned)items), mg((unsigned)((waves + 3) / 4));
+    const hipEvent_t d = a.merge ? nullptr : done;
+#define PAGED_KERNEL(D_, KV_)                                                                                                  \
+    (a.many ? f32 ? launch_done(paged_many_kernel<D_, KV_, 2, 2>, grid, block, 0, st, d, a)                                    \
+                  : launch_done(paged_many_kernel<D_, KV_, 1, 1>, grid, block, 0, st, d, a)                                    \
+            : f32 ? launch_done(paged_few_kernel<D_, KV_, 2>, grid, block, 0, st, d, a)                                        \
+                  : launch_done(paged_few_kernel<D_, KV_, 1>, grid, block, 0, st, d, a))
+    const hipError_t e = D == 128 ? (bf ? PAGED_KERNEL(128, DT_BF16) : PAGED_KERNEL(128, DT_F16))
+                                  : (bf ? PAGED_KERNEL(64, DT_BF16) : PAGED_KERNEL(64, DT_F16));
+#undef PAGED_KERNEL
+    if (e != hipSuccess || !a.merge) return e;
     return D == 128 ? launch_done(paged_merge_kernel<128>, mg, block, 0, st, done, a)
                     : launch_done(paged_merge_kernel<64>, mg, block, 0, st, done, a);
 }
