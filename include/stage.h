@@ -512,7 +512,7 @@ typedef struct KVStep KVStep;
  * aligned to 16 bytes, kept until the pool is freed.  pair_axis: host uint8 [D/2] or
  * NULL: which of n_axes positions turns rotary pair i, as for images and video (time,
  * height, width); NULL: the first (n_axes 1).  Free pages are handed out lowest first.
- * Bound to the stage, and freed before it, after its sequences and steps.
+ * Bound to the stage, and freed before it; the sequences and steps that are left go with it.
  * Errors: INVALID (NULL, alignment, an axis out of range), CAPACITY (n_pages < 1, more
  * than 2^31 - 1 rows; n_axes), UNSUPPORTED (page_rows), OOM, HIP. */
 int kv_pages_create(Stage* stage, int n_pages, int page_rows, void* k, void* v, const uint8_t* pair_axis, int n_axes, KVPages** out);

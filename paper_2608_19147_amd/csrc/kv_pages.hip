@@ -4,8 +4,24 @@
 
 #include <numeric>
 
+// A pool's sequences and steps, which go with it.
+struct Member {
+    Member *before = nullptr, *after = nullptr;
+    virtual ~Member() {
+        if (before) before->after = after;
+        if (after) after->before = before;
+    }
+    void join(Member& head) {
+        before = &head;
+        after = head.after;
+        if (after) after->before = this;
+        head.after = this;
+    }
+};
+
 struct KVPages {
     Stage* stage = nullptr;
+    Member members;
     PagedPool p{};
     int page_rows = 0, n_axes = 1;
     uint8_t* axis = nullptr;                       // device [D / 2], or null
@@ -31,17 +47,17 @@ struct KVPages {
         low = std::min<size_t>(low, page / 64);
         ++n_free;
     }
-    int slot(const std::vector<int>& pages, int row) const { return (pages[row / page_rows] << p.shift) + row % page_rows; }
-    int pages_for(int rows) const { return (rows + page_rows - 1) / page_rows; }
+    int slot(const std::vector<int>& pages, int row) const { return (pages[row >> p.shift] << p.shift) + (row & (page_rows - 1)); }
+    int pages_for(int rows) const { return (int)(((unsigned)rows + page_rows - 1) >> p.shift); }
 };
 
-struct KVSeq {
+struct KVSeq : Member {
     KVPages* pool = nullptr;
     std::vector<int> pages;
     int length = 0;
 };
 
-struct KVStep {
+struct KVStep : Member {
     KVPages* pool = nullptr;
     uint8_t* dev = nullptr;
     size_t cap = 0;
@@ -61,7 +77,7 @@ struct KVStep {
         const StageConfig& c = pool->stage->cfg;
         return merge ? parts * c.n_q_heads * (size_t)(c.head_dim * 4 + 8) : 0;
     }
-    ~KVStep() {
+    ~KVStep() override {
         for (int i = 0; i < 2; ++i) {
             if (host[i]) (void)hipHostFree(host[i]);
             if (ev[i]) (void)hipEventDestroy(ev[i]);
@@ -102,6 +118,22 @@ struct Taken {
     DeviceGuard dev_((st)->device);     \
     HIP_TRY(dev_.err);                  \
     if (int rc_ = not_captured(s)) return rc_
+
+// Metadata of a call to the device, as meta_upload sends it, but up to 64 KB by a kernel that reads the pinned copy: a copy
+// command between two kernels takes some 15 us of the stream, such a kernel 4.
+constexpr size_t SEND_BYTES = 64 << 10;
+int send(Stage* st, const void* host, size_t bytes, hipStream_t s, const uint8_t** dev) {
+    if (bytes > SEND_BYTES) return meta_upload(st, host, bytes, s, dev);
+    if (int rc = ensure_meta(st, std::max<size_t>(bytes, 16))) return rc;
+    const int slot = st->ring_i;
+    st->ring_i = (st->ring_i + 1) % META_RING;
+    if (st->meta_ev_used[slot]) HIP_TRY(hipEventSynchronize(st->meta_ev[slot]));
+    std::memcpy(st->meta_host[slot], host, bytes);
+    HIP_TRY(launch_paged_send(st->meta_host[slot], st->meta_dev, bytes, s, st->meta_ev[slot]));
+    st->meta_ev_used[slot] = true;
+    *dev = st->meta_dev;
+    return STAGE_OK;
+}
 
 int no_room(const KVPages* pool, size_t need) {
     return fail(STAGE_E_CAPACITY, std::to_string(need) + " pages needed, " + std::to_string(pool->n_free) + " free");
@@ -495,8 +527,12 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     put(o_masks, L.masks.data(), L.masks.size() * 4);
     put(o_moves, moves.data(), moves.size() * sizeof(int2));
     step->planned = false;                         // until the new plan is there
-    HIP_TRY(hipMemcpyAsync(step->dev, hb, bytes, hipMemcpyHostToDevice, s));
-    HIP_TRY(hipEventRecord(step->ev[step->ring], s));
+    if (bytes <= SEND_BYTES) {
+        HIP_TRY(launch_paged_send(hb, step->dev, bytes, s, step->ev[step->ring]));
+    } else {
+        HIP_TRY(hipMemcpyAsync(step->dev, hb, bytes, hipMemcpyHostToDevice, s));
+        HIP_TRY(hipEventRecord(step->ev[step->ring], s));
+    }
     step->used[step->ring] = true;
     step->ring ^= 1;
     if (!moves.empty()) HIP_TRY(launch_paged_copy(pool->p, (const int2*)(step->dev + o_moves), (int)moves.size(), s, nullptr));
@@ -605,7 +641,7 @@ int fill(KVSeq* seq, const uint16_t* k, const uint16_t* v, const int16_t* table,
     HIP_TRY(order_on(st, s));
     WorkOn work(st, s);
     const uint8_t* d = nullptr;
-    if (int rc = meta_upload(st, meta.data(), meta.size(), s, &d)) return rc;
+    if (int rc = send(st, meta.data(), meta.size(), s, &d)) return rc;
     if (!moves.empty()) HIP_TRY(launch_paged_copy(pool->p, (const int2*)d, (int)moves.size(), s, nullptr));
     HIP_TRY(launch_paged_fill(pool->p, k, v, table, S, slot, cap, start, (const int*)(d + moves.size() * sizeof(int2)), n, s, st->done_ev));
     work.launched();
@@ -669,6 +705,7 @@ int kv_pages_free(KVPages* pool) {
         if (!pool) return fail(STAGE_E_INVALID, "pool is NULL");
         DeviceGuard dev(pool->stage->device);
         (void)hipDeviceSynchronize();
+        while (pool->members.after) delete pool->members.after;
         delete pool->fwd;
         if (pool->ws) (void)hipFree(pool->ws);
         if (pool->axis) (void)hipFree(pool->axis);
@@ -689,6 +726,7 @@ int kv_seq_create(KVPages* pool, KVSeq** out) {
         *out = nullptr;
         KVSeq* q = new KVSeq();
         q->pool = pool;
+        q->join(pool->members);
         *out = q;
         return STAGE_OK;
     });
@@ -740,6 +778,7 @@ int kv_seq_fork(KVSeq* const* seqs, const int32_t* lengths, const uint8_t* const
             if (kp)
                 for (first = 0; first < len && kp[first];) ++first;
             k.shared = first / pr;
+            k.rows.reserve(len - k.shared * pr);
             for (int j = k.shared * pr; j < len; ++j)
                 if (!kp || kp[j]) k.rows.push_back(j);
             k.kept = k.shared * pr + (int)k.rows.size();
@@ -773,12 +812,15 @@ int kv_seq_fork(KVSeq* const* seqs, const int32_t* lengths, const uint8_t* const
             HIP_TRY(order_on(st, s));
             WorkOn work(st, s);
             const uint8_t* d = nullptr;
-            if (int rc = meta_upload(st, moves.data(), moves.size() * sizeof(int2), s, &d)) return rc;
+            if (int rc = send(st, moves.data(), moves.size() * sizeof(int2), s, &d)) return rc;
             HIP_TRY(launch_paged_copy(pool->p, (const int2*)d, (int)moves.size(), s, st->done_ev));
             work.launched();
         }
         taken.keep();
-        for (int i = 0; i < n; ++i) out[i] = made[i].release();
+        for (int i = 0; i < n; ++i) {
+            made[i]->join(pool->members);
+            out[i] = made[i].release();
+        }
         return STAGE_OK;
     });
 }
@@ -826,7 +868,7 @@ int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream) {
             HIP_TRY(order_on(st, s));
             WorkOn work(st, s);
             const uint8_t* d = nullptr;
-            if (int rc = meta_upload(st, moves.data(), moves.size() * sizeof(int2), s, &d)) return rc;
+            if (int rc = send(st, moves.data(), moves.size() * sizeof(int2), s, &d)) return rc;
             HIP_TRY(fresh ? launch_paged_copy(pool->p, (const int2*)d, (int)moves.size(), s, st->done_ev)
                           : launch_paged_slide(pool->p, (const int2*)d, (int)moves.size(), s, st->done_ev));
             work.launched();
@@ -886,7 +928,7 @@ int kv_seq_read(KVSeq* seq, int layer, int start, int count, void* k_out, void* 
         HIP_TRY(order_on(st, s));
         WorkOn work(st, s);
         const uint8_t* d = nullptr;
-        if (int rc = meta_upload(st, slots.data(), slots.size() * 4, s, &d)) return rc;
+        if (int rc = send(st, slots.data(), slots.size() * 4, s, &d)) return rc;
         HIP_TRY(launch_paged_read(pool->p, layer, (const int*)d, count, (uint16_t*)k_out, (uint16_t*)v_out, s, st->done_ev));
         work.launched();
         return STAGE_OK;
@@ -899,6 +941,7 @@ int kv_step_create(KVPages* pool, KVStep** out) {
         *out = nullptr;
         KVStep* step = new KVStep();
         step->pool = pool;
+        step->join(pool->members);
         *out = step;
         return STAGE_OK;
     });

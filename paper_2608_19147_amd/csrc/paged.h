@@ -56,6 +56,8 @@ struct PagedWrite {
 };
 hipError_t launch_paged_write(const PagedWrite& a, int D, hipStream_t st, hipEvent_t done);
 
+// Bytes (rounded up to 16) from pinned host memory to the device.
+hipError_t launch_paged_send(const void* host, void* dev, size_t bytes, hipStream_t st, hipEvent_t done);
 // Rows moves[i].x -> moves[i].y (slots) of every layer, K and V; no row is both read and written.
 hipError_t launch_paged_copy(const PagedPool& p, const int2* moves, int n, hipStream_t st, hipEvent_t done);
 // The same where rows may overlap: sources and destinations ascend, a source is never below its destination's place in

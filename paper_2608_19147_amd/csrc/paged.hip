@@ -1007,6 +1007,11 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedPool p, int layer,
         *(u32x4_any*)(dst + (size_t)r * p.D) = *(const u32x4*)(base + slot_at(p, slots[r], head));
 }
 
+__global__ __launch_bounds__(256) void paged_send_kernel(const u32x4* host, u32x4* dev, int n) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) dev[i] = host[i];
+}
+
 // Grid of a move of n rows in `pieces` pieces.
 bool move_grid(int n, int pieces, int& chunks, dim3& grid) {
     chunks = (n + MOVE_ROWS - 1) / MOVE_ROWS;
@@ -1043,6 +1048,12 @@ hipError_t launch_paged_write(const PagedWrite& a, int D, hipStream_t st, hipEve
     const dim3 grid(a.M, a.M >= 512 ? 1 : steps);  // few rows: a step of heads a workgroup
     return D == 128 ? launch_done(paged_write_kernel<128>, grid, dim3(256), 0, st, done, a)
                     : launch_done(paged_write_kernel<64>, grid, dim3(256), 0, st, done, a);
+}
+
+hipError_t launch_paged_send(const void* host, void* dev, size_t bytes, hipStream_t st, hipEvent_t done) {
+    const int n = (int)((bytes + 15) / 16);
+    if (n < 1 || bytes > (1u << 24)) return hipErrorInvalidValue;
+    return launch_done(paged_send_kernel, dim3((n + 255) / 256), dim3(256), 0, st, done, (const u32x4*)host, (u32x4*)dev, n);
 }
 
 hipError_t launch_paged_copy(const PagedPool& p, const int2* moves, int n, hipStream_t st, hipEvent_t done) {

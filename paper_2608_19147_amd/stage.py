@@ -704,7 +704,6 @@ class PagePool:
         self.v = torch.zeros(shape, dtype=stage.kv_dtype, device=dev)
         # the zeros are there before any stream's first call on the pool
         torch.cuda.current_stream(dev).synchronize()
-        self._members: "weakref.WeakSet" = weakref.WeakSet()
         h = ctypes.c_void_p()
         check(self.lib.kv_pages_create(stage.handle, self.n_pages, self.page_rows, self.k.data_ptr(), self.v.data_ptr(),
                                        None if axis is None else axis.ctypes.data, self.n_axes, ctypes.byref(h)))
@@ -712,10 +711,8 @@ class PagePool:
         _LIVE_POOLS.add(self)
 
     def free(self) -> None:
-        """Free the pool's sequences and steps, then the pool."""
+        """Free the pool, and its sequences and steps with it."""
         if getattr(self, "handle", None):
-            for m in list(self._members):
-                m.free()
             check(self.lib.kv_pages_free(self.handle))
             self.handle = None
             self.k = self.v = None
@@ -735,7 +732,7 @@ class PagePool:
     def new_sequence(self) -> "PagedSequence":
         h = ctypes.c_void_p()
         check(self.lib.kv_seq_create(self.handle, ctypes.byref(h)))
-        return PagedSequence(self, h)
+        return PagedSequence(self, h.value)
 
     def new_step(self) -> "PagedStep":
         return PagedStep(self)
@@ -761,7 +758,7 @@ class PagePool:
         out = (ctypes.c_void_p * n)()
         check(self.lib.kv_seq_fork((ctypes.c_void_p * n)(*[q.handle for q in seqs]), None if lens is None else lens.ctypes.data, kp, n,
                                    out, _pool_stream(self.stage, stream)))
-        return [PagedSequence(self, ctypes.c_void_p(h)) for h in out]
+        return [PagedSequence(self, h) for h in out]
 
 
 def _pool_stream(stage: Stage, stream) -> int:
@@ -772,20 +769,24 @@ class PagedSequence:
     """A sequence of cache rows in a pool's pages (``PagePool.new_sequence``, ``PagePool.fork``)."""
 
     def __init__(self, pool: PagePool, handle):
-        self.pool, self.lib, self.handle = pool, pool.lib, handle
-        pool._members.add(self)
+        self.pool, self.lib, self._handle = pool, pool.lib, handle
+
+    @property
+    def handle(self):
+        if self._handle is None or self.pool.handle is None:
+            raise ValueError("the sequence has been freed")
+        return self._handle
 
     def _check(self, pool: PagePool) -> None:
-        if self.handle is None:
-            raise ValueError("the sequence has been freed")
         if self.pool is not pool:
             raise ValueError("the sequence belongs to another pool")
+        self.handle                                # raises if it has been freed
 
     def free(self) -> None:
         """Give back the pages that no other sequence holds."""
-        if getattr(self, "handle", None):
-            check(self.lib.kv_seq_free(self.handle))
-            self.handle = None
+        h, self._handle = self._handle, None
+        if h is not None and self.pool.handle is not None:
+            check(self.lib.kv_seq_free(h))
 
     def __del__(self):
         try:
@@ -913,15 +914,21 @@ class PagedStep:
         sh = pool.stage.shape
         self._nq, self._nk = sh.n_q_heads * sh.head_dim, sh.n_kv_heads * sh.head_dim
         h = ctypes.c_void_p()
+        self._handle = None
         check(self.lib.kv_step_create(pool.handle, ctypes.byref(h)))
-        self.handle = h
+        self._handle = h.value
         self.rows = self._ws = 0
-        pool._members.add(self)
+
+    @property
+    def handle(self):
+        if self._handle is None or self.pool.handle is None:
+            raise ValueError("the step has been freed")
+        return self._handle
 
     def free(self) -> None:
-        if getattr(self, "handle", None):
-            check(self.lib.kv_step_free(self.handle))
-            self.handle = None
+        h, self._handle = self._handle, None
+        if h is not None and self.pool.handle is not None:
+            check(self.lib.kv_step_free(h))
 
     def __del__(self):
         try:
