@@ -745,8 +745,13 @@ class PagePool:
         n = len(seqs)
         if lengths is not None and len(lengths) != n or keep is not None and len(keep) != n:
             raise ValueError(f"lengths and keep must have {n} entries")
+        if self.handle is None:
+            raise ValueError("the pool has been freed")
+        handles = []
         for q in seqs:
-            q._check(self)
+            if q.pool is not self or q._handle is None:
+                q._check(self)
+            handles.append(q._handle)
         lens = None if lengths is None else np.ascontiguousarray(lengths, dtype=np.int32)
         masks, kp = None, None
         if keep is not None:
@@ -756,7 +761,7 @@ class PagePool:
                     raise ValueError(f"keep[{i}] must have one entry per row")
             kp = (ctypes.c_void_p * n)(*[None if m is None else m.ctypes.data for m in masks])
         out = (ctypes.c_void_p * n)()
-        check(self.lib.kv_seq_fork((ctypes.c_void_p * n)(*[q.handle for q in seqs]), None if lens is None else lens.ctypes.data, kp, n,
+        check(self.lib.kv_seq_fork((ctypes.c_void_p * n)(*handles), None if lens is None else lens.ctypes.data, kp, n,
                                    out, _pool_stream(self.stage, stream)))
         return [PagedSequence(self, h) for h in out]
 
@@ -768,29 +773,38 @@ def _pool_stream(stage: Stage, stream) -> int:
 class PagedSequence:
     """A sequence of cache rows in a pool's pages (``PagePool.new_sequence``, ``PagePool.fork``)."""
 
-    def __init__(self, pool: PagePool, handle):
-        self.pool, self.lib, self._handle = pool, pool.lib, handle
+    __slots__ = ("pool", "_handle")                              # a fork makes many at once
+
+    def __init__(self, pool: PagePool, handle: int):
+        self.pool, self._handle = pool, handle
 
     @property
-    def handle(self):
+    def handle(self) -> int:
         if self._handle is None or self.pool.handle is None:
             raise ValueError("the sequence has been freed")
         return self._handle
 
+    @property
+    def lib(self):
+        return self.pool.lib
+
     def _check(self, pool: PagePool) -> None:
         if self.pool is not pool:
             raise ValueError("the sequence belongs to another pool")
-        self.handle                                # raises if it has been freed
+        self.handle                                              # raises if it has been freed
 
     def free(self) -> None:
         """Give back the pages that no other sequence holds."""
-        h, self._handle = self._handle, None
-        if h is not None and self.pool.handle is not None:
-            check(self.lib.kv_seq_free(h))
+        h = self._handle
+        if h is not None:
+            self._handle = None
+            if self.pool.handle is not None:
+                check(self.pool.lib.kv_seq_free(h))
 
     def __del__(self):
         try:
-            self.free()
+            if self._handle is not None:
+                self.free()
         except Exception:
             pass
 
