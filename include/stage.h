@@ -492,7 +492,8 @@ int stage_tree_accept(Stage* stage, const int32_t* parents, const int32_t* token
  * A capturing stream is refused (STAGE_E_UNSUPPORTED), but for kv_step_write and
  * kv_step_attend: they use the step's metadata and the caller's memory alone, so a
  * graph can hold them; its replays are ordered by the caller, behind the step's plan
- * (synchronize before the capture), and a step that was captured takes no other plan.
+ * (synchronize before the capture), a step that was captured takes no other plan, and
+ * its metadata stays until the pool is freed, which has to outlive the graph.
  * The pages of a sequence that is freed, truncated or compacted may be taken by the
  * next call that needs pages, behind the work issued before it; steps that were
  * planned with it, and graphs that hold them, then read other rows.
@@ -579,18 +580,19 @@ int kv_step_free(KVStep* step);
 
 /* Make room for the new rows in each sequence (whose length is then P + n_tokens; a
  * shared last page is replaced by a copy), and lay out the step: M = sum of n_tokens
- * rows, request-major.
+ * rows, request-major.  The new rows hold what their pages held until kv_step_write has
+ * stored them, in every layer: fork or read them after that.
  * Errors: INVALID (NULL, n_tokens < 1, positions for some only), STATE_MISMATCH (another
  * pool's sequence, one twice), CAPACITY (M, a position, free pages, rows, masks above
- * 2^31 words), UNSUPPORTED (capturing stream, a captured step), OOM, HIP; nothing has
- * changed on error. */
+ * 2^31 words), UNSUPPORTED (capturing stream, a captured step), OOM, HIP; no sequence
+ * has changed on error (the step may have lost the plan that it had). */
 int kv_step_plan(KVStep* step, const KVStepRequest* reqs, int n_req, void* stream);
 
 /* One layer's new rows: q [M][Hq D], k, v [M][Hkv D] (F32, F16 or BF16, one dtype; row
  * strides ld count elements; no alignment beyond the element's).  Pair (i, i + D/2) of
  * every q and k head turns by its axis' position (none without positions); k and v go to
  * their rows of the pages, q to q_out [M][Hq D] (F32, F16 or BF16), which may be q itself
- * (same dtype and stride).
+ * (same dtype and stride), and overlaps none of q, k and v otherwise.
  * Errors: INVALID (NULL, dtype, layer, a step without plan), SHAPE (strides), HIP. */
 int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype,
                   void* q_out, int64_t ldqo, int q_out_dtype, void* stream);
@@ -603,7 +605,7 @@ int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
  * that sees none gives zeros.  q: kv_dtype, or F32 (as two terms of kv_dtype: within
  * 2^-17 of each element in bf16, 2^-22 in fp16); out: F32, F16 or BF16, not overlapping q.
  * Scores and sums in fp32; probabilities enter as one or two terms of kv_dtype (two where
- * a kv head has at most 64 query vectors of the run, and with F32 queries).  What rows
+ * a kv head has at most 16 query vectors of a run of rows, and with F32 queries).  What rows
  * that are not seen hold, infinities and NaN too, reaches no result.
  * workspace: device memory of kv_step_workspace bytes, aligned to 16, not used by another
  * call at the same time (two graphs need two).

@@ -949,6 +949,7 @@ int kv_step_create(KVPages* pool, KVStep** out) {
 
 int kv_step_free(KVStep* step) {
     if (!step) return fail(STAGE_E_INVALID, "step is NULL");
+    if (step->captured) return STAGE_OK;           // a graph may still read its metadata: it goes with the pool
     DeviceGuard dev(step->pool->stage->device);
     (void)hipDeviceSynchronize();                  // queued work may still read its metadata
     delete step;
@@ -982,6 +983,7 @@ int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const voi
         if (!dtype_ok(dtype) || !dtype_ok(q_out_dtype)) return fail(STAGE_E_INVALID, "dtypes must be F32, F16 or BF16");
         const int64_t nq = (int64_t)c.n_q_heads * c.head_dim, nk = (int64_t)c.n_kv_heads * c.head_dim;
         if (ldq < nq || ldqo < nq || ldk < nk || ldv < nk) return fail(STAGE_E_SHAPE, "row stride below the row length");
+        if (q_out == q && (q_out_dtype != dtype || ldqo != ldq)) return fail(STAGE_E_INVALID, "q_out is q in another dtype or stride");
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;

@@ -518,11 +518,13 @@ def test_load_from_a_state(stages):
 
 # ------------------------------------------------------------------ the forward over sequences
 
-@pytest.fixture(scope="module")
-def pair():
+@pytest.fixture(scope="module", params=[128, 64])
+def pair(request):
+    """A stage of the matrix-core products, and one of another group size, which has none."""
+    import dataclasses
     import synth
     from gpu_cases import Pair
-    p = Pair(synth.TINY, 77)
+    p = Pair(dataclasses.replace(synth.TINY, group_size=request.param), 77)
     yield p
     p.close()
 
@@ -595,7 +597,12 @@ def test_forward_generates_from_forks(pair):
     prompt = synth.make_hidden(pair.shape, 90, 0, 8).cuda()
     states = [st.new_state(1, 200) for _ in range(3)]
     for g in states:
-        st.prefill(g, np.arange(90), prompt)
+        if pair.shape.group_size == 128:
+            st.prefill(g, np.arange(90), prompt)
+        else:                                                    # no prefill there
+            for at in (0, 45):
+                pos = np.arange(at, at + 45, dtype=np.int32)[None]
+                st.forward([Request(g, pos, np.ones((1, at + 45), np.uint8))], prompt[at:at + 45].contiguous())
     pool = st.new_pages(40, 16)
     base = pool.new_sequence()
     base.load(states[0])
@@ -688,7 +695,16 @@ def test_graphs_of_a_step(stages):
     with pytest.raises(StageError) as e:                         # the graphs hold this plan
         step.plan([PagedRequest(seqs[0], 1)])
     assert e.value.code == -7
-    del held
+    step.free()                                                  # they hold it still
+    other = pool.new_step()
+    other.plan([PagedRequest(seqs[0], 1)])
+    s, x, graph, out = held[0]
+    with torch.cuda.stream(s):
+        x.copy_(xs[5])
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, eager[5])
+    del held, graph
     pool.free()
 
 
