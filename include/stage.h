@@ -538,8 +538,9 @@ int kv_seq_pages(const KVSeq* seq, int32_t* pages_out, int capacity, int* count_
  * UNSUPPORTED (capturing stream), OOM, HIP; nothing is created on error. */
 int kv_seq_fork(KVSeq* const* seqs, const int32_t* lengths, const uint8_t* const* keep, int n, KVSeq** out, void* stream);
 
-/* Drop the rows with keep[j] == 0 (host uint8 [length]) and close the others up, in
- * place; shared pages that change are replaced by new ones.
+/* Drop the rows with keep[j] == 0 (host uint8 [length]) and close the others up: from the
+ * page of the first one on into new pages, or, where too few are free, in place (shared
+ * pages that change are replaced by new ones).
  * Errors: INVALID (NULL), CAPACITY (free pages), UNSUPPORTED (capturing stream), OOM, HIP. */
 int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream);
 
