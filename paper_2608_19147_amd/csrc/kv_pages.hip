@@ -182,7 +182,7 @@ struct Layout {
 // What a workgroup's start and end, and a partial result of a query vector, cost beside a step of 32 keys of a tile.
 constexpr double START_STEPS = 6, PART_STEPS = 1.0 / 16;
 constexpr int SPLIT_STEPS = 8;                     // fewest steps of a split
-constexpr int SHARE_QUERIES = 64;                  // a sequence with more query vectors a kv head fills tiles alone
+constexpr int SHARE_QUERIES = 128;                 // a sequence with more query vectors a kv head fills tiles alone
 
 // The runs of a batch: sequences sorted by their whole pages, so that those that share pages are neighbours.  A common
 // beginning becomes a run of them all where that saves more steps of tiles than its starts and partial results cost (12
@@ -219,8 +219,17 @@ struct RunBuilder {
             while (lcp < lim && a[lcp] == b[lcp]) ++lcp;
             // sets with the same page at lcp; a sequence that ends there is alone
             std::vector<int> ends;
-            long rows = 0, set_rows = 0, apart = 0;
+            long rows = 0, set_rows = 0;
+            double apart = 0;
             auto tiles = [&](long r) { return (r * gs + PAGED_MANY - 1) / PAGED_MANY; };
+            // a tile's last queries take half a tile up to 64 of them (loads of rows bound a smaller one), so sets that fill
+            // halves save no product (48 x 15 rows of 4 heads 64 us shared, 52 apart), and sets of 80 do (48 x 10 rows of 8 145
+            // apart, 110 shared).  Two halves cost a little more than a whole: 48 x 8 rows of 8 behind 30000 to 60000 shared keys
+            // are 7 to 10% slower apart, 12 x 8 rows and 16 x 16 rows of 4 behind 60000 to 100000 6 to 11% faster.
+            auto work = [&](long r) {
+                const long q = r * gs, rest = q % PAGED_MANY;
+                return q / PAGED_MANY + (rest == 0 ? 0.0 : rest <= 64 ? 0.5 : 1.0);
+            };
             for (int j = 0; j < cnt; ++j) {
                 rows += n[order[j]];
                 set_rows += n[order[j]];
@@ -228,11 +237,11 @@ struct RunBuilder {
                                   (*pages[order[j + 1]])[lcp] != (*pages[order[j]])[lcp];
                 if (!last) continue;
                 ends.push_back(j + 1);
-                apart += tiles(set_rows);
+                apart += work(set_rows);
                 set_rows = 0;
             }
             const double steps = (lcp - from) * pr / 32.0;
-            if (steps * (apart - tiles(rows)) > START_STEPS * tiles(rows) + PART_STEPS * rows * gs) {
+            if (steps * (apart - work(rows)) > START_STEPS * tiles(rows) + PART_STEPS * rows * gs) {
                 parent = add(order, cnt, from * pr, lcp * pr, parent, true);
                 from = lcp;
             }
