@@ -321,8 +321,9 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >
 // ---- tiles of up to 16 query vectors
 //
 // Decoding rows.  The four waves take alternate steps of 16 keys (one page's) and are merged through LDS.  Bound by memory
-// (4 x 131072 rows of 8 x 128: 308 us, 5.7 TB/s; a large read 6.2): what counts is bytes in flight.  A wave holds NB steps in LDS of its own; it reads all of a step into registers, then
-// asks for the step NB further on in its place, so that no barrier stands between.  A probability enters as its rounded
+// (four caches of 81920 to 131072 rows of 8 x 128: 309 us, 5.65 TB/s; a large read 6.2): what counts is bytes in flight.
+// A wave holds NB steps in LDS of its own; it reads all of a step into registers, then asks for the step NB further on in
+// its place, so that no barrier stands between.  A probability enters as its rounded
 // part and the residual (2^-17 in bf16), in one product: the second operand's 32 k slots hold 16 keys twice, those of V^T
 // repeat them.
 template <int D, int KVDT, int QT, int NB>
@@ -525,7 +526,7 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
 }
 
 // Batches of nothing else: at most 128 registers a wave and 33 KB of LDS, so that four workgroups share a CU (16 x 8 KB
-// under way; 4 x 131072 rows of 8 x 128: two workgroups of 16 KB a wave 359 us, four of 8 KB 315).
+// under way; four caches of 81920 to 131072 rows: two workgroups of 16 KB a wave 359 us, four of 8 KB 315).
 template <int D, int KVDT, int QT>
 __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[32768];
@@ -541,8 +542,8 @@ __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
 // groups, which take alternate steps of 32 keys.  A group's waves share a ring of NQT steps; alone (NQT = 1) a wave reads
 // its step into registers before it asks for the next.  A step of a wave takes 512 cycles of products, some 640 of vector
 // instructions (256 of them exponentials) and a share of LDS, which its two waves a SIMD hardly overlap: 4 x 1024 rows of 32
-// heads of 128 behind 2048 take 205 us, 840 TFLOP/s, where a product of 8192 x 8192 x 8192 reaches 1077.  (The next step's
-// scores under way while this one's become probabilities: 20% slower; steps of 64 keys: 4%; wave priorities: 0 to 3%.)
+// heads of 128 behind 2048 take 197 to 210 us, 820 to 870 TFLOP/s, where a product of 8192 x 8192 x 8192 reaches 1077.  (The next step's
+// scores under way while this one's become probabilities: 12% slower; steps of 64 keys: 4%; wave priorities: 1% faster to 9% slower.)
 // PT: terms of a probability (1: rounded to the cache's type, while the sum keeps it whole).
 template <int D, int KVDT, int QT, int PT, int NQT>
 __device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml, uint32_t* words) {
