@@ -55,6 +55,9 @@ struct KVSeq : Member {
     KVPages* pool = nullptr;
     std::vector<int> pages;
     int length = 0;
+    std::vector<KVStep*> steps;                    // whose plans have rows of it
+    void lose(int len);                            // rows from len on
+    ~KVSeq() override { lose(-1); }
 };
 
 struct KVStep : Member {
@@ -72,12 +75,18 @@ struct KVStep : Member {
     int M = 0, n_items = 0;
     size_t parts = 0;
     size_t o_items = 0, o_rows = 0, o_list = 0, o_tables = 0, o_slots = 0, o_pos = 0, o_masks = 0;
+    std::vector<std::pair<KVSeq*, int>> of;        // its sequences, and their rows with the new ones
 
     size_t part_bytes() const {
         const StageConfig& c = pool->stage->cfg;
         return merge ? parts * c.n_q_heads * (size_t)(c.head_dim * 4 + 8) : 0;
     }
+    void leave() {                                 // its sequences forget it
+        for (auto& x : of) x.first->steps.erase(std::remove(x.first->steps.begin(), x.first->steps.end(), this), x.first->steps.end());
+        of.clear();
+    }
     ~KVStep() override {
+        leave();
         for (int i = 0; i < 2; ++i) {
             if (host[i]) (void)hipHostFree(host[i]);
             if (ev[i]) (void)hipEventDestroy(ev[i]);
@@ -85,6 +94,20 @@ struct KVStep : Member {
         if (dev) (void)hipFree(dev);
     }
 };
+
+// A plan with one of the rows is none: its pages may soon be another sequence's.
+void KVSeq::lose(int len) {
+    for (size_t i = 0; i < steps.size();) {
+        KVStep* step = steps[i];
+        const auto x = std::find_if(step->of.begin(), step->of.end(), [&](const auto& y) { return y.first == this; });
+        if (x->second <= len) {
+            ++i;
+            continue;
+        }
+        step->planned = false;
+        step->leave();                             // (takes it out of `steps`)
+    }
+}
 
 namespace {
 
@@ -546,7 +569,14 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     put(o_pos, L.pos.data(), L.pos.size() * 4);
     put(o_masks, L.masks.data(), L.masks.size() * 4);
     put(o_moves, moves.data(), moves.size() * sizeof(int2));
+    std::vector<std::pair<KVSeq*, int>> of;
+    of.reserve(ps.size());
+    for (const Planned& p : ps) {
+        of.emplace_back(p.seq, p.P + p.n);
+        p.seq->steps.reserve(p.seq->steps.size() + 1);
+    }
     step->planned = false;                         // until the new plan is there
+    step->leave();
     if (bytes <= SEND_BYTES) {
         HIP_TRY(launch_paged_send(hb, step->dev, bytes, s, step->ev[step->ring]));
     } else {
@@ -563,7 +593,9 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
         if (p.copy_last) pool->give(p.seq->pages.back());
         p.seq->pages.swap(p.pages);
         p.seq->length = p.P + p.n;
+        p.seq->steps.push_back(step);
     }
+    step->of.swap(of);
     step->planned = true;
     step->turned = turned;
     step->merge = L.merge;
@@ -893,6 +925,7 @@ int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream) {
             work.launched();
         }
         taken.keep();
+        seq->lose(first);
         for (int p : gone) pool->give(p);
         seq->pages.swap(pages);
         seq->length = kept;
@@ -903,6 +936,7 @@ int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream) {
 int kv_seq_truncate(KVSeq* seq, int new_len) {
     if (!seq) return fail(STAGE_E_INVALID, "sequence is NULL");
     if (new_len < 0 || new_len > seq->length) return fail(STAGE_E_INVALID, "new_len must be in [0, length]");
+    seq->lose(new_len);
     const size_t n = seq->pool->pages_for(new_len);
     while (seq->pages.size() > n) {
         seq->pool->give(seq->pages.back());

@@ -231,6 +231,42 @@ def refusals():
     return got
 
 
+def lost_rows():
+    """What a step answers once its sequences have lost rows: [case, write's status, attend's]."""
+    out = []
+    keep = lambda n, drop: array((np.arange(n) != drop).astype(np.uint8))
+    other = {}
+    for name, change in (
+            ("nothing", lambda p, q: 0),
+            ("a fork", lambda p, q: fork([q], 1)[0]),
+            ("a fork cut", lambda p, q: lib.kv_seq_truncate(fork([q], 1)[1][0], 3)),
+            ("rows behind it", lambda p, q: lib.kv_seq_append(q, p.rows, p.rows, 9, None) or lib.kv_seq_truncate(q, 45)),
+            ("another step", lambda p, q: plan(other["step"], [request(q, 4)])),
+            ("no row dropped", lambda p, q: lib.kv_seq_compact(q, keep(45, -1), None)),
+            ("cut", lambda p, q: lib.kv_seq_truncate(q, 44)),
+            ("cut and refilled", lambda p, q: lib.kv_seq_truncate(q, 40) or lib.kv_seq_append(q, p.rows, p.rows, 5, None)),
+            ("compacted", lambda p, q: lib.kv_seq_compact(q, keep(45, 7), None)),
+            ("freed", lambda p, q: lib.kv_seq_free(q))):
+        p = Pool()
+        q, r, step = p.seq(40), p.seq(3), p.step()
+        other["step"] = p.step()
+        assert plan(step, [request(q, 5), request(r, 2)]) == 0
+        assert change(p, q) == 0, name
+        out.append([name, *use(step, p)])
+        if name == "cut":                                        # planned again, it has a plan; and the other sequence is free of it
+            assert plan(step, [request(r, 2)]) == 0 and lib.kv_seq_free(q) == 0
+            out.append(["planned again", *use(step, p)])
+        assert lib.kv_step_free(step) == 0 and lib.kv_seq_free(r) == 0 and lib.kv_pages_free(p.h) == 0, name
+    return out
+
+
+def use(step, p, q_out=None, ld=4 * 64):
+    big = p.rows
+    w = lib.kv_step_write(step, 0, big, ld, big + (1 << 18), 128, big + (1 << 19), 128, 2, q_out or big + (3 << 18), ld, 2, None)
+    a = lib.kv_step_attend(step, 0, big, 2, ld, big + (3 << 18), 2, ld, 0.0, big + (1 << 20), 1 << 19, None)
+    return w, a
+
+
 def workspace():
     """A step with partial results refuses a workspace that is missing, too small or not aligned."""
     p = Pool(200)

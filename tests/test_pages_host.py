@@ -71,3 +71,10 @@ def test_capture(ask):
 
 def test_workspace(ask):
     assert ask("workspace") == [True, -1, -1, -1, 0]
+
+
+def test_lost_rows(ask):
+    """A step whose sequences have lost rows that it covers has no plan: its rows may be another sequence's by then."""
+    kept = {"nothing", "a fork", "a fork cut", "rows behind it", "another step", "no row dropped", "planned again"}
+    for name, write, attend in ask("lost_rows"):
+        assert [write, attend] == ([0, 0] if name in kept else [-1, -1]), name
