@@ -596,7 +596,7 @@ int kv_step_plan(KVStep* step, const KVStepRequest* reqs, int n_req, void* strea
  * every q and k head turns by its axis' position (none without positions); k and v go to
  * their rows of the pages, q to q_out [M][Hq D] (F32, F16 or BF16), which may be q itself
  * (same dtype and stride), and overlaps none of q, k and v otherwise.
- * Errors: INVALID (NULL, dtype, layer, a step without plan), SHAPE (strides), HIP. */
+ * Errors: INVALID (NULL, dtype, layer, a step without plan, overlap), SHAPE (strides), HIP. */
 int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype,
                   void* q_out, int64_t ldqo, int q_out_dtype, void* stream);
 
@@ -612,7 +612,7 @@ int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
  * that are not seen hold, infinities and NaN too, reaches no result.
  * workspace: device memory of kv_step_workspace bytes, aligned to 16, not used by another
  * call at the same time (two graphs need two).
- * Errors: INVALID (NULL, dtype, layer, scale, workspace, a step without plan), SHAPE
+ * Errors: INVALID (NULL, dtype, layer, scale, workspace, overlap, a step without plan), SHAPE
  * (strides), HIP. */
 int kv_step_attend(KVStep* step, int layer, const void* q, int q_dtype, int64_t ldq, void* out, int out_dtype, int64_t ldo, float scale,
                    void* workspace, int64_t workspace_bytes, void* stream);

@@ -162,6 +162,15 @@ int no_room(const KVPages* pool, size_t need) {
     return fail(STAGE_E_CAPACITY, std::to_string(need) + " pages needed, " + std::to_string(pool->n_free) + " free");
 }
 
+// Whether two arrays of m rows (row and ld bytes) share memory; rows of one stride may lie between each other.
+bool overlap(const void* a, int64_t row_a, int64_t ld_a, const void* b, int64_t row_b, int64_t ld_b, int m) {
+    const int64_t d = (int64_t)((uintptr_t)b - (uintptr_t)a);
+    if (d >= (m - 1) * ld_a + row_a || -d >= (m - 1) * ld_b + row_b) return false;
+    if (m == 1 || ld_a != ld_b) return true;
+    const int64_t at = ((d % ld_a) + ld_a) % ld_a;
+    return at < row_a || at + row_b > ld_a;
+}
+
 // Whether n rows moved in every layer's pieces are one launch (paged.hip).
 bool one_launch(const PagedPool& p, size_t n) { return (n + 63) / 64 * 2 * p.layers * p.Hkv < ((size_t)1 << 24) && n <= INT_MAX; }
 
@@ -1036,7 +1045,11 @@ int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const voi
         if (!dtype_ok(dtype) || !dtype_ok(q_out_dtype)) return fail(STAGE_E_INVALID, "dtypes must be F32, F16 or BF16");
         const int64_t nq = (int64_t)c.n_q_heads * c.head_dim, nk = (int64_t)c.n_kv_heads * c.head_dim;
         if (ldq < nq || ldqo < nq || ldk < nk || ldv < nk) return fail(STAGE_E_SHAPE, "row stride below the row length");
-        if (q_out == q && (q_out_dtype != dtype || ldqo != ldq)) return fail(STAGE_E_INVALID, "q_out is q in another dtype or stride");
+        const int e = dtype == STAGE_DTYPE_F32 ? 4 : 2, eo = q_out_dtype == STAGE_DTYPE_F32 ? 4 : 2;
+        const bool in_place = q_out == q && q_out_dtype == dtype && ldqo == ldq;
+        if ((!in_place && overlap(q, nq * e, ldq * e, q_out, nq * eo, ldqo * eo, step->M)) ||
+            overlap(k, nk * e, ldk * e, q_out, nq * eo, ldqo * eo, step->M) || overlap(v, nk * e, ldv * e, q_out, nq * eo, ldqo * eo, step->M))
+            return fail(STAGE_E_INVALID, "q_out overlaps q, k or v (it may be q itself, in its dtype and stride)");
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;
@@ -1086,6 +1099,8 @@ int kv_step_attend(KVStep* step, int layer, const void* q, int q_dtype, int64_t 
         if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(STAGE_E_INVALID, "scale must be finite and not negative");
         const int64_t nq = (int64_t)c.n_q_heads * c.head_dim;
         if (ldq < nq || ldo < nq) return fail(STAGE_E_SHAPE, "row stride below the row length");
+        const int e = q_dtype == STAGE_DTYPE_F32 ? 4 : 2, eo = out_dtype == STAGE_DTYPE_F32 ? 4 : 2;
+        if (overlap(q, nq * e, ldq * e, out, nq * eo, ldo * eo, step->M)) return fail(STAGE_E_INVALID, "out overlaps q");
         if (step->merge && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < (int64_t)step->part_bytes()))
             return fail(STAGE_E_INVALID, "workspace too small (kv_step_workspace) or not aligned to 16 bytes");
         DeviceGuard dev(st->device);

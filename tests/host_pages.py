@@ -267,6 +267,23 @@ def use(step, p, q_out=None, ld=4 * 64):
     return w, a
 
 
+def overlaps():
+    """Statuses of writes and attentions whose output shares memory with an input, or lies between its rows."""
+    p = Pool()
+    step = p.step()
+    assert plan(step, [request(p.seq(20), 3)]) == 0
+    b, far, ws, W = p.rows, p.rows + (1 << 19), p.rows + (1 << 20), 4 * 64
+    write = lambda q, k, v, out, ld=W, ldo=W: lib.kv_step_write(step, 0, q, ld, k, ld, v, ld, 2, out, ldo, 2, None)
+    attend = lambda q, out, ld=W, ldo=W: lib.kv_step_attend(step, 0, q, 2, ld, out, 2, ldo, 0.0, ws, 1 << 19, None)
+    k, v = far, far + (1 << 16)
+    return {
+        "allowed": [write(b, k, v, b), write(b, b + 2 * W, b + 2 * W + 256, b, 2 * W, 2 * W), write(b, k, v, b + 2 * W, 2 * W, 2 * W),
+                    write(b, k, v, b + 2 * 3 * W), attend(b, b + 2 * 3 * W), attend(b, b + 2 * W, 2 * W, 2 * W)],
+        "refused": [write(b, k, v, b + 2), write(b, k, v, k), write(b, k, v, v + 2), write(b, k, v, b + 2 * W, 2 * W, 3 * W),
+                    attend(b, b), attend(b, b + 2), attend(b, b + 2 * W), attend(b, b - 2, 2 * W, 2 * W), attend(b, b + 2 * W, 2 * W, 3 * W)],
+    }
+
+
 def workspace():
     """A step with partial results refuses a workspace that is missing, too small or not aligned."""
     p = Pool(200)
@@ -275,7 +292,7 @@ def workspace():
     assert plan(step, [request(q, 1)]) == 0
     n = ctypes.c_int64()
     assert lib.kv_step_workspace(step, ctypes.byref(n)) == 0
-    call = lambda ws, size: lib.kv_step_attend(step, 0, p.rows, 2, 256, p.rows, 2, 256, 0.0, ws, size, None)
+    call = lambda ws, size: lib.kv_step_attend(step, 0, p.rows, 2, 256, p.rows + 512, 2, 256, 0.0, ws, size, None)
     return [n.value > 0, call(None, n.value), call(p.rows, n.value - 1), call(p.rows + 4, n.value), call(p.rows, n.value)]
 
 

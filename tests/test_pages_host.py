@@ -78,3 +78,8 @@ def test_lost_rows(ask):
     kept = {"nothing", "a fork", "a fork cut", "rows behind it", "another step", "no row dropped", "planned again"}
     for name, write, attend in ask("lost_rows"):
         assert [write, attend] == ([0, 0] if name in kept else [-1, -1]), name
+
+
+def test_overlapping_outputs(ask):
+    got = ask("overlaps")
+    assert got["allowed"] == [0] * 6 and got["refused"] == [-1] * 9, got
