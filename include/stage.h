@@ -495,8 +495,9 @@ int stage_tree_accept(Stage* stage, const int32_t* parents, const int32_t* token
  * (synchronize before the capture), a step that was captured takes no other plan, and
  * its metadata stays until the pool is freed, which has to outlive the graph.
  * The pages of a sequence that is freed, truncated or compacted may be taken by the
- * next call that needs pages, behind the work issued before it; steps that were
- * planned with it, and graphs that hold them, then read other rows.
+ * next call that needs pages, behind the work issued before it.  Steps that were planned
+ * with rows of them have no plan then (kv_step_plan); graphs that hold such a plan would
+ * write and read other rows.
  * The calling thread's current device is left as it was.
  * ------------------------------------------------------------------------ */
 
@@ -582,9 +583,10 @@ int kv_step_free(KVStep* step);
 /* Make room for the new rows in each sequence (whose length is then P + n_tokens; a
  * shared last page is replaced by a copy), and lay out the step: M = sum of n_tokens
  * rows, request-major.  The plan stands until one of its sequences loses rows that it
- * covers (kv_seq_truncate below its length then, kv_seq_compact, kv_seq_free); a graph
- * that has captured it must not be replayed from then on.  The new rows hold what their pages held until kv_step_write has
- * stored them, in every layer: fork or read them after that.
+ * covers, or has a page of them replaced (kv_seq_truncate below its length then,
+ * kv_seq_compact from the page of the first dropped row on, kv_seq_free); a graph that
+ * has captured it must not be replayed from then on.  The new rows hold what their pages
+ * held until kv_step_write has stored them, in every layer: fork or read them after that.
  * Errors: INVALID (NULL, n_tokens < 1, positions for some only), STATE_MISMATCH (another
  * pool's sequence, one twice), CAPACITY (M, a position, free pages, rows, masks above
  * 2^31 words), UNSUPPORTED (capturing stream, a captured step), OOM, HIP; no sequence

@@ -56,7 +56,7 @@ struct KVSeq : Member {
     std::vector<int> pages;
     int length = 0;
     std::vector<KVStep*> steps;                    // whose plans have rows of it
-    void lose(int len);                            // rows from len on
+    void lose(int len);                            // rows from len on, or their pages
     ~KVSeq() override { lose(-1); }
 };
 
@@ -934,7 +934,8 @@ int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream) {
             work.launched();
         }
         taken.keep();
-        seq->lose(first);
+        // from the first row of a replaced page on: its plans would write and read what may be another sequence's
+        seq->lose(moved && pages[t0] != seq->pages[t0] ? t0 * pr : first);
         for (int p : gone) pool->give(p);
         seq->pages.swap(pages);
         seq->length = kept;

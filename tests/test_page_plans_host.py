@@ -1,0 +1,44 @@
+"""Plans of the paged cache whose sequences get other pages, on the stand-in for the
+HIP runtime (hip_host.cpp): a step answers as long as its pages are its sequences'."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2608_19147_amd import _lib
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    """ask(question, *arguments): what host_page_plans.py answers."""
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2608_19147_amd import build
+
+        build.build()
+    so = str(tmp_path_factory.mktemp("host") / "hip_host.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", os.path.join(HERE, "hip_host.cpp"), "-o", so], check=True)
+
+    def run(*args):
+        env = {**os.environ, "LD_PRELOAD": so, "STAGE_PERSISTENT": "0", "OPENBLAS_NUM_THREADS": "1"}
+        r = subprocess.run([sys.executable, os.path.join(HERE, "host_page_plans.py"), *args], env=env, capture_output=True, text=True,
+                           timeout=120)
+        assert r.returncode == 0, r.stderr
+        return json.loads(r.stdout)
+
+    return run
+
+
+def _check(got, replaced):
+    """[same pages, write, attend] of each case: those named had a page of the plan replaced, and its step has no plan."""
+    for name, (same, write, attend) in got.items():
+        assert same == (name not in replaced), name
+        assert [write, attend] == ([0, 0] if same else [-1, -1]), name
+
+
+def test_compaction(ask):
+    """The old pages of a compaction may be another sequence's next: a plan with rows in one of them is withdrawn."""
+    _check(ask("compacted"), {"in its last page, into new pages", "in its last page, in place of a shared one"})
