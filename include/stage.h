@@ -584,9 +584,11 @@ int kv_step_free(KVStep* step);
  * shared last page is replaced by a copy), and lay out the step: M = sum of n_tokens
  * rows, request-major.  The plan stands until one of its sequences loses rows that it
  * covers, or has a page of them replaced (kv_seq_truncate below its length then,
- * kv_seq_compact from the page of the first dropped row on, kv_seq_free); a graph that
- * has captured it must not be replayed from then on.  The new rows hold what their pages
- * held until kv_step_write has stored them, in every layer: fork or read them after that.
+ * kv_seq_compact from the page of the first dropped row on, kv_seq_free, the copy of a
+ * shared last page by kv_seq_append, kv_seq_load, another step's plan or a forward); a
+ * graph that has captured it must not be replayed from then on.  The new rows hold what
+ * their pages held until kv_step_write has stored them, in every layer: fork or read them
+ * after that.
  * Errors: INVALID (NULL, n_tokens < 1, positions for some only), STATE_MISMATCH (another
  * pool's sequence, one twice), CAPACITY (M, a position, free pages, rows, masks above
  * 2^31 words), UNSUPPORTED (capturing stream, a captured step), OOM, HIP; no sequence
@@ -622,8 +624,9 @@ int kv_step_attend(KVStep* step, int layer, const void* q, int q_dtype, int64_t 
 /* stage_forward over sequences of one pool: plans them as kv_step_plan does (positions
  * are required), then takes hidden_in [M][H] through every layer.  A new row must see at
  * least one row.  A forward that fails leaves every sequence's rows as they were (its
- * copy of a shared last page may stay).  Masked-out rows stay and are hidden as in stage_forward, or leave by
- * kv_seq_truncate and kv_seq_compact.
+ * copy of a shared last page may stay, and withdraws plans as in kv_step_plan).
+ * Masked-out rows stay and are hidden as in stage_forward, or leave by kv_seq_truncate
+ * and kv_seq_compact.
  * Errors: as kv_step_plan and stage_forward (M at most STAGE_MAX_ROWS). */
 int stage_forward_paged(Stage* stage, const KVStepRequest* reqs, int n_req, const void* hidden_in, void* hidden_out, void* stream);
 

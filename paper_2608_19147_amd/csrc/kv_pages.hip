@@ -599,7 +599,10 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     // ---- nothing fails from here on
     taken.keep();
     for (Planned& p : ps) {
-        if (p.copy_last) pool->give(p.seq->pages.back());
+        if (p.copy_last) {
+            p.seq->lose(p.P / pr * pr);            // other steps' plans with rows of the page that is replaced
+            pool->give(p.seq->pages.back());
+        }
         p.seq->pages.swap(p.pages);
         p.seq->length = p.P + p.n;
         p.seq->steps.push_back(step);
@@ -707,7 +710,10 @@ int fill(KVSeq* seq, const uint16_t* k, const uint16_t* v, const int16_t* table,
     HIP_TRY(launch_paged_fill(pool->p, k, v, table, S, slot, cap, start, (const int*)(d + moves.size() * sizeof(int2)), n, s, st->done_ev));
     work.launched();
     taken.keep();
-    if (!moves.empty()) pool->give(seq->pages.back());
+    if (!moves.empty()) {
+        seq->lose((int)(seq->pages.size() - 1) * pool->page_rows);   // plans with rows of the page that is replaced
+        pool->give(seq->pages.back());
+    }
     seq->pages.swap(pages);
     seq->length += n;
     return STAGE_OK;

@@ -1,11 +1,12 @@
 """Run as a program under tests/hip_host.cpp's stand-in for the HIP runtime, like
 host_pages.py: what becomes of a step's plan when its sequences get other pages, as JSON."""
+import ctypes
 import json
 import sys
 
 import numpy as np
 
-from host_pages import PAGE, Pool, array, fork, lib, pages, plan, request, use
+from host_pages import H, PAGE, Pool, _lib, array, fork, host, length, lib, pages, plan, request, use
 
 
 def _drop(n, *rows):
@@ -49,6 +50,52 @@ def compacted():
         "in its last page, in place of a shared one": _after(in_place_shared),
         "behind its pages": _after(lambda p, q: lib.kv_seq_compact(q, _drop(70, 48), None)),
     }
+
+
+def copied():
+    """A shared last page is replaced by a copy before rows are added to it."""
+    def shared(add, cut):
+        def change(p, q):
+            rc, (kid,) = fork([q], 1, [64])                      # four whole pages, of which q's rows up to `cut` stay
+            assert rc == 0 and lib.kv_seq_truncate(q, cut) == 0
+            assert add(p, q) == 0
+            assert cut == 64 or pages(kid)[cut // PAGE] != pages(q)[cut // PAGE]
+            return lib.kv_seq_free(kid)
+        return change
+
+    def load(p, q):
+        state = ctypes.c_void_p()
+        assert lib.kv_state_alloc(p.st, 1, 64, ctypes.byref(state)) == 0
+        rows = array(np.zeros((1, 2, 8, 64), np.uint16))
+        assert lib.kv_append(state, rows, rows, 8, 0, None) == 0
+        rc = lib.kv_seq_load(q, state, 0, 1, 3, None)
+        assert lib.kv_state_free(state) == 0
+        return rc
+
+    def forward(p, q, fail=False):
+        x, y, pos = (array(np.zeros((64, H), np.uint16)), array(np.zeros((64, H), np.uint16)), array(np.zeros(64, np.int32)))
+        reqs = (_lib.KVStepRequest * 1)(request(q, 2, pos))
+        n = len(pages(q))
+        last, rows = pages(q)[-1], length(q)
+        if fail:                                                 # behind the plan and its copy
+            host.host_start(4, 0, 0)
+        rc = lib.stage_forward_paged(p.st, reqs, 1, x, y, None)
+        host.host_start(0, 0, 0)
+        if fail:
+            assert rc == -5 and length(q) == rows and len(pages(q)) == n and pages(q)[-1] != last
+        return 0 if fail else rc
+
+    ways = {
+        "append": lambda p, q: lib.kv_seq_append(q, p.rows, p.rows, 2, None),
+        "load": load,
+        "another step's plan": lambda p, q: plan(p.step(), [request(q, 2)]),
+        "forward": forward,
+        "a forward that fails": lambda p, q: forward(p, q, True),
+    }
+    out = {f"{name}, in its last page": _after(shared(f, 45)) for name, f in ways.items()}
+    out.update({f"{name}, in the next page": _after(shared(f, 50)) for name, f in ways.items()})
+    out["append, nothing shared"] = _after(shared(ways["append"], 64))
+    return out
 
 
 if __name__ == "__main__":

@@ -42,3 +42,9 @@ def _check(got, replaced):
 def test_compaction(ask):
     """The old pages of a compaction may be another sequence's next: a plan with rows in one of them is withdrawn."""
     _check(ask("compacted"), {"in its last page, into new pages", "in its last page, in place of a shared one"})
+
+
+def test_copies(ask):
+    """So is one with rows in a shared last page that is replaced by a copy."""
+    got = ask("copied")
+    _check(got, {name for name in got if "last page" in name})
