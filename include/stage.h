@@ -599,8 +599,11 @@ int kv_step_plan(KVStep* step, const KVStepRequest* reqs, int n_req, void* strea
  * strides ld count elements; no alignment beyond the element's).  Pair (i, i + D/2) of
  * every q and k head turns by its axis' position (none without positions); k and v go to
  * their rows of the pages, q to q_out [M][Hq D] (F32, F16 or BF16), which may be q itself
- * (same dtype and stride), and overlaps none of q, k and v otherwise.
- * Errors: INVALID (NULL, dtype, layer, a step without plan, overlap), SHAPE (strides), HIP. */
+ * (same dtype and stride), and overlaps none of q, k and v otherwise.  Refused while a
+ * fork shares a page of the step's new rows, and a graph that holds the call must not be
+ * replayed then: the fork's rows would change.
+ * Errors: INVALID (NULL, dtype, layer, a step without plan, overlap, shared rows), SHAPE
+ * (strides), HIP. */
 int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype,
                   void* q_out, int64_t ldqo, int q_out_dtype, void* stream);
 

@@ -61,6 +61,7 @@ struct KVSeq : Member {
 };
 
 struct KVStep : Member {
+    struct Rows { KVSeq* seq; int begin, end; };   // the new rows of one of its sequences
     KVPages* pool = nullptr;
     uint8_t* dev = nullptr;
     size_t cap = 0;
@@ -75,15 +76,21 @@ struct KVStep : Member {
     int M = 0, n_items = 0;
     size_t parts = 0;
     size_t o_items = 0, o_rows = 0, o_list = 0, o_tables = 0, o_slots = 0, o_pos = 0, o_masks = 0;
-    std::vector<std::pair<KVSeq*, int>> of;        // its sequences, and their rows with the new ones
+    std::vector<Rows> of;
 
     size_t part_bytes() const {
         const StageConfig& c = pool->stage->cfg;
         return merge ? parts * c.n_q_heads * (size_t)(c.head_dim * 4 + 8) : 0;
     }
     void leave() {                                 // its sequences forget it
-        for (auto& x : of) x.first->steps.erase(std::remove(x.first->steps.begin(), x.first->steps.end(), this), x.first->steps.end());
+        for (Rows& x : of) x.seq->steps.erase(std::remove(x.seq->steps.begin(), x.seq->steps.end(), this), x.seq->steps.end());
         of.clear();
+    }
+    bool shared() const {                          // whether a page of its new rows is some other sequence's too
+        for (const Rows& x : of)
+            for (int t = x.begin >> pool->p.shift; t <= (x.end - 1) >> pool->p.shift; ++t)
+                if (pool->refs[x.seq->pages[t]] > 1) return true;
+        return false;
     }
     ~KVStep() override {
         leave();
@@ -99,8 +106,8 @@ struct KVStep : Member {
 void KVSeq::lose(int len) {
     for (size_t i = 0; i < steps.size();) {
         KVStep* step = steps[i];
-        const auto x = std::find_if(step->of.begin(), step->of.end(), [&](const auto& y) { return y.first == this; });
-        if (x->second <= len) {
+        const auto x = std::find_if(step->of.begin(), step->of.end(), [&](const KVStep::Rows& y) { return y.seq == this; });
+        if (x->end <= len) {
             ++i;
             continue;
         }
@@ -578,10 +585,10 @@ int plan(KVStep* step, const KVStepRequest* reqs, int n_req, int M, size_t mask_
     put(o_pos, L.pos.data(), L.pos.size() * 4);
     put(o_masks, L.masks.data(), L.masks.size() * 4);
     put(o_moves, moves.data(), moves.size() * sizeof(int2));
-    std::vector<std::pair<KVSeq*, int>> of;
+    std::vector<KVStep::Rows> of;
     of.reserve(ps.size());
     for (const Planned& p : ps) {
-        of.emplace_back(p.seq, p.P + p.n);
+        of.push_back(KVStep::Rows{p.seq, p.P, p.P + p.n});
         p.seq->steps.reserve(p.seq->steps.size() + 1);
     }
     step->planned = false;                         // until the new plan is there
@@ -1057,6 +1064,7 @@ int kv_step_write(KVStep* step, int layer, const void* q, int64_t ldq, const voi
         if ((!in_place && overlap(q, nq * e, ldq * e, q_out, nq * eo, ldqo * eo, step->M)) ||
             overlap(k, nk * e, ldk * e, q_out, nq * eo, ldqo * eo, step->M) || overlap(v, nk * e, ldv * e, q_out, nq * eo, ldqo * eo, step->M))
             return fail(STAGE_E_INVALID, "q_out overlaps q, k or v (it may be q itself, in its dtype and stride)");
+        if (step->shared()) return fail(STAGE_E_INVALID, "a page of the step's new rows is shared since they were planned");
         DeviceGuard dev(st->device);
         HIP_TRY(dev.err);
         hipStream_t s = (hipStream_t)stream;

@@ -98,5 +98,20 @@ def copied():
     return out
 
 
+def shared():
+    """What a step answers (write, attend) while a fork shares a page of its new rows, and once it does no more."""
+    out = {}
+    for name, rows in (("a page before them", 32), ("a page of them", 48), ("all", 64)):
+        p = Pool()
+        q, step = p.seq(40), p.step()
+        assert plan(step, [request(q, 24)]) == 0
+        rc, (kid,) = fork([q], 1, [rows])
+        assert rc == 0
+        got = [*use(step, p)]
+        assert lib.kv_seq_free(kid) == 0
+        out[name] = [*got, *use(step, p)]
+    return out
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*sys.argv[2:])))

@@ -48,3 +48,9 @@ def test_copies(ask):
     """So is one with rows in a shared last page that is replaced by a copy."""
     got = ask("copied")
     _check(got, {name for name in got if "last page" in name})
+
+
+def test_shared_rows(ask):
+    """Nothing writes into a page while it is shared: the rows of a fork stay as they were when it was made."""
+    got = ask("shared")
+    assert got == {"a page before them": [0, 0, 0, 0], "a page of them": [-1, 0, 0, 0], "all": [-1, 0, 0, 0]}
