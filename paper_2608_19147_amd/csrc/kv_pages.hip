@@ -317,7 +317,7 @@ void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table
         int most = 0;
         for (const Run& r : runs) {
             const int n = steps(r.k0, r.k1), S = (n + C - 1) / C, t = tiles(r), q = r.n_rows * gs;
-            all += (double)t * (n + S * START_STEPS) + (S > 1 || r.parent >= 0 || r.shared ? S * q * PART_STEPS : 0.0);
+            all += (double)t * (n + S * START_STEPS) + (S > 1 || r.parent >= 0 || r.shared ? (double)S * q * PART_STEPS : 0.0);
             most = std::max(most, (n + S - 1) / S);
             wgs += (long)t * S;
         }

@@ -6,6 +6,7 @@ import sys
 
 import numpy as np
 
+from host_stage import quant
 from host_pages import H, PAGE, Pool, _lib, array, fork, host, length, lib, pages, plan, request, use
 
 
@@ -111,6 +112,26 @@ def shared():
         assert lib.kv_seq_free(kid) == 0
         out[name] = [*got, *use(step, p)]
     return out
+
+
+def long_prompt(rows):
+    """Statuses of a plan of 8192 rows of 64 heads on one kv head behind `rows` keys, and the bytes of its workspace by row and head."""
+    n, D = 8192, 64
+    dims = {"wq": (64 * D, H), "wk": (D, H), "wv": (D, H), "wo": (H, 64 * D), "wg": (688, H), "wu": (688, H), "wd": (H, 688)}
+    layer = _lib.LayerWeights(attn_norm=array(np.zeros(H, np.uint16)), ffn_norm=array(np.zeros(H, np.uint16)),
+                              **{name: quant(*d) for name, d in dims.items()})
+    cfg = _lib.StageConfig(n_layers=1, hidden=H, n_q_heads=64, n_kv_heads=1, head_dim=D, ffn=688, group_size=128, rms_eps=1e-5,
+                           act_dtype=_lib.DTYPE_BF16, kv_dtype=_lib.DTYPE_BF16, rope_theta=10000.0, max_positions=64, rope_cos_sin=None)
+    st, pool, q, step = (ctypes.c_void_p() for _ in range(4))
+    assert lib.stage_create(ctypes.byref(cfg), ctypes.byref(layer), 0, None, ctypes.byref(st)) == 0, lib.stage_last_error()
+    count = (int(rows) + n) // 256 + 2
+    k, v, x = (array(np.zeros(count * 256 * D + 8, np.uint16)) // 16 * 16 + 16 for _ in range(3))
+    assert lib.kv_pages_create(st, count, 256, k, v, None, 1, ctypes.byref(pool)) == 0
+    assert lib.kv_seq_create(pool, ctypes.byref(q)) == 0 and lib.kv_step_create(pool, ctypes.byref(step)) == 0
+    assert lib.kv_seq_append(q, x, x, int(rows), None) == 0, lib.stage_last_error()
+    got = plan(step, [request(q, n)])
+    size = ctypes.c_int64()
+    return [got, lib.kv_step_workspace(step, ctypes.byref(size)), size.value / (n * 64)]
 
 
 if __name__ == "__main__":

@@ -54,3 +54,13 @@ def test_shared_rows(ask):
     """Nothing writes into a page while it is shared: the rows of a fork stay as they were when it was made."""
     got = ask("shared")
     assert got == {"a page before them": [0, 0, 0, 0], "a page of them": [-1, 0, 0, 0], "all": [-1, 0, 0, 0]}
+
+
+@pytest.mark.parametrize("rows", [1 << 20, 1 << 21])
+def test_longest_prompts(ask, rows):
+    """Costs of splits are computed wide enough for the most rows behind millions of keys (4096 splits of 2^19 query vectors pass 2^31).
+    A split's partial results cost a 16th of a step a query vector, over 512 places; S splits save at most half of the longest one's
+    steps, as the last ones leave places empty: S 2^19 / (16 512) <= steps / 2.  A partial result is 64 + 2 floats."""
+    plan, size, each = ask("long_prompt", str(rows))
+    steps = (rows + 8192) // 32
+    assert [plan, size] == [0, 0] and each / (4 * 66) <= steps / 128
