@@ -576,7 +576,8 @@ typedef struct KVStepRequest {
     const uint8_t* attention_mask_rows;
 } KVStepRequest;
 
-/* A step holds the metadata of one batch on the device, and can be planned again. */
+/* A step holds the metadata of one batch on the device, and can be planned again.  A
+ * freed one waits for nothing; its memory is the pool's next step's, or goes with the pool. */
 int kv_step_create(KVPages* pool, KVStep** out);
 int kv_step_free(KVStep* step);
 

@@ -30,6 +30,7 @@ struct KVPages {
     size_t low = 0;                                // no word before it has one
     int n_free = 0;
     KVStep* fwd = nullptr;                         // of stage_forward_paged
+    KVStep* spare = nullptr;                       // steps that were freed, for the next ones
     uint8_t* ws = nullptr;                         // and its workspace, grown on need
     size_t ws_cap = 0;
 
@@ -63,6 +64,7 @@ struct KVSeq : Member {
 struct KVStep : Member {
     struct Rows { KVSeq* seq; int begin, end; };   // the new rows of one of its sequences
     KVPages* pool = nullptr;
+    KVStep* next = nullptr;                        // of the pool's spare ones
     uint8_t* dev = nullptr;
     size_t cap = 0;
     uint8_t* host[2] = {nullptr, nullptr};         // pinned
@@ -1015,9 +1017,14 @@ int kv_step_create(KVPages* pool, KVStep** out) {
     return guarded([&]() -> int {
         if (!pool || !out) return fail(STAGE_E_INVALID, "NULL argument");
         *out = nullptr;
-        KVStep* step = new KVStep();
-        step->pool = pool;
-        step->join(pool->members);
+        KVStep* step = pool->spare;
+        if (step) {
+            pool->spare = step->next;
+        } else {
+            step = new KVStep();
+            step->pool = pool;
+            step->join(pool->members);
+        }
         *out = step;
         return STAGE_OK;
     });
@@ -1026,9 +1033,12 @@ int kv_step_create(KVPages* pool, KVStep** out) {
 int kv_step_free(KVStep* step) {
     if (!step) return fail(STAGE_E_INVALID, "step is NULL");
     if (step->captured) return STAGE_OK;           // a graph may still read its metadata: it goes with the pool
-    DeviceGuard dev(step->pool->stage->device);
-    (void)hipDeviceSynchronize();                  // queued work may still read its metadata
-    delete step;
+    // Queued work may still read its metadata, and to wait for that would end a capture of any thread.  The next step of the
+    // pool takes it over: its plan is sent behind the work that is queued.
+    step->planned = false;
+    step->leave();
+    step->next = step->pool->spare;
+    step->pool->spare = step;
     return STAGE_OK;
 }
 

@@ -17,7 +17,7 @@ struct dim3 { uint32_t x, y, z; };
 namespace {
 std::string notes;
 int last = 0, fail_at = 0, launches = 0, capturing = 0;
-long alloc_fail_at = 0, allocs = 0, malloc_fail_at = 0, mallocs = 0, live = 0;
+long alloc_fail_at = 0, allocs = 0, malloc_fail_at = 0, mallocs = 0, live = 0, syncs = 0;
 intptr_t handles = 100;
 long long max_malloc = 0;
 dim3 cfg_grid, cfg_block;
@@ -67,9 +67,9 @@ int hipMalloc(ptr* p, size_t n) {
     ++live;
     return *p ? 0 : (last = 2);
 }
-int hipFree(ptr p) { live -= p ? 1 : 0; free(p); return 0; }
+int hipFree(ptr p) { live -= p ? 1 : 0; ++syncs; free(p); return 0; }
 int hipHostMalloc(ptr* p, size_t n, unsigned) { *p = calloc(n ? n : 1, 1); return *p ? 0 : 2; }
-int hipHostFree(ptr p) { free(p); return 0; }
+int hipHostFree(ptr p) { ++syncs; free(p); return 0; }
 int hipMemcpy(void* d, const void* s, size_t n, int) { memcpy(d, s, n); return 0; }
 int hipMemcpyAsync(void* d, const void* s, size_t n, int, ptr) { memcpy(d, s, n); return 0; }
 int hipMemset(void* d, int v, size_t n) { memset(d, v, n); return 0; }
@@ -86,7 +86,7 @@ int hipStreamWaitEvent(ptr st, ptr e, unsigned) { note('W', st, e); return 0; }
 int hipStreamSynchronize(ptr) { return 0; }
 int hipStreamIsCapturing(ptr, int* c) { *c = capturing; return 0; }
 
-int hipDeviceSynchronize() { return 0; }
+int hipDeviceSynchronize() { ++syncs; return 0; }
 int hipDeviceGetAttribute(int* v, int, int) { *v = 256; return 0; }
 int hipGetDevice(int* d) { *d = 0; return 0; }
 int hipSetDevice(int) { return 0; }
@@ -117,6 +117,8 @@ int host_last_error() { return last; }
 // From now on the `at`-th hipMalloc fails, 0 none.
 void host_fail_malloc(long at) { malloc_fail_at = at; mallocs = 0; }
 long host_live() { return live; }
+// Calls that wait for the device, and end a capture that is under way.
+long host_syncs() { return syncs; }
 long long host_largest_malloc() { return max_malloc; }
 
 }  // extern "C"

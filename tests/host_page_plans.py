@@ -134,5 +134,41 @@ def long_prompt(rows):
     return [got, lib.kv_step_workspace(step, ctypes.byref(size)), size.value / (n * 64)]
 
 
+def freed_steps():
+    """Frees of steps and sequences: whether one waited for the device; device allocations of 20 steps made, planned and freed one
+    after the other beyond the first's; what a new one answers before it has a plan, and after."""
+    host.host_syncs.restype = ctypes.c_long
+    p = Pool()
+    q = p.seq(40)
+
+    def one():
+        step = p.step()
+        none = [*use(step, p), plan(step, [request(q, 1)]), *use(step, p)]
+        before = host.host_syncs()
+        assert lib.kv_step_free(step) == 0
+        return none, host.host_syncs() - before
+
+    first = one()
+    live = host.host_live()
+    rest = [one() for _ in range(20)]
+    live = host.host_live() - live
+    two = p.step(), p.step()                                     # at the same time: each its own
+    assert plan(two[0], [request(q, 1)]) == 0
+    both = [*use(two[0], p), *use(two[1], p)]
+    # a step that a graph holds is not another's
+    host.host_start(0, 0, 1)
+    held = use(two[0], p)
+    host.host_start(0, 0, 0)
+    assert lib.kv_step_free(two[0]) == 0
+    third = p.step()
+    again = third.value == two[0].value
+    before = host.host_syncs()
+    assert lib.kv_seq_free(q) == 0
+    waits = host.host_syncs() - before
+    assert lib.kv_pages_free(p.h) == 0
+    return dict(answers=[first[0], *[r[0] for r in rest]], waits=[first[1], waits, *[r[1] for r in rest]], live=live, both=both, held=held,
+                again=again)
+
+
 if __name__ == "__main__":
     print(json.dumps(globals()[sys.argv[1]](*sys.argv[2:])))

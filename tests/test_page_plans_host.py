@@ -64,3 +64,11 @@ def test_longest_prompts(ask, rows):
     plan, size, each = ask("long_prompt", str(rows))
     steps = (rows + 8192) // 32
     assert [plan, size] == [0, 0] and each / (4 * 66) <= steps / 128
+
+
+def test_freed_steps(ask):
+    """A step's end waits for nothing (a collected one would end a capture that is under way): the pool keeps its memory for the next."""
+    got = ask("freed_steps")
+    assert all(a == [-1, -1, 0, 0, 0] for a in got["answers"])
+    assert got["waits"] == [0] * 22 and got["live"] == 0
+    assert got["both"] == [0, 0, -1, -1] and got["held"] == [0, 0] and not got["again"]
