@@ -95,6 +95,32 @@ def _on(stage, stream, device):
     return int(stream.cuda_stream), empty
 
 
+def _count(n, name: str) -> int:
+    """n as the C calls take it: ctypes would narrow it to some other number."""
+    n = int(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} {n} is out of range")
+    return n
+
+
+def _int32(a, name: str) -> np.ndarray:
+    """Whole numbers as a contiguous int32 array; others, and those that it does not hold, are refused."""
+    a = np.asarray(a)
+    if a.dtype != np.int32:
+        with np.errstate(invalid="ignore"):
+            b = a.astype(np.int32)
+        if (a != b).any():
+            raise ValueError(f"{name} must be whole numbers below 2^31")
+        a = b
+    return np.ascontiguousarray(a)
+
+
+def _mask8(a) -> np.ndarray:
+    """A mask as contiguous uint8: what is not zero stays so."""
+    a = np.asarray(a)
+    return np.ascontiguousarray(a if a.dtype == np.uint8 else a != 0, dtype=np.uint8)
+
+
 def _weights_on(stage, stream, t: torch.Tensor) -> int:
     """The stream handle of a call that packs weights from ``t``, on the stage's device or on the host."""
     return _on(stage, stream, t.device if t.is_cuda else torch.device("cuda", stage.device_index))[0]
@@ -752,10 +778,10 @@ class PagePool:
             if q.pool is not self or q._handle is None:
                 q._check(self)
             handles.append(q._handle)
-        lens = None if lengths is None else np.ascontiguousarray(lengths, dtype=np.int32)
+        lens = None if lengths is None else _int32(lengths, "lengths")
         masks, kp = None, None
         if keep is not None:
-            masks = [None if k is None else np.ascontiguousarray(k, dtype=np.uint8) for k in keep]
+            masks = [None if k is None else _mask8(k) for k in keep]
             for i, m in enumerate(masks):
                 if m is not None and m.shape != (int(lens[i]) if lens is not None else seqs[i].length,):
                     raise ValueError(f"keep[{i}] must have one entry per row")
@@ -824,12 +850,12 @@ class PagedSequence:
         return out.tolist()
 
     def truncate(self, new_len: int) -> None:
-        check(self.lib.kv_seq_truncate(self.handle, int(new_len)))
+        check(self.lib.kv_seq_truncate(self.handle, _count(new_len, "length")))
 
     def compact(self, keep, stream=None) -> int:
         """Drop the rows that ``keep`` (uint8 [length], nonzero = kept) does not keep
         and close the others up.  Returns the new length."""
-        keep = np.ascontiguousarray(keep, dtype=np.uint8)
+        keep = _mask8(keep)
         if keep.shape != (self.length,):
             raise ValueError(f"keep must have {self.length} entries")
         check(self.lib.kv_seq_compact(self.handle, keep.ctypes.data, _pool_stream(self.pool.stage, stream)))
@@ -853,7 +879,8 @@ class PagedSequence:
         """Append rows [start, start + count) of a slot of a KV state, as the slot sees them."""
         if count is None:
             count = state.length - start
-        check(self.lib.kv_seq_load(self.handle, state.handle, int(slot), int(start), int(count), _pool_stream(self.pool.stage, stream)))
+        check(self.lib.kv_seq_load(self.handle, state.handle, _count(slot, "slot"), _count(start, "start"), _count(count, "count"),
+                                   _pool_stream(self.pool.stage, stream)))
 
     def read(self, layer: int, start: int = 0, count: Optional[int] = None, stream=None):
         """Rows [start, start + count) of one layer: K, V [Hkv, count, D]."""
@@ -865,7 +892,8 @@ class PagedSequence:
         dev = torch.device("cuda", st.device_index)
         sp, empty = _on(st, stream, dev)
         k, v = (empty((st.shape.n_kv_heads, count, st.shape.head_dim), dtype=st.kv_dtype, device=dev) for _ in range(2))
-        check(self.lib.kv_seq_read(self.handle, int(layer), int(start), int(count), k.data_ptr() or 16, v.data_ptr() or 16, sp))
+        check(self.lib.kv_seq_read(self.handle, _count(layer, "layer"), _count(start, "start"), _count(count, "count"), k.data_ptr() or 16,
+                                   v.data_ptr() or 16, sp))
         return k, v
 
 
@@ -897,10 +925,10 @@ def _step_requests(requests: Sequence[PagedRequest]):
     arr = (_lib.KVStepRequest * len(requests))()
     keep = []
 
-    def put(a, dtype, shape, name):
+    def put(a, shape, name):
         if a is None:
             return None
-        a = np.ascontiguousarray(a, dtype=dtype)
+        a = _int32(a, name) if name == "positions" else _mask8(a)
         if a.shape != shape and a.size == int(np.prod(shape)) and len(shape) == 2 and shape[0] == 1:
             a = a.reshape(shape)
         if a.shape != shape:
@@ -910,11 +938,12 @@ def _step_requests(requests: Sequence[PagedRequest]):
 
     for c, r in zip(arr, requests):
         r.seq._check(r.seq.pool)
-        n, T = int(r.n_tokens), r.seq.length + int(r.n_tokens)
+        n = _count(r.n_tokens, "n_tokens")
+        T = r.seq.length + n
         c.seq, c.n_tokens = r.seq.handle, n
-        c.positions = put(r.positions, np.int32, (r.seq.pool.n_axes, n), "positions")
-        c.attention_mask = put(r.mask, np.uint8, (T,), "mask")
-        c.attention_mask_rows = put(r.mask_rows, np.uint8, (n, T), "mask_rows")
+        c.positions = put(r.positions, (r.seq.pool.n_axes, n), "positions")
+        c.attention_mask = put(r.mask, (T,), "mask")
+        c.attention_mask_rows = put(r.mask_rows, (n, T), "mask_rows")
     return arr, keep
 
 
@@ -981,7 +1010,7 @@ class PagedStep:
             q_out, ldo = empty((self.rows, self._nq), dtype=st.kv_dtype, device=dev), self._nq
         else:
             ldo = self._in(q_out, self._nq, "q_out", dev)
-        check(self.lib.kv_step_write(self.handle, layer, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _DT_OF[q.dtype],
+        check(self.lib.kv_step_write(self.handle, _count(layer, "layer"), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _DT_OF[q.dtype],
                                      q_out.data_ptr(), ldo, _DT_OF[q_out.dtype], sp))
         return q_out
 
@@ -1008,6 +1037,6 @@ class PagedStep:
                 raise ValueError("out has another dtype")
             ldo = self._in(out, self._nq, "out", dev)
         room = empty(self._ws, dtype=torch.uint8, device=dev) if self._ws else None
-        check(self.lib.kv_step_attend(self.handle, layer, q.data_ptr(), _DT_OF[q.dtype], ldq, out.data_ptr(), _DT_OF[out.dtype], ldo,
+        check(self.lib.kv_step_attend(self.handle, _count(layer, "layer"), q.data_ptr(), _DT_OF[q.dtype], ldq, out.data_ptr(), _DT_OF[out.dtype], ldo,
                                       scale or 0.0, room.data_ptr() if room is not None else None, self._ws, sp))
         return out
