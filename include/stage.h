@@ -617,7 +617,9 @@ int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
  * 2^-17 of each element in bf16, 2^-22 in fp16); out: F32, F16 or BF16, not overlapping q.
  * Scores and sums in fp32; probabilities enter as one or two terms of kv_dtype (two where
  * a kv head has at most 16 query vectors of a run of rows, and with F32 queries).  What rows
- * that are not seen hold, infinities and NaN too, reaches no result.
+ * that are not seen hold, infinities and NaN too, reaches no result; an infinite value of v
+ * that is seen gives that infinity (NaN where a weight is zero in fp32, or with one of the
+ * other sign).
  * workspace: device memory of kv_step_workspace bytes, aligned to 16, not used by another
  * call at the same time (two graphs need two).
  * Errors: INVALID (NULL, dtype, layer, scale, workspace, overlap, a step without plan), SHAPE

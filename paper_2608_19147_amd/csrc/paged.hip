@@ -119,12 +119,15 @@ __device__ __forceinline__ void settle(u32x4 (&v)[N]) {
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
+// The place in the wave, from no register, so that none is kept for an item's second pass.
+__device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+
 // This lane's part of the direct loads of 16 rows of a page, a kilobyte (1024 / (2 D) rows) an instruction: byte offsets
 // into the rows, for K and V.
 template <int D>
-__device__ __forceinline__ uint32_t lane_k() { const int l = threadIdx.x & 63, r = l / (D / 8); return r * 2 * D + 16 * (l % (D / 8) ^ swz_k<D>(r)); }
+__device__ __forceinline__ uint32_t lane_k(int l) { const int r = l / (D / 8); return r * 2 * D + 16 * (l % (D / 8) ^ swz_k<D>(r)); }
 template <int D>
-__device__ __forceinline__ uint32_t lane_v() { const int l = threadIdx.x & 63, r = l / (D / 8); return r * 2 * D + 16 * (l % (D / 8) ^ swz_v<D>(r)); }
+__device__ __forceinline__ uint32_t lane_v(int l) { const int r = l / (D / 8); return r * 2 * D + 16 * (l % (D / 8) ^ swz_v<D>(r)); }
 // 16 rows at src (the same in every lane) to LDS.  The instruction's offset moves both places; a later kilobyte's swizzle is
 // the first's with one bit turned.
 template <int D, bool ISV>
@@ -287,6 +290,17 @@ __device__ __forceinline__ float load_query(const PagedAttend& a, size_t at, int
     }
 }
 
+// Whether one of these results is infinite or no number.
+template <int MB, class V>
+__device__ __forceinline__ bool no_numbers(const V (&o)[MB]) {
+    float t = 0.f;                                 // 0 times a number is 0
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (unsigned j = 0; j < sizeof(V) / 4; ++j) t = __builtin_fmaf(o[mb][j], 0.f, t);
+    return t != 0.f;
+}
+
 // Four neighbouring dims of a query vector's result: a partial one, or times inv to out.
 template <int D>
 __device__ __forceinline__ void put_result(const PagedAttend& a, const PagedRow& r, size_t part, int head, int d, const f32x4_t& v, float inv) {
@@ -302,6 +316,11 @@ __device__ __forceinline__ void put_result(const PagedAttend& a, const PagedRow&
         *(u32x2_any*)((uint16_t*)a.out + at) = a.out_dt == DT_BF16 ? u32x2{pack2<DT_BF16>(x[0], x[1]), pack2<DT_BF16>(x[2], x[3])}
                                                                    : u32x2{pack2<DT_F16>(x[0], x[1]), pack2<DT_F16>(x[2], x[3])};
     }
+}
+
+// Whether one of the four waves has said so in its words, `apart` words from each other.
+__device__ __forceinline__ bool any_wave(const uint32_t* words, int apart) {
+    return (words[0] | words[apart]) | (words[2 * apart] | words[3 * apart]);
 }
 
 // s where bit b of the bits is set, else -infinity.
@@ -326,12 +345,16 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >
 // its place, so that no barrier stands between.  A probability enters as its rounded
 // part and the residual (2^-17 in bf16), in one product: the second operand's 32 k slots hold 16 keys twice, those of V^T
 // repeat them.
-template <int D, int KVDT, int QT, int NB>
-__device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml, uint32_t* words) {
+//
+// Values of V that are no numbers are looked for in steps that not every row sees whole.  In the others an infinite one would
+// be NaN by the probability's two terms (p inf + r inf, r <= 0), or by a probability that is zero in 16 bits.  An item with
+// such a result (true is returned, nothing is written) is computed again with every step looked at (EACH): what holds numbers
+// pays a look at its results, not at its values (one row 8.8 -> 9.0 us, four trees 15.3 -> 15.5, other batches within 1%).
+template <int D, int KVDT, int QT, int NB, bool EACH = false>
+__device__ __forceinline__ bool few_item(const PagedAttend& a, const PagedItem& it, int g, int wave, uint8_t* lds, float2* sml, uint32_t* words) {
     constexpr int AK = 16, RB = 2 * D, SB = AK * RB, KT = D / 32, MB = D / 16, KG = 4;
     constexpr int NL = 2 * SB / 1024;              // loads of a step
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ql = lane & 15, lg = lane >> 4;
+    const int lane = EACH ? (int)here(lane_id()) : lane_id(), ql = lane & 15, lg = lane >> 4;
     const int Hq = a.Hkv * a.gs, pmask = (1 << a.shift) - 1;
     const int s0 = it.kb / AK, s1 = (it.ke + AK - 1) / AK, turns = (s1 - s0 + KG - 1) / KG;
     uint8_t* ring = lds + wave * NB * 2 * SB;
@@ -345,7 +368,7 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
         mask = r->mask;
     }
     const size_t head_at = ((size_t)g << a.shift) * RB, page_bytes = ((size_t)a.Hkv << a.shift) * RB;
-    const uint32_t lk = lane_k<D>(), lv = lane_v<D>();
+    const uint32_t lk = lane_k<D>(lane), lv = lane_v<D>(lane);
     auto page_of = [&](int i) { return uniform_load(a.tables, (size_t)it.table + (min(AK * (s0 + wave + KG * i), it.ke - 1) >> a.shift)); };
     int page = page_of(0);                         // of the step asked for next, known a step ahead
     auto issue = [&](int i) {                      // this wave's step i; every row of a page may be read
@@ -385,7 +408,7 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
         if (NB == 1 || i + NB - 1 >= turns) wait_loads<0>();   // step i is there
         else if (masked) wait_loads<(NB - 1) * (NL + 1)>();
         else wait_loads<(NB - 1) * NL>();
-        const bool whole = open && k0 >= it.kb && k0 + AK <= it.ke;
+        const bool whole = !EACH && open && k0 >= it.kb && k0 + AK <= it.ke;
         uint32_t in = 0xFFFFu, see = 0xFFFFu;      // keys of the step in the run; those that this lane's query vector sees
         bool work = true;
         if (!whole) {
@@ -494,14 +517,20 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
     __syncthreads();                               // every wave has read its last step
     f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][64]
     if (lg == 0) sml[wave * 16 + ql] = float2{base, lsum};
+    if constexpr (!EACH) {
+        const bool bad = __any(no_numbers(o));
+        if (lane == 0) words[0] = bad;             // (the wave has read its words)
+    }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) so[(wave * MB + mb) * 64 + lane] = o[mb];
     __syncthreads();
+    if constexpr (!EACH)
+        if (any_wave(words - wave * NB * 64, NB * 64)) return true;
     int cq = it.q0 + ql;
     asm volatile("" : "+v"(cq));                   // its row is read again: it need not stay in registers through the loop
-    if (cq >= it.q0 + it.nq) return;
+    if (cq >= it.q0 + it.nq) return false;
     const PagedRow ri = a.list[it.rows + cq / a.gs];
-    if (it.slot >= ri.nparts) return;              // (a row that ends before this run has no part of it)
+    if (it.slot >= ri.nparts) return false;        // (a row that ends before this run has no part of it)
     const int head = g * a.gs + cq % a.gs;
     const size_t part = ((size_t)(ri.part + it.slot) * Hq + head);
     float top = -INFINITY, sum = 0.f, f[KG];
@@ -523,6 +552,19 @@ __device__ __forceinline__ void few_item(const PagedAttend& a, const PagedItem& 
         for (int k = 0; k < KG; ++k) v += so[(k * MB + mb) * 64 + lane] * f[k];
         put_result<D>(a, ri, part, head, 16 * mb + 4 * lg, v, inv);
     }
+    return false;
+}
+
+// Every query vector of an item, 16 at a time, each step looked at.  LDS may still be read by the item's first pass.
+template <int D, int KVDT, int QT, int NB>
+__device__ __forceinline__ void each_step(const PagedAttend& a, PagedItem it, int g, int wave, uint8_t* lds, float2* sml, uint32_t* words) {
+    const int end = it.q0 + it.nq;
+#pragma unroll 1
+    for (; it.q0 < end; it.q0 += PAGED_FEW) {
+        __syncthreads();
+        it.nq = min(end - it.q0, PAGED_FEW);
+        few_item<D, KVDT, QT, NB, true>(a, it, g, wave, lds, sml, words);
+    }
 }
 
 // Batches of nothing else: at most 128 registers a wave and 33 KB of LDS, so that four workgroups share a CU (16 x 8 KB
@@ -533,7 +575,9 @@ __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
     __shared__ float2 sml[64];
     __shared__ uint32_t words[4 * 128 / D * 64];
     const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
-    few_item<D, KVDT, QT, 128 / D>(a, uniform_load(a.items, b), g, lds, sml, words);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const PagedItem it = uniform_load(a.items, b);
+    if (few_item<D, KVDT, QT, 128 / D>(a, it, g, wave, lds, sml, words)) each_step<D, KVDT, QT, 128 / D>(a, it, g, wave, lds, sml, words);
 }
 
 // ---- tiles of up to 128 query vectors
@@ -546,11 +590,10 @@ __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
 // scores under way while this one's become probabilities: 12% slower; steps of 64 keys: 4%; wave priorities: 1% faster to 9% slower.)
 // PT: terms of a probability (1: rounded to the cache's type, while the sum keeps it whole).
 template <int D, int KVDT, int QT, int PT, int NQT>
-__device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem& it, int g, uint8_t* lds, float2* sml, uint32_t* words) {
+__device__ __forceinline__ bool many_item(const PagedAttend& a, const PagedItem& it, int g, int wave, uint8_t* lds, float2* sml, uint32_t* words) {
     constexpr int AK = 32, RB = 2 * D, SB = AK * RB, KT = D / 16, MB = D / 32, KG = 4 / NQT, NB = NQT;
     constexpr int NL = 2 * SB / 1024 / NQT;        // a wave's loads of a step
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qt = wave % NQT, kg = wave / NQT, ql = lane & 31, h = lane >> 5;
+    const int lane = lane_id(), qt = wave % NQT, kg = wave / NQT, ql = lane & 31, h = lane >> 5;
     const int Hq = a.Hkv * a.gs, pmask = (1 << a.shift) - 1;
     const int s0 = it.kb / AK, s1 = (it.ke + AK - 1) / AK, turns = (s1 - s0 + KG - 1) / KG;
     uint8_t* ring = lds + kg * NB * 2 * SB;
@@ -566,7 +609,7 @@ __device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem&
     }
 
     const size_t head_at = ((size_t)g << a.shift) * RB, page_bytes = ((size_t)a.Hkv << a.shift) * RB;
-    const uint32_t lk = lane_k<D>(), lv = lane_v<D>();
+    const uint32_t lk = lane_k<D>(lane), lv = lane_v<D>(lane);
     // a wave's 16-row parts of a step's K and V: all four, two of one, or one; their pages are known a step ahead
     constexpr int NP = 4 / NQT, PG = NQT == 4 ? 1 : 2;
     int page[PG];
@@ -756,18 +799,21 @@ __device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem&
     base = base == -INFINITY ? base : base * sc;
     auto quad = [&](int q) { return f32x4_t{o[q / 4][q % 4 * 4], o[q / 4][q % 4 * 4 + 1], o[q / 4][q % 4 * 4 + 2], o[q / 4][q % 4 * 4 + 3]}; };
     f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][4][64]
+    const bool bad = __any(no_numbers(o));         // as in few_item
+    if (lane == 0) words[0] = bad;
     if constexpr (KG > 1) {
         __syncthreads();                           // every wave has read its last step
         if (h == 0) sml[wave * 32 + ql] = float2{base, lsum};
 #pragma unroll
         for (int q = 0; q < 4 * MB; ++q) so[(wave * MB * 4 + q) * 64 + lane] = quad(q);
-        __syncthreads();
     }
+    __syncthreads();
+    if (any_wave(words - wave * NB * 64, NB * 64)) return true;
     int cq = c0;
     asm volatile("" : "+v"(cq));
-    if (cq >= it.q0 + it.nq) return;
+    if (cq >= it.q0 + it.nq) return false;
     const PagedRow ri = a.list[it.rows + cq / a.gs];
-    if (it.slot >= ri.nparts) return;
+    if (it.slot >= ri.nparts) return false;
     const int head = g * a.gs + cq % a.gs;
     const size_t part = ((size_t)(ri.part + it.slot) * Hq + head);
     if constexpr (KG == 1) {
@@ -794,6 +840,7 @@ __device__ __forceinline__ void many_item(const PagedAttend& a, const PagedItem&
             put_result<D>(a, ri, part, head, 8 * q + 4 * h, v, inv);
         }
     }
+    return false;
 }
 
 template <int D, int KVDT, int QT, int PT>
@@ -802,11 +849,13 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
     __shared__ float2 sml[128];
     __shared__ uint32_t words[4 * 4 * 64];
     const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const PagedItem it = uniform_load(a.items, b);
-    if (it.nq <= 16) few_item<D, KVDT, QT, 2>(a, it, g, lds, sml, words);
-    else if (it.nq <= 32) many_item<D, KVDT, QT, PT, 1>(a, it, g, lds, sml, words);
-    else if (it.nq <= 64) many_item<D, KVDT, QT, PT, 2>(a, it, g, lds, sml, words);
-    else many_item<D, KVDT, QT, PT, 4>(a, it, g, lds, sml, words);
+    const bool again = it.nq <= 16   ? few_item<D, KVDT, QT, 2>(a, it, g, wave, lds, sml, words)
+                       : it.nq <= 32 ? many_item<D, KVDT, QT, PT, 1>(a, it, g, wave, lds, sml, words)
+                       : it.nq <= 64 ? many_item<D, KVDT, QT, PT, 2>(a, it, g, wave, lds, sml, words)
+                                     : many_item<D, KVDT, QT, PT, 4>(a, it, g, wave, lds, sml, words);
+    if (again) each_step<D, KVDT, QT, 2>(a, it, g, wave, lds, sml, words);
 }
 
 // Rows with several partial results: m = max m_r, o = sum o_r 2^(m_r - m) / sum l_r 2^(m_r - m), added in the order of the
