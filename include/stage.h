@@ -615,8 +615,10 @@ int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
  * softmax of scale q.k (scale 0: 1/sqrt(D)) over the rows that each new row sees; a row
  * that sees none gives zeros.  q: kv_dtype, or F32 (as two terms of kv_dtype: within
  * 2^-17 of each element in bf16, 2^-22 in fp16); out: F32, F16 or BF16, not overlapping q.
- * Scores and sums in fp32; probabilities enter as one or two terms of kv_dtype (two where
- * a kv head has at most 16 query vectors of a run of rows, and with F32 queries).  What rows
+ * Scores and sums in fp32.  Probabilities enter as two terms of kv_dtype; with q in kv_dtype,
+ * those of a sequence with more than 128 new query vectors a kv head (a prompt) as one, while
+ * their sum keeps them whole.  How many follows from a row's own request, not from the others
+ * of its step; the order of its sums, and with it its last bits, follow from both.  What rows
  * that are not seen hold, infinities and NaN too, reaches no result; an infinite value of v
  * that is seen gives that infinity (NaN where a weight is zero in fp32, or with one of the
  * other sign).

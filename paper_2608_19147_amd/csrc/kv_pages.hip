@@ -353,7 +353,8 @@ void lay_out_items(const KVPages* pool, int n_cus, const std::vector<int>& table
             for (int j = 0; j < r.splits; ++j) {
                 const int kb = std::max(r.k0, a0 + j * r.chunk), ke = std::min({r.k1, a0 + (j + 1) * r.chunk, high});
                 if (ke <= kb) break;
-                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, masked ? 2 : low >= ke});
+                const bool two = r.shared || (long)r.n_rows * gs <= SHARE_QUERIES;   // of the row's own sequence: the same in all its runs
+                L.items.push_back(PagedItem{r.rows, q, nq, kb, ke, table_off[r.seq], r.slot + j, (masked ? 2 : low >= ke) | (two ? 4 : 0)});
                 cost.push_back(steps(kb, ke));
             }
         }

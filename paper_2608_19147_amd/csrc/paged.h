@@ -19,7 +19,7 @@ struct PagedItem {
     int kb, ke;                                    // keys, by their place in the sequence
     int table;                                     // of a sequence that holds the run: tables[table + key / page_rows] is its page
     int slot;                                      // which of a row's partial results this is
-    int open;                                      // 1: no row's limit or mask cuts the run, 2: some row has a mask
+    int open;                                      // 1: no row's limit or mask cuts the run, 2: some row has a mask; + 4: probabilities in two terms
 };
 struct PagedRow {
     int row;

@@ -588,7 +588,10 @@ __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
 // instructions (256 of them exponentials) and a share of LDS, which its two waves a SIMD hardly overlap: 4 x 1024 rows of 32
 // heads of 128 behind 2048 take 197 to 210 us, 820 to 870 TFLOP/s, where a product of 8192 x 8192 x 8192 reaches 1077.  (The next step's
 // scores under way while this one's become probabilities: 12% slower; steps of 64 keys: 4%; wave priorities: 1% faster to 9% slower.)
-// PT: terms of a probability (1: rounded to the cache's type, while the sum keeps it whole).
+// PT: terms of a probability.  One (rounded to the cache's type, while the sum keeps it whole) for prompts alone, whose products
+// bound them (4 x 1024 rows 208 us, two terms 267; 4 x 128 rows 50 and 58) and whose tiles hold nobody else's rows: a row's bits
+// must not follow from what is batched with it.  Two cost the others 5 to 13% (64 rows 32.8 -> 34.7 us, trees 15.5 -> 16.7,
+// verifies 32.4 -> 35.2, 12 x 10 rows 42.7 -> 48.8).
 template <int D, int KVDT, int QT, int PT, int NQT>
 __device__ __forceinline__ bool many_item(const PagedAttend& a, const PagedItem& it, int g, int wave, uint8_t* lds, float2* sml, uint32_t* words) {
     constexpr int AK = 32, RB = 2 * D, SB = AK * RB, KT = D / 16, MB = D / 32, KG = 4 / NQT, NB = NQT;
@@ -843,7 +846,7 @@ __device__ __forceinline__ bool many_item(const PagedAttend& a, const PagedItem&
     return false;
 }
 
-template <int D, int KVDT, int QT, int PT>
+template <int D, int KVDT, int QT>
 __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * 2 * 32 * 2 * D];
     __shared__ float2 sml[128];
@@ -851,10 +854,14 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(PagedAttend a) {
     const int b = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), g = __builtin_amdgcn_readfirstlane(blockIdx.x % a.Hkv);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const PagedItem it = uniform_load(a.items, b);
+    const bool two = QT == 2 || (it.open & 4);
     const bool again = it.nq <= 16   ? few_item<D, KVDT, QT, 2>(a, it, g, wave, lds, sml, words)
-                       : it.nq <= 32 ? many_item<D, KVDT, QT, PT, 1>(a, it, g, wave, lds, sml, words)
-                       : it.nq <= 64 ? many_item<D, KVDT, QT, PT, 2>(a, it, g, wave, lds, sml, words)
-                                     : many_item<D, KVDT, QT, PT, 4>(a, it, g, wave, lds, sml, words);
+                       : it.nq <= 32 ? two ? many_item<D, KVDT, QT, 2, 1>(a, it, g, wave, lds, sml, words)
+                                           : many_item<D, KVDT, QT, QT, 1>(a, it, g, wave, lds, sml, words)
+                       : it.nq <= 64 ? two ? many_item<D, KVDT, QT, 2, 2>(a, it, g, wave, lds, sml, words)
+                                           : many_item<D, KVDT, QT, QT, 2>(a, it, g, wave, lds, sml, words)
+                       : two         ? many_item<D, KVDT, QT, 2, 4>(a, it, g, wave, lds, sml, words)
+                                     : many_item<D, KVDT, QT, QT, 4>(a, it, g, wave, lds, sml, words);
     if (again) each_step<D, KVDT, QT, 2>(a, it, g, wave, lds, sml, words);
 }
 
@@ -1085,8 +1092,8 @@ hipError_t launch_paged_attend(const PagedAttend& a, int D, int kv_dt, hipStream
     const dim3 block(256), grid((unsigned)items), mg((unsigned)((waves + 3) / 4));
     const hipEvent_t d = a.merge ? nullptr : done;
 #define PAGED_KERNEL(D_, KV_)                                                                                                  \
-    (a.many ? f32 ? launch_done(paged_many_kernel<D_, KV_, 2, 2>, grid, block, 0, st, d, a)                                    \
-                  : launch_done(paged_many_kernel<D_, KV_, 1, 1>, grid, block, 0, st, d, a)                                    \
+    (a.many ? f32 ? launch_done(paged_many_kernel<D_, KV_, 2>, grid, block, 0, st, d, a)                                       \
+                  : launch_done(paged_many_kernel<D_, KV_, 1>, grid, block, 0, st, d, a)                                       \
             : f32 ? launch_done(paged_few_kernel<D_, KV_, 2>, grid, block, 0, st, d, a)                                        \
                   : launch_done(paged_few_kernel<D_, KV_, 1>, grid, block, 0, st, d, a))
     const hipError_t e = D == 128 ? (bf ? PAGED_KERNEL(128, DT_BF16) : PAGED_KERNEL(128, DT_F16))
