@@ -105,8 +105,8 @@ def _count(n, name: str) -> int:
 
 def _int32(a, name: str) -> np.ndarray:
     """Whole numbers as a contiguous int32 array; others, and those that it does not hold, are refused."""
-    a = np.asarray(a)
-    if a.dtype != np.int32:
+    if not (isinstance(a, np.ndarray) and a.dtype == np.int32):
+        a = np.asarray(a)
         with np.errstate(invalid="ignore"):
             b = a.astype(np.int32)
         if (a != b).any():
@@ -117,8 +117,9 @@ def _int32(a, name: str) -> np.ndarray:
 
 def _mask8(a) -> np.ndarray:
     """A mask as contiguous uint8: what is not zero stays so."""
-    a = np.asarray(a)
-    return np.ascontiguousarray(a if a.dtype == np.uint8 else a != 0, dtype=np.uint8)
+    if not (isinstance(a, np.ndarray) and a.dtype == np.uint8):
+        a = np.asarray(a) != 0
+    return np.ascontiguousarray(a, dtype=np.uint8)
 
 
 def _weights_on(stage, stream, t: torch.Tensor) -> int:
