@@ -388,7 +388,7 @@ __device__ __forceinline__ bool few_item(const PagedAttend& a, const PagedItem& 
     float sc = a.scale2;
     {
         const int cq = min(it.q0 + ql, it.q0 + it.nq - 1);
-        sc *= load_query<KVDT, QT, KT, 4>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * lg, 32, qf);
+        sc = fmaxf(sc * load_query<KVDT, QT, KT, 4>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * lg, 32, qf), 0x1p-149f);   // (above zero: no score is the base's times zero)
     }
     limit = (int)here((uint32_t)limit);
     mask = (int)here((uint32_t)mask);
@@ -642,7 +642,7 @@ __device__ __forceinline__ bool many_item(const PagedAttend& a, const PagedItem&
     float sc = a.scale2;
     {
         const int cq = min(c0, it.q0 + it.nq - 1);
-        sc *= load_query<KVDT, QT, KT, 2>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * h, 16, qf);
+        sc = fmaxf(sc * load_query<KVDT, QT, KT, 2>(a, (size_t)a.list[it.rows + cq / a.gs].row * a.ldq + (size_t)(g * a.gs + cq % a.gs) * D + 8 * h, 16, qf), 0x1p-149f);   // (above zero: no score is the base's times zero)
     }
 
     limit = (int)here((uint32_t)limit);

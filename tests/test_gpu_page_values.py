@@ -114,3 +114,28 @@ def test_shared_rows(kv, D, q_dtype, copies, n):
         v[100, 9] = math.inf
         v[-1, 10] = -math.inf
     _check(*_attend(kv, D, q_dtype, n, 800, put, True, copies=copies))
+
+
+@pytest.mark.parametrize("kv,D", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("n", [1, 10, 40])
+@pytest.mark.parametrize("size", [0.0, 1e-40, 1e-30])
+@pytest.mark.parametrize("scale", [1e-9, 1e-44, None])
+def test_smallest_scores(kv, D, n, size, scale):
+    """Queries and scales whose scores all round to zero: the mean of what a row sees (their product is no fp32 number above zero)."""
+    st = ref.make_stage(kv=kv, D=D, **W)
+    pool = st.new_pages(40, 16)
+    s = pool.new_sequence()
+    s.append(ref.rows(st, 300, 1), ref.rows(st, 300, 2))
+    step = pool.new_step()
+    step.plan([PagedRequest(s, n)])
+    g = torch.Generator(device="cuda").manual_seed(3)
+    new = [torch.randn((n, 2 * D), device="cuda", generator=g).to(st.kv_dtype) for _ in range(2)]
+    q = torch.randn((n, 4 * D), device="cuda", generator=g) * size
+    step.write(0, q.to(st.kv_dtype), *new)
+    out = step.attend(0, q, scale=scale).view(n, 4, D).double()
+    k, v = s.read(0)
+    o, a, s_abs, s_top = ref.attend(q.view(n, 4, D), k, v, ref.sees(300, n), scale or 1 / math.sqrt(D))
+    bound = ref.attend_bound(o, a, s_abs, s_top, 300 + n, D, st.kv_dtype, torch.float32, torch.float32)
+    assert ((out - o).abs() <= bound).all()
+    pool.free()
+    st.close()
