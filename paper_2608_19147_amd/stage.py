@@ -982,7 +982,9 @@ class PagedStep:
 
     def plan(self, requests: Sequence[PagedRequest], stream=None) -> None:
         """Make room for the new rows of each request's sequence, whose length grows by
-        them, and lay out the step."""
+        them, and lay out the step.  The plan stands until one of the sequences loses
+        rows that it covers, or has a page of them replaced (``compact``, or rows added
+        to a shared last page)."""
         for r in requests:
             r.seq._check(self.pool)
         arr, keep = _step_requests(requests)
@@ -1001,7 +1003,8 @@ class PagedStep:
               stream=None) -> torch.Tensor:
         """Turn q [M, Hq D] and k [M, Hkv D] by the rows' positions, store k and v [M,
         Hkv D] in their rows of the pages, and return q (in the KV dtype, or in
-        ``q_out``).  Rows may be parts of wider ones; all of one dtype."""
+        ``q_out``).  Rows may be parts of wider ones; all of one dtype.  Refused while a
+        fork shares a page of the step's new rows."""
         st, dev = self.pool.stage, q.device
         ldq, ldk, ldv = self._in(q, self._nq, "q"), self._in(k, self._nk, "k", dev), self._in(v, self._nk, "v", dev)
         if q.dtype != k.dtype or q.dtype != v.dtype:
