@@ -614,7 +614,8 @@ int kv_step_workspace(const KVStep* step, int64_t* bytes_out);
 /* out [M][Hq D] = attention of the rotated queries q [M][Hq D] over one layer's pages:
  * softmax of scale q.k (scale 0: 1/sqrt(D)) over the rows that each new row sees; a row
  * that sees none gives zeros.  q: kv_dtype, or F32 (as two terms of kv_dtype: within
- * 2^-17 of each element in bf16, 2^-22 in fp16); out: F32, F16 or BF16, not overlapping q.
+ * 2^-17 of each element in bf16; in fp16 within 2^-22 of it or 2^-25 of the largest of its
+ * D, whichever is more); out: F32, F16 or BF16, not overlapping q.
  * Scores and sums in fp32.  Probabilities enter as two terms of kv_dtype; with q in kv_dtype,
  * those of a sequence with more than 128 new query vectors a kv head (a prompt) as one, while
  * their sum keeps them whole.  How many follows from a row's own request, not from the others

@@ -227,7 +227,7 @@ constexpr int SHARE_QUERIES = 128;                 // a sequence with more query
 
 // The runs of a batch: sequences sorted by their whole pages, so that those that share pages are neighbours.  A common
 // beginning becomes a run of them all where that saves more steps of tiles than its starts and partial results cost (12
-// sequences of 5 rows that share 288 keys, and 2048 by fours: one run for the 288 35.4 us, none 32.9); what follows is laid
+// sequences of 5 rows that share 288 keys, and 2048 by fours: one run for the 288 38.9 us, none 35.6); what follows is laid
 // out for each set with a common next page.  A sequence that fills tiles by itself keeps its keys in one run: shared rows
 // save it no product, and partial results would be written and read for every one of its rows.
 struct RunBuilder {
@@ -264,9 +264,9 @@ struct RunBuilder {
             double apart = 0;
             auto tiles = [&](long r) { return (r * gs + PAGED_MANY - 1) / PAGED_MANY; };
             // a tile's last queries take half a tile up to 64 of them (loads of rows bound a smaller one), so sets that fill
-            // halves save no product (48 x 15 rows of 4 heads 64 us shared, 52 apart), and sets of 80 do (48 x 10 rows of 8 145
-            // apart, 110 shared).  Two halves cost a little more than a whole: 48 x 8 rows of 8 behind 30000 to 60000 shared keys
-            // are 7 to 10% slower apart, 12 x 8 rows and 16 x 16 rows of 4 behind 60000 to 100000 6 to 11% faster.
+            // halves save no product (48 x 15 rows of 4 heads 73 us shared, 54 apart), and sets of 80 do (48 x 10 rows of 8 168
+            // apart, 125 shared).  Two halves cost a little more than a whole: 48 x 8 rows of 8 behind 30000 to 60000 shared keys
+            // are 6 to 10% slower apart, 12 x 8 rows behind 60000 11% faster.
             auto work = [&](long r) {
                 const long q = r * gs, rest = q % PAGED_MANY;
                 return q / PAGED_MANY + (rest == 0 ? 0.0 : rest <= 64 ? 0.5 : 1.0);
@@ -918,7 +918,7 @@ int kv_seq_compact(KVSeq* seq, const uint8_t* keep, void* stream) {
         const int kept = t0 * pr + (int)rows.size(), n_pages = pool->pages_for(kept);
         const bool moved = kept > first;           // else only a tail is dropped
         // into new pages where there are enough, all rows at once; else in place, in order, by one thread per 16 bytes of a row
-        // (16 layers of 8 x 128: 64 rows 12 and 26 us, 1024 rows 32 and 220)
+        // (16 layers of 8 x 128: 64 rows 14 and 24 us, 1024 rows 33 and 215)
         const bool fresh = moved && n_pages - t0 <= pool->n_free && one_launch(pool->p, rows.size());
         size_t need = 0;
         if (moved)

@@ -340,7 +340,7 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >
 // ---- tiles of up to 16 query vectors
 //
 // Decoding rows.  The four waves take alternate steps of 16 keys (one page's) and are merged through LDS.  Bound by memory
-// (four caches of 81920 to 131072 rows of 8 x 128: 309 us, 5.65 TB/s; a large read 6.2): what counts is bytes in flight.
+// (four caches of 81920 to 131072 rows of 8 x 128: 308 us, 5.67 TB/s; a large read 6.2): what counts is bytes in flight.
 // A wave holds NB steps in LDS of its own; it reads all of a step into registers, then asks for the step NB further on in
 // its place, so that no barrier stands between.  A probability enters as its rounded
 // part and the residual (2^-17 in bf16), in one product: the second operand's 32 k slots hold 16 keys twice, those of V^T
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(256, 4) void paged_few_kernel(PagedAttend a) {
 // groups, which take alternate steps of 32 keys.  A group's waves share a ring of NQT steps; alone (NQT = 1) a wave reads
 // its step into registers before it asks for the next.  A step of a wave takes 512 cycles of products, some 640 of vector
 // instructions (256 of them exponentials) and a share of LDS, which its two waves a SIMD hardly overlap: 4 x 1024 rows of 32
-// heads of 128 behind 2048 take 197 to 210 us, 820 to 870 TFLOP/s, where a product of 8192 x 8192 x 8192 reaches 1077.  (The next step's
+// heads of 128 behind 2048 take 197 to 209 us, 825 to 875 TFLOP/s, where a product of 8192 x 8192 x 8192 reaches 1077.  (The next step's
 // scores under way while this one's become probabilities: 12% slower; steps of 64 keys: 4%; wave priorities: 1% faster to 9% slower.)
 // PT: terms of a probability.  One (rounded to the cache's type, while the sum keeps it whole) for prompts alone, whose products
 // bound them (4 x 1024 rows 208 us, two terms 267; 4 x 128 rows 50 and 58) and whose tiles hold nobody else's rows: a row's bits
@@ -995,8 +995,8 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWrite a) {
 // ------------------------------------------------------------------ moves of rows
 //
 // Bound by memory: a row of one layer, kv head and K or V is D values in one piece, 16 bytes a thread; a workgroup moves
-// up to 64 rows of it, four loads a thread in flight (16 layers of 8 x 128: 40 rows to each of 64 pages 38 us, 4.7 TB/s; 3400
-// rows closed up 78 us, 5.7 TB/s).
+// up to 64 rows of it, four loads a thread in flight (16 layers of 8 x 128: 40 rows to each of 64 pages 37 us, 4.8 TB/s; 3400
+// rows closed up 81 us, 5.5 TB/s).
 
 constexpr int MOVE_ROWS = 64;
 
