@@ -348,8 +348,9 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >
 //
 // Values of V that are no numbers are looked for in steps that not every row sees whole.  In the others an infinite one would
 // be NaN by the probability's two terms (p inf + r inf, r <= 0), or by a probability that is zero in 16 bits.  An item with
-// such a result (true is returned, nothing is written) is computed again with every step looked at (EACH): what holds numbers
-// pays a look at its results, not at its values (one row 8.8 -> 9.0 us, four trees 15.3 -> 15.5, other batches within 1%).
+// such a result (true is returned, nothing is written) is computed again with every step looked at (EACH), unless the sum of
+// the probabilities is none either (a query or key with NaN: the result stays NaN): what holds numbers pays a look at its
+// results, not at its values (one row 8.8 -> 9.0 us, four trees 15.3 -> 15.5, other batches within 1%).
 template <int D, int KVDT, int QT, int NB, bool EACH = false>
 __device__ __forceinline__ bool few_item(const PagedAttend& a, const PagedItem& it, int g, int wave, uint8_t* lds, float2* sml, uint32_t* words) {
     constexpr int AK = 16, RB = 2 * D, SB = AK * RB, KT = D / 32, MB = D / 16, KG = 4;
@@ -518,7 +519,7 @@ __device__ __forceinline__ bool few_item(const PagedAttend& a, const PagedItem& 
     f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][64]
     if (lg == 0) sml[wave * 16 + ql] = float2{base, lsum};
     if constexpr (!EACH) {
-        const bool bad = __any(no_numbers(o));
+        const bool bad = __any(lsum - lsum == 0.f && no_numbers(o));
         if (lane == 0) words[0] = bad;             // (the wave has read its words)
     }
 #pragma unroll
@@ -802,7 +803,7 @@ __device__ __forceinline__ bool many_item(const PagedAttend& a, const PagedItem&
     base = base == -INFINITY ? base : base * sc;
     auto quad = [&](int q) { return f32x4_t{o[q / 4][q % 4 * 4], o[q / 4][q % 4 * 4 + 1], o[q / 4][q % 4 * 4 + 2], o[q / 4][q % 4 * 4 + 3]}; };
     f32x4_t* so = (f32x4_t*)lds;                   // [wave][MB][4][64]
-    const bool bad = __any(no_numbers(o));         // as in few_item
+    const bool bad = __any(lsum - lsum == 0.f && no_numbers(o));   // as in few_item
     if (lane == 0) words[0] = bad;
     if constexpr (KG > 1) {
         __syncthreads();                           // every wave has read its last step

@@ -139,3 +139,35 @@ def test_smallest_scores(kv, D, n, size, scale):
     assert ((out - o).abs() <= bound).all()
     pool.free()
     st.close()
+
+
+@pytest.mark.parametrize("kv,D,q_dtype", CASES)
+@pytest.mark.parametrize("copies,n", [(1, 1), (12, 1), (5, 5), (3, 40), (1, 150)])
+def test_queries_that_are_no_numbers(kv, D, q_dtype, copies, n):
+    """A row whose query holds NaN (a padded one, say) is NaN in that head; the others are as without it, bit for bit, an infinite
+    value among the rows that they see too."""
+    for infinite in (False, True):
+        st = ref.make_stage(kv=kv, D=D, **W)
+        pool = st.new_pages(80 + 12 * copies, 16)
+        base = pool.new_sequence()
+        base.append(ref.rows(st, 700, 1), ref.rows(st, 700, 2))
+        if infinite:
+            pool.v[0, base.pages[5], :, 3, 7] = math.inf
+        seqs = pool.fork([base] * copies)
+        step = pool.new_step()
+        step.plan([PagedRequest(s, n) for s in seqs])
+        g = torch.Generator(device="cuda").manual_seed(n)
+        M = n * copies
+        q = torch.randn((M, 4 * D), device="cuda", generator=g).to(q_dtype)
+        new = [torch.randn((M, 2 * D), device="cuda", generator=g).to(st.kv_dtype) for _ in range(2)]
+        step.write(0, q.to(st.kv_dtype), *new)
+        clean = step.attend(0, q)
+        bad = q.clone()
+        bad[M // 2, D + 1] = math.nan
+        out = step.attend(0, bad)
+        assert torch.isnan(out[M // 2, D:2 * D]).all()
+        out[M // 2, D:2 * D] = clean[M // 2, D:2 * D]
+        assert torch.equal(out, clean)
+        assert torch.isinf(clean).sum() == (4 * M if infinite else 0)
+        pool.free()
+        st.close()
